@@ -78,6 +78,7 @@ extern "C" {
 #define FUSION_DEV_INTERNAL 8    /* an internal consistency check failed (a library bug) */
 #define FUSION_DEV_BAD_IDS 16    /* a sample id outside [0, max_batch) */
 #define FUSION_DEV_TIMEOUT 32    /* a bounded wait inside a kernel gave up (outputs of that sample skipped) */
+#define FUSION_DEV_BAD_CACHE 64  /* a cache length or page id out of range, or no room for the appended rows */
 
 /* ---- storage types and stage flags --------------------------------------- */
 #define FUSION_F32 0
@@ -97,6 +98,12 @@ extern "C" {
 /* Size-aware attention (fusion_attention): head width and the longest sample. */
 #define FUSION_ATTN_HEAD_DIM 64
 #define FUSION_ATTN_MAX_TOKENS 1024
+
+/* Key-value cache (fusion_cache): bounds of its shape. */
+#define FUSION_CACHE_MAX_BATCH 65535
+#define FUSION_CACHE_MAX_PAGE_TOKENS 1024
+#define FUSION_CACHE_MAX_HEAD_DIM 256
+#define FUSION_CACHE_MAX_HEADS 1024
 
 /* Pooling of an MLP exit head (fusion_mlp_head.pool). */
 #define FUSION_POOL_CLS 0     /* the CLS row (the paper's CLS-only head, block 10) */
@@ -140,6 +147,30 @@ typedef struct fusion_mlp_head {
     int32_t classes;      /* C >= 1 */
     float tau;            /* exit threshold */
 } fusion_mlp_head;
+
+/* A paged cache of keys and values, as a decoder keeps them for the tokens before the new one (here: a compacted image's
+ * tokens, then its own).  Position j of sequence b lies in page page_table[b, j / page_tokens] at place j % page_tokens.
+ * A merged token keeps its size, and every token the attention weight that it has received.  All pointers are device
+ * memory owned by the caller, who also assigns the pages: entries of the table for positions that are neither held nor
+ * written are not read, and sequences may share pages only in calls that write to neither of them (fusion_cache_attention
+ * writes where `weights` is given); a page stands once in a row.
+ * Shape.  max_batch in [0, FUSION_CACHE_MAX_BATCH]; page_tokens a power of two up to FUSION_CACHE_MAX_PAGE_TOKENS;
+ * head_dim a multiple of 8 up to FUSION_CACHE_MAX_HEAD_DIM; kv_heads in [1, FUSION_CACHE_MAX_HEADS]; max_pages >= 1 with
+ * max_pages * page_tokens <= 2^30; num_pages >= 1 with num_pages * kv_heads * page_tokens < 2^32.  k and v are 16-byte
+ * aligned. */
+typedef struct fusion_cache {
+    int32_t max_batch;         /* sequences */
+    int32_t max_pages;         /* pages of a sequence, at most */
+    int32_t page_tokens;       /* tokens of a page */
+    int32_t kv_heads;          /* key (and value) heads */
+    int32_t head_dim;          /* width of a head */
+    int64_t num_pages;         /* pages in the pools */
+    void *k, *v;               /* [num_pages, kv_heads, page_tokens, head_dim], dtype */
+    float *sizes;              /* [num_pages, page_tokens] token sizes (0: a masked token); NULL: all 1 */
+    float *weights;            /* [num_pages, page_tokens] accumulated attention weights; NULL: not kept */
+    const int32_t *page_table; /* [max_batch, max_pages] */
+    const int32_t *lengths;    /* [max_batch] tokens held, in [0, max_pages * page_tokens] */
+} fusion_cache;
 
 /* Human-readable name of a return code or of a single FUSION_DEV_* bit. */
 const char *fusion_status_string(int code);
@@ -435,6 +466,68 @@ int fusion_stage_mlp(int dtype, int flags, fusion_ragged in, const void *x, int3
                      int32_t *offsets_out, int32_t *ids_out, int32_t *batch_out, int32_t *keep_idx,
                      int32_t *a_match, void *workspace, size_t workspace_bytes, int32_t *dev_status,
                      void *stream);
+
+/*
+ * Bytes of scratch of the fusion_cache_* calls on this cache (its shape and whether `weights` is NULL are read) with up to
+ * `heads` query heads, or 0 for a shape that they refuse; zero-filled before its first use, reusable without clearing, and
+ * not to be shared by calls that overlap (as fusion_workspace_size).  With weights it holds a float per query head and token.
+ */
+size_t fusion_cache_workspace_size(fusion_cache cache, int32_t heads);
+
+/*
+ * fusion_cache_append: the rows of a ragged batch go to the ends of their sequences.  Row r of sample i (n_i >= 0 rows)
+ * becomes position lengths[t] + r of sequence t, where t = in.ids[i], or i when in.ids is NULL: its keys and values, its
+ * size (sizes[row], 1 when sizes is NULL) and its accumulated weight so far (scores[row], 0 when NULL), the latter two
+ * where the cache keeps them.  Then lengths_out[t] = lengths[t] + n_i, and the lengths of the other sequences are copied;
+ * lengths_out may be the cache's own lengths.  (Apart from them, the rows are not yet part of the sequences: a caller can
+ * take them back by keeping the old lengths.)
+ * k, v: [in.max_rows, kv_heads, head_dim] with rows k_stride and v_stride elements apart (a packed projection's slices;
+ * any stride >= 0 that keeps rows 16-byte aligned), 16-byte aligned.  in.max_tokens has no upper bound here.
+ * Errors: FUSION_ERR_SHAPE for a cache shape out of range or in.max_batch > cache.max_batch; FUSION_ERR_INVALID_ARG for
+ * NULL or misaligned pointers or strides; FUSION_ERR_WORKSPACE.  Device bits, each of which leaves that sample out (and its
+ * sequence's length as it is): BAD_OFFSETS, BAD_IDS (an id outside [0, cache.max_batch), or two samples of one id), BAD_CACHE
+ * (a length out of range, a page id out of range among those written, no room); BAD_BATCH leaves all samples out.
+ */
+int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                        int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
+                        size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * fusion_cache_attention: the attention of one new token per sequence over its cache (its own key and value appended
+ * before).  For sequence b of length n, query head a (of key head h = a / (heads / kv_heads)):
+ *   x_j = scale q_a . k_hj + log s_j,   out[b, a, :] = sum_j softmax_j(x)_j v_hj
+ * over the visible tokens j with s_j > 0: all of them for window 0, else the first `sinks` and the last `window`.  A merged
+ * token of size s weighs like the s tokens that it replaced (as in fusion_attention); a token of size 0 has no part in the
+ * result, whatever its key and value hold.  No token left, or every x_j = -inf: the row is 0.  Where the cache keeps weights,
+ * weights_j += sum_a softmax_j(x_a) for the visible tokens, summed in float32 in the order of the heads.
+ * q: [max_batch, heads, head_dim], dtype, sequences q_stride elements apart (>= 0, rows 16-byte aligned), 16-byte aligned;
+ * out: [max_batch, heads, head_dim], dtype, 16-byte aligned.  heads: a multiple of kv_heads, at most
+ * FUSION_CACHE_MAX_HEADS.  scale: finite.  window, sinks: >= 0.  Logits, sums and the output are accumulated in float32; in
+ * bf16 the probabilities are rounded to bf16 (the operand of the second product) after their sum was taken.
+ * Errors: FUSION_ERR_SHAPE, FUSION_ERR_INVALID_ARG, FUSION_ERR_WORKSPACE; device bit BAD_CACHE (a length out of range, or the
+ * page id of a visible token: that sequence is not written).
+ */
+int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
+                           int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
+                           int32_t *dev_status, void *stream);
+
+/*
+ * fusion_cache_evict: prunes each sequence to its budget by accumulated attention weight.  A sequence of length n keeps
+ * m = min(max(budget[b], 0), n) tokens: the first s = min(sinks, m), the last r = min(recent, m - s), and the m - s - r of
+ * largest weight of those between (ties: lowest position).  The kept tokens, in ascending position, become positions
+ * 0 .. m - 1, with their keys, values, sizes and weights; lengths_out[b] = m, and keep_idx[b, i] is the old position of the
+ * new position i < m (the rest of the row is left as it is; positions that do not fit in a row are not stored; keep_idx may be NULL).
+ * page_table_out NULL or the cache's own: in place.  Otherwise [max_batch, max_pages_out] pages of the same pools, none of
+ * which holds a token of a sequence; the old pages are left as they are.  lengths_out may be the cache's own lengths.
+ * budget: [max_batch]; sinks, recent: >= 0; max_pages_out >= 1 (read only with page_table_out); keep_stride >= 1: elements
+ * of a keep_idx row.
+ * Errors: FUSION_ERR_SHAPE, FUSION_ERR_INVALID_ARG (also for a cache without weights), FUSION_ERR_WORKSPACE; device bits
+ * BAD_CACHE (a length or page id out of range, no room for m tokens) and NONFINITE (a NaN or infinite weight among those compared): that sequence
+ * is left as it is, and lengths_out, where it is not the cache's own, is 0.
+ */
+int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int32_t sinks, int32_t recent,
+                       const int32_t *page_table_out, int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx,
+                       int32_t keep_stride, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

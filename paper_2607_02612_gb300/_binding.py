@@ -29,6 +29,7 @@ FUSION_DEV_NONFINITE = 4
 FUSION_DEV_INTERNAL = 8
 FUSION_DEV_BAD_IDS = 16
 FUSION_DEV_TIMEOUT = 32
+FUSION_DEV_BAD_CACHE = 64
 FUSION_F32 = 0
 FUSION_BF16 = 1
 FUSION_STAGE_MERGE = 1
@@ -39,6 +40,10 @@ FUSION_FUSED_PLAN_MAX_BATCH = 1024
 FUSION_MAX_DIM = 1024
 FUSION_ATTN_HEAD_DIM = 64
 FUSION_ATTN_MAX_TOKENS = 1024
+FUSION_CACHE_MAX_BATCH = 65535
+FUSION_CACHE_MAX_PAGE_TOKENS = 1024
+FUSION_CACHE_MAX_HEAD_DIM = 256
+FUSION_CACHE_MAX_HEADS = 1024
 FUSION_POOL_CLS = 0
 FUSION_POOL_SPATIAL = 1
 
@@ -46,7 +51,8 @@ EXPORTED = ("fusion_status_string", "fusion_version", "fusion_profile_next", "fu
             "fusion_merge", "fusion_exit_check", "fusion_exit_check_noalloc", "fusion_prune", "fusion_compact",
             "fusion_stage", "fusion_merge_router", "fusion_token_scores", "fusion_exit_mlp_workspace_size",
             "fusion_exit_check_mlp", "fusion_attention", "fusion_stage_mlp",
-            "fusion_stage_mlp_workspace_size", "fusion_set_launch_gate")
+            "fusion_stage_mlp_workspace_size", "fusion_set_launch_gate", "fusion_cache_workspace_size",
+            "fusion_cache_append", "fusion_cache_attention", "fusion_cache_evict")
 
 
 class FusionError(RuntimeError):
@@ -70,6 +76,13 @@ class fusion_exit_head(ctypes.Structure):
     _fields_ = [("ln_gamma", ctypes.c_void_p), ("ln_beta", ctypes.c_void_p),
                 ("ln_eps", ctypes.c_float), ("weight", ctypes.c_void_p),
                 ("bias", ctypes.c_void_p), ("classes", ctypes.c_int32), ("tau", ctypes.c_float)]
+
+
+class fusion_cache(ctypes.Structure):
+    _fields_ = [("max_batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("page_tokens", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("num_pages", ctypes.c_int64),
+                ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("sizes", ctypes.c_void_p),
+                ("weights", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
 
 
 _lib = None
@@ -120,6 +133,14 @@ def load(path: Optional[str] = None):
     lib.fusion_attention.argtypes = [ctypes.c_int, R, V, I32, I32, V, V, V, V]
     lib.fusion_stage_mlp.argtypes = [ctypes.c_int, ctypes.c_int, R, V, I32, V, I32, V, V, V, V, fusion_mlp_head, V,
                                      V, V, V, V, V, V, V, V, V, V, V, SZ, V, V]
+    C = fusion_cache
+    lib.fusion_cache_workspace_size.argtypes = [C, I32]
+    lib.fusion_cache_workspace_size.restype = SZ
+    lib.fusion_cache_append.argtypes = [ctypes.c_int, C, R, V, I64, V, I64, V, V, V, V, SZ, V, V]
+    lib.fusion_cache_attention.argtypes = [ctypes.c_int, C, V, I64, I32, F, I32, I32, V, V, SZ, V, V]
+    lib.fusion_cache_evict.argtypes = [ctypes.c_int, C, V, I32, I32, V, I32, V, V, I32, V, SZ, V, V]
+    for name in ("fusion_cache_append", "fusion_cache_attention", "fusion_cache_evict"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("fusion_merge", "fusion_exit_check", "fusion_exit_check_noalloc", "fusion_prune",
                  "fusion_compact", "fusion_stage", "fusion_merge_router", "fusion_token_scores",
                  "fusion_exit_check_mlp", "fusion_attention", "fusion_stage_mlp",
@@ -167,6 +188,12 @@ def mlp_head(pool: int, gamma, beta, eps: float, w1, b1, hidden: int, w2, b2, cl
              tau: float) -> fusion_mlp_head:
     return fusion_mlp_head(int(pool), _ptr(gamma), _ptr(beta), float(eps), _ptr(w1), _ptr(b1), int(hidden),
                            _ptr(w2), _ptr(b2), int(classes), float(tau))
+
+
+def cache(max_batch: int, max_pages: int, page_tokens: int, kv_heads: int, head_dim: int, num_pages: int, k, v,
+          sizes, weights, page_table, lengths) -> fusion_cache:
+    return fusion_cache(int(max_batch), int(max_pages), int(page_tokens), int(kv_heads), int(head_dim), int(num_pages),
+                        _ptr(k), _ptr(v), _ptr(sizes), _ptr(weights), _ptr(page_table), _ptr(lengths))
 
 
 def check(rc: int) -> None:
@@ -309,3 +336,31 @@ def fusion_stage_mlp(dtype, flags, in_, x, dim, keys, key_dim, sizes, scores, r,
                                    _ptr(offsets_out), _ptr(ids_out), _ptr(batch_out), _ptr(keep_idx),
                                    _ptr(a_match), _ptr(workspace), int(workspace_bytes), _ptr(dev_status),
                                    _stream(stream))
+
+
+def fusion_cache_workspace_size(cache, heads: int) -> int:
+    return int(load().fusion_cache_workspace_size(cache, int(heads)))
+
+
+def fusion_cache_append(dtype, cache, in_, k, k_stride, v, v_stride, sizes, scores, lengths_out, workspace,
+                        workspace_bytes, dev_status, stream=None) -> int:
+    """Rows of a ragged batch to the ends of their cached sequences; k and v as addresses or contiguous tensors."""
+    return load().fusion_cache_append(int(dtype), cache, in_, _ptr(k), int(k_stride), _ptr(v), int(v_stride), _ptr(sizes),
+                                      _ptr(scores), _ptr(lengths_out), _ptr(workspace), int(workspace_bytes),
+                                      _ptr(dev_status), _stream(stream))
+
+
+def fusion_cache_attention(dtype, cache, q, q_stride, heads, scale, window, sinks, out, workspace, workspace_bytes,
+                           dev_status, stream=None) -> int:
+    """Attention of one new token per sequence over its cache; q as an address or a contiguous tensor."""
+    return load().fusion_cache_attention(int(dtype), cache, _ptr(q), int(q_stride), int(heads), float(scale), int(window),
+                                         int(sinks), _ptr(out), _ptr(workspace), int(workspace_bytes), _ptr(dev_status),
+                                         _stream(stream))
+
+
+def fusion_cache_evict(dtype, cache, budget, sinks, recent, page_table_out, max_pages_out, lengths_out, keep_idx,
+                       keep_stride, workspace, workspace_bytes, dev_status, stream=None) -> int:
+    """Prunes each cached sequence to its budget by accumulated attention weight."""
+    return load().fusion_cache_evict(int(dtype), cache, _ptr(budget), int(sinks), int(recent), _ptr(page_table_out),
+                                     int(max_pages_out), _ptr(lengths_out), _ptr(keep_idx), int(keep_stride),
+                                     _ptr(workspace), int(workspace_bytes), _ptr(dev_status), _stream(stream))

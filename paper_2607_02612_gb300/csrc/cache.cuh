@@ -1,0 +1,108 @@
+// What the kernels of the paged key-value cache share: the cache as the device sees it, the scratch they
+// carve from the caller's workspace, and the host's launchers.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include "common.cuh"
+
+namespace fz {
+
+// Row of token `place` of page `page` for key head h in the pools: (page * kv_heads + h) * page_tokens + place,
+// an unsigned 32-bit number (the host refuses pools of more rows); its bytes are rows * dim * element size apart.
+struct Cache {
+    int max_batch, max_pages, shift, kv_heads, dim;   // shift: log2 of page_tokens
+    unsigned num_pages;
+    int capacity;                   // max_pages * page_tokens
+    unsigned char *k, *v;
+    float *sizes, *weights;         // by slot: page * page_tokens + place; NULL: none
+    const int *table;
+    const int *lengths;
+};
+
+// The page that holds position pos of sequence b; false when its id is out of range.
+__device__ __forceinline__ bool cache_page(const Cache &c, int b, int pos, unsigned &page) {
+    page = (unsigned)c.table[(size_t)b * c.max_pages + (pos >> c.shift)];
+    return page < c.num_pages;
+}
+// Length of sequence b, or -1 when it is out of range.
+__device__ __forceinline__ int cache_length(const Cache &c, int b) {
+    const int n = c.lengths[b];
+    return n >= 0 && n <= c.capacity ? n : -1;
+}
+
+// Scratch behind the counters of the workspace.  Attention: log-sum-exps, partial results of sequences that
+// several CTAs share, logits (only where weights are accumulated).  Eviction: the kept slots and their counts.
+constexpr int kCacheMaxCtas = 512;   // CTAs of the attention kernel; each has two partial results at most
+constexpr int kCacheMaxQ = 32;       // query heads of a key head that one CTA takes
+struct CacheWs {
+    size_t counters, lse, part_ml, part, logits, keep, plan, total;
+    long long lstride;               // logits of one (sequence, head)
+};
+inline CacheWs cache_ws_layout(int max_batch, int max_pages, int page_tokens, int kv_heads, int dim, int heads, bool weights) {
+    const size_t b = max_batch > 0 ? max_batch : 1, cap = (size_t)max_pages * page_tokens;
+    const int group = heads / kv_heads, nq = group < 8 ? 8 : group < kCacheMaxQ ? (group + 7) / 8 * 8 : kCacheMaxQ;
+    CacheWs L;
+    L.lstride = (long long)((cap + 3) / 4 * 4);
+    L.counters = 0;
+    L.lse = align256(sizeof(int) * (size_t)kWsCounters);
+    L.part_ml = L.lse + align256(b * heads * 4);
+    L.part = L.part_ml + align256((size_t)2 * kCacheMaxCtas * nq * 8);
+    L.logits = L.part + align256((size_t)2 * kCacheMaxCtas * nq * dim * 4);
+    const size_t attn = L.logits + (weights ? align256(b * heads * (size_t)L.lstride * 4) : 0);
+    L.plan = L.lse;
+    L.keep = L.plan + align256(b * 8);
+    const size_t evict = weights ? L.keep + align256(b * cap * 4) : 0;
+    L.total = attn > evict ? attn : evict;
+    return L;
+}
+
+struct CacheAttnParams {
+    Cache c;
+    const void *q;
+    long long q_stride;    // elements between the sequences' queries
+    int heads, group;      // group: query heads of a key head
+    float scale2;          // scale * log2(e)
+    int window, sinks;     // window 0: every token is visible
+    int most;              // visible tokens of a sequence, at most
+    void *out;
+    float *lse;            // [max_batch, heads] base 2
+    float2 *part_ml;       // (maximum, sum) of the partial results' rows
+    float *part;
+    float *logits;         // base 2; NULL: no weights
+    long long lstride;
+    int *counters;
+    int *status;
+};
+cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStream_t s);
+
+struct CacheAppendParams {
+    Cache c;
+    Ragged in;
+    const unsigned char *k, *v;
+    long long k_stride, v_stride;   // bytes between rows
+    const float *sizes, *scores;
+    int *lengths_out;
+    int in_place;                   // lengths_out is the cache's own
+    int *counters;
+    int *status;
+};
+cudaError_t launch_cache_append(int dtype, const CacheAppendParams &p, cudaStream_t s);
+
+struct CacheEvictParams {
+    Cache c;
+    const int *budget;
+    int sinks, recent;
+    const int *table_out;
+    int pages_out;                  // entries of a row of table_out
+    int in_place;                   // table_out is the cache's own
+    int *lengths_out;
+    int *keep_idx;
+    int keep_stride;
+    int2 *plan;                     // [max_batch]: kept tokens (-1: leave the sequence), the first one that moves
+    unsigned *keep;                 // [max_batch, capacity] slots of the kept tokens
+    int *status;
+};
+cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_t s);
+
+}  // namespace fz

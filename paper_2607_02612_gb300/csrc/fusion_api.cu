@@ -5,6 +5,7 @@
 
 #include <cmath>
 
+#include "cache.cuh"
 #include "launch.h"
 
 namespace fz {
@@ -210,6 +211,7 @@ const char *fusion_status_string(int code) {
         case FUSION_DEV_INTERNAL: return "device: internal consistency check failed";
         case FUSION_DEV_BAD_IDS: return "device: sample id out of range";
         case FUSION_DEV_TIMEOUT: return "device: a bounded wait timed out";
+        case FUSION_DEV_BAD_CACHE: return "device: cache length or page id out of range, or no room";
         default: return "unknown status";
     }
 }
@@ -758,6 +760,173 @@ int fusion_stage_mlp(int dtype, int flags, fusion_ragged in, const void *x, int3
     return stage_impl(dtype, flags, in, x, dim, keys, key_dim, sizes, scores, r, rho, nullptr, &head, exit_mask, logits,
                       max_prob, x_out, sizes_out, scores_out, offsets_out, ids_out, batch_out, keep_idx, a_match,
                       workspace, workspace_bytes, dev_status, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// the paged key-value cache
+// ---------------------------------------------------------------------------
+namespace {
+int check_cache(const fusion_cache &c) {
+    if (c.max_batch < 0 || c.max_batch > FUSION_CACHE_MAX_BATCH) return FUSION_ERR_SHAPE;
+    if (c.page_tokens < 1 || c.page_tokens > FUSION_CACHE_MAX_PAGE_TOKENS || (c.page_tokens & (c.page_tokens - 1)))
+        return FUSION_ERR_SHAPE;
+    if (c.kv_heads < 1 || c.kv_heads > FUSION_CACHE_MAX_HEADS) return FUSION_ERR_SHAPE;
+    if (c.head_dim < 8 || c.head_dim > FUSION_CACHE_MAX_HEAD_DIM || c.head_dim % 8) return FUSION_ERR_SHAPE;
+    if (c.max_pages < 1 || (int64_t)c.max_pages * c.page_tokens > (1 << 30)) return FUSION_ERR_SHAPE;
+    if (c.num_pages < 1 || c.num_pages > 0xFFFFFFFFll / ((int64_t)c.kv_heads * c.page_tokens)) return FUSION_ERR_SHAPE;
+    return FUSION_OK;
+}
+
+int check_cache_pointers(const fusion_cache &c) {
+    if (!c.k || !c.v || !c.page_table || !c.lengths || !aligned16(c.k) || !aligned16(c.v)) return FUSION_ERR_INVALID_ARG;
+    return FUSION_OK;
+}
+
+int check_heads(const fusion_cache &c, int32_t heads) {
+    return heads >= c.kv_heads && heads <= FUSION_CACHE_MAX_HEADS && heads % c.kv_heads == 0 ? FUSION_OK : FUSION_ERR_SHAPE;
+}
+
+CacheWs cache_ws(const fusion_cache &c, int32_t heads) {
+    return cache_ws_layout(c.max_batch, c.max_pages, c.page_tokens, c.kv_heads, c.head_dim, heads, c.weights != nullptr);
+}
+
+int check_cache_ws(const void *ws, size_t bytes, size_t need) {
+    return ws && aligned16(ws) && bytes >= need ? FUSION_OK : FUSION_ERR_WORKSPACE;
+}
+
+int log2_of(int32_t v) {
+    int s = 0;
+    while ((1 << s) < v) ++s;
+    return s;
+}
+
+Cache dev(const fusion_cache &c) {
+    return Cache{c.max_batch, c.max_pages, log2_of(c.page_tokens), c.kv_heads, c.head_dim, (unsigned)c.num_pages,
+                 c.max_pages * c.page_tokens, static_cast<unsigned char *>(c.k), static_cast<unsigned char *>(c.v),
+                 c.sizes, c.weights, c.page_table, c.lengths};
+}
+
+// Rows `stride` elements apart, 16-byte aligned.
+bool good_stride(int dtype, int64_t stride) { return stride >= 0 && stride % (dtype == FUSION_BF16 ? 8 : 4) == 0; }
+}  // namespace
+
+extern "C" {
+
+size_t fusion_cache_workspace_size(fusion_cache cache, int32_t heads) {
+    if (check_cache(cache) != FUSION_OK || check_heads(cache, heads) != FUSION_OK) return 0;
+    return cache_ws(cache, heads).total;
+}
+
+int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                        int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
+                        size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_cache_pointers(cache));
+    if (!in.offsets) return FUSION_ERR_INVALID_ARG;
+    if (in.max_batch < 0 || in.max_batch > cache.max_batch || in.max_tokens < 1) return FUSION_ERR_SHAPE;
+    if (in.max_rows < 0 || in.max_rows > INT32_MAX) return FUSION_ERR_SHAPE;
+    if (!k || !v || !lengths_out || !aligned16(k) || !aligned16(v)) return FUSION_ERR_INVALID_ARG;
+    if (!good_stride(dtype, k_stride) || !good_stride(dtype, v_stride)) return FUSION_ERR_INVALID_ARG;
+    FZ_TRY(check_cache_ws(workspace, workspace_bytes, align256(sizeof(int) * (size_t)kWsCounters)));
+    const int es = dtype == FUSION_BF16 ? 2 : 4;
+    CacheAppendParams p{};
+    p.c = dev(cache);
+    p.in = dev(in);
+    p.k = static_cast<const unsigned char *>(k);
+    p.v = static_cast<const unsigned char *>(v);
+    p.k_stride = k_stride * es;
+    p.v_stride = v_stride * es;
+    p.sizes = sizes;
+    p.scores = scores;
+    p.lengths_out = lengths_out;
+    p.in_place = lengths_out == cache.lengths;
+    p.counters = static_cast<int *>(workspace);
+    p.status = dev_status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const ProfileEvents ev = take_profile();
+    record(ev.start, s);
+    record(ev.mid, s);
+    const int rc = cuda_rc(launch_cache_append(dtype, p, s));
+    record(ev.end, s);
+    return rc;
+}
+
+int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
+                           int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
+                           int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_heads(cache, heads));
+    FZ_TRY(check_cache_pointers(cache));
+    if (!q || !out || !aligned16(q) || !aligned16(out) || !good_stride(dtype, q_stride)) return FUSION_ERR_INVALID_ARG;
+    if (!std::isfinite(scale) || window < 0 || sinks < 0) return FUSION_ERR_INVALID_ARG;
+    const CacheWs L = cache_ws(cache, heads);
+    FZ_TRY(check_cache_ws(workspace, workspace_bytes, L.total));
+    unsigned char *wb = static_cast<unsigned char *>(workspace);
+    CacheAttnParams p{};
+    p.c = dev(cache);
+    p.q = q;
+    p.q_stride = q_stride;
+    p.heads = heads;
+    p.group = heads / cache.kv_heads;
+    p.scale2 = scale * 1.4426950408889634f;   // log2(e)
+    const int capacity = p.c.capacity;
+    p.window = window < capacity ? window : capacity;   // (their sum stays below 2^31)
+    p.sinks = sinks < capacity ? sinks : capacity;
+    p.most = p.window && p.window + p.sinks < capacity ? p.window + p.sinks : capacity;
+    p.out = out;
+    p.lse = reinterpret_cast<float *>(wb + L.lse);
+    p.part_ml = reinterpret_cast<float2 *>(wb + L.part_ml);
+    p.part = reinterpret_cast<float *>(wb + L.part);
+    p.logits = cache.weights ? reinterpret_cast<float *>(wb + L.logits) : nullptr;
+    p.lstride = L.lstride;
+    p.counters = reinterpret_cast<int *>(wb + L.counters);
+    p.status = dev_status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const ProfileEvents ev = take_profile();
+    record(ev.start, s);
+    record(ev.mid, s);
+    const int rc = cuda_rc(launch_cache_attention(dtype, p, s));
+    record(ev.end, s);
+    return rc;
+}
+
+int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int32_t sinks, int32_t recent,
+                       const int32_t *page_table_out, int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx,
+                       int32_t keep_stride, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_cache_pointers(cache));
+    if (!cache.weights || !budget || !lengths_out || sinks < 0 || recent < 0) return FUSION_ERR_INVALID_ARG;
+    if (keep_idx && keep_stride < 1) return FUSION_ERR_INVALID_ARG;
+    if (page_table_out && page_table_out != cache.page_table && max_pages_out < 1) return FUSION_ERR_SHAPE;
+    const CacheWs L = cache_ws(cache, cache.kv_heads);
+    FZ_TRY(check_cache_ws(workspace, workspace_bytes, L.total));
+    unsigned char *wb = static_cast<unsigned char *>(workspace);
+    CacheEvictParams p{};
+    p.c = dev(cache);
+    p.budget = budget;
+    p.sinks = sinks;
+    p.recent = recent;
+    p.in_place = !page_table_out || page_table_out == cache.page_table;
+    p.table_out = p.in_place ? cache.page_table : page_table_out;
+    p.pages_out = p.in_place ? cache.max_pages : max_pages_out;
+    p.lengths_out = lengths_out;
+    p.keep_idx = keep_idx;
+    p.keep_stride = keep_stride;
+    p.plan = reinterpret_cast<int2 *>(wb + L.plan);
+    p.keep = reinterpret_cast<unsigned *>(wb + L.keep);
+    p.status = dev_status;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const ProfileEvents ev = take_profile();
+    record(ev.start, s);
+    record(ev.mid, s);
+    const int rc = cuda_rc(launch_cache_evict(dtype, p, s));
+    record(ev.end, s);
+    return rc;
 }
 
 }  // extern "C"

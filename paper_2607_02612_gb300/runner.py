@@ -72,6 +72,105 @@ def device_batch(dtype: str, offsets, x, keys, sizes, scores, ids=None, max_toke
 
 
 @dataclass
+class RaggedRows:
+    """The samples that rows belong to, without the rows (a DeviceBatch describes its own in the same way)."""
+    max_batch: int
+    max_tokens: int
+    max_rows: int
+    offsets: torch.Tensor
+    batch: Optional[torch.Tensor] = None
+    ids: Optional[torch.Tensor] = None
+
+    def ragged(self) -> fb.fusion_ragged:
+        return fb.ragged(self.max_batch, self.max_tokens, self.max_rows, self.offsets, self.batch, self.ids)
+
+
+def _rows_ptr(t: torch.Tensor, rows: int, kv_heads: int, head_dim: int, dtype: str, device, what: str):
+    """Address and row stride of `rows` rows, [rows, heads * dim] or [rows, heads, dim], any stride between rows and
+    contiguous inside one."""
+    width = kv_heads * head_dim
+    flat = t.dim() == 2 and t.shape[1] == width and (t.stride(1) == 1 or width == 1)
+    split = t.dim() == 3 and tuple(t.shape[1:]) == (kv_heads, head_dim) and t.stride(2) == 1 and \
+        (t.stride(1) == head_dim or kv_heads == 1)
+    if t.dtype != TORCH_DTYPE[dtype] or t.device != device or not (flat or split) or t.shape[0] < rows:
+        raise fb.FusionError(f"{what}: at least {rows} {TORCH_DTYPE[dtype]} rows of {kv_heads} x {head_dim} elements on {device}, "
+                             "contiguous inside a row, expected")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+
+
+def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device, what: str, least: int = 0, dim: int = 1):
+    """t (None passes) is a contiguous tensor of this type on this device, of `dim` dimensions and at least `least` elements."""
+    if t is not None and (t.dtype != dtype or t.device != device or t.dim() != dim or t.numel() < least or
+                          not t.is_contiguous()):
+        raise fb.FusionError(f"{what}: a contiguous {dim}-dimensional {dtype} tensor of at least {least} elements on {device} "
+                             "expected")
+
+
+@dataclass
+class DeviceCache:
+    """A paged key-value cache on the device (fusion_cache) with the scratch of its calls, which also fixes the number
+    of query heads.  Calls on one cache that may overlap on the device (other streams) need a cache object each."""
+    dtype: str
+    heads: int
+    k: torch.Tensor            # [num_pages, kv_heads, page_tokens, head_dim]
+    v: torch.Tensor
+    page_table: torch.Tensor   # [max_batch, max_pages] int32
+    lengths: torch.Tensor      # [max_batch] int32
+    sizes: Optional[torch.Tensor] = None     # [num_pages, page_tokens] float32
+    weights: Optional[torch.Tensor] = None
+    workspace: Optional[torch.Tensor] = None
+    ws_bytes: int = 0
+
+    def __post_init__(self):
+        pages, kv_heads, page_tokens, dim = self.k.shape
+        ok = self.k.dtype == self.v.dtype == TORCH_DTYPE[self.dtype] and self.v.shape == self.k.shape
+        ok = ok and self.page_table.dim() == 2 and self.page_table.dtype == torch.int32
+        ok = ok and self.lengths.shape == self.page_table.shape[:1] and self.lengths.dtype == torch.int32
+        for t in (self.sizes, self.weights):
+            ok = ok and (t is None or (t.shape == (pages, page_tokens) and t.dtype == torch.float32))
+        ok = ok and all(t is None or t.device == self.k.device
+                        for t in (self.v, self.page_table, self.lengths, self.sizes, self.weights))
+        if not ok:
+            raise fb.FusionError("cache tensors of the wrong shape, type or device")
+        self.max_batch, self.max_pages = (int(n) for n in self.page_table.shape)
+        self.kv_heads, self.page_tokens, self.head_dim = int(kv_heads), int(page_tokens), int(dim)
+        self._c = fb.cache(self.max_batch, self.max_pages, page_tokens, kv_heads, dim, pages, self.k, self.v, self.sizes,
+                           self.weights, self.page_table, self.lengths)
+        self.ws_bytes = fb.fusion_cache_workspace_size(self._c, self.heads)
+        if self.ws_bytes == 0:
+            raise fb.FusionError("cache shape or number of heads out of range")
+        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.k.device)
+        self._one = None   # the offsets of one row per sequence
+
+    def c_struct(self) -> fb.fusion_cache:
+        return self._c
+
+    def one_row_each(self) -> RaggedRows:
+        if self._one is None:
+            self._one = RaggedRows(self.max_batch, 1, self.max_batch,
+                                   torch.arange(self.max_batch + 1, dtype=torch.int32, device=self.k.device))
+        return self._one
+
+
+def cache_of(dtype: str, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, heads: int,
+             sizes: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None) -> DeviceCache:
+    """A cache over the caller's pools, page table and lengths."""
+    return DeviceCache(dtype, int(heads), k, v, page_table, lengths, sizes, weights)
+
+
+def device_cache(dtype: str, max_batch: int, max_tokens: int, heads: int, kv_heads: int, head_dim: int, *,
+                 page_tokens: int = 16, sizes: bool = False, weights: bool = False, device="cuda") -> DeviceCache:
+    """An empty cache with room for max_tokens tokens in each sequence, its pages laid out one sequence after another."""
+    per = -(-max_tokens // page_tokens)
+    pages = max(1, max_batch * per)
+    pool = lambda: torch.zeros((pages, kv_heads, page_tokens, head_dim), dtype=TORCH_DTYPE[dtype], device=device)   # noqa: E731
+    per_token = lambda on: torch.zeros((pages, page_tokens), dtype=torch.float32, device=device) if on else None   # noqa: E731
+    table = torch.arange(max_batch * per, dtype=torch.int32, device=device).view(max_batch, per)
+    return DeviceCache(dtype, heads, pool(), pool(), table, torch.zeros(max_batch, dtype=torch.int32, device=device),
+                       per_token(sizes), per_token(weights))
+
+
+@dataclass
 class HeadTensors:
     gamma: torch.Tensor
     beta: torch.Tensor
@@ -208,6 +307,60 @@ class Fusion:
                                                     dtype=torch.bfloat16, device=self.device)
         fb.check(fb.fusion_attention(DTYPE_CODE["bf16"], b.ragged(), qkv, heads, fb.FUSION_ATTN_HEAD_DIM, sizes, o,
                                      self.status))
+        return o
+
+    def cache_append(self, c: DeviceCache, k: torch.Tensor, v: torch.Tensor, rows=None, *,
+                     sizes: Optional[torch.Tensor] = None, scores: Optional[torch.Tensor] = None,
+                     lengths_out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Appends the rows of k and v ([rows, kv_heads * head_dim], any stride between rows) to the sequences that `rows`
+        (a DeviceBatch or RaggedRows; None: one row per sequence) says; returns the new lengths (the cache's own, raised
+        in place, unless lengths_out is given)."""
+        rows = rows if rows is not None else c.one_row_each()
+        dev = c.k.device
+        kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.dtype, dev, "keys")
+        vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.dtype, dev, "values")
+        _need(sizes, torch.float32, dev, "sizes", rows.max_rows)
+        _need(scores, torch.float32, dev, "scores", rows.max_rows)
+        o = lengths_out if lengths_out is not None else c.lengths
+        _need(o, torch.int32, dev, "lengths_out", c.max_batch)
+        with torch.cuda.device(c.k.device):
+            fb.check(fb.fusion_cache_append(DTYPE_CODE[c.dtype], c.c_struct(), rows.ragged(), kp, ks, vp, vs, sizes, scores,
+                                            o, c.workspace, c.ws_bytes, self.status))
+        return o
+
+    def cache_attention(self, c: DeviceCache, q: torch.Tensor, *, scale: Optional[float] = None, window: int = 0,
+                        sinks: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Attention of one new token per sequence, q [max_batch, heads, head_dim] (any stride between sequences), over
+        the visible tokens of its cache; accumulates the weights where the cache keeps them.  scale None:
+        head_dim ** -0.5.  Returns [max_batch, heads, head_dim]."""
+        qp, qs = _rows_ptr(q, c.max_batch, c.heads, c.head_dim, c.dtype, c.k.device, "queries")
+        _need(out, TORCH_DTYPE[c.dtype], c.k.device, "out", c.max_batch * c.heads * c.head_dim, 3)
+        o = out if out is not None else torch.empty((c.max_batch, c.heads, c.head_dim), dtype=TORCH_DTYPE[c.dtype],
+                                                    device=c.k.device)
+        with torch.cuda.device(c.k.device):
+            fb.check(fb.fusion_cache_attention(DTYPE_CODE[c.dtype], c.c_struct(), qp, qs, c.heads,
+                                               c.head_dim ** -0.5 if scale is None else scale, window, sinks, o, c.workspace,
+                                               c.ws_bytes, self.status))
+        return o
+
+    def cache_evict(self, c: DeviceCache, budget: torch.Tensor, *, sinks: int = 0, recent: int = 0,
+                    page_table_out: Optional[torch.Tensor] = None, lengths_out: Optional[torch.Tensor] = None,
+                    keep_idx: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Prunes each sequence to budget[b] tokens by accumulated weight, in place or into other pages; keep_idx
+        [max_batch, n] receives the kept positions.  Returns the new lengths (the cache's own unless lengths_out is given)."""
+        o, dev = lengths_out if lengths_out is not None else c.lengths, c.k.device
+        _need(o, torch.int32, dev, "lengths_out", c.max_batch)
+        _need(budget, torch.int32, dev, "budget", c.max_batch)
+        _need(page_table_out, torch.int32, dev, "page_table_out", dim=2)
+        _need(keep_idx, torch.int32, dev, "keep_idx", dim=2)
+        for t, what in ((page_table_out, "page_table_out"), (keep_idx, "keep_idx")):
+            if t is not None and t.shape[0] < c.max_batch:
+                raise fb.FusionError(f"{what}: a row per sequence expected")
+        with torch.cuda.device(dev):
+            fb.check(fb.fusion_cache_evict(DTYPE_CODE[c.dtype], c.c_struct(), budget, sinks, recent, page_table_out,
+                                           page_table_out.shape[1] if page_table_out is not None else 0, o, keep_idx,
+                                           keep_idx.shape[1] if keep_idx is not None else 0, c.workspace, c.ws_bytes,
+                                           self.status))
         return o
 
     def exit_check(self, b: DeviceBatch, head: HeadTensors) -> Dict[str, torch.Tensor]:

@@ -1,0 +1,173 @@
+"""The key-value cache calls on the host: what they refuse before anything is enqueued, the workspace's size, the runner's
+checks; and the reference that the GPU tests compare with, against itself (no GPU needed)."""
+import itertools
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+
+import cache_reference as ref  # noqa: E402
+import paper_2607_02612_gb300 as fz  # noqa: E402
+from paper_2607_02612_gb300 import runner  # noqa: E402
+
+FAKE = 0x100000   # never dereferenced: every call below fails a host check first
+SHAPE = dict(max_batch=4, max_pages=10, page_tokens=16, kv_heads=2, head_dim=64, num_pages=40, k=FAKE, v=FAKE, sizes=None,
+             weights=FAKE, page_table=FAKE, lengths=FAKE)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def lib():
+    fz.build()
+
+
+def cache(**kw):
+    return fz.cache(**{**SHAPE, **kw})
+
+
+def size(heads=8, **kw):
+    return fz.fusion_cache_workspace_size(cache(**kw), heads)
+
+
+def append(c=None, **kw):
+    a = dict(dtype=fz.FUSION_BF16, cache=c if c is not None else cache(), in_=fz.ragged(4, 5000, 20000, FAKE), k=FAKE,
+             k_stride=128, v=FAKE, v_stride=128, sizes=None, scores=None, lengths_out=FAKE, workspace=FAKE,
+             workspace_bytes=size(), dev_status=FAKE, stream=0)
+    a.update(kw)
+    return fz.fusion_cache_append(*a.values())
+
+
+def attention(c=None, **kw):
+    a = dict(dtype=fz.FUSION_BF16, cache=c if c is not None else cache(), q=FAKE, q_stride=512, heads=8, scale=0.125, window=0,
+             sinks=0, out=FAKE, workspace=FAKE, workspace_bytes=size(), dev_status=FAKE, stream=0)
+    a.update(kw)
+    return fz.fusion_cache_attention(*a.values())
+
+
+def evict(c=None, **kw):
+    a = dict(dtype=fz.FUSION_BF16, cache=c if c is not None else cache(), budget=FAKE, sinks=1, recent=2, page_table_out=None,
+             max_pages_out=0, lengths_out=FAKE, keep_idx=None, keep_stride=0, workspace=FAKE, workspace_bytes=size(),
+             dev_status=FAKE, stream=0)
+    a.update(kw)
+    return fz.fusion_cache_evict(*a.values())
+
+
+BAD_SHAPES = [dict(max_batch=-1), dict(max_batch=fz.FUSION_CACHE_MAX_BATCH + 1), dict(page_tokens=0), dict(page_tokens=24),
+              dict(page_tokens=2 * fz.FUSION_CACHE_MAX_PAGE_TOKENS), dict(kv_heads=0), dict(head_dim=4), dict(head_dim=12),
+              dict(head_dim=fz.FUSION_CACHE_MAX_HEAD_DIM + 8), dict(max_pages=0), dict(max_pages=(1 << 26) + 1),
+              dict(num_pages=0), dict(num_pages=1 << 27), dict(num_pages=1 << 40)]
+
+
+@pytest.mark.parametrize("call", [append, attention, evict])
+def test_bad_shapes_are_refused(call):
+    for kw in BAD_SHAPES:
+        assert call(cache(**kw)) == fz.FUSION_ERR_SHAPE, kw
+        assert size(**kw) == 0, kw
+    for kw in (dict(k=None), dict(v=None), dict(page_table=None), dict(lengths=None), dict(k=FAKE + 8), dict(v=FAKE + 2)):
+        assert call(cache(**kw)) == fz.FUSION_ERR_INVALID_ARG, kw
+    assert call(dtype=2) == fz.FUSION_ERR_DTYPE
+    for kw in (dict(workspace=None), dict(workspace=FAKE + 8), dict(workspace_bytes=1000)):
+        assert call(**kw) == fz.FUSION_ERR_WORKSPACE, kw
+
+
+def test_append_rejects_bad_arguments():
+    for kw in (dict(in_=fz.ragged(5, 10, 100, FAKE)), dict(in_=fz.ragged(-1, 10, 100, FAKE)), dict(in_=fz.ragged(4, 0, 100, FAKE)),
+               dict(in_=fz.ragged(4, 10, -1, FAKE)), dict(in_=fz.ragged(4, 10, 1 << 31, FAKE))):
+        assert append(**kw) == fz.FUSION_ERR_SHAPE, kw
+    for kw in (dict(k=None), dict(v=None), dict(lengths_out=None), dict(k=FAKE + 4), dict(v=FAKE + 8), dict(k_stride=-128),
+               dict(v_stride=132), dict(in_=fz.ragged(4, 10, 100, None))):
+        assert append(**kw) == fz.FUSION_ERR_INVALID_ARG, kw
+    assert append(dtype=fz.FUSION_F32, k_stride=130) == fz.FUSION_ERR_INVALID_ARG
+
+
+def test_attention_rejects_bad_arguments():
+    for heads in (0, 1, 9, -2, fz.FUSION_CACHE_MAX_HEADS + 2):
+        assert attention(heads=heads) == fz.FUSION_ERR_SHAPE, heads
+        assert size(heads) == 0
+    for kw in (dict(q=None), dict(out=None), dict(q=FAKE + 2), dict(out=FAKE + 8), dict(q_stride=-8), dict(q_stride=516),
+               dict(scale=math.nan), dict(scale=math.inf), dict(window=-1), dict(sinks=-1)):
+        assert attention(**kw) == fz.FUSION_ERR_INVALID_ARG, kw
+    assert attention(workspace_bytes=size() - 1) == fz.FUSION_ERR_WORKSPACE
+    assert attention(heads=16, workspace_bytes=size(8)) == fz.FUSION_ERR_WORKSPACE
+
+
+def test_evict_rejects_bad_arguments():
+    assert evict(cache(weights=None)) == fz.FUSION_ERR_INVALID_ARG
+    for kw in (dict(budget=None), dict(lengths_out=None), dict(sinks=-1), dict(recent=-1), dict(keep_idx=FAKE, keep_stride=0)):
+        assert evict(**kw) == fz.FUSION_ERR_INVALID_ARG, kw
+    assert evict(page_table_out=FAKE + 64, max_pages_out=0) == fz.FUSION_ERR_SHAPE
+
+
+def test_workspace_size():
+    assert size() > 0 and size() % 256 == 0
+    assert size(16) > size(8) > size(8, weights=None)
+    assert size(max_pages=1000) > size()
+    assert size(max_batch=0) > 0
+
+
+def test_constants_and_status():
+    text = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "fusion.h")).read()
+    for name in ("FUSION_CACHE_MAX_BATCH", "FUSION_CACHE_MAX_PAGE_TOKENS", "FUSION_CACHE_MAX_HEAD_DIM", "FUSION_CACHE_MAX_HEADS",
+                 "FUSION_DEV_BAD_CACHE"):
+        assert f"#define {name} {getattr(fz, name)}" in text
+    assert "cache" in fz.fusion_status_string(fz.FUSION_DEV_BAD_CACHE)
+
+
+def test_runner_refuses_tensors_that_do_not_fit():
+    rows = lambda t, n, h=2, d=8, dtype="f32": runner._rows_ptr(t, n, h, d, dtype, torch.device("cpu"), "rows")   # noqa: E731
+    t = torch.zeros(4, 16)
+    assert rows(t, 4) == (t.data_ptr(), 16) and rows(t.view(4, 2, 8), 3)[1] == 16
+    packed = torch.zeros(4, 48)
+    assert rows(packed[:, 16:32], 4) == (packed.data_ptr() + 64, 48)
+    assert rows(packed[:, 16:32].unflatten(1, (2, 8)), 4)[1] == 48
+    for bad in (t[:3], t.double(), t.bfloat16(), torch.zeros(4, 8), torch.zeros(4, 32)[:, ::2], torch.zeros(4, 8, 2).transpose(1, 2),
+                torch.zeros(64), torch.zeros(4, 2, 16)[:, :, :8]):
+        with pytest.raises(fz.FusionError):
+            rows(bad, 4)
+    for bad in (torch.zeros(4), torch.zeros(3, dtype=torch.int32), torch.zeros(8, dtype=torch.int32)[::2],
+                torch.zeros(4, 1, dtype=torch.int32)):
+        with pytest.raises(fz.FusionError):
+            runner._need(bad, torch.int32, torch.device("cpu"), "lengths", 4)
+    pool, per, table, n = torch.zeros(6, 2, 16, 8), torch.zeros(6, 16), torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for bad in ((pool, pool[:5], table, n, None), (pool, pool, table.long(), n, None), (pool, pool, table, n[:2], None),
+                (pool, pool, table, n, per[:5]), (pool, pool.bfloat16(), table, n, None), (pool, pool, table[0], n, None)):
+        with pytest.raises(fz.FusionError):
+            runner.cache_of("f32", *bad[:4], heads=4, sizes=bad[4])
+
+
+# ---- the reference itself --------------------------------------------------------------------------------------------
+def test_reference_eviction_against_enumeration():
+    """The kept middle has the largest sum of weights, and of the sets with that sum the lexicographically smallest."""
+    g = torch.Generator().manual_seed(1)
+    for _ in range(60):
+        n = int(torch.randint(0, 9, (1,), generator=g))
+        w = (torch.randint(0, 4, (n,), generator=g) / 4).tolist()
+        budget, sinks, recent = (int(torch.randint(lo, 9, (1,), generator=g)) for lo in (-1, 0, 0))
+        m = min(max(budget, 0), n)
+        s = min(sinks, m)
+        r = min(recent, m - s)
+        best = max(itertools.combinations(range(s, n - r), m - s - r), key=lambda c: (sum(w[j] for j in c), [-j for j in c]))
+        assert ref.chosen(w, n, budget, sinks, recent) == [*range(s), *best, *range(n - r, n)]
+
+
+def test_reference_attention_of_merged_tokens():
+    """A token of size s weighs like s tokens of size 1, and one of size 0 like none."""
+    c = ref.make("f32", [6], 1, 8, 4, sizes="whole", weights=True, seed=2)
+    at = ref.places(c, 0, torch.arange(6))
+    c["sizes"][at] = torch.tensor([1.0, 3.0, 0.0, 2.0, 1.0, 1.0])
+    c["weights"][at] = 0.0
+    rep = torch.tensor([0, 1, 1, 1, 3, 3, 4, 5])
+    d = ref.make("f32", [8], 1, 8, 4, weights=True, seed=3)
+    to = ref.places(d, 0, torch.arange(8))
+    for name in ("k", "v"):
+        d[name][to[0], :, to[1]] = c[name][at[0][rep], :, at[1][rep]]
+    d["weights"][to] = 0.0
+    q = torch.randn(1, 3, 8)
+    a, _, wa, _ = ref.attention(c, q, "f32")
+    b, _, wb, _ = ref.attention(d, q, "f32")
+    assert torch.allclose(a, b, rtol=1e-12, atol=1e-14)
+    assert torch.allclose(wa[at], torch.zeros(6, dtype=torch.float64).index_add_(0, rep, wb[to]), rtol=1e-12, atol=1e-14)
+    assert abs(float(wb[to].sum()) - 3.0) < 1e-12     # the heads' probabilities

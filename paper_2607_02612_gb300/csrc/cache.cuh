@@ -41,7 +41,7 @@ struct CacheWs {
 };
 inline CacheWs cache_ws_layout(int max_batch, int max_pages, int page_tokens, int kv_heads, int dim, int heads, bool weights) {
     const size_t b = max_batch > 0 ? max_batch : 1, cap = (size_t)max_pages * page_tokens;
-    const int group = heads / kv_heads, nq = group < 8 ? 8 : group < kCacheMaxQ ? (group + 7) / 8 * 8 : kCacheMaxQ;
+    const int group = heads / kv_heads, nq = group <= 8 ? 8 : group <= 16 ? 16 : kCacheMaxQ;
     CacheWs L;
     L.lstride = (long long)((cap + 3) / 4 * 4);
     L.counters = 0;
@@ -74,6 +74,7 @@ struct CacheAttnParams {
     int *counters;
     int *status;
 };
+cudaError_t launch_cache_attention_bf16(const CacheAttnParams &p, cudaStream_t s);   // without the weights
 cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStream_t s);
 
 struct CacheAppendParams {

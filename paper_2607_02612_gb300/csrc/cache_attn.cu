@@ -9,119 +9,12 @@
 // warp takes TT tokens of each round through stages of its own (cp.async) and keeps its own running maximum, sum and
 // output.  Where a run ends with a (sequence, key head) the warps join in shared memory; a (sequence, key head) that
 // several runs share leaves partial results, which the last of its CTAs to arrive joins in the order of the runs.
-#include "cache.cuh"
+#include "cache_rounds.cuh"
 
 namespace fz {
 namespace {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
-constexpr int kMinRounds = 2;       // of a CTA: fewer and the join costs more than the split gains
-constexpr float kLow = -3.0e38f;    // a maximum over nothing: finite, so that (-inf) - kLow is -inf
-constexpr float kNoPage = 3.0e38f;  // in the place of a log2 size (at most 128): the token's page id is out of range
-
-__device__ __forceinline__ float ex2(float x) {   // 2^x, one MUFU instruction (2^-inf = 0)
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void *src, bool read) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
-}
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-// Visible tokens of a sequence of n tokens: the j-th is position j (j < sinks) or j + n - visible.
-__device__ __forceinline__ int visible(const CacheAttnParams &p, int n) {
-    return p.window ? min(n, p.window + p.sinks) : n;
-}
-
-// The batch's rounds (or tiles): every thread sums a run of sequences, a scan over the CTA gives the total; then the
-// sequence of the rounds' number `first` is found by the thread whose run holds it.
-template <int THREADS>
-struct Batch {
-    long long excl[THREADS / 32 + 1];
-    long long total;
-    int b;                // sequence of the first round
-    long long rem;        // and the rounds of that sequence before it
-};
-__device__ __forceinline__ long long rounds_of(const CacheAttnParams &p, int b, int tokens, int heads) {
-    const int n = cache_length(p.c, b);
-    return n <= 0 ? 0 : (long long)((visible(p, n) + tokens - 1) / tokens) * heads;
-}
-template <int THREADS>
-__device__ long long batch_total(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long &mine, long long &before) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = ceil_div(p.c.max_batch, THREADS), b0 = min(tid * per, p.c.max_batch), b1 = min(b0 + per, p.c.max_batch);
-    mine = 0;
-    for (int b = b0; b < b1; ++b) mine += rounds_of(p, b, tokens, heads);
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += v;
-    }
-    if (lane == 31) s.excl[warp] = incl;
-    __syncthreads();
-    if (tid == 0) {
-        long long t = 0;
-        for (int w = 0; w < THREADS / 32; ++w) {
-            const long long v = s.excl[w];
-            s.excl[w] = t;
-            t += v;
-        }
-        s.total = t;
-    }
-    __syncthreads();
-    before = s.excl[warp] + incl - mine;
-    return s.total;
-}
-template <int THREADS>
-__device__ void batch_find(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long mine, long long before, long long first) {
-    if (first >= before && first < before + mine) {
-        const int per = ceil_div(p.c.max_batch, THREADS);
-        long long at = before;
-        for (int b = threadIdx.x * per;; ++b) {
-            const long long r = rounds_of(p, b, tokens, heads);
-            if (first < at + r) {
-                s.b = b;
-                s.rem = first - at;
-                break;
-            }
-            at += r;
-        }
-    }
-    __syncthreads();
-}
-
-// Where in the batch a round lies.
-struct Place {
-    int b, vh, u;          // sequence, key head (times query chunk), round
-    int n, vis, rounds;    // length, visible tokens, rounds of one key head
-};
-__device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens) {
-    s.n = max(cache_length(p.c, s.b), 0);
-    s.vis = visible(p, s.n);
-    s.rounds = (s.vis + tokens - 1) / tokens;
-}
-__device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, int tokens, int vheads) {
-    if (++s.u < s.rounds) return;
-    s.u = 0;
-    if (++s.vh < vheads) return;
-    s.vh = 0;
-    do {
-        if (++s.b >= p.c.max_batch) {
-            s.rounds = s.vis = 0;
-            return;
-        }
-        place_sequence(p, s, tokens);
-    } while (s.rounds == 0);
-}
-
-// A token that a warp will load: its page (from the table, a round before its size) and place in it.
-struct Token {
-    unsigned page;
-    int place;       // -1: no token here
-    int vh;
-};
+using namespace rounds;
 
 // The CTA's shared memory: per warp and stage TT rows of K, TT rows of V; then the tokens' log2 sizes, the queries, the
 // warps' joined output.
@@ -149,81 +42,19 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Cache &c = p.c;
-    const int vheads = c.kv_heads * chunks, es = (int)sizeof(T);
-
-    // sequences without tokens: zeros (and a length out of range is told)
-    for (int b = blockIdx.x; b < c.max_batch; b += gridDim.x) {
-        const int n = cache_length(c, b);
-        if (n > 0) continue;
-        if (n < 0) {
-            if (tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
-            continue;
-        }
-        uint4 *o = reinterpret_cast<uint4 *>(p.out) + (size_t)b * p.heads * c.dim * es / 16;
-        for (int e = tid; e < p.heads * c.dim * es / 16; e += kThreads) o[e] = make_uint4(0u, 0u, 0u, 0u);
-    }
-
-    long long mine, before;
-    const long long total = batch_total(p, batch, kRound, vheads, mine, before);
-    const long long most = (total + kMinRounds - 1) / kMinRounds;
-    const int ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;   // that take part
-    if ((int)blockIdx.x >= ctas) return;
-    const long long r0 = total * blockIdx.x / ctas, r1 = total * (blockIdx.x + 1) / ctas;
-    batch_find(p, batch, kRound, vheads, mine, before, r0);
+    const int vheads = c.kv_heads * chunks;
+    empty_sequences<T>(p);
+    Run run;
     Place at;
-    at.b = batch.b;
-    place_sequence(p, at, kRound);
-    at.vh = (int)(batch.rem / at.rounds);
-    at.u = (int)(batch.rem % at.rounds);
-    Place ahead = at;          // of the token that load_token takes next
-    long long ahead_r = r0;
+    if (!find_run(p, batch, kRound, vheads, run, at)) return;
+    const long long r0 = run.r0, r1 = run.r1;
 
     unsigned char *stages = sm + warp * S * L::kStage;
     float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
     float *pw = reinterpret_cast<float *>(sm + L::kP) + warp * TT * NQ;
     float *qs = reinterpret_cast<float *>(sm + L::kQ);
     float *join = reinterpret_cast<float *>(sm + L::kJoin);
-    const int row_chunks = c.dim * es / 16;   // 16-byte chunks of a row that exist
-
-    // the page of this lane's token of the round `ahead`, then the next round
-    bool bad = false;
-    auto load_token = [&]() {
-        Token t;
-        t.place = -1;
-        t.page = 0;
-        t.vh = ahead.vh;
-        if (ahead_r < r1) {
-            const int j = ahead.u * kRound + warp * TT + lane;
-            if (lane < TT && j < ahead.vis) {
-                const int pos = p.window && j >= p.sinks ? j + ahead.n - ahead.vis : j;
-                if (cache_page(c, ahead.b, pos, t.page)) t.place = pos & ((1 << c.shift) - 1);
-                else t.place = -2;
-            }
-            ++ahead_r;
-            place_next(p, ahead, kRound, vheads);
-        }
-        return t;
-    };
-    auto load_size = [&](const Token &t) {
-        return t.place < 0 ? 0.0f : c.sizes ? c.sizes[((size_t)t.page << c.shift) + t.place] : 1.0f;
-    };
-    // the rows of a round into a stage; rows without a token (or of size zero) are zeros and weigh nothing
-    auto issue = [&](const Token &t, float size, int st) {
-        const unsigned row = ((t.page * (unsigned)c.kv_heads + (unsigned)(t.vh / chunks)) << c.shift) + (unsigned)t.place;
-        const unsigned live = __ballot_sync(0xFFFFFFFFu, t.place >= 0 && size != 0.0f);
-        if (lane < TT) lsz[st * TT + lane] = t.place == -2 ? kNoPage : t.place >= 0 && size != 0.0f ? log2f(size) : -INFINITY;
-        unsigned char *ks = stages + st * L::kStage, *vs = ks + TT * L::kRow;
-#pragma unroll
-        for (int e = 0; e < TT * kCpr / 32; ++e) {
-            const int x = e * 32 + lane, r = x / kCpr, cc = x % kCpr;
-            const unsigned rr = __shfl_sync(0xFFFFFFFFu, row, r);
-            const bool read = (live >> r & 1u) && cc < row_chunks;
-            const size_t off = read ? ((size_t)rr * row_chunks + cc) * 16 : 0;
-            const int sw = (r * kCpr + (cc ^ (((r & 1) << 2 | (r >> 1 & 3)) & (kCpr - 1)))) * 16;
-            cp_async16_zfill(smem_addr(ks + sw), c.k + off, read);
-            cp_async16_zfill(smem_addr(vs + sw), c.v + off, read);
-        }
-    };
+    auto swizzle = [](int r) { return ((r & 1) << 2 | (r >> 1 & 3)) & (kCpr - 1); };
     // the scaled queries of a (sequence, key head) as float32
     auto load_q = [&](int b, int vh, float *dst) {
         const int h = vh / chunks, ch = vh % chunks;
@@ -235,19 +66,17 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
         }
     };
 
-    Token t0 = load_token(), t1;
+    Stream<T, DP, TT> in;
+    in.begin(p, at, run, vheads, warp, lane);
 #pragma unroll
     for (int s = 0; s < S - 1; ++s) {
-        t1 = load_token();
-        issue(t0, load_size(t0), s);
+        in.issue(p, chunks, vheads, warp, lane, stages + s * L::kStage, lsz + s * TT, swizzle);
         cp_async_commit();
-        t0 = t1;
     }
-    t1 = load_token();
-    float size0 = load_size(t0);
     load_q(at.b, at.vh, qs);
     if (tid == 0) s_bad = 0;
     __syncthreads();
+    bool bad = false;
 
     float m[NQ], l[NQ], o[NQ][kD];
     auto reset = [&]() {
@@ -263,13 +92,10 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
     int st = 0, qpar = 0;
     long long seg0 = r0 - at.u;   // first round of the (sequence, key head)
     for (long long r = r0; r < r1; ++r) {
-        // ---- loads: rows of round r + S - 1, size of the one after, page of the one after that
         __syncwarp();
-        issue(t0, size0, st == 0 ? S - 1 : st - 1);
+        const int next_st = st == 0 ? S - 1 : st - 1;
+        in.issue(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
         cp_async_commit();
-        t0 = t1;
-        size0 = load_size(t0);
-        t1 = load_token();
         cp_async_wait<S - 1>();
         __syncwarp();
 
@@ -284,14 +110,14 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
             const int quad = lane & 3;
 #pragma unroll
             for (int k = 0; k < TT / 8; ++k) {
-                const int row = 8 * k + (lane >> 2), sw = (row & 1) << 2 | (row >> 1 & 3);
+                const int row = 8 * k + (lane >> 2), sw = swizzle(row);
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) x[k][q] = 0.0f;
 #pragma unroll
                 for (int i = 0; i < kCpr / 4; ++i) {
                     const int cc = 4 * i + quad;
                     float kv[kPer];
-                    chunk_to_f(*reinterpret_cast<const uint4 *>(ks + (row * kCpr + (cc ^ (sw & (kCpr - 1)))) * 16), kv);
+                    chunk_to_f(*reinterpret_cast<const uint4 *>(ks + (row * kCpr + (cc ^ sw)) * 16), kv);
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
 #pragma unroll
@@ -337,12 +163,12 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
             // ---- o += p v: every lane has kD dims
 #pragma unroll 4
             for (int row = 0; row < TT; ++row) {
-                const int sw = (row & 1) << 2 | (row >> 1 & 3), cc = lane * kD / kPer;
+                const int sw = swizzle(row), cc = lane * kD / kPer;
                 float v[kD];
 #pragma unroll
                 for (int d = 0; d < kD; ++d) {
                     const int cd = cc + d / kPer;
-                    v[d] = Elem<T>::to_f(reinterpret_cast<const T *>(vs + (row * kCpr + (cd ^ (sw & (kCpr - 1)))) * 16)[(lane * kD + d) % kPer]);
+                    v[d] = Elem<T>::to_f(reinterpret_cast<const T *>(vs + (row * kCpr + (cd ^ sw)) * 16)[(lane * kD + d) % kPer]);
                 }
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
@@ -410,39 +236,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
             }
             if (seg_bad && tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
             if (!whole) {
-                // the runs c0 .. c1 share it: the last one to arrive joins their results in order
-                auto run_of = [&](long long x) { return (int)(((x + 1) * ctas + total - 1) / total) - 1; };
-                const int c0 = run_of(seg0), c1 = run_of(seg0 + at.rounds - 1);
-                __threadfence();
-                __syncthreads();
-                if (tid == 0) {
-                    s_last = atomicAdd(&p.counters[c0], 1) == c1 - c0;
-                    if (s_last) p.counters[c0] = 0;
-                    __threadfence();
-                }
-                __syncthreads();
-                if (s_last) {
-                    for (int e = tid; e < nq * c.dim; e += kThreads) {
-                        const int q = e / c.dim, d = e % c.dim;
-                        float M = kLow, sum = 0.0f, ls = 0.0f;
-                        bool none = false;
-                        for (int k = c0; k <= c1; ++k) {
-                            const size_t ps = ((size_t)2 * k + (k == c0)) * NQ + q;
-                            const float2 ml = __ldcg(&p.part_ml[ps]);
-                            if (ml.y < 0.0f) {
-                                none = true;
-                                break;
-                            }
-                            const float mn = fmaxf(M, ml.x), f0 = ex2(M - mn), f1 = ex2(ml.x - mn);
-                            sum = sum * f0 + __ldcg(&p.part[ps * c.dim + d]) * f1;
-                            ls = ls * f0 + ml.y * f1;
-                            M = mn;
-                        }
-                        if (!none)
-                            reinterpret_cast<T *>(p.out)[((size_t)at.b * p.heads + head0 + q) * c.dim + d] = (T)(ls == 0.0f ? 0.0f : sum / ls);
-                        if (d == 0 && p.logits) p.lse[(size_t)at.b * p.heads + head0 + q] = none || ls == 0.0f ? INFINITY : M + log2f(ls);
-                    }
-                }
+                join_runs<T, NQ>(p, run, seg0, seg0 + at.rounds, (size_t)at.b * p.heads + head0, nq, s_last);
             }
             if (tid == 0) s_bad = 0;
             __syncthreads();
@@ -487,40 +281,26 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
     }
 }
 
-template <typename T, int DP, int NQ, int TT, int S>
+template <int DP, int NQ, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
-    using L = Layout<T, DP, NQ, TT, S>;
-    int dev = 0, sms = 0, occ = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_cache_attn<T, DP, NQ, TT, S>, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kTotal);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, k_cache_attn<T, DP, NQ, TT, S>, kThreads, L::kTotal);
-    if (e != cudaSuccess) return e;
-    const int chunks = ceil_div(p.group, NQ);
-    const long long rounds = (long long)p.c.max_batch * p.c.kv_heads * chunks * ceil_div(p.most, kWarps * TT);
-    long long ctas = (long long)sms * (occ < 1 ? 1 : occ);
-    if (ctas > kCacheMaxCtas) ctas = kCacheMaxCtas;
-    if (ctas > rounds) ctas = rounds;
-    k_cache_attn<T, DP, NQ, TT, S><<<(unsigned)(ctas < 1 ? 1 : ctas), kThreads, L::kTotal, s>>>(p, chunks);
-    return cudaGetLastError();
+    using L = Layout<float, DP, NQ, TT, S>;
+    return launch_rounds(k_cache_attn<float, DP, NQ, TT, S>, L::kTotal, p, ceil_div(p.group, NQ), kWarps * TT, s);
 }
-template <typename T, int NQ>
+template <int NQ>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {
-    constexpr int k = 4 / (int)sizeof(T);
-    if (p.c.dim <= 64) return launch<T, 64, NQ, 16 * k, 3>(p, s);
-    if (p.c.dim <= 128) return launch<T, 128, NQ, 8 * k, 3>(p, s);
-    return launch<T, 256, NQ, 8, 3>(p, s);
+    if (p.c.dim <= 64) return launch<64, NQ, 16, 3>(p, s);
+    if (p.c.dim <= 128) return launch<128, NQ, 8, 3>(p, s);
+    return launch<256, NQ, 8, 3>(p, s);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStream_t s) {
     if (p.c.max_batch == 0) return cudaSuccess;
-    cudaError_t e;
-    if (dtype == FUSION_BF16)
-        e = p.group == 1 ? launch_dim<__nv_bfloat16, 1>(p, s) : p.group <= 4 ? launch_dim<__nv_bfloat16, 4>(p, s) : launch_dim<__nv_bfloat16, 8>(p, s);
-    else
-        e = p.group == 1 ? launch_dim<float, 1>(p, s) : p.group <= 4 ? launch_dim<float, 4>(p, s) : launch_dim<float, 8>(p, s);
+    const cudaError_t e = dtype == FUSION_BF16 ? launch_cache_attention_bf16(p, s)
+                          : p.group == 1       ? launch_dim<1>(p, s)
+                          : p.group <= 4       ? launch_dim<4>(p, s)
+                                               : launch_dim<8>(p, s);
     if (e != cudaSuccess || !p.logits) return e;
     const long long tiles = (long long)p.c.max_batch * ceil_div(p.most, kWeightThreads);
     k_cache_weights<<<(unsigned)(tiles < 1216 ? tiles : 1216), kWeightThreads, 0, s>>>(p);

@@ -1,0 +1,359 @@
+// bf16 attention of one new token per sequence over the paged cache (the formulas and the cut into rounds: cache_attn.cu),
+// both products on the warp's matrix instruction m16n8k16.
+//
+// The tokens are the M rows and the query heads of a key head the N columns, so that a group of up to eight heads fills the
+// instruction's smallest N: S^T = K Q^T (A: 16 tokens x 16 dims of K as it lies, B: the queries), then O^T += V^T P^T (A: 16
+// dims x 16 tokens, V's rows read transposed, B: the probabilities, whose accumulator layout becomes the operand's by one 8 x 8
+// transposition per 8 tokens).  A lane's accumulators of both products belong to the same two heads, so the running maximum
+// and the rescaling need no exchange but the maximum over a column's tokens.
+//
+// What bounds it: memory.  A token's K and V of one key head, 4 dim bytes, give 4 dim group flops: for a group of 8, 8 flops
+// per byte where tensor cores break even near 280, so tcgen05's 128-row tiles would be idle all the same, with a round trip
+// through tensor memory between the products.
+#include "cache_rounds.cuh"
+
+namespace fz {
+namespace {
+
+using namespace rounds;
+
+__device__ __forceinline__ void ldsm_x4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                 : "r"(addr));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {   // an 8 x 8 matrix of b16, a row per four lanes
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+
+// Shared memory of a CTA: per warp S stages of TT rows of K and of V, the tokens' log2 sizes, the queries, and room for
+// the join of the warps' outputs, kJoinQ heads at a time.
+template <int DP, int NT, int TT, int S>
+struct Layout {
+    static constexpr int kNq = 8 * NT, kRow = 2 * DP, kStage = 2 * TT * kRow;
+    static constexpr int kJoinQ = NT < 4 ? 4 : 2, kPitch = DP + 4;
+    static constexpr int kLsz = kWarps * S * kStage;
+    static constexpr int kQ = kLsz + kWarps * S * TT * 4;
+    static constexpr int kJoin = kQ + kNq * kRow;
+    static constexpr int kTotal = kJoin + kWarps * kJoinQ * kPitch * 4;
+};
+
+template <int DP, int NT, int TT, int S>
+__global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, int chunks) {
+    using L = Layout<DP, NT, TT, S>;
+    constexpr int kNq = L::kNq, kRound = kWarps * TT, kRow = L::kRow, kKs = DP / 16, kMt = TT / 16;
+    constexpr int kQPer = (kNq * DP / 8 + kThreads - 1) / kThreads;   // 16-byte chunks of the queries per thread
+    constexpr bool kQRegs = NT * DP <= 256;                           // the queries' fragments stay in registers
+    extern __shared__ __align__(128) unsigned char sm[];
+    __shared__ Batch<kThreads> batch;
+    __shared__ float s_m[kWarps][kNq], s_l[kWarps][kNq];
+    __shared__ int s_bad, s_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const Cache &c = p.c;
+    const int vheads = c.kv_heads * chunks;
+    empty_sequences<__nv_bfloat16>(p);
+    Run run;
+    Place at;
+    if (!find_run(p, batch, kRound, vheads, run, at)) return;
+    const long long r0 = run.r0, r1 = run.r1;
+
+    unsigned char *stages = sm + warp * S * L::kStage, *qs = sm + L::kQ;
+    float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
+    float *join = reinterpret_cast<float *>(sm + L::kJoin);
+    auto swizzle = [](int r) { return r & 7; };
+
+    Stream<__nv_bfloat16, DP, TT> in;
+    in.begin(p, at, run, vheads, warp, lane);
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) {
+        in.issue(p, chunks, vheads, warp, lane, stages + s * L::kStage, lsz + s * TT, swizzle);
+        cp_async_commit();
+    }
+    // the queries of a (sequence, key head): read ahead into registers, then written to shared memory
+    uint4 qv[kQPer];
+    auto read_q = [&](int b, int vh) {
+        const int h = vh / chunks, ch = vh % chunks;
+        const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)b * p.q_stride + (size_t)(h * p.group + ch * kNq) * c.dim;
+#pragma unroll
+        for (int k = 0; k < kQPer; ++k) {
+            const int e = tid + k * kThreads, q = e / (DP / 8), cc = e % (DP / 8);
+            qv[k] = q < min(kNq, p.group - ch * kNq) && cc * 8 < c.dim ? *reinterpret_cast<const uint4 *>(src + (size_t)q * c.dim + cc * 8)
+                                                                     : make_uint4(0u, 0u, 0u, 0u);
+        }
+    };
+    auto write_q = [&]() {
+#pragma unroll
+        for (int k = 0; k < kQPer; ++k) {
+            const int e = tid + k * kThreads, q = e / (DP / 8), cc = e % (DP / 8);
+            if (q < kNq) *reinterpret_cast<uint4 *>(qs + q * kRow + ((cc ^ (q & 7)) << 4)) = qv[k];
+        }
+    };
+    read_q(at.b, at.vh);
+    write_q();
+    if (tid == 0) s_bad = 0;
+    __syncthreads();
+
+    float m[NT][2], l[NT][2], o[kKs][NT][4];
+    uint32_t qf[kQRegs ? kKs : 1][NT][2];
+    bool bad = false;
+    auto q_fragments = [&](int ks2, int n, uint32_t (&r)[4]) {   // of two steps of 16 dims
+        ldsm_x4(smem_addr(qs) + (8 * n + (lane & 7)) * kRow + (((4 * ks2 + (lane >> 3)) ^ (lane & 7)) << 4), r[0], r[1], r[2], r[3]);
+    };
+    auto begin_head = [&]() {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            m[n][0] = m[n][1] = kLow;
+            l[n][0] = l[n][1] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kKs; ++k) o[k][n][0] = o[k][n][1] = o[k][n][2] = o[k][n][3] = 0.0f;
+            if constexpr (kQRegs) {
+#pragma unroll
+                for (int k = 0; k < kKs; k += 2) {
+                    uint32_t r[4];
+                    q_fragments(k / 2, n, r);
+                    qf[k][n][0] = r[0];
+                    qf[k][n][1] = r[1];
+                    qf[k + 1][n][0] = r[2];
+                    qf[k + 1][n][1] = r[3];
+                }
+            }
+        }
+    };
+    begin_head();
+    int st = 0;
+    long long seg0 = r0 - at.u;   // first round of the (sequence, key head)
+    for (long long r = r0; r < r1; ++r) {
+        __syncwarp();
+        const int next_st = st == 0 ? S - 1 : st - 1;
+        in.issue(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
+        cp_async_commit();
+        cp_async_wait<S - 1>();
+        __syncwarp();
+
+        const uint32_t ks = smem_addr(stages + st * L::kStage), vs = ks + TT * kRow;
+        const float *lz = lsz + st * TT;
+        const int j0 = at.u * kRound + warp * TT;
+        const int h = at.vh / chunks, ch = at.vh % chunks, nq = min(kNq, p.group - ch * kNq), head0 = h * p.group + ch * kNq;
+        if (j0 < at.vis) {
+            // ---- S^T = K Q^T
+            float x[kMt][NT][4];
+#pragma unroll
+            for (int i = 0; i < kMt; ++i)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[i][n][0] = x[i][n][1] = x[i][n][2] = x[i][n][3] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kKs; k += 2) {
+                uint32_t b[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if constexpr (kQRegs) {
+                        b[n][0] = qf[k][n][0];
+                        b[n][1] = qf[k][n][1];
+                        b[n][2] = qf[k + 1][n][0];
+                        b[n][3] = qf[k + 1][n][1];
+                    } else {
+                        q_fragments(k / 2, n, b[n]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < kMt; ++i)
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk) {
+                        uint32_t a[4];
+                        ldsm_x4(ks + (16 * i + (lane & 15)) * kRow + (((2 * (k + kk) + (lane >> 4)) ^ (lane & 7)) << 4), a[0], a[1], a[2], a[3]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) mma_bf16_16816(x[i][n], a, b[n][2 * kk], b[n][2 * kk + 1]);
+                    }
+            }
+            // ---- logits in base 2; a masked token's are -inf
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+                const float z0 = lz[16 * i + g], z1 = lz[16 * i + 8 + g];
+                const bool off0 = z0 == -INFINITY || z0 == kNoPage, off1 = z1 == -INFINITY || z1 == kNoPage;
+                bad |= z0 == kNoPage || z1 == kNoPage;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    x[i][n][0] = off0 ? -INFINITY : fmaf(x[i][n][0], p.scale2, z0);
+                    x[i][n][1] = off0 ? -INFINITY : fmaf(x[i][n][1], p.scale2, z0);
+                    x[i][n][2] = off1 ? -INFINITY : fmaf(x[i][n][2], p.scale2, z1);
+                    x[i][n][3] = off1 ? -INFINITY : fmaf(x[i][n][3], p.scale2, z1);
+                }
+                if (p.logits) {
+                    float *dst = p.logits + ((size_t)at.b * p.heads + head0) * p.lstride + j0 + 16 * i + g;
+                    const bool in0 = j0 + 16 * i + g < at.vis, in1 = j0 + 16 * i + 8 + g < at.vis;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (8 * n + 2 * t + e < nq) {
+                                if (in0) dst[(8 * n + 2 * t + e) * p.lstride] = x[i][n][e];
+                                if (in1) dst[(8 * n + 2 * t + e) * p.lstride + 8] = x[i][n][2 + e];
+                            }
+                }
+            }
+            // ---- the running maximum grows: O and the sums follow
+            float mx[NT][2];
+            bool grows = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    mx[n][e] = m[n][e];
+#pragma unroll
+                    for (int i = 0; i < kMt; ++i) mx[n][e] = fmaxf(mx[n][e], fmaxf(x[i][n][e], x[i][n][2 + e]));
+                    grows |= mx[n][e] > m[n][e];
+                }
+            if (__any_sync(0xFFFFFFFFu, grows)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int s = 4; s < 32; s <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xFFFFFFFFu, mx[n][e], s));
+                        const float f = ex2(m[n][e] - mx[n][e]);
+                        m[n][e] = mx[n][e];
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int k = 0; k < kKs; ++k) {
+                            o[k][n][e] *= f;
+                            o[k][n][2 + e] *= f;
+                        }
+                    }
+            }
+            // ---- O^T += V^T P^T
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+                uint32_t b[NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float p0 = ex2(x[i][n][0] - m[n][0]), p1 = ex2(x[i][n][1] - m[n][1]);
+                    const float p2 = ex2(x[i][n][2] - m[n][0]), p3 = ex2(x[i][n][3] - m[n][1]);
+                    l[n][0] += p0 + p2;
+                    l[n][1] += p1 + p3;
+                    b[n][0] = transpose8(pack(p0, p1));
+                    b[n][1] = transpose8(pack(p2, p3));
+                }
+#pragma unroll
+                for (int k = 0; k < kKs; ++k) {
+                    uint32_t a[4];
+                    ldsm_x4_t(vs + (16 * i + (lane & 7) + ((lane >> 4) << 3)) * kRow + (((2 * k + (lane >> 3 & 1)) ^ (lane & 7)) << 4), a);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) mma_bf16_16816(o[k][n], a, b[n][0], b[n][1]);
+                }
+            }
+        }
+
+        // ---- the end of a (sequence, key head), or of the run: the warps' results together
+        if (at.u + 1 == at.rounds || r + 1 == r1) {
+            if (r + 1 < r1) {
+                Place next = at;
+                place_next(p, next, kRound, vheads);
+                read_q(next.b, next.vh);
+            }
+            if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(&s_bad, 1);
+            bad = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int s = 4; s < 32; s <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], s);
+                    if (g == 0) {
+                        s_m[warp][8 * n + 2 * t + e] = m[n][e];
+                        s_l[warp][8 * n + 2 * t + e] = l[n][e];
+                    }
+                }
+            __syncthreads();
+            write_q();   // every warp is past its products with the old ones
+            const bool whole = seg0 >= r0 && seg0 + at.rounds <= r1, seg_bad = s_bad != 0;
+            const int slot = 2 * blockIdx.x + (seg0 >= r0 ? 1 : 0);   // of a partial result
+            const size_t head = (size_t)at.b * p.heads + head0;
+            float f[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float M = s_m[0][8 * n + 2 * t + e];
+#pragma unroll
+                    for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][8 * n + 2 * t + e]);
+                    f[n][e] = ex2(m[n][e] - M);
+                }
+#pragma unroll
+            for (int q1 = 0; q1 < kNq; q1 += L::kJoinQ) {
+                if (q1 >= nq) break;
+                if (2 * t >= q1 % 8 && 2 * t < q1 % 8 + L::kJoinQ) {
+                    float *dst = join + (warp * L::kJoinQ + 2 * t - q1 % 8) * L::kPitch + g;
+#pragma unroll
+                    for (int k = 0; k < kKs; ++k) {
+                        dst[16 * k] = o[k][q1 / 8][0] * f[q1 / 8][0];
+                        dst[16 * k + L::kPitch] = o[k][q1 / 8][1] * f[q1 / 8][1];
+                        dst[16 * k + 8] = o[k][q1 / 8][2] * f[q1 / 8][0];
+                        dst[16 * k + 8 + L::kPitch] = o[k][q1 / 8][3] * f[q1 / 8][1];
+                    }
+                }
+                __syncthreads();
+                for (int e = tid; e < L::kJoinQ * DP / 4; e += kThreads) {
+                    const int qq = e / (DP / 4), q = q1 + qq, d = e % (DP / 4) * 4;
+                    if (q >= nq || d >= c.dim) continue;
+                    float M = s_m[0][q], ls = 0.0f;
+#pragma unroll
+                    for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
+                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) {
+                        ls += s_l[w][q] * ex2(s_m[w][q] - M);
+                        const float4 v = *reinterpret_cast<const float4 *>(join + (w * L::kJoinQ + qq) * L::kPitch + d);
+                        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+                    }
+                    if (whole) {
+                        const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+                        if (!seg_bad)
+                            *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + (head + q) * c.dim + d) =
+                                ls == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack(sum.x * inv, sum.y * inv), pack(sum.z * inv, sum.w * inv));
+                        if (d == 0 && p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+                    } else {
+                        *reinterpret_cast<float4 *>(p.part + ((size_t)slot * kNq + q) * c.dim + d) = sum;
+                        if (d == 0) p.part_ml[(size_t)slot * kNq + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                    }
+                }
+                __syncthreads();
+            }
+            if (seg_bad && tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
+            if (!whole) join_runs<__nv_bfloat16, kNq>(p, run, seg0, seg0 + at.rounds, head, nq, s_last);
+            __syncthreads();
+            if (tid == 0) s_bad = 0;
+            __syncthreads();
+            begin_head();
+            seg0 = r + 1;
+        }
+        place_next(p, at, kRound, vheads);
+        if (++st == S) st = 0;
+    }
+    cp_async_wait<0>();
+}
+
+template <int DP, int NT, int TT, int S>
+cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
+    using L = Layout<DP, NT, TT, S>;
+    return launch_rounds(k_cache_attn_mma<DP, NT, TT, S>, L::kTotal, p, ceil_div(p.group, 8 * NT), kWarps * TT, s);
+}
+template <int NT>
+cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {
+    if (p.c.dim <= 64) return launch<64, NT, 32, 3>(p, s);
+    if (p.c.dim <= 128) return launch<128, NT, 16, 3>(p, s);
+    return launch<256, NT < 2 ? NT : 2, 16, 3>(p, s);   // (four would need more registers than a thread has)
+}
+
+}  // namespace
+
+cudaError_t launch_cache_attention_bf16(const CacheAttnParams &p, cudaStream_t s) {
+    return p.group <= 8 ? launch_dim<1>(p, s) : p.group <= 16 ? launch_dim<2>(p, s) : launch_dim<4>(p, s);
+}
+
+}  // namespace fz

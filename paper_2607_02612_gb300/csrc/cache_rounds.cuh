@@ -1,0 +1,272 @@
+// What the attention kernels over the paged cache share: the batch cut into rounds of equal runs per CTA, the tokens of a
+// round on their way into shared memory, and the join of runs that share a (sequence, key head).
+#pragma once
+
+#include "cache.cuh"
+
+namespace fz {
+namespace rounds {
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kMinRounds = 2;       // of a CTA: fewer and the join costs more than the split gains
+constexpr float kLow = -3.0e38f;    // a maximum over nothing: finite, so that (-inf) - kLow is -inf
+constexpr float kNoPage = 3.0e38f;  // in the place of a log2 size (at most 128): the token's page id is out of range
+
+__device__ __forceinline__ float ex2(float x) {   // 2^x, one MUFU instruction (2^-inf = 0)
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void *src, bool read) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
+}
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+// Visible tokens of a sequence of n tokens: the j-th is position j (j < sinks) or j + n - visible.
+__device__ __forceinline__ int visible(const CacheAttnParams &p, int n) {
+    return p.window ? min(n, p.window + p.sinks) : n;
+}
+
+// The batch's rounds (or tiles): every thread sums a run of sequences, a scan over the CTA gives the total; then the
+// sequence of the rounds' number `first` is found by the thread whose run holds it.
+template <int THREADS>
+struct Batch {
+    long long excl[THREADS / 32 + 1];
+    long long total;
+    int b;                // sequence of the first round
+    long long rem;        // and the rounds of that sequence before it
+};
+__device__ __forceinline__ long long rounds_of(const CacheAttnParams &p, int b, int tokens, int heads) {
+    const int n = cache_length(p.c, b);
+    return n <= 0 ? 0 : (long long)((visible(p, n) + tokens - 1) / tokens) * heads;
+}
+template <int THREADS>
+__device__ long long batch_total(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long &mine, long long &before) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = ceil_div(p.c.max_batch, THREADS), b0 = min(tid * per, p.c.max_batch), b1 = min(b0 + per, p.c.max_batch);
+    mine = 0;
+    for (int b = b0; b < b1; ++b) mine += rounds_of(p, b, tokens, heads);
+    long long incl = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+    }
+    if (lane == 31) s.excl[warp] = incl;
+    __syncthreads();
+    if (tid == 0) {
+        long long t = 0;
+        for (int w = 0; w < THREADS / 32; ++w) {
+            const long long v = s.excl[w];
+            s.excl[w] = t;
+            t += v;
+        }
+        s.total = t;
+    }
+    __syncthreads();
+    before = s.excl[warp] + incl - mine;
+    return s.total;
+}
+template <int THREADS>
+__device__ void batch_find(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long mine, long long before, long long first) {
+    if (first >= before && first < before + mine) {
+        const int per = ceil_div(p.c.max_batch, THREADS);
+        long long at = before;
+        for (int b = threadIdx.x * per;; ++b) {
+            const long long r = rounds_of(p, b, tokens, heads);
+            if (first < at + r) {
+                s.b = b;
+                s.rem = first - at;
+                break;
+            }
+            at += r;
+        }
+    }
+    __syncthreads();
+}
+
+// Where in the batch a round lies.
+struct Place {
+    int b, vh, u;          // sequence, key head (times query chunk), round
+    int n, vis, rounds;    // length, visible tokens, rounds of one key head
+};
+__device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens) {
+    s.n = max(cache_length(p.c, s.b), 0);
+    s.vis = visible(p, s.n);
+    s.rounds = (s.vis + tokens - 1) / tokens;
+}
+__device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, int tokens, int vheads) {
+    if (++s.u < s.rounds) return;
+    s.u = 0;
+    if (++s.vh < vheads) return;
+    s.vh = 0;
+    do {
+        if (++s.b >= p.c.max_batch) {
+            s.rounds = s.vis = 0;
+            return;
+        }
+        place_sequence(p, s, tokens);
+    } while (s.rounds == 0);
+}
+
+// The run of rounds of this CTA.
+struct Run {
+    long long total, r0, r1;   // rounds of the batch; this CTA's
+    int ctas;                  // that take part
+    // the run that holds round x (run k begins at total * k / ctas)
+    __device__ __forceinline__ int of(long long x) const { return (int)(((x + 1) * ctas + total - 1) / total) - 1; }
+};
+
+// A token that a warp will load: its page (from the table, a round before its size) and place in it.
+struct Token {
+    unsigned page;
+    int place;       // -1: no token here
+    int vh;
+};
+
+// Tokens of the rounds to come, a warp's share of TT per round: the page is read two rounds before the token's rows are
+// asked for, the size one round before.  Rows without a token, or of size zero, arrive as zeros and weigh nothing (log2
+// size -inf), whatever the cache holds there.
+template <typename T, int DP, int TT>
+struct Stream {
+    static constexpr int kRow = DP * (int)sizeof(T), kCpr = kRow / 16, kStage = 2 * TT * kRow, kRound = kWarps * TT;
+    Place ahead;             // of the next token to look up
+    long long ahead_r, r1;
+    Token t0, t1;            // t0's rows are asked for next (its size is here), then t1's
+    float size0;
+
+    __device__ __forceinline__ Token look_up(const CacheAttnParams &p, int vheads, int warp, int lane) {
+        Token t{0u, -1, ahead.vh};
+        if (ahead_r < r1) {
+            const int j = ahead.u * kRound + warp * TT + lane;
+            if (lane < TT && j < ahead.vis) {
+                const int pos = p.window && j >= p.sinks ? j + ahead.n - ahead.vis : j;
+                t.place = cache_page(p.c, ahead.b, pos, t.page) ? pos & ((1 << p.c.shift) - 1) : -2;
+            }
+            ++ahead_r;
+            place_next(p, ahead, kRound, vheads);
+        }
+        return t;
+    }
+    __device__ __forceinline__ float size_of(const CacheAttnParams &p, const Token &t) const {
+        return t.place < 0 ? 0.0f : p.c.sizes ? p.c.sizes[((size_t)t.page << p.c.shift) + t.place] : 1.0f;
+    }
+    // Asks for t0's rows (K, then V, rows of kRow bytes with chunk c of row r at c ^ swizzle(r)) and moves on.
+    template <typename Swizzle>
+    __device__ __forceinline__ void issue(const CacheAttnParams &p, int chunks, int vheads, int warp, int lane, unsigned char *stage,
+                                          float *lsz, Swizzle swizzle) {
+        const int row_chunks = p.c.dim * (int)sizeof(T) / 16;   // that exist
+        const unsigned row = ((t0.page * (unsigned)p.c.kv_heads + (unsigned)(t0.vh / chunks)) << p.c.shift) + (unsigned)t0.place;
+        const bool live = t0.place >= 0 && size0 != 0.0f;
+        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live);
+        if (lane < TT) lsz[lane] = t0.place == -2 ? kNoPage : live ? log2f(size0) : -INFINITY;
+#pragma unroll
+        for (int e = 0; e < TT * kCpr / 32; ++e) {
+            const int x = e * 32 + lane, r = x / kCpr, cc = x % kCpr;
+            const unsigned rr = __shfl_sync(0xFFFFFFFFu, row, r);
+            const bool read = (lives >> r & 1u) && cc < row_chunks;
+            const size_t off = read ? ((size_t)rr * row_chunks + cc) * 16 : 0;
+            const uint32_t dst = smem_addr(stage) + (r * kCpr + (cc ^ swizzle(r))) * 16;
+            cp_async16_zfill(dst, p.c.k + off, read);
+            cp_async16_zfill(dst + TT * kRow, p.c.v + off, read);
+        }
+        t0 = t1;
+        size0 = size_of(p, t0);
+        t1 = look_up(p, vheads, warp, lane);
+    }
+    __device__ __forceinline__ void begin(const CacheAttnParams &p, const Place &at, const Run &run, int vheads, int warp, int lane) {
+        ahead = at;
+        ahead_r = run.r0;
+        r1 = run.r1;
+        t0 = look_up(p, vheads, warp, lane);
+        t1 = look_up(p, vheads, warp, lane);
+        size0 = size_of(p, t0);
+    }
+};
+
+// Zeros for sequences without tokens (a length out of range is told, its row left), dealt out over the grid.
+template <typename T>
+__device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
+    const int row = p.heads * p.c.dim * (int)sizeof(T) / 16;
+    for (int b = blockIdx.x; b < p.c.max_batch; b += gridDim.x) {
+        const int n = cache_length(p.c, b);
+        if (n > 0) continue;
+        if (n < 0) {
+            if (threadIdx.x == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
+            continue;
+        }
+        uint4 *o = reinterpret_cast<uint4 *>(p.out) + (size_t)b * row;
+        for (int e = threadIdx.x; e < row; e += kThreads) o[e] = make_uint4(0u, 0u, 0u, 0u);
+    }
+}
+
+// This CTA's run and where it begins; false: it has none.
+__device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThreads> &s, int tokens, int vheads, Run &run, Place &at) {
+    long long mine, before;
+    run.total = batch_total(p, s, tokens, vheads, mine, before);
+    const long long most = (run.total + kMinRounds - 1) / kMinRounds;
+    run.ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
+    if ((int)blockIdx.x >= run.ctas) return false;
+    run.r0 = run.total * blockIdx.x / run.ctas;
+    run.r1 = run.total * (blockIdx.x + 1) / run.ctas;
+    batch_find(p, s, tokens, vheads, mine, before, run.r0);
+    at.b = s.b;
+    place_sequence(p, at, tokens);
+    at.vh = (int)(s.rem / at.rounds);
+    at.u = (int)(s.rem % at.rounds);
+    return true;
+}
+
+// After a CTA has written its partial result of the (sequence, key head) of rounds [seg0, seg1): the last of the runs that
+// share it joins their results in order.  Result k lies in slot 2 k + 1 where the (sequence, key head) begins in run k, else in
+// slot 2 k; a sum below zero marks one with a bad page.
+template <typename T, int NQ>
+__device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, long long seg0, long long seg1, size_t head, int nq,
+                                          int &s_last) {
+    const int c0 = run.of(seg0), c1 = run.of(seg1 - 1), tid = threadIdx.x, dim = p.c.dim;
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) {
+        s_last = atomicAdd(&p.counters[c0], 1) == c1 - c0;
+        if (s_last) p.counters[c0] = 0;
+        __threadfence();
+    }
+    __syncthreads();
+    if (!s_last) return;
+    for (int e = tid; e < nq * dim; e += kThreads) {
+        const int q = e / dim, d = e % dim;
+        float M = kLow, sum = 0.0f, ls = 0.0f;
+        bool none = false;
+        for (int k = c0; k <= c1; ++k) {
+            const size_t ps = ((size_t)2 * k + (k == c0)) * NQ + q;
+            const float2 ml = __ldcg(&p.part_ml[ps]);
+            none |= ml.y < 0.0f;
+            const float mn = fmaxf(M, ml.x), f0 = ex2(M - mn), f1 = ex2(ml.x - mn);
+            sum = sum * f0 + __ldcg(&p.part[ps * dim + d]) * f1;
+            ls = ls * f0 + ml.y * f1;
+            M = mn;
+        }
+        if (!none) reinterpret_cast<T *>(p.out)[(head + q) * dim + d] = (T)(ls == 0.0f ? 0.0f : sum / ls);
+        if (d == 0 && p.logits) p.lse[head + q] = none || ls == 0.0f ? INFINITY : M + log2f(ls);
+    }
+}
+
+// Host: as many CTAs as the GPU holds at once, or as there can be rounds.
+template <typename Kernel>
+cudaError_t launch_rounds(Kernel *kernel, int smem, const CacheAttnParams &p, int chunks, int tokens, cudaStream_t s) {
+    int dev = 0, sms = 0, occ = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kernel, kThreads, smem);
+    if (e != cudaSuccess) return e;
+    const long long rounds = (long long)p.c.max_batch * p.c.kv_heads * chunks * ceil_div(p.most, tokens);
+    long long ctas = (long long)sms * (occ < 1 ? 1 : occ);
+    if (ctas > kCacheMaxCtas) ctas = kCacheMaxCtas;
+    if (ctas > rounds) ctas = rounds;
+    kernel<<<(unsigned)(ctas < 1 ? 1 : ctas), kThreads, smem, s>>>(p, chunks);
+    return cudaGetLastError();
+}
+
+}  // namespace rounds
+}  // namespace fz

@@ -284,7 +284,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
 template <int DP, int NQ, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
     using L = Layout<float, DP, NQ, TT, S>;
-    return launch_rounds(k_cache_attn<float, DP, NQ, TT, S>, L::kTotal, p, ceil_div(p.group, NQ), kWarps * TT, s);
+    return launch_rounds<k_cache_attn<float, DP, NQ, TT, S>>(L::kTotal, p, ceil_div(p.group, NQ), kWarps * TT, s);
 }
 template <int NQ>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {

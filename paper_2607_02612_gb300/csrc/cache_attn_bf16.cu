@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
 template <int DP, int NT, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
     using L = Layout<DP, NT, TT, S>;
-    return launch_rounds(k_cache_attn_mma<DP, NT, TT, S>, L::kTotal, p, ceil_div(p.group, 8 * NT), kWarps * TT, s);
+    return launch_rounds<k_cache_attn_mma<DP, NT, TT, S>>(L::kTotal, p, ceil_div(p.group, 8 * NT), kWarps * TT, s);
 }
 template <int NT>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {

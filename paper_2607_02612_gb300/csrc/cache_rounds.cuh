@@ -2,6 +2,8 @@
 // round on their way into shared memory, and the join of runs that share a (sequence, key head).
 #pragma once
 
+#include <atomic>
+
 #include "cache.cuh"
 
 namespace fz {
@@ -251,20 +253,34 @@ __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &r
     }
 }
 
-// Host: as many CTAs as the GPU holds at once, or as there can be rounds.
-template <typename Kernel>
-cudaError_t launch_rounds(Kernel *kernel, int smem, const CacheAttnParams &p, int chunks, int tokens, cudaStream_t s) {
-    int dev = 0, sms = 0, occ = 0;
+// Host: as many CTAs as the GPU holds at once, or as there can be rounds.  What depends on the kernel and the device alone is
+// asked once (asking costs the host 4 us a call).
+template <auto Kernel>
+cudaError_t resident_ctas(int smem, int &ctas) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
+    int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
-    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, kernel, kThreads, smem);
+    if (e != cudaSuccess) return e;
+    ctas = dev < kDevices ? known[dev].load(std::memory_order_acquire) : 0;
+    if (ctas > 0) return cudaSuccess;
+    int sms = 0, occ = 0;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, Kernel, kThreads, smem);
+    if (e != cudaSuccess) return e;
+    ctas = sms * (occ < 1 ? 1 : occ);
+    if (dev < kDevices) known[dev].store(ctas, std::memory_order_release);
+    return cudaSuccess;
+}
+template <auto Kernel>
+cudaError_t launch_rounds(int smem, const CacheAttnParams &p, int chunks, int tokens, cudaStream_t s) {
+    int ctas = 0;
+    const cudaError_t e = resident_ctas<Kernel>(smem, ctas);
     if (e != cudaSuccess) return e;
     const long long rounds = (long long)p.c.max_batch * p.c.kv_heads * chunks * ceil_div(p.most, tokens);
-    long long ctas = (long long)sms * (occ < 1 ? 1 : occ);
     if (ctas > kCacheMaxCtas) ctas = kCacheMaxCtas;
-    if (ctas > rounds) ctas = rounds;
-    kernel<<<(unsigned)(ctas < 1 ? 1 : ctas), kThreads, smem, s>>>(p, chunks);
+    Kernel<<<(unsigned)(ctas < rounds ? ctas : rounds), kThreads, smem, s>>>(p, chunks);
     return cudaGetLastError();
 }
 

@@ -4,6 +4,7 @@ every step of the computation runs in libfusion.so.
 """
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass, field
 from typing import Dict, List, Optional
 
@@ -71,7 +72,7 @@ def device_batch(dtype: str, offsets, x, keys, sizes, scores, ids=None, max_toke
         ids=None if ids is None else torch.from_numpy(np.asarray(ids, np.int32)).to(device))
 
 
-@dataclass
+@dataclass(frozen=True)
 class RaggedRows:
     """The samples that rows belong to, without the rows (a DeviceBatch describes its own in the same way)."""
     max_batch: int
@@ -81,29 +82,46 @@ class RaggedRows:
     batch: Optional[torch.Tensor] = None
     ids: Optional[torch.Tensor] = None
 
+    def __post_init__(self):
+        object.__setattr__(self, "_c", fb.ragged(self.max_batch, self.max_tokens, self.max_rows, self.offsets, self.batch,
+                                                 self.ids))
+
     def ragged(self) -> fb.fusion_ragged:
-        return fb.ragged(self.max_batch, self.max_tokens, self.max_rows, self.offsets, self.batch, self.ids)
+        return self._c
 
 
-def _rows_ptr(t: torch.Tensor, rows: int, kv_heads: int, head_dim: int, dtype: str, device, what: str):
+_HERE = contextlib.nullcontext()
+
+
+def _on(device: int):
+    """The device as the current one (no context object where it is already: 1.5 us a call)."""
+    return _HERE if torch.cuda.current_device() == device else torch.cuda.device(device)
+
+
+def _rows_ptr(t: torch.Tensor, rows: int, heads: int, head_dim: int, dtype: torch.dtype, device: int, what: str):
     """Address and row stride of `rows` rows, [rows, heads * dim] or [rows, heads, dim], any stride between rows and
-    contiguous inside one."""
-    width = kv_heads * head_dim
-    flat = t.dim() == 2 and t.shape[1] == width and (t.stride(1) == 1 or width == 1)
-    split = t.dim() == 3 and tuple(t.shape[1:]) == (kv_heads, head_dim) and t.stride(2) == 1 and \
-        (t.stride(1) == head_dim or kv_heads == 1)
-    if t.dtype != TORCH_DTYPE[dtype] or t.device != device or not (flat or split) or t.shape[0] < rows:
-        raise fb.FusionError(f"{what}: at least {rows} {TORCH_DTYPE[dtype]} rows of {kv_heads} x {head_dim} elements on {device}, "
+    contiguous inside one; device: an index (-1: the host)."""
+    shape, width = t.shape, heads * head_dim
+    if len(shape) == 2:
+        ok = shape[1] == width and (width == 1 or t.stride(1) == 1)
+    else:
+        ok = len(shape) == 3 and shape[1] == heads and shape[2] == head_dim
+        ok = ok and (t.is_contiguous() or (t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)))
+    if not ok or t.dtype != dtype or t.get_device() != device or shape[0] < rows:
+        raise fb.FusionError(f"{what}: at least {rows} {dtype} rows of {heads} x {head_dim} elements on device {device}, "
                              "contiguous inside a row, expected")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else width
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else width
 
 
-def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device, what: str, least: int = 0, dim: int = 1):
-    """t (None passes) is a contiguous tensor of this type on this device, of `dim` dimensions and at least `least` elements."""
-    if t is not None and (t.dtype != dtype or t.device != device or t.dim() != dim or t.numel() < least or
-                          not t.is_contiguous()):
-        raise fb.FusionError(f"{what}: a contiguous {dim}-dimensional {dtype} tensor of at least {least} elements on {device} "
-                             "expected")
+def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str, least: int = 0, dim: int = 1):
+    """The address of t (None: None), a contiguous tensor of this type on this device, of `dim` dimensions and at least
+    `least` elements."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.get_device() != device or t.dim() != dim or t.numel() < least or not t.is_contiguous():
+        raise fb.FusionError(f"{what}: a contiguous {dim}-dimensional {dtype} tensor of at least {least} elements on device "
+                             f"{device} expected")
+    return t.data_ptr()
 
 
 @dataclass
@@ -134,12 +152,18 @@ class DeviceCache:
             raise fb.FusionError("cache tensors of the wrong shape, type or device")
         self.max_batch, self.max_pages = (int(n) for n in self.page_table.shape)
         self.kv_heads, self.page_tokens, self.head_dim = int(kv_heads), int(page_tokens), int(dim)
+        if not self.k.is_cuda:
+            raise fb.FusionError("device tensors expected")
         self._c = fb.cache(self.max_batch, self.max_pages, page_tokens, kv_heads, dim, pages, self.k, self.v, self.sizes,
                            self.weights, self.page_table, self.lengths)
         self.ws_bytes = fb.fusion_cache_workspace_size(self._c, self.heads)
         if self.ws_bytes == 0:
             raise fb.FusionError("cache shape or number of heads out of range")
         self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.k.device)
+        self.device, self.index = self.k.device, self.k.get_device()
+        self.code, self.torch_dtype = DTYPE_CODE[self.dtype], TORCH_DTYPE[self.dtype]
+        self.scale = self.head_dim ** -0.5
+        self._ws = self.workspace.data_ptr()
         self._one = None   # the offsets of one row per sequence
 
     def c_struct(self) -> fb.fusion_cache:
@@ -316,16 +340,15 @@ class Fusion:
         (a DeviceBatch or RaggedRows; None: one row per sequence) says; returns the new lengths (the cache's own, raised
         in place, unless lengths_out is given)."""
         rows = rows if rows is not None else c.one_row_each()
-        dev = c.k.device
-        kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.dtype, dev, "keys")
-        vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.dtype, dev, "values")
-        _need(sizes, torch.float32, dev, "sizes", rows.max_rows)
-        _need(scores, torch.float32, dev, "scores", rows.max_rows)
+        kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "keys")
+        vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "values")
+        zp = _need(sizes, torch.float32, c.index, "sizes", rows.max_rows)
+        wp = _need(scores, torch.float32, c.index, "scores", rows.max_rows)
         o = lengths_out if lengths_out is not None else c.lengths
-        _need(o, torch.int32, dev, "lengths_out", c.max_batch)
-        with torch.cuda.device(c.k.device):
-            fb.check(fb.fusion_cache_append(DTYPE_CODE[c.dtype], c.c_struct(), rows.ragged(), kp, ks, vp, vs, sizes, scores,
-                                            o, c.workspace, c.ws_bytes, self.status))
+        op = _need(o, torch.int32, c.index, "lengths_out", c.max_batch)
+        with _on(c.index):
+            fb.check(fb.fusion_cache_append(c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp, wp, op, c._ws, c.ws_bytes,
+                                            self.status.data_ptr()))
         return o
 
     def cache_attention(self, c: DeviceCache, q: torch.Tensor, *, scale: Optional[float] = None, window: int = 0,
@@ -333,34 +356,33 @@ class Fusion:
         """Attention of one new token per sequence, q [max_batch, heads, head_dim] (any stride between sequences), over
         the visible tokens of its cache; accumulates the weights where the cache keeps them.  scale None:
         head_dim ** -0.5.  Returns [max_batch, heads, head_dim]."""
-        qp, qs = _rows_ptr(q, c.max_batch, c.heads, c.head_dim, c.dtype, c.k.device, "queries")
-        _need(out, TORCH_DTYPE[c.dtype], c.k.device, "out", c.max_batch * c.heads * c.head_dim, 3)
-        o = out if out is not None else torch.empty((c.max_batch, c.heads, c.head_dim), dtype=TORCH_DTYPE[c.dtype],
-                                                    device=c.k.device)
-        with torch.cuda.device(c.k.device):
-            fb.check(fb.fusion_cache_attention(DTYPE_CODE[c.dtype], c.c_struct(), qp, qs, c.heads,
-                                               c.head_dim ** -0.5 if scale is None else scale, window, sinks, o, c.workspace,
-                                               c.ws_bytes, self.status))
-        return o
+        qp, qs = _rows_ptr(q, c.max_batch, c.heads, c.head_dim, c.torch_dtype, c.index, "queries")
+        if out is None:
+            out = torch.empty((c.max_batch, c.heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
+        op = _need(out, c.torch_dtype, c.index, "out", c.max_batch * c.heads * c.head_dim, 3)
+        with _on(c.index):
+            fb.check(fb.fusion_cache_attention(c.code, c.c_struct(), qp, qs, c.heads, c.scale if scale is None else scale,
+                                               window, sinks, op, c._ws, c.ws_bytes, self.status.data_ptr()))
+        return out
 
     def cache_evict(self, c: DeviceCache, budget: torch.Tensor, *, sinks: int = 0, recent: int = 0,
                     page_table_out: Optional[torch.Tensor] = None, lengths_out: Optional[torch.Tensor] = None,
                     keep_idx: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Prunes each sequence to budget[b] tokens by accumulated weight, in place or into other pages; keep_idx
         [max_batch, n] receives the kept positions.  Returns the new lengths (the cache's own unless lengths_out is given)."""
-        o, dev = lengths_out if lengths_out is not None else c.lengths, c.k.device
-        _need(o, torch.int32, dev, "lengths_out", c.max_batch)
-        _need(budget, torch.int32, dev, "budget", c.max_batch)
-        _need(page_table_out, torch.int32, dev, "page_table_out", dim=2)
-        _need(keep_idx, torch.int32, dev, "keep_idx", dim=2)
+        o = lengths_out if lengths_out is not None else c.lengths
+        op = _need(o, torch.int32, c.index, "lengths_out", c.max_batch)
+        bp = _need(budget, torch.int32, c.index, "budget", c.max_batch)
+        tp = _need(page_table_out, torch.int32, c.index, "page_table_out", dim=2)
+        kp = _need(keep_idx, torch.int32, c.index, "keep_idx", dim=2)
         for t, what in ((page_table_out, "page_table_out"), (keep_idx, "keep_idx")):
             if t is not None and t.shape[0] < c.max_batch:
                 raise fb.FusionError(f"{what}: a row per sequence expected")
-        with torch.cuda.device(dev):
-            fb.check(fb.fusion_cache_evict(DTYPE_CODE[c.dtype], c.c_struct(), budget, sinks, recent, page_table_out,
-                                           page_table_out.shape[1] if page_table_out is not None else 0, o, keep_idx,
-                                           keep_idx.shape[1] if keep_idx is not None else 0, c.workspace, c.ws_bytes,
-                                           self.status))
+        with _on(c.index):
+            fb.check(fb.fusion_cache_evict(c.code, c.c_struct(), bp, sinks, recent, tp,
+                                           page_table_out.shape[1] if tp is not None else 0, op, kp,
+                                           keep_idx.shape[1] if kp is not None else 0, c._ws, c.ws_bytes,
+                                           self.status.data_ptr()))
         return o
 
     def exit_check(self, b: DeviceBatch, head: HeadTensors) -> Dict[str, torch.Tensor]:

@@ -117,7 +117,7 @@ def test_constants_and_status():
 
 
 def test_runner_refuses_tensors_that_do_not_fit():
-    rows = lambda t, n, h=2, d=8, dtype="f32": runner._rows_ptr(t, n, h, d, dtype, torch.device("cpu"), "rows")   # noqa: E731
+    rows = lambda t, n, h=2, d=8, dtype="f32": runner._rows_ptr(t, n, h, d, runner.TORCH_DTYPE[dtype], -1, "rows")   # noqa: E731
     t = torch.zeros(4, 16)
     assert rows(t, 4) == (t.data_ptr(), 16) and rows(t.view(4, 2, 8), 3)[1] == 16
     packed = torch.zeros(4, 48)
@@ -130,7 +130,7 @@ def test_runner_refuses_tensors_that_do_not_fit():
     for bad in (torch.zeros(4), torch.zeros(3, dtype=torch.int32), torch.zeros(8, dtype=torch.int32)[::2],
                 torch.zeros(4, 1, dtype=torch.int32)):
         with pytest.raises(fz.FusionError):
-            runner._need(bad, torch.int32, torch.device("cpu"), "lengths", 4)
+            runner._need(bad, torch.int32, -1, "lengths", 4)
     pool, per, table, n = torch.zeros(6, 2, 16, 8), torch.zeros(6, 16), torch.zeros(3, 2, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
     for bad in ((pool, pool[:5], table, n, None), (pool, pool, table.long(), n, None), (pool, pool, table, n[:2], None),
                 (pool, pool, table, n, per[:5]), (pool, pool.bfloat16(), table, n, None), (pool, pool, table[0], n, None)):

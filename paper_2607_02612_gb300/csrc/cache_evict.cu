@@ -3,10 +3,9 @@
 // lowest position).  Kept rows move, in ascending position, to positions 0 .. m - 1.
 //
 // k_cache_select, a CTA (or a cluster of them, for long sequences) per sequence: the ordered keys of the weights stay in
-// registers, and the smallest kept key T is the largest T of which count(key >= T) is still the number wanted, two bits per
-// step (three counts, one barrier).  Counting costs the same whatever the weights are; a histogram's atomics meet in a few
-// bins, since attention weights share a few exponents (8 bits per pass: 43 us for 32 sequences of up to 8192, 103 us for one of
-// 32768).  One scan over the counts of all warps then places the kept tokens.
+// registers; the smallest kept key is found from its 11 top bits down by three histograms (11 bits spread weights, which share
+// a few exponents, over enough bins that their atomics rarely meet; a pass whose bin is kept whole is the last).  One scan
+// over the counts of all warps then places the kept tokens.
 //
 // k_cache_move copies the rows.  Into other pages: any CTA any rows.  In place: a team of CTAs (a cluster) per (sequence, key
 // head, K or V) takes the rows in ascending position, a step of them at a time, all read before any is written.  That is safe
@@ -17,7 +16,8 @@
 namespace fz {
 namespace {
 
-constexpr int kSelThreads = 1024, kSelWarps = kSelThreads / 32, kKeys = 16;   // keys of a thread in registers
+constexpr int kKeys = 16;    // keys of a thread in registers
+constexpr int kBins = 2048;  // of a histogram
 
 __device__ __forceinline__ unsigned slot_of(const Cache &c, int b, int pos) {
     unsigned page;
@@ -54,14 +54,25 @@ __device__ __forceinline__ void exchange(Exchange &x, int &par, int rank, int4 v
     par ^= 1;
 }
 
+// Two numbers at the same place of CTA k of the cluster.
+__device__ __forceinline__ int2 peer_pair(const int *here, int k) {
+    uint32_t theirs;
+    int2 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(theirs) : "r"(smem_addr(here)), "r"(k));
+    asm volatile("ld.shared::cluster.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(theirs) : "memory");
+    return v;
+}
+
 // C: CTAs of a sequence; each takes a run of the positions that are compared.
-template <int C>
+template <int C, int kSelThreads>
 __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p) {
+    constexpr int kSelWarps = kSelThreads / 32, kMine = kBins / kSelThreads;   // bins of a thread
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = C == 1 ? 0 : (int)cluster_rank();
     const Cache &c = p.c;
     __shared__ Exchange box;
-    __shared__ int3 s_cnt[2][kSelWarps];
+    __shared__ __align__(16) int hist[kBins];
+    __shared__ int s_warp[kSelWarps], s_digit[3];
     __shared__ int s_scan[kKeys * kSelWarps];
     __shared__ int s_first;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -84,6 +95,7 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
 
     // ---- the pages that are read and written, the weights that are compared
     bool wrong = n < 0, nan = false;
+    unsigned key[kKeys];
     if (!wrong) {
         const int pages_n = (n + (1 << c.shift) - 1) >> c.shift, pages_m = (m + (1 << c.shift) - 1) >> c.shift;
         wrong = pages_m > p.pages_out;
@@ -91,23 +103,29 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
         if (!p.in_place)
             for (int e = tid; e < min(pages_m, p.pages_out); e += kSelThreads)
                 wrong |= (unsigned)p.table_out[(size_t)b * p.pages_out + e] >= c.num_pages;
-    }
-    wrong = __syncthreads_or(wrong);
-    unsigned key[kKeys];
-    if (!wrong) {
+        // (all pages, then all weights: no branch between the loads)
+        const int top = max(end - 1, 0);   // (row b has a position 0)
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i) key[i] = (unsigned)c.table[(size_t)b * c.max_pages + (min(at + i * kSelThreads + tid, top) >> c.shift)];
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i)
+            key[i] = __float_as_uint(c.weights[((key[i] < c.num_pages ? key[i] : 0u) << c.shift) +
+                                               (unsigned)(min(at + i * kSelThreads + tid, top) & ((1 << c.shift) - 1))]);
 #pragma unroll
         for (int i = 0; i < kKeys; ++i) {
-            const int j = at + i * kSelThreads + tid;
-            float w = 0.0f;
-            if (j < end) w = c.weights[slot_of(c, b, j)];
-            nan |= !isfinite(w);
-            key[i] = j < end ? ordered_bits(w) : 0u;   // (no finite weight has the key 0)
+            const bool here = at + i * kSelThreads + tid < end;
+            nan |= here && !isfinite(__uint_as_float(key[i]));
+            key[i] = here ? ordered_bits(__uint_as_float(key[i])) : 0u;   // (no finite weight has the key 0)
         }
-        for (int j = at + kKeys * kSelThreads + tid; j < end; j += kSelThreads) nan |= !isfinite(c.weights[slot_of(c, b, j)]);
+        for (int j = at + kKeys * kSelThreads + tid; j < end; j += kSelThreads) {
+            unsigned page;
+            if (cache_page(c, b, j, page)) nan |= !isfinite(c.weights[(page << c.shift) + (unsigned)(j & ((1 << c.shift) - 1))]);
+        }
     }
+    for (int e = tid; e < kBins; e += kSelThreads) hist[e] = 0;
     {
-        const int any = __syncthreads_or(nan);
-        exchange<C>(box, par, rank, make_int4(any, wrong, 0, 0));
+        const int any_nan = __syncthreads_or(nan), any_wrong = __syncthreads_or(wrong);
+        exchange<C>(box, par, rank, make_int4(any_nan, any_wrong, 0, 0));
         nan = wrong = false;
         for (int k = 0; k < C; ++k) {
             nan |= box.box[par ^ 1][k].x != 0;
@@ -123,81 +141,105 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
         return;   // (after an exchange: nobody writes to a CTA's box any more)
     }
 
-    // ---- T: the largest with count(key >= T) >= want
+    // ---- T, the smallest kept key, from the top digit down; `left`: kept keys among those that share T's digits so far
     unsigned T = 0;
-    bool exact = false;   // count(key >= T) == want: no ties to break
-    int flip = 0;
-    if (choose && want > 0) {
-        for (int shift = 30; shift >= 0 && !exact; shift -= 2) {
-            const unsigned t1 = T | 1u << shift, t2 = T | 2u << shift, t3 = T | 3u << shift;
-            int n1 = 0, n2 = 0, n3 = 0;
+    int left = want;
+    bool exact = want == 0;   // every key that shares T's digits is kept: no ties to break
+#pragma unroll 1
+    for (int shift = 21; choose && !exact && shift >= 0; shift -= shift > 11 ? 11 : 10) {
+        const unsigned width = shift > 0 ? 11u : 10u, top = shift == 21 ? 0u : 0xFFFFFFFFu << (shift + width);   // 11, 11 and 10 bits
 #pragma unroll
-            for (int i = 0; i < kKeys; ++i) {
-                if (at + i * kSelThreads >= end) break;
-                n1 += key[i] >= t1;
-                n2 += key[i] >= t2;
-                n3 += key[i] >= t3;
-            }
-            for (int j = at + kKeys * kSelThreads + tid; j < end; j += kSelThreads) {
-                const unsigned o = key_at(j);
-                n1 += o >= t1;
-                n2 += o >= t2;
-                n3 += o >= t3;
-            }
-            n1 = __reduce_add_sync(0xFFFFFFFFu, n1);
-            n2 = __reduce_add_sync(0xFFFFFFFFu, n2);
-            n3 = __reduce_add_sync(0xFFFFFFFFu, n3);
-            if (lane == 0) s_cnt[flip][warp] = make_int3(n1, n2, n3);
-            __syncthreads();
-            const int3 v = s_cnt[flip][lane];
-            flip ^= 1;
-            n1 = __reduce_add_sync(0xFFFFFFFFu, v.x);
-            n2 = __reduce_add_sync(0xFFFFFFFFu, v.y);
-            n3 = __reduce_add_sync(0xFFFFFFFFu, v.z);
-            if constexpr (C > 1) {
-                exchange<C>(box, par, rank, make_int4(n1, n2, n3, 0));
-                n1 = n2 = n3 = 0;
-                for (int k = 0; k < C; ++k) {
-                    const int4 o = box.box[par ^ 1][k];
-                    n1 += o.x;
-                    n2 += o.y;
-                    n3 += o.z;
-                }
-            }
-            const int got = n3 >= want ? n3 : n2 >= want ? n2 : n1;
-            T = n3 >= want ? t3 : n2 >= want ? t2 : n1 >= want ? t1 : T;
-            exact = got == want;
+        for (int i = 0; i < kKeys; ++i)
+            if (key[i] != 0u && (key[i] & top) == T) atomicAdd(&hist[key[i] >> shift & (kBins - 1)], 1);
+        for (int j = at + kKeys * kSelThreads + tid; j < end; j += kSelThreads) {
+            const unsigned o = key_at(j);
+            if ((o & top) == T) atomicAdd(&hist[o >> shift & (kBins - 1)], 1);
         }
+        if constexpr (C > 1) {
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        // counts from the largest digit down, kMine a thread; the cluster's histograms are summed on the way
+        const int low_bin = kBins - (tid + 1) * kMine;
+        int v[kMine], incl = 0;
+#pragma unroll
+        for (int x = 0; x < kMine; x += 2) {
+            int2 w = make_int2(0, 0);
+            if constexpr (C > 1) {
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    const int2 u = peer_pair(&hist[low_bin + x], k);
+                    w.x += u.x;
+                    w.y += u.y;
+                }
+            } else {
+                w = *reinterpret_cast<const int2 *>(&hist[low_bin + x]);
+            }
+            v[x] = w.x;
+            v[x + 1] = w.y;
+            incl += w.x + w.y;
+        }
+        const int mine = incl;
+#pragma unroll
+        for (int s = 1; s < 32; s <<= 1) {
+            const int u = __shfl_up_sync(0xFFFFFFFFu, incl, s);
+            if (lane >= s) incl += u;
+        }
+        if (lane == 31) s_warp[warp] = incl;
+        __syncthreads();
+        {
+            const int w = lane < kSelWarps ? s_warp[lane] : 0;
+            incl += (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)(lane < warp ? w : 0));
+        }
+        int before = incl - mine;
+        if (before < left && left <= incl) {   // one thread
+            bool found = false;
+#pragma unroll
+            for (int x = kMine - 1; x >= 0; --x) {
+                if (!found && before + v[x] >= left) {
+                    found = true;
+                    s_digit[0] = low_bin + x;
+                    s_digit[1] = before;
+                    s_digit[2] = v[x];
+                }
+                before += v[x];
+            }
+        }
+        if constexpr (C > 1) {   // (nobody clears a histogram that another reads)
+            cluster_arrive();
+            cluster_wait();
+        } else {
+            __syncthreads();
+        }
+        T |= (unsigned)s_digit[0] << shift;
+        left -= s_digit[1];
+        exact = s_digit[2] == left;
+        for (int e = tid; e < kBins; e += kSelThreads) hist[e] = 0;
+        __syncthreads();
     }
     // kept: keys above the threshold, and the first `ties` of those equal to it
     const unsigned above = want == 0 ? 0xFFFFFFFFu : exact ? T - 1u : T;
-    // ---- per warp and row of kSelThreads positions: keys above (low half), keys equal (high half); then a scan in order
+    const bool tied = choose && !exact;
+    // ---- per warp and row of kSelThreads positions: keys above (low half), keys equal (high half), kKeys rows at a time
     int total_a = 0, total_e = 0, evicted = n;   // evicted: the first position that goes
     const int rows = (end - at + kSelThreads - 1) / kSelThreads;
-    auto key_of = [&](int i, int j) {   // beyond the registers: read again
-        unsigned o = 0u;
-        if (i < kKeys) {
-#pragma unroll
-            for (int k = 0; k < kKeys; ++k)
-                if (k == i) o = key[k];
-        } else if (j < end) {
-            o = key_at(j);
-        }
-        return o;
+    auto count = [&](int i, unsigned o, bool here) {
+        const unsigned ba = __ballot_sync(0xFFFFFFFFu, here && o > above), be = __ballot_sync(0xFFFFFFFFu, here && tied && o == above);
+        if (lane == 0) s_scan[i * kSelWarps + warp] = __popc(ba) | __popc(be) << 16;
     };
-    // the kept tokens' slots; row blocks of kKeys rows, whose counts fit in shared memory; two passes where the ties' number
-    // or the other CTAs' counts have to be known first
-    auto count_block = [&](int i0) {
+    auto count_block = [&](int i0) {   // (rows that do not exist count nothing)
+        if (i0 == 0) {
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) count(i, key[i], at + i * kSelThreads + tid < end);
+        } else {
 #pragma unroll 1
-        for (int i = i0; i < min(rows, i0 + kKeys); ++i) {
-            const unsigned o = key_of(i, at + i * kSelThreads + tid);
-            const bool here = at + i * kSelThreads + tid < end;
-            const unsigned ba = __ballot_sync(0xFFFFFFFFu, here && o > above), be = __ballot_sync(0xFFFFFFFFu, here && !exact && want > 0 && o == above);
-            if (lane == 0) s_scan[(i - i0) * kSelWarps + warp] = __popc(ba) | __popc(be) << 16;
+            for (int i = 0; i < kKeys; ++i) {
+                const int j = at + (i0 + i) * kSelThreads + tid;
+                count(i, j < end ? key_at(j) : 0u, j < end);
+            }
         }
-        if (i0 + kKeys > rows)   // rows that do not exist
-            for (int i = max(rows - i0, 0); i < kKeys; ++i)
-                if (lane == 0) s_scan[i * kSelWarps + warp] = 0;
     };
     for (int i0 = 0; i0 < rows; i0 += kKeys) {
         count_block(i0);
@@ -207,7 +249,7 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
         v = (int)__reduce_add_sync(0xFFFFFFFFu, (unsigned)v);
         total_a += v & 0xFFFF;
         total_e += (unsigned)v >> 16;
-        __syncthreads();
+        if (rows > kKeys) __syncthreads();
     }
     int before_a = 0, before_e = 0, all_a = total_a;
     if constexpr (C > 1) {
@@ -224,8 +266,8 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
     }
     const int ties = want - all_a;   // of the equal keys
     unsigned *keep = p.keep + (size_t)b * c.capacity;
-    auto put = [&](int i, int j) {
-        keep[i] = slot_of(c, b, j);
+    auto put = [&](int i, int j, unsigned slot) {
+        keep[i] = slot;
         if (p.keep_idx && i < p.keep_stride) p.keep_idx[(size_t)b * p.keep_stride + i] = j;
     };
     for (int i0 = 0; i0 < rows; i0 += kKeys) {
@@ -233,12 +275,13 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
             count_block(i0);
             __syncthreads();
         }
-        // an exclusive scan of the counts: every warp for itself, 16 numbers a lane
-        int mine = 0, part[kKeys];
+        // an exclusive scan of the counts: every warp for itself, kPart numbers a lane
+        constexpr int kPart = kKeys * kSelWarps / 32;
+        int mine = 0, part[kPart];
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k) {
+        for (int k = 0; k < kPart; ++k) {
             part[k] = mine;
-            mine += s_scan[lane * kKeys + k];
+            mine += s_scan[lane * kPart + k];
         }
         int incl = mine;
 #pragma unroll
@@ -247,21 +290,32 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
             if (lane >= s) incl += v;
         }
         const int excl = incl - mine, block = __shfl_sync(0xFFFFFFFFu, incl, 31);
-        // (the number of row i, warp w is the (i * kSelWarps + w)-th: lane 2 i + w / 16, its (w % 16)-th)
+        // (the number of row i, warp w is the (i * kSelWarps + w)-th: lane 2 i + w / kPart, its (w % kPart)-th)
         int pre = excl;
 #pragma unroll
-        for (int k = 0; k < kKeys; ++k)
-            if (k == (warp & 15)) pre += part[k];
-#pragma unroll 1
-        for (int i = i0; i < min(rows, i0 + kKeys); ++i) {
-            const int j = at + i * kSelThreads + tid;
-            const unsigned o = key_of(i, j);
-            const bool a = j < end && o > above, e = j < end && !exact && want > 0 && o == above;
+        for (int k = 0; k < kPart; ++k)
+            if (k == warp % kPart) pre += part[k];
+        auto place = [&](int i, int j, unsigned o, unsigned slot) {
+            const bool a = j < end && o > above, e = j < end && tied && o == above;
             const unsigned ba = __ballot_sync(0xFFFFFFFFu, a), be = __ballot_sync(0xFFFFFFFFu, e), lt = (1u << lane) - 1u;
-            const int q = __shfl_sync(0xFFFFFFFFu, pre, 2 * (i - i0) + (warp >> 4));
-            const int na = before_a + (q & 0xFFFF) + __popc(ba & lt), ne = before_e + ((unsigned)q >> 16) + __popc(be & lt);
-            if (a || (e && ne < ties)) put(first + na + min(ne, ties), j);
+            const int q = __shfl_sync(0xFFFFFFFFu, pre, 2 * i + warp / kPart);
+            const int na = before_a + (q & 0xFFFF) + __popc(ba & lt), ne = before_e + (int)((unsigned)q >> 16) + __popc(be & lt);
+            if (a || (e && ne < ties)) put(first + na + min(ne, ties), j, slot);
             else if (j < end) evicted = min(evicted, j);
+        };
+        if (i0 == 0) {
+            unsigned slot[kKeys];
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i) slot[i] = slot_of(c, b, min(at + i * kSelThreads + tid, max(end - 1, 0)));
+#pragma unroll
+            for (int i = 0; i < kKeys; ++i)
+                if (i < rows) place(i, at + i * kSelThreads + tid, key[i], slot[i]);
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < kKeys && i0 + i < rows; ++i) {
+                const int j = at + (i0 + i) * kSelThreads + tid;
+                place(i, j, j < end ? key_at(j) : 0u, slot_of(c, b, min(j, end - 1)));
+            }
         }
         before_a += block & 0xFFFF;
         before_e += (unsigned)block >> 16;
@@ -269,10 +323,10 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
     }
     // ---- the tokens that stay anyway
     if (choose) {
-        for (int i = rank * kSelThreads + tid; i < first; i += C * kSelThreads) put(i, i);
-        for (int i = rank * kSelThreads + tid; i < last; i += C * kSelThreads) put(m - last + i, n - last + i);
+        for (int i = rank * kSelThreads + tid; i < first; i += C * kSelThreads) put(i, i, slot_of(c, b, i));
+        for (int i = rank * kSelThreads + tid; i < last; i += C * kSelThreads) put(m - last + i, n - last + i, slot_of(c, b, n - last + i));
     } else {
-        for (int i = rank * kSelThreads + tid; i < m; i += C * kSelThreads) put(i, i);
+        for (int i = rank * kSelThreads + tid; i < m; i += C * kSelThreads) put(i, i, slot_of(c, b, i));
     }
     // ---- nothing before the first evicted position moves in place
     if (tid == 0) s_first = n;
@@ -358,7 +412,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams
     }
 }
 
-template <int C>
+template <int C, int kSelThreads>
 cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(C, (unsigned)p.c.max_batch);
@@ -369,7 +423,7 @@ cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
     a[0].val.clusterDim = {C, 1, 1};
     cfg.attrs = a;
     cfg.numAttrs = C > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, k_cache_select<C>, p);
+    return cudaLaunchKernelEx(&cfg, k_cache_select<C, kSelThreads>, p);
 }
 
 }  // namespace
@@ -377,9 +431,15 @@ cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
 cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_t s) {
     if (p.c.max_batch == 0) return cudaSuccess;
     const int head_chunks = p.c.dim * (dtype == FUSION_BF16 ? 2 : 4) / 16;
-    // as many CTAs as hold a sequence's keys in registers, up to 8
-    const int need = ceil_div(p.c.capacity, kKeys * kSelThreads);
-    cudaError_t e = need <= 1 ? launch_select<1>(p, s) : need <= 2 ? launch_select<2>(p, s) : need <= 4 ? launch_select<4>(p, s) : launch_select<8>(p, s);
+    // threads that hold a sequence's keys in registers: few where they do, since every warp more costs instructions (8 x 577:
+    // 1024 threads 16.5 us, 256 ... ), then clusters of up to 8 CTAs
+    const int cap = p.c.capacity, k = kKeys;
+    cudaError_t e = cap <= 256 * k    ? launch_select<1, 256>(p, s)
+                    : cap <= 512 * k  ? launch_select<1, 512>(p, s)
+                    : cap <= 1024 * k ? launch_select<1, 1024>(p, s)
+                    : cap <= 2048 * k ? launch_select<2, 1024>(p, s)
+                    : cap <= 4096 * k ? launch_select<4, 1024>(p, s)
+                                      : launch_select<8, 1024>(p, s);
     if (e != cudaSuccess) return e;
     // a team per (sequence, job): enough CTAs to fill the GPU a few times, no more than a sequence has steps for
     const int jobs = 2 * p.c.kv_heads + 1, step = kMoveThreads / head_chunks * kPer;

@@ -345,9 +345,10 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
 
 constexpr int kMoveThreads = 512, kPer = 8;   // kPer 16-byte chunks of a thread in flight
 // gridDim.x CTAs per (sequence, key head, K or V; the last job: sizes and weights); in place they are a cluster.
+// A row's chunks are dealt out over `parts` teams.
 template <bool kInPlace>
-__global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, int head_chunks) {
-    const int b = blockIdx.z, job = blockIdx.y, tid = threadIdx.x, team = gridDim.x, member = blockIdx.x;
+__global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, int head_chunks, int parts) {
+    const int b = blockIdx.z, job = blockIdx.y / parts, part = blockIdx.y % parts, tid = threadIdx.x, team = gridDim.x, member = blockIdx.x;
     const Cache &c = p.c;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int2 plan = p.plan[b];
@@ -385,7 +386,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams
         return pool + (size_t)((((slot >> c.shift) * (unsigned)c.kv_heads + h) << c.shift) + (slot & low)) * head_chunks * 16;
     };
     // rows of a step: as many whole rows as the CTA's chunks give; a thread has the same chunk of rows `stride` apart
-    const int stride = kMoveThreads / head_chunks, chunk = tid % head_chunks, r0 = tid / head_chunks, step = stride * kPer;
+    const int mine = head_chunks / parts, stride = kMoveThreads / mine, chunk = part * mine + tid % mine, r0 = tid / mine, step = stride * kPer;
     const bool idle = r0 >= stride;
     uint4 v[kPer];
     auto load = [&](int i0) {
@@ -436,21 +437,27 @@ cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_
     const int cap = p.c.capacity, k = kKeys;
     cudaError_t e = cap <= 256 * k    ? launch_select<1, 256>(p, s)
                     : cap <= 512 * k  ? launch_select<1, 512>(p, s)
-                    : cap <= 1024 * k ? launch_select<1, 1024>(p, s)
-                    : cap <= 2048 * k ? launch_select<2, 1024>(p, s)
-                    : cap <= 4096 * k ? launch_select<4, 1024>(p, s)
+                    : cap <= 1024 * k ? launch_select<2, 512>(p, s)
+                    : cap <= 2048 * k ? launch_select<4, 512>(p, s)
+                    : cap <= 4096 * k ? launch_select<8, 512>(p, s)
                                       : launch_select<8, 1024>(p, s);
     if (e != cudaSuccess) return e;
     // a team per (sequence, job): enough CTAs to fill the GPU a few times, no more than a sequence has steps for
-    const int jobs = 2 * p.c.kv_heads + 1, step = kMoveThreads / head_chunks * kPer;
+    const int jobs = 2 * p.c.kv_heads + 1;
     const long long most = p.in_place ? p.c.capacity : (long long)p.pages_out << p.c.shift;
     long long team = (p.in_place ? 608ll : 2432ll) / ((long long)jobs * p.c.max_batch);
+    int parts = 1;
+    while (p.in_place && team > 8 && head_chunks / parts >= 16 && head_chunks / parts % 2 == 0) {   // (not below 128 bytes of a row)
+        parts *= 2;
+        team /= 2;
+    }
+    const int step = kMoveThreads / (head_chunks / parts) * kPer;
     const long long steps = (most + step - 1) / step;
     if (team > steps) team = steps;
     if (p.in_place) team = team >= 8 ? 8 : team >= 4 ? 4 : team >= 2 ? 2 : 1;
     if (team < 1) team = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)team, (unsigned)jobs, (unsigned)p.c.max_batch);
+    cfg.gridDim = dim3((unsigned)team, (unsigned)((jobs - 1) * parts + 1), (unsigned)p.c.max_batch);
     cfg.blockDim = dim3(kMoveThreads);
     cfg.stream = s;
     cudaLaunchAttribute a[2];
@@ -460,7 +467,7 @@ cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_
     a[1].val.clusterDim = {(unsigned)team, 1, 1};
     cfg.attrs = a;
     cfg.numAttrs = p.in_place ? 2 : 1;
-    return p.in_place ? cudaLaunchKernelEx(&cfg, k_cache_move<true>, p, head_chunks) : cudaLaunchKernelEx(&cfg, k_cache_move<false>, p, head_chunks);
+    return p.in_place ? cudaLaunchKernelEx(&cfg, k_cache_move<true>, p, head_chunks, parts) : cudaLaunchKernelEx(&cfg, k_cache_move<false>, p, head_chunks, parts);
 }
 
 }  // namespace fz

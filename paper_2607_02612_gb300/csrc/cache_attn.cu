@@ -29,7 +29,8 @@ struct Layout {
     static constexpr int kP = kLsz + kWarps * S * TT * 4; // float [kWarps][TT][NQ]
     static constexpr int kQ = kP + kWarps * TT * NQ * 4;  // float [2][NQ][DP]
     static constexpr int kJoin = kQ + 2 * NQ * DP * 4;    // float [kWarps][kJoinQ][kJoinPitch]
-    static constexpr int kTotal = kJoin + kWarps * kJoinQ * kJoinPitch * 4;
+    static constexpr int kJoinBytes = kWarps * kJoinQ * kJoinPitch * 4;
+    static constexpr int kTotal = kJoin + (kJoinBytes > kJoinScratch<NQ> ? kJoinBytes : kJoinScratch<NQ>);   // (or the join of the runs)
 };
 
 template <typename T, int DP, int NQ, int TT, int S>
@@ -43,10 +44,13 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Cache &c = p.c;
     const int vheads = c.kv_heads * chunks;
-    empty_sequences<T>(p);
+    if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Run run;
     Place at;
-    if (!find_run(p, batch, kRound, vheads, run, at)) return;
+    if (!find_run(p, batch, kRound, vheads, run, at)) {
+        empty_sequences<T>(p);
+        return;
+    }
     const long long r0 = run.r0, r1 = run.r1;
 
     unsigned char *stages = sm + warp * S * L::kStage;
@@ -67,12 +71,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
     };
 
     Stream<T, DP, TT> in;
-    in.begin(p, at, run, vheads, warp, lane);
-#pragma unroll
-    for (int s = 0; s < S - 1; ++s) {
-        in.issue(p, chunks, vheads, warp, lane, stages + s * L::kStage, lsz + s * TT, swizzle);
-        cp_async_commit();
-    }
+    in.template begin<S>(p, at, run, chunks, vheads, warp, lane, stages, lsz, swizzle);
+    empty_sequences<T>(p);
     load_q(at.b, at.vh, qs);
     if (tid == 0) s_bad = 0;
     __syncthreads();
@@ -94,8 +94,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
     for (long long r = r0; r < r1; ++r) {
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
-        in.issue(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
-        cp_async_commit();
+        in.next(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
         cp_async_wait<S - 1>();
         __syncwarp();
 
@@ -236,7 +235,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
             }
             if (seg_bad && tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
             if (!whole) {
-                join_runs<T, NQ>(p, run, seg0, seg0 + at.rounds, (size_t)at.b * p.heads + head0, nq, s_last);
+                join_runs<T, NQ>(p, run, seg0, seg0 + at.rounds, (size_t)at.b * p.heads + head0, nq, join, s_last);
             }
             if (tid == 0) s_bad = 0;
             __syncthreads();
@@ -251,31 +250,36 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
 }
 
 // weights_j += sum over the query heads of 2^(x - lse): a thread per visible token, the heads in order.
+// A programmatic dependent of the attention kernel: it finds its tokens meanwhile.
 constexpr int kWeightThreads = 256;
 __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParams p) {
     __shared__ Batch<kWeightThreads> batch;
     const Cache &c = p.c;
     long long mine, before;
     const long long total = batch_total(p, batch, kWeightThreads, 1, mine, before);
-    const long long r0 = total * blockIdx.x / gridDim.x, r1 = total * (blockIdx.x + 1) / gridDim.x;
-    if (r0 >= r1) return;
-    batch_find(p, batch, kWeightThreads, 1, mine, before, r0);
+    Run run;
+    run.cut(total, (int)gridDim.x);
+    if (run.r0 >= run.r1) return;
+    batch_find(p, batch, kWeightThreads, 1, mine, before, run.r0);
     Place at;
     at.b = batch.b;
     place_sequence(p, at, kWeightThreads);
     at.vh = 0;
     at.u = (int)batch.rem;
-    for (long long r = r0; r < r1; ++r) {
+    for (long long r = run.r0; r < run.r1; ++r) {
         const int j = at.u * kWeightThreads + threadIdx.x;
-        unsigned page;
+        unsigned page = 0;
         const int pos = p.window && j >= p.sinks ? j + at.n - at.vis : j;
-        if (j < at.vis && cache_page(c, at.b, pos, page)) {
-            const float *x = p.logits + (size_t)at.b * p.heads * p.lstride + j, *lse = p.lse + (size_t)at.b * p.heads;
-            float w = 0.0f;
-#pragma unroll 8
-            for (int h = 0; h < p.heads; ++h) w += ex2(x[h * p.lstride] - lse[h]);
+        const bool here = j < at.vis && cache_page(c, at.b, pos, page);
+        if (r == run.r0) asm volatile("griddepcontrol.wait;" ::: "memory");
+        if (here) {
             float *dst = c.weights + ((size_t)page << c.shift) + (pos & ((1 << c.shift) - 1));
-            *dst += w;
+            const float *x = p.logits + (size_t)at.b * p.heads * p.lstride + j, *lse = p.lse + (size_t)at.b * p.heads;
+            const float old = *dst;
+            float w = 0.0f;
+#pragma unroll 16
+            for (int h = 0; h < p.heads; ++h) w += ex2(x[h * p.lstride] - lse[h]);
+            *dst = old + w;
         }
         place_next(p, at, kWeightThreads, 1);
     }
@@ -303,8 +307,16 @@ cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStre
                                                : launch_dim<8>(p, s);
     if (e != cudaSuccess || !p.logits) return e;
     const long long tiles = (long long)p.c.max_batch * ceil_div(p.most, kWeightThreads);
-    k_cache_weights<<<(unsigned)(tiles < 1216 ? tiles : 1216), kWeightThreads, 0, s>>>(p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(tiles < 1216 ? tiles : 1216));
+    cfg.blockDim = dim3(kWeightThreads);
+    cfg.stream = s;
+    cudaLaunchAttribute a[1];
+    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = a;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k_cache_weights, p);
 }
 
 }  // namespace fz

@@ -41,7 +41,8 @@ struct Layout {
     static constexpr int kLsz = kWarps * S * kStage;
     static constexpr int kQ = kLsz + kWarps * S * TT * 4;
     static constexpr int kJoin = kQ + kNq * kRow;
-    static constexpr int kTotal = kJoin + kWarps * kJoinQ * kPitch * 4;
+    static constexpr int kJoinBytes = kWarps * kJoinQ * kPitch * 4;
+    static constexpr int kTotal = kJoin + (kJoinBytes > kJoinScratch<kNq> ? kJoinBytes : kJoinScratch<kNq>);   // (or the join of the runs)
 };
 
 template <int DP, int NT, int TT, int S>
@@ -57,10 +58,13 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const Cache &c = p.c;
     const int vheads = c.kv_heads * chunks;
-    empty_sequences<__nv_bfloat16>(p);
+    if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Run run;
     Place at;
-    if (!find_run(p, batch, kRound, vheads, run, at)) return;
+    if (!find_run(p, batch, kRound, vheads, run, at)) {
+        empty_sequences<__nv_bfloat16>(p);
+        return;
+    }
     const long long r0 = run.r0, r1 = run.r1;
 
     unsigned char *stages = sm + warp * S * L::kStage, *qs = sm + L::kQ;
@@ -68,13 +72,6 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
     float *join = reinterpret_cast<float *>(sm + L::kJoin);
     auto swizzle = [](int r) { return r & 7; };
 
-    Stream<__nv_bfloat16, DP, TT> in;
-    in.begin(p, at, run, vheads, warp, lane);
-#pragma unroll
-    for (int s = 0; s < S - 1; ++s) {
-        in.issue(p, chunks, vheads, warp, lane, stages + s * L::kStage, lsz + s * TT, swizzle);
-        cp_async_commit();
-    }
     // the queries of a (sequence, key head): read ahead into registers, then written to shared memory
     uint4 qv[kQPer];
     auto read_q = [&](int b, int vh) {
@@ -95,7 +92,10 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
         }
     };
     read_q(at.b, at.vh);
+    Stream<__nv_bfloat16, DP, TT> in;
+    in.template begin<S>(p, at, run, chunks, vheads, warp, lane, stages, lsz, swizzle);
     write_q();
+    empty_sequences<__nv_bfloat16>(p);
     if (tid == 0) s_bad = 0;
     __syncthreads();
 
@@ -131,8 +131,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
     for (long long r = r0; r < r1; ++r) {
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
-        in.issue(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
-        cp_async_commit();
+        in.next(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
         cp_async_wait<S - 1>();
         __syncwarp();
 
@@ -325,7 +324,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
                 __syncthreads();
             }
             if (seg_bad && tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
-            if (!whole) join_runs<__nv_bfloat16, kNq>(p, run, seg0, seg0 + at.rounds, head, nq, s_last);
+            if (!whole) join_runs<__nv_bfloat16, kNq>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
             __syncthreads();
             if (tid == 0) s_bad = 0;
             __syncthreads();

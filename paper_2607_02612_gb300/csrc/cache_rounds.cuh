@@ -111,12 +111,25 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
     } while (s.rounds == 0);
 }
 
-// The run of rounds of this CTA.
+// The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.
 struct Run {
-    long long total, r0, r1;   // rounds of the batch; this CTA's
-    int ctas;                  // that take part
-    // the run that holds round x (run k begins at total * k / ctas)
-    __device__ __forceinline__ int of(long long x) const { return (int)(((x + 1) * ctas + total - 1) / total) - 1; }
+    long long total, len, more;
+    long long r0, r1;   // this CTA's
+    int ctas;
+    __device__ __forceinline__ void cut(long long rounds, int n) {
+        total = rounds;
+        ctas = n;
+        // (a 64-bit division takes 0.1 us)
+        len = total >> 32 ? total / n : (long long)((unsigned)total / (unsigned)n);
+        more = total - len * n;
+        r0 = begin(blockIdx.x);
+        r1 = begin(blockIdx.x + 1);
+    }
+    __device__ __forceinline__ long long begin(long long k) const { return len * k + (k < more ? k : more); }
+    __device__ __forceinline__ int of(long long x) const {   // the run that holds round x
+        const long long big = more * (len + 1);
+        return (int)(x < big ? x / (len + 1) : more + (x - big) / len);
+    }
 };
 
 // A token that a warp will load: its page (from the table, a round before its size) and place in it.
@@ -153,15 +166,15 @@ struct Stream {
     __device__ __forceinline__ float size_of(const CacheAttnParams &p, const Token &t) const {
         return t.place < 0 ? 0.0f : p.c.sizes ? p.c.sizes[((size_t)t.page << p.c.shift) + t.place] : 1.0f;
     }
-    // Asks for t0's rows (K, then V, rows of kRow bytes with chunk c of row r at c ^ swizzle(r)) and moves on.
+    // Asks for a token's rows (K, then V, rows of kRow bytes with chunk c of row r at c ^ swizzle(r)).
     template <typename Swizzle>
-    __device__ __forceinline__ void issue(const CacheAttnParams &p, int chunks, int vheads, int warp, int lane, unsigned char *stage,
-                                          float *lsz, Swizzle swizzle) {
+    __device__ __forceinline__ void ask(const CacheAttnParams &p, const Token &t, float size, int chunks, int lane, unsigned char *stage,
+                                        float *lsz, Swizzle swizzle) {
         const int row_chunks = p.c.dim * (int)sizeof(T) / 16;   // that exist
-        const unsigned row = ((t0.page * (unsigned)p.c.kv_heads + (unsigned)(t0.vh / chunks)) << p.c.shift) + (unsigned)t0.place;
-        const bool live = t0.place >= 0 && size0 != 0.0f;
+        const unsigned row = ((t.page * (unsigned)p.c.kv_heads + (unsigned)(t.vh / chunks)) << p.c.shift) + (unsigned)t.place;
+        const bool live = t.place >= 0 && size != 0.0f;
         const unsigned lives = __ballot_sync(0xFFFFFFFFu, live);
-        if (lane < TT) lsz[lane] = t0.place == -2 ? kNoPage : live ? log2f(size0) : -INFINITY;
+        if (lane < TT) lsz[lane] = t.place == -2 ? kNoPage : live ? log2f(size) : -INFINITY;
 #pragma unroll
         for (int e = 0; e < TT * kCpr / 32; ++e) {
             const int x = e * 32 + lane, r = x / kCpr, cc = x % kCpr;
@@ -172,17 +185,35 @@ struct Stream {
             cp_async16_zfill(dst, p.c.k + off, read);
             cp_async16_zfill(dst + TT * kRow, p.c.v + off, read);
         }
+        cp_async_commit();
+    }
+    // The next round's rows into `stage`.
+    template <typename Swizzle>
+    __device__ __forceinline__ void next(const CacheAttnParams &p, int chunks, int vheads, int warp, int lane, unsigned char *stage, float *lsz,
+                                         Swizzle swizzle) {
+        ask(p, t0, size0, chunks, lane, stage, lsz, swizzle);
         t0 = t1;
         size0 = size_of(p, t0);
         t1 = look_up(p, vheads, warp, lane);
     }
-    __device__ __forceinline__ void begin(const CacheAttnParams &p, const Place &at, const Run &run, int vheads, int warp, int lane) {
+    // The first S - 1 rounds' rows (all pages asked for at once, then all sizes).
+    template <int S, typename Swizzle>
+    __device__ __forceinline__ void begin(const CacheAttnParams &p, const Place &at, const Run &run, int chunks, int vheads, int warp, int lane,
+                                          unsigned char *stages, float *lsz, Swizzle swizzle) {
         ahead = at;
         ahead_r = run.r0;
         r1 = run.r1;
-        t0 = look_up(p, vheads, warp, lane);
-        t1 = look_up(p, vheads, warp, lane);
-        size0 = size_of(p, t0);
+        Token t[S + 1];
+        float size[S];
+#pragma unroll
+        for (int s = 0; s <= S; ++s) t[s] = look_up(p, vheads, warp, lane);
+#pragma unroll
+        for (int s = 0; s < S; ++s) size[s] = size_of(p, t[s]);
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], chunks, lane, stages + s * kStage, lsz + s * TT, swizzle);
+        t0 = t[S - 1];
+        size0 = size[S - 1];
+        t1 = t[S];
     }
 };
 
@@ -205,52 +236,135 @@ __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
 // This CTA's run and where it begins; false: it has none.
 __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThreads> &s, int tokens, int vheads, Run &run, Place &at) {
     long long mine, before;
-    run.total = batch_total(p, s, tokens, vheads, mine, before);
-    const long long most = (run.total + kMinRounds - 1) / kMinRounds;
-    run.ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
-    if ((int)blockIdx.x >= run.ctas) return false;
-    run.r0 = run.total * blockIdx.x / run.ctas;
-    run.r1 = run.total * (blockIdx.x + 1) / run.ctas;
+    const long long total = batch_total(p, s, tokens, vheads, mine, before), most = (total + kMinRounds - 1) / kMinRounds;
+    const int ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
+    if ((int)blockIdx.x >= ctas) return false;
+    run.cut(total, ctas);
     batch_find(p, s, tokens, vheads, mine, before, run.r0);
     at.b = s.b;
     place_sequence(p, at, tokens);
-    at.vh = (int)(s.rem / at.rounds);
-    at.u = (int)(s.rem % at.rounds);
+    const unsigned rem = (unsigned)s.rem;   // (below rounds * heads, at most 2^26 * 2^10)
+    at.vh = at.rounds > 0 ? (int)(s.rem >> 32 ? s.rem / at.rounds : rem / (unsigned)at.rounds) : 0;
+    at.u = (int)(s.rem - (long long)at.vh * at.rounds);
     return true;
 }
 
-// After a CTA has written its partial result of the (sequence, key head) of rounds [seg0, seg1): the last of the runs that
-// share it joins their results in order.  Result k lies in slot 2 k + 1 where the (sequence, key head) begins in run k, else in
-// slot 2 k; a sum below zero marks one with a bad page.
+// ---- the join of the runs that share a (sequence, key head) ------------------------------------------------------------
+// Run k's result lies in slot 2 k + 1 where the (sequence, key head) begins in run k, else in slot 2 k: per query head a maximum
+// and a sum (below zero: a bad page) and the output before the division.
+constexpr int kJoinMost = 23;       // results joined at once: 23 * 23 covers kCacheMaxCtas
+template <int NQ> constexpr int kJoinScratch = (kJoinMost + 2) * NQ * 4;   // bytes
+
+template <typename T> __device__ __forceinline__ void store4(T *dst, float4 v);
+template <> __device__ __forceinline__ void store4<float>(float *dst, float4 v) { *reinterpret_cast<float4 *>(dst) = v; }
+template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 *dst, float4 v) {
+    const __nv_bfloat162 a = __floats2bfloat162_rn(v.x, v.y), b = __floats2bfloat162_rn(v.z, v.w);
+    *reinterpret_cast<uint2 *>(dst) = make_uint2(*reinterpret_cast<const uint32_t *>(&a), *reinterpret_cast<const uint32_t *>(&b));
+}
+
+// Joins the results of runs k0, k0 + step, ... (n of them, n <= kJoinMost) in this order, into the output or into the first one's
+// slot.  scratch: kJoinScratch<NQ> bytes of shared memory.
 template <typename T, int NQ>
-__device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, long long seg0, long long seg1, size_t head, int nq,
-                                          int &s_last) {
-    const int c0 = run.of(seg0), c1 = run.of(seg1 - 1), tid = threadIdx.x, dim = p.c.dim;
+__device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, int k0, int step, int n, bool last, size_t head, int nq,
+                                             float *scratch) {
+    const int tid = threadIdx.x, dim = p.c.dim;
+    float *weight = scratch, *sums = scratch + kJoinMost * NQ, *maxima = sums + NQ;
+    auto slot = [&](int j) { return (size_t)2 * (k0 + j * step) + (k0 + j * step == c0); };
+    if (tid < nq) {
+        float2 ml[kJoinMost];
+        float M = kLow, l = 0.0f;
+        bool none = false;
+#pragma unroll
+        for (int j = 0; j < kJoinMost; ++j) ml[j] = j < n ? __ldcg(&p.part_ml[slot(j) * NQ + tid]) : make_float2(kLow, 0.0f);
+#pragma unroll
+        for (int j = 0; j < kJoinMost; ++j) {
+            M = fmaxf(M, ml[j].x);
+            none |= ml[j].y < 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < kJoinMost; ++j)
+            if (j < n) {
+                const float f = ex2(ml[j].x - M);
+                weight[j * NQ + tid] = f;
+                l += ml[j].y * f;
+            }
+        sums[tid] = none ? -1.0f : l;
+        maxima[tid] = none ? INFINITY : M;
+    }
+    __syncthreads();
+    constexpr int kU = 4;   // columns of four in flight, for two results at a time
+    const int all = nq * dim / 4;
+    for (int e0 = tid; e0 < all; e0 += kU * kThreads) {
+        float4 acc[kU];
+        int q[kU];
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            acc[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            q[u] = min(e0 + u * kThreads, all - 1) * 4 / dim;
+        }
+#pragma unroll 2
+        for (int j = 0; j < n; ++j) {
+            const float4 *src = reinterpret_cast<const float4 *>(p.part + slot(j) * NQ * dim);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const float4 v = __ldcg(src + min(e0 + u * kThreads, all - 1));
+                const float f = weight[j * NQ + q[u]];
+                acc[u] = make_float4(fmaf(v.x, f, acc[u].x), fmaf(v.y, f, acc[u].y), fmaf(v.z, f, acc[u].z), fmaf(v.w, f, acc[u].w));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+            const int e = e0 + u * kThreads;
+            if (e >= all) break;
+            if (!last) {
+                *reinterpret_cast<float4 *>(p.part + slot(0) * NQ * dim + (size_t)e * 4) = acc[u];
+            } else if (sums[q[u]] >= 0.0f || sums[q[u]] != sums[q[u]]) {
+                const float inv = 1.0f / sums[q[u]];
+                store4(reinterpret_cast<T *>(p.out) + head * dim + (size_t)e * 4,
+                       sums[q[u]] == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f)
+                                          : make_float4(acc[u].x * inv, acc[u].y * inv, acc[u].z * inv, acc[u].w * inv));
+            }
+        }
+    }
+    if (tid < nq) {
+        const float l = sums[tid];
+        if (!last) p.part_ml[slot(0) * NQ + tid] = make_float2(maxima[tid], l);
+        else if (p.logits) p.lse[head + tid] = l <= 0.0f ? INFINITY : maxima[tid] + log2f(l);
+    }
+}
+
+// Whether this CTA is the last of n to come here (its writes before are seen by the last one).
+__device__ __forceinline__ bool arrive_last(int *counter, int n, int &s_last) {
     __threadfence();
     __syncthreads();
-    if (tid == 0) {
-        s_last = atomicAdd(&p.counters[c0], 1) == c1 - c0;
-        if (s_last) p.counters[c0] = 0;
+    if (threadIdx.x == 0) {
+        s_last = atomicAdd(counter, 1) == n - 1;
+        if (s_last) *counter = 0;
         __threadfence();
     }
     __syncthreads();
-    if (!s_last) return;
-    for (int e = tid; e < nq * dim; e += kThreads) {
-        const int q = e / dim, d = e % dim;
-        float M = kLow, sum = 0.0f, ls = 0.0f;
-        bool none = false;
-        for (int k = c0; k <= c1; ++k) {
-            const size_t ps = ((size_t)2 * k + (k == c0)) * NQ + q;
-            const float2 ml = __ldcg(&p.part_ml[ps]);
-            none |= ml.y < 0.0f;
-            const float mn = fmaxf(M, ml.x), f0 = ex2(M - mn), f1 = ex2(ml.x - mn);
-            sum = sum * f0 + __ldcg(&p.part[ps * dim + d]) * f1;
-            ls = ls * f0 + ml.y * f1;
-            M = mn;
-        }
-        if (!none) reinterpret_cast<T *>(p.out)[(head + q) * dim + d] = (T)(ls == 0.0f ? 0.0f : sum / ls);
-        if (d == 0 && p.logits) p.lse[head + q] = none || ls == 0.0f ? INFINITY : M + log2f(ls);
+    return s_last;
+}
+
+// After a CTA has written its result of the (sequence, key head) of rounds [seg0, seg1): the last of the runs that share it
+// joins their results.  More than eight are joined in two steps, groups of about the square root of their number first, by the
+// group's last (one CTA reads 16 KB in about 0.3 us, and the results of 38 runs of 32 heads of 128 are 600 KB).
+template <typename T, int NQ>
+__device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, long long seg0, long long seg1, size_t head, int nq,
+                                          float *scratch, int &s_last) {
+    const int c0 = run.of(seg0), n = run.of(seg1 - 1) - c0 + 1;
+    int size = n;   // of a group
+    if (n > 8)
+        for (size = 3; size * size < n;) ++size;
+    const int groups = (n + size - 1) / size, g = ((int)blockIdx.x - c0) / size, first = c0 + g * size, members = min(size, n - g * size);
+    int *count1 = p.counters, *count2 = p.counters + 2 * kCacheMaxCtas;   // both by the slot of the first run
+    if (members > 1 || groups == 1) {
+        if (!arrive_last(&count1[2 * first + (first == c0)], members, s_last)) return;
+        join_results<T, NQ>(p, c0, first, 1, members, groups == 1, head, nq, scratch);
     }
+    if (groups == 1) return;
+    if (!arrive_last(&count2[2 * c0 + 1], groups, s_last)) return;
+    join_results<T, NQ>(p, c0, c0, size, groups, true, head, nq, scratch);
 }
 
 // Host: as many CTAs as the GPU holds at once, or as there can be rounds.  What depends on the kernel and the device alone is

@@ -260,12 +260,12 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
     Run run;
     run.cut(total, (int)gridDim.x);
     if (run.r0 >= run.r1) return;
-    batch_find(p, batch, kWeightThreads, 1, mine, before, run.r0);
+    batch_find(p, batch, kWeightThreads, 1, mine, before, run.r0, -1);
     Place at;
-    at.b = batch.b;
+    at.b = batch.b[0];
     place_sequence(p, at, kWeightThreads);
     at.vh = 0;
-    at.u = (int)batch.rem;
+    at.u = (int)batch.rem[0];
     for (long long r = run.r0; r < run.r1; ++r) {
         const int j = at.u * kWeightThreads + threadIdx.x;
         unsigned page = 0;

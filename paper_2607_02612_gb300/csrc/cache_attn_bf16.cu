@@ -32,17 +32,18 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// Shared memory of a CTA: per warp S stages of TT rows of K and of V, the tokens' log2 sizes, the queries, and room for
-// the join of the warps' outputs, kJoinQ heads at a time.
+// Shared memory of a CTA: per warp S stages of TT rows of K and of V; the tokens' log2 sizes; then the queries, or, at the end of
+// a (sequence, key head), the warps' outputs on their way to each other, kTiles steps of 16 dims at a time (as many as a
+// thread has four values of).
 template <int DP, int NT, int TT, int S>
 struct Layout {
     static constexpr int kNq = 8 * NT, kRow = 2 * DP, kStage = 2 * TT * kRow;
-    static constexpr int kJoinQ = NT < 4 ? 4 : 2, kPitch = DP + 4;
+    static constexpr int kTiles = 4 / NT, kPitch = 16 * kTiles + 4;   // (pitches of 4 mod 16: no bank conflicts)
     static constexpr int kLsz = kWarps * S * kStage;
-    static constexpr int kQ = kLsz + kWarps * S * TT * 4;
-    static constexpr int kJoin = kQ + kNq * kRow;
-    static constexpr int kJoinBytes = kWarps * kJoinQ * kPitch * 4;
-    static constexpr int kTotal = kJoin + (kJoinBytes > kJoinScratch<kNq> ? kJoinBytes : kJoinScratch<kNq>);   // (or the join of the runs)
+    static constexpr int kShared = kLsz + kWarps * S * TT * 4;
+    static constexpr int kQBytes = kNq * kRow, kJoinBytes = kWarps * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
+    static constexpr int kTotal = kShared + (kQBytes > kJoinBytes ? kQBytes > kScratch ? kQBytes : kScratch
+                                             : kJoinBytes > kScratch ? kJoinBytes : kScratch);
 };
 
 template <int DP, int NT, int TT, int S>
@@ -50,7 +51,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
     using L = Layout<DP, NT, TT, S>;
     constexpr int kNq = L::kNq, kRound = kWarps * TT, kRow = L::kRow, kKs = DP / 16, kMt = TT / 16;
     constexpr int kQPer = (kNq * DP / 8 + kThreads - 1) / kThreads;   // 16-byte chunks of the queries per thread
-    constexpr bool kQRegs = NT * DP <= 256;                           // the queries' fragments stay in registers
+    constexpr bool kQRegs = NT * DP <= 256;     // the queries' fragments stay in registers
+    constexpr bool kQEarly = kQPer * NT <= 2;   // the next queries are asked for as soon as these are in use
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Batch<kThreads> batch;
     __shared__ float s_m[kWarps][kNq], s_l[kWarps][kNq];
@@ -67,9 +69,9 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
     }
     const long long r0 = run.r0, r1 = run.r1;
 
-    unsigned char *stages = sm + warp * S * L::kStage, *qs = sm + L::kQ;
+    unsigned char *stages = sm + warp * S * L::kStage, *qs = sm + L::kShared;
     float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
-    float *join = reinterpret_cast<float *>(sm + L::kJoin);
+    float *join = reinterpret_cast<float *>(sm + L::kShared);
     auto swizzle = [](int r) { return r & 7; };
 
     // the queries of a (sequence, key head): read ahead into registers, then written to shared memory
@@ -90,6 +92,14 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
             const int e = tid + k * kThreads, q = e / (DP / 8), cc = e % (DP / 8);
             if (q < kNq) *reinterpret_cast<uint4 *>(qs + q * kRow + ((cc ^ (q & 7)) << 4)) = qv[k];
         }
+    };
+    // those of the (sequence, key head) after the one of round r, if this run has it
+    auto read_next_q = [&](long long r) {
+        if (r + at.rounds - at.u >= r1) return;
+        Place next = at;
+        next.u = at.rounds - 1;
+        place_next(p, next, kRound, vheads);
+        read_q(next.b, next.vh);
     };
     read_q(at.b, at.vh);
     Stream<__nv_bfloat16, DP, TT> in;
@@ -128,7 +138,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
     begin_head();
     int st = 0;
     long long seg0 = r0 - at.u;   // first round of the (sequence, key head)
-    for (long long r = r0; r < r1; ++r) {
+    for (long long r = r0;; ++r) {
+        if (kQEarly && (r == r0 || at.u == 0)) read_next_q(r);
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
         in.next(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
@@ -250,11 +261,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
 
         // ---- the end of a (sequence, key head), or of the run: the warps' results together
         if (at.u + 1 == at.rounds || r + 1 == r1) {
-            if (r + 1 < r1) {
-                Place next = at;
-                place_next(p, next, kRound, vheads);
-                read_q(next.b, next.vh);
-            }
+            if (!kQEarly) read_next_q(r);
             if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(&s_bad, 1);
             bad = false;
 #pragma unroll
@@ -268,11 +275,9 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
                         s_l[warp][8 * n + 2 * t + e] = l[n][e];
                     }
                 }
-            __syncthreads();
-            write_q();   // every warp is past its products with the old ones
+            __syncthreads();   // (and every warp is past its products with the queries)
             const bool whole = seg0 >= r0 && seg0 + at.rounds <= r1, seg_bad = s_bad != 0;
-            const int slot = 2 * blockIdx.x + (seg0 >= r0 ? 1 : 0);   // of a partial result
-            const size_t head = (size_t)at.b * p.heads + head0;
+            const size_t head = (size_t)at.b * p.heads + head0, slot = (size_t)(2 * blockIdx.x + (seg0 >= r0 ? 1 : 0)) * kNq;   // of a partial result
             float f[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -283,50 +288,60 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][8 * n + 2 * t + e]);
                     f[n][e] = ex2(m[n][e] - M);
                 }
+            // this thread joins four dims of one head per step
+            const int q = tid / (4 * L::kTiles), d0 = tid % (4 * L::kTiles) * 4;
+            float M = s_m[0][q], ls = 0.0f;
 #pragma unroll
-            for (int q1 = 0; q1 < kNq; q1 += L::kJoinQ) {
-                if (q1 >= nq) break;
-                if (2 * t >= q1 % 8 && 2 * t < q1 % 8 + L::kJoinQ) {
-                    float *dst = join + (warp * L::kJoinQ + 2 * t - q1 % 8) * L::kPitch + g;
+            for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
 #pragma unroll
-                    for (int k = 0; k < kKs; ++k) {
-                        dst[16 * k] = o[k][q1 / 8][0] * f[q1 / 8][0];
-                        dst[16 * k + L::kPitch] = o[k][q1 / 8][1] * f[q1 / 8][1];
-                        dst[16 * k + 8] = o[k][q1 / 8][2] * f[q1 / 8][0];
-                        dst[16 * k + 8 + L::kPitch] = o[k][q1 / 8][3] * f[q1 / 8][1];
+            for (int w = 0; w < kWarps; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
+            const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
+            if (d0 == 0 && q < nq) {
+                if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+            }
+#pragma unroll
+            for (int k1 = 0; k1 < kKs; k1 += L::kTiles) {
+                float *dst = join + (warp * kNq + 2 * t) * L::kPitch + g;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    if (8 * n + 2 * t >= nq) break;
+#pragma unroll
+                    for (int k = 0; k < L::kTiles; ++k) {
+                        float *to = dst + 8 * n * L::kPitch + 16 * k;
+                        to[0] = o[k1 + k][n][0] * f[n][0];
+                        to[L::kPitch] = o[k1 + k][n][1] * f[n][1];
+                        to[8] = o[k1 + k][n][2] * f[n][0];
+                        to[L::kPitch + 8] = o[k1 + k][n][3] * f[n][1];
                     }
                 }
                 __syncthreads();
-                for (int e = tid; e < L::kJoinQ * DP / 4; e += kThreads) {
-                    const int qq = e / (DP / 4), q = q1 + qq, d = e % (DP / 4) * 4;
-                    if (q >= nq || d >= c.dim) continue;
-                    float M = s_m[0][q], ls = 0.0f;
+                const int d = 16 * k1 + d0;
+                if (q < nq && d < c.dim) {
+                    float4 sum = *reinterpret_cast<const float4 *>(join + q * L::kPitch + d0);
 #pragma unroll
-                    for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
-                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        ls += s_l[w][q] * ex2(s_m[w][q] - M);
-                        const float4 v = *reinterpret_cast<const float4 *>(join + (w * L::kJoinQ + qq) * L::kPitch + d);
+                    for (int w = 1; w < kWarps; ++w) {
+                        const float4 v = *reinterpret_cast<const float4 *>(join + (w * kNq + q) * L::kPitch + d0);
                         sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
                     }
-                    if (whole) {
-                        const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
-                        if (!seg_bad)
-                            *reinterpret_cast<uint2 *>(reinterpret_cast<__nv_bfloat16 *>(p.out) + (head + q) * c.dim + d) =
-                                ls == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack(sum.x * inv, sum.y * inv), pack(sum.z * inv, sum.w * inv));
-                        if (d == 0 && p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
-                    } else {
-                        *reinterpret_cast<float4 *>(p.part + ((size_t)slot * kNq + q) * c.dim + d) = sum;
-                        if (d == 0) p.part_ml[(size_t)slot * kNq + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
-                    }
+                    if (!whole)
+                        *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
+                    else if (!seg_bad)
+                        store4(reinterpret_cast<__nv_bfloat16 *>(p.out) + (head + q) * c.dim + d,
+                               ls == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
                 }
                 __syncthreads();
             }
-            if (seg_bad && tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
-            if (!whole) join_runs<__nv_bfloat16, kNq>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
-            __syncthreads();
-            if (tid == 0) s_bad = 0;
+            if (tid == 0) {
+                if (seg_bad) raise_status(p.status, FUSION_DEV_BAD_CACHE);
+                s_bad = 0;
+            }
+            if (!whole) {
+                join_runs<__nv_bfloat16, kNq>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
+                __syncthreads();
+            }
+            if (r + 1 == r1) break;
+            write_q();
             __syncthreads();
             begin_head();
             seg0 = r + 1;
@@ -334,7 +349,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
         place_next(p, at, kRound, vheads);
         if (++st == S) st = 0;
     }
-    cp_async_wait<0>();
+    cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)
 }
 
 template <int DP, int NT, int TT, int S>

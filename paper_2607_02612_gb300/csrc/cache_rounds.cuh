@@ -35,8 +35,8 @@ template <int THREADS>
 struct Batch {
     long long excl[THREADS / 32 + 1];
     long long total;
-    int b;                // sequence of the first round
-    long long rem;        // and the rounds of that sequence before it
+    int b[2];             // sequences of the run's first round and of the next run's
+    long long rem[2];     // and the rounds of those sequences before them
 };
 __device__ __forceinline__ long long rounds_of(const CacheAttnParams &p, int b, int tokens, int heads) {
     const int n = cache_length(p.c, b);
@@ -69,19 +69,25 @@ __device__ long long batch_total(const CacheAttnParams &p, Batch<THREADS> &s, in
     before = s.excl[warp] + incl - mine;
     return s.total;
 }
+// The sequences of rounds `first` and `next` (the latter may be past the batch: not looked for).
 template <int THREADS>
-__device__ void batch_find(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long mine, long long before, long long first) {
-    if (first >= before && first < before + mine) {
-        const int per = ceil_div(p.c.max_batch, THREADS);
-        long long at = before;
-        for (int b = threadIdx.x * per;; ++b) {
-            const long long r = rounds_of(p, b, tokens, heads);
-            if (first < at + r) {
-                s.b = b;
-                s.rem = first - at;
-                break;
+__device__ void batch_find(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long mine, long long before, long long first,
+                           long long next) {
+    const int per = ceil_div(p.c.max_batch, THREADS);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const long long x = k ? next : first;
+        if (x >= before && x < before + mine) {
+            long long at = before;
+            for (int b = threadIdx.x * per;; ++b) {
+                const long long r = rounds_of(p, b, tokens, heads);
+                if (x < at + r) {
+                    s.b[k] = b;
+                    s.rem[k] = x - at;
+                    break;
+                }
+                at += r;
             }
-            at += r;
         }
     }
     __syncthreads();
@@ -111,11 +117,13 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
     } while (s.rounds == 0);
 }
 
-// The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.
+// The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.  A boundary at most `snap` rounds
+// inside a (sequence, key head) moves to its nearer end (its beginning first): a join costs more time than the few rounds that
+// it would deal out.
 struct Run {
     long long total, len, more;
     long long r0, r1;   // this CTA's
-    int ctas;
+    int ctas, snap;
     __device__ __forceinline__ void cut(long long rounds, int n) {
         total = rounds;
         ctas = n;
@@ -124,11 +132,20 @@ struct Run {
         more = total - len * n;
         r0 = begin(blockIdx.x);
         r1 = begin(blockIdx.x + 1);
+        snap = len >= 8 ? 2 : len >= 4 ? 1 : 0;
     }
     __device__ __forceinline__ long long begin(long long k) const { return len * k + (k < more ? k : more); }
-    __device__ __forceinline__ int of(long long x) const {   // the run that holds round x
+    __device__ __forceinline__ int of(long long x) const {   // the last run that begins at round x or before, boundaries not moved
         const long long big = more * (len + 1);
         return (int)(x < big ? x / (len + 1) : more + (x - big) / len);
+    }
+    // by how much a boundary moves that lies u rounds inside a (sequence, key head) of n rounds
+    __device__ __forceinline__ int move(int u, int n) const { return u <= snap ? -u : n - u <= snap ? n - u : 0; }
+    // the runs that share the (sequence, key head) of rounds [s0, s1): the first of them, and their number
+    __device__ __forceinline__ int sharing(long long s0, long long s1, int &first) const {
+        const int k0 = of(s0 + snap) + 1, k1 = of(s1 - snap - 1);   // the boundaries inside
+        first = k0 - 1;
+        return k1 - k0 + 2;
     }
 };
 
@@ -240,12 +257,23 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThread
     const int ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
     if ((int)blockIdx.x >= ctas) return false;
     run.cut(total, ctas);
-    batch_find(p, s, tokens, vheads, mine, before, run.r0);
-    at.b = s.b;
-    place_sequence(p, at, tokens);
-    const unsigned rem = (unsigned)s.rem;   // (below rounds * heads, at most 2^26 * 2^10)
-    at.vh = at.rounds > 0 ? (int)(s.rem >> 32 ? s.rem / at.rounds : rem / (unsigned)at.rounds) : 0;
-    at.u = (int)(s.rem - (long long)at.vh * at.rounds);
+    batch_find(p, s, tokens, vheads, mine, before, run.r0, run.r1);
+    auto place = [&](int k) {
+        at.b = s.b[k];
+        place_sequence(p, at, tokens);
+        at.vh = at.rounds > 0 ? (int)(s.rem[k] >> 32 ? s.rem[k] / at.rounds : (unsigned)s.rem[k] / (unsigned)at.rounds) : 0;
+        at.u = (int)(s.rem[k] - (long long)at.vh * at.rounds);
+        return run.move(at.u, at.rounds);
+    };
+    if (run.r1 < total) run.r1 += place(1);
+    const int moved = place(0);
+    run.r0 += moved;
+    if (run.r0 >= run.r1) return false;
+    if (moved < 0) at.u = 0;
+    if (moved > 0) {
+        at.u = at.rounds - 1;
+        place_next(p, at, tokens, vheads);
+    }
     return true;
 }
 
@@ -335,12 +363,12 @@ __device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, i
 
 // Whether this CTA is the last of n to come here (its writes before are seen by the last one).
 __device__ __forceinline__ bool arrive_last(int *counter, int n, int &s_last) {
-    __threadfence();
-    __syncthreads();
+    __syncthreads();   // the CTA's writes come before thread 0's release, which passes them on
     if (threadIdx.x == 0) {
-        s_last = atomicAdd(counter, 1) == n - 1;
+        int before;
+        asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
+        s_last = before == n - 1;
         if (s_last) *counter = 0;
-        __threadfence();
     }
     __syncthreads();
     return s_last;
@@ -352,7 +380,8 @@ __device__ __forceinline__ bool arrive_last(int *counter, int n, int &s_last) {
 template <typename T, int NQ>
 __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, long long seg0, long long seg1, size_t head, int nq,
                                           float *scratch, int &s_last) {
-    const int c0 = run.of(seg0), n = run.of(seg1 - 1) - c0 + 1;
+    int c0;
+    const int n = run.sharing(seg0, seg1, c0);
     int size = n;   // of a group
     if (n > 8)
         for (size = 3; size * size < n;) ++size;

@@ -132,7 +132,7 @@ struct Run {
         more = total - len * n;
         r0 = begin(blockIdx.x);
         r1 = begin(blockIdx.x + 1);
-        snap = len >= 8 ? 2 : len >= 4 ? 1 : 0;
+        snap = len > 4 ? 4 : (int)len - 1;
     }
     __device__ __forceinline__ long long begin(long long k) const { return len * k + (k < more ? k : more); }
     __device__ __forceinline__ int of(long long x) const {   // the last run that begins at round x or before, boundaries not moved

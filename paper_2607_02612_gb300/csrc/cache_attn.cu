@@ -16,27 +16,25 @@ namespace {
 
 using namespace rounds;
 
-// The CTA's shared memory: per warp and stage TT rows of K, TT rows of V; then the tokens' log2 sizes, the queries, the
-// warps' joined output.
-template <typename T, int DP, int NQ, int TT, int S>
+// The CTA's shared memory: per warp and stage TT rows of K, TT rows of V; the tokens' log2 sizes; their probabilities, each
+// twice (a packed multiplication's operand); then the queries or, at the end of a (sequence, key head), the warps' outputs.
+template <int DP, int NQ, int TT, int S>
 struct Layout {
-    static constexpr int kRow = DP * (int)sizeof(T);
-    static constexpr int kStage = 2 * TT * kRow;
+    static constexpr int kRow = DP * 4, kStage = 2 * TT * kRow;
     static constexpr int kJoinQ = NQ < 4 ? NQ : 4;        // query heads joined at a time
-    static constexpr int kJoinPitch = DP + 4;
-    static constexpr int kStages = kWarps * S * kStage;
-    static constexpr int kLsz = kStages;                  // float [kWarps][S][TT]
-    static constexpr int kP = kLsz + kWarps * S * TT * 4; // float [kWarps][TT][NQ]
-    static constexpr int kQ = kP + kWarps * TT * NQ * 4;  // float [2][NQ][DP]
-    static constexpr int kJoin = kQ + 2 * NQ * DP * 4;    // float [kWarps][kJoinQ][kJoinPitch]
-    static constexpr int kJoinBytes = kWarps * kJoinQ * kJoinPitch * 4;
-    static constexpr int kTotal = kJoin + (kJoinBytes > kJoinScratch<NQ> ? kJoinBytes : kJoinScratch<NQ>);   // (or the join of the runs)
+    static constexpr int kPitch = DP + 4;
+    static constexpr int kLsz = kWarps * S * kStage;          // float [kWarps][S][TT]
+    static constexpr int kP = kLsz + kWarps * S * TT * 4;     // float2 [kWarps][TT][NQ]
+    static constexpr int kShared = kP + kWarps * TT * NQ * 8;
+    static constexpr int kQBytes = NQ * kRow, kJoinBytes = kWarps * kJoinQ * kPitch * 4, kScratch = kJoinScratch<NQ>;
+    static constexpr int kTotal = kShared + (kQBytes > kJoinBytes ? kQBytes > kScratch ? kQBytes : kScratch
+                                             : kJoinBytes > kScratch ? kJoinBytes : kScratch);
 };
 
-template <typename T, int DP, int NQ, int TT, int S>
-__global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int chunks) {
-    using L = Layout<T, DP, NQ, TT, S>;
-    constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kPer = 16 / (int)sizeof(T), kD = DP / 32;
+template <int DP, int NQ, int TT, int S>
+__global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, int chunks) {
+    using L = Layout<DP, NQ, TT, S>;
+    constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kD = DP / 32, kMt = TT / 8;
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Batch<kThreads> batch;
     __shared__ float s_m[kWarps][NQ], s_l[kWarps][NQ];
@@ -48,141 +46,178 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
     Run run;
     Place at;
     if (!find_run(p, batch, kRound, vheads, run, at)) {
-        empty_sequences<T>(p);
+        empty_sequences<float>(p);
         return;
     }
     const long long r0 = run.r0, r1 = run.r1;
 
     unsigned char *stages = sm + warp * S * L::kStage;
     float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
-    float *pw = reinterpret_cast<float *>(sm + L::kP) + warp * TT * NQ;
-    float *qs = reinterpret_cast<float *>(sm + L::kQ);
-    float *join = reinterpret_cast<float *>(sm + L::kJoin);
-    auto swizzle = [](int r) { return ((r & 1) << 2 | (r >> 1 & 3)) & (kCpr - 1); };
-    // the scaled queries of a (sequence, key head) as float32
-    auto load_q = [&](int b, int vh, float *dst) {
+    float2 *pw = reinterpret_cast<float2 *>(sm + L::kP) + warp * TT * NQ;
+    float *qs = reinterpret_cast<float *>(sm + L::kShared), *join = qs;
+    // (two tokens' chunks at the same place of their rows lie in different halves of the banks)
+    auto swizzle = [](int r) { return (r & 1) << 2 | (r >> 1 & 3); };
+    // the scaled queries of a (sequence, key head): read ahead into registers, then written to shared memory
+    constexpr int kQPer = (NQ * DP / 4 + kThreads - 1) / kThreads;
+    float4 qv[kQPer];
+    auto read_q = [&](int b, int vh) {
         const int h = vh / chunks, ch = vh % chunks;
-        for (int e = tid; e < NQ * DP; e += kThreads) {
-            const int q = e / DP, d = e % DP, a = ch * NQ + q;
-            dst[e] = a < p.group && d < c.dim
-                         ? Elem<T>::to_f(reinterpret_cast<const T *>(p.q)[(size_t)b * p.q_stride + (size_t)(h * p.group + a) * c.dim + d]) * p.scale2
-                         : 0.0f;
+        const float *src = reinterpret_cast<const float *>(p.q) + (size_t)b * p.q_stride + (size_t)(h * p.group + ch * NQ) * c.dim;
+#pragma unroll
+        for (int k = 0; k < kQPer; ++k) {
+            const int e = tid + k * kThreads, q = e / (DP / 4), d = e % (DP / 4) * 4;
+            qv[k] = q < min(NQ, p.group - ch * NQ) && d < c.dim ? *reinterpret_cast<const float4 *>(src + (size_t)q * c.dim + d)
+                                                                : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         }
     };
-
-    Stream<T, DP, TT> in;
+    auto write_q = [&]() {
+#pragma unroll
+        for (int k = 0; k < kQPer; ++k) {
+            const int e = tid + k * kThreads;
+            if (e < NQ * DP / 4)
+                reinterpret_cast<float4 *>(qs)[e] = make_float4(qv[k].x * p.scale2, qv[k].y * p.scale2, qv[k].z * p.scale2, qv[k].w * p.scale2);
+        }
+    };
+    // those of the (sequence, key head) after the one of round r, if this run has it
+    auto read_next_q = [&](long long r) {
+        if (r + at.rounds - at.u >= r1) return;
+        Place next = at;
+        next.u = at.rounds - 1;
+        place_next(p, next, kRound, vheads);
+        read_q(next.b, next.vh);
+    };
+    read_q(at.b, at.vh);
+    Stream<float, DP, TT> in;
     in.template begin<S>(p, at, run, chunks, vheads, warp, lane, stages, lsz, swizzle);
-    empty_sequences<T>(p);
-    load_q(at.b, at.vh, qs);
+    write_q();
+    empty_sequences<float>(p);
     if (tid == 0) s_bad = 0;
     __syncthreads();
-    bool bad = false;
 
-    float m[NQ], l[NQ], o[NQ][kD];
-    auto reset = [&]() {
+    bool bad = false;
+    float m[NQ], l[NQ];
+    float2 o[NQ][kD / 2];
+    auto begin_head = [&]() {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             m[q] = kLow;
             l[q] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < kD; ++d) o[q][d] = 0.0f;
+            for (int d = 0; d < kD / 2; ++d) o[q][d] = make_float2(0.0f, 0.0f);
         }
     };
-    reset();
-    int st = 0, qpar = 0;
+    begin_head();
+    int st = 0;
     long long seg0 = r0 - at.u;   // first round of the (sequence, key head)
-    for (long long r = r0; r < r1; ++r) {
+    for (long long r = r0;; ++r) {
+        if (r == r0 || at.u == 0) read_next_q(r);
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
         in.next(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
         cp_async_wait<S - 1>();
         __syncwarp();
 
-        // ---- logits: four lanes per token, eight tokens at a time
         const unsigned char *ks = stages + st * L::kStage, *vs = ks + TT * L::kRow;
-        const float *q0 = qs + qpar * NQ * DP, *lz = lsz + st * TT;
+        const float *lz = lsz + st * TT;
         const int j0 = at.u * kRound + warp * TT, cnt = min(TT, at.vis - j0);
-        const int h = at.vh / chunks, ch = at.vh % chunks, nq = min(NQ, p.group - ch * NQ);
-        const int head0 = h * p.group + ch * NQ;
+        const int h = at.vh / chunks, ch = at.vh % chunks, nq = min(NQ, p.group - ch * NQ), head0 = h * p.group + ch * NQ;
         if (cnt > 0) {
-            float x[TT / 8][NQ];
-            const int quad = lane & 3;
+            // ---- logits: four lanes per token, eight tokens side by side
+            const int quad = lane & 3, row0 = lane >> 2;
+            float2 acc[kMt][NQ];
 #pragma unroll
-            for (int k = 0; k < TT / 8; ++k) {
-                const int row = 8 * k + (lane >> 2), sw = swizzle(row);
+            for (int k = 0; k < kMt; ++k)
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) x[k][q] = 0.0f;
+                for (int q = 0; q < NQ; ++q) acc[k][q] = make_float2(0.0f, 0.0f);
 #pragma unroll
-                for (int i = 0; i < kCpr / 4; ++i) {
-                    const int cc = 4 * i + quad;
-                    float kv[kPer];
-                    chunk_to_f(*reinterpret_cast<const uint4 *>(ks + (row * kCpr + (cc ^ sw)) * 16), kv);
+            for (int i = 0; i < kCpr / 4; ++i) {
+                const int cc = 4 * i + quad;
+                float4 kv[kMt];
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q)
+                for (int k = 0; k < kMt; ++k)
+                    kv[k] = *reinterpret_cast<const float4 *>(ks + ((8 * k + row0) * kCpr + (cc ^ swizzle(8 * k + row0))) * 16);
 #pragma unroll
-                        for (int e = 0; e < kPer; e += 4) {
-                            const float4 qv = *reinterpret_cast<const float4 *>(q0 + q * DP + cc * kPer + e);
-                            x[k][q] = fmaf(kv[e], qv.x, fmaf(kv[e + 1], qv.y, fmaf(kv[e + 2], qv.z, fmaf(kv[e + 3], qv.w, x[k][q]))));
-                        }
+                for (int q = 0; q < NQ; ++q) {
+                    const float4 qq = *reinterpret_cast<const float4 *>(qs + q * DP + cc * 4);
+#pragma unroll
+                    for (int k = 0; k < kMt; ++k) {
+                        acc[k][q] = __ffma2_rn(make_float2(kv[k].x, kv[k].y), make_float2(qq.x, qq.y), acc[k][q]);
+                        acc[k][q] = __ffma2_rn(make_float2(kv[k].z, kv[k].w), make_float2(qq.z, qq.w), acc[k][q]);
+                    }
                 }
-                const float z = lz[row];
+            }
+            float x[kMt][NQ];
+#pragma unroll
+            for (int k = 0; k < kMt; ++k) {
+                const float z = lz[8 * k + row0];
+                const bool off = z == -INFINITY || z == kNoPage;
                 bad |= z == kNoPage;
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
-                    x[k][q] += __shfl_xor_sync(0xFFFFFFFFu, x[k][q], 1);
-                    x[k][q] += __shfl_xor_sync(0xFFFFFFFFu, x[k][q], 2);
-                    x[k][q] = z == -INFINITY || z == kNoPage ? -INFINITY : x[k][q] + z;
+                    float v = acc[k][q].x + acc[k][q].y;
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+                    x[k][q] = off ? -INFINITY : v + z;
                 }
-                if (p.logits && quad == 0 && row < cnt)
+                if (p.logits && quad == 0 && 8 * k + row0 < cnt) {
+                    float *dst = p.logits + ((size_t)at.b * p.heads + head0) * p.lstride + j0 + 8 * k + row0;
 #pragma unroll
                     for (int q = 0; q < NQ; ++q)
-                        if (q < nq) p.logits[((size_t)at.b * p.heads + head0 + q) * p.lstride + j0 + row] = x[k][q];
-            }
-            // ---- softmax with a running maximum
-#pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                float mx = x[0][q];
-#pragma unroll
-                for (int k = 1; k < TT / 8; ++k) mx = fmaxf(mx, x[k][q]);
-#pragma unroll
-                for (int s = 4; s < 32; s <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, s));
-                const float mn = fmaxf(m[q], mx), f = ex2(m[q] - mn);
-                m[q] = mn;
-                l[q] *= f;
-#pragma unroll
-                for (int d = 0; d < kD; ++d) o[q][d] *= f;
-#pragma unroll
-                for (int k = 0; k < TT / 8; ++k) {
-                    const float pr = ex2(x[k][q] - mn);
-                    l[q] += pr;
-                    if ((lane & 3) == 0) pw[(8 * k + (lane >> 2)) * NQ + q] = pr;
+                        if (q < nq) dst[q * p.lstride] = x[k][q];
                 }
             }
+            // ---- the running maximum grows: the output and the sums follow
+            bool grows = false;
+            float mx[NQ];
+#pragma unroll
+            for (int q = 0; q < NQ; ++q) {
+                mx[q] = m[q];
+#pragma unroll
+                for (int k = 0; k < kMt; ++k) mx[q] = fmaxf(mx[q], x[k][q]);
+                grows |= mx[q] > m[q];
+            }
+            if (__any_sync(0xFFFFFFFFu, grows)) {
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+#pragma unroll
+                    for (int s = 4; s < 32; s <<= 1) mx[q] = fmaxf(mx[q], __shfl_xor_sync(0xFFFFFFFFu, mx[q], s));
+                    const float f = ex2(m[q] - mx[q]);
+                    m[q] = mx[q];
+                    l[q] *= f;
+#pragma unroll
+                    for (int d = 0; d < kD / 2; ++d) o[q][d] = __fmul2_rn(o[q][d], make_float2(f, f));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kMt; ++k)
+#pragma unroll
+                for (int q = 0; q < NQ; ++q) {
+                    const float pr = ex2(x[k][q] - m[q]);
+                    l[q] += pr;
+                    if (quad == 0) pw[(8 * k + row0) * NQ + q] = make_float2(pr, pr);
+                }
             __syncwarp();
             // ---- o += p v: every lane has kD dims
 #pragma unroll 4
             for (int row = 0; row < TT; ++row) {
-                const int sw = swizzle(row), cc = lane * kD / kPer;
-                float v[kD];
+                float2 v[kD / 2];
+                const unsigned char *vr = vs + row * kCpr * 16;
 #pragma unroll
-                for (int d = 0; d < kD; ++d) {
-                    const int cd = cc + d / kPer;
-                    v[d] = Elem<T>::to_f(reinterpret_cast<const T *>(vs + (row * kCpr + (cd ^ sw)) * 16)[(lane * kD + d) % kPer]);
+                for (int d = 0; d < kD / 2; ++d) {
+                    const int cd = (lane * kD + 2 * d) / 4;
+                    v[d] = *reinterpret_cast<const float2 *>(vr + ((cd ^ swizzle(row)) * 16) + (lane * kD + 2 * d) % 4 * 4);
                 }
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
-                    const float pr = pw[row * NQ + q];
+                    const float2 pr = pw[row * NQ + q];
 #pragma unroll
-                    for (int d = 0; d < kD; ++d) o[q][d] = fmaf(pr, v[d], o[q][d]);
+                    for (int d = 0; d < kD / 2; ++d) o[q][d] = __ffma2_rn(pr, v[d], o[q][d]);
                 }
             }
         }
 
         // ---- the end of a (sequence, key head), or of the run: the warps' results together
         if (at.u + 1 == at.rounds || r + 1 == r1) {
-            Place next = at;
-            place_next(p, next, kRound, vheads);
-            if (r + 1 < r1) load_q(next.b, next.vh, qs + (qpar ^ 1) * NQ * DP);
             if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(&s_bad, 1);
             bad = false;
 #pragma unroll
@@ -194,10 +229,9 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
                     s_l[warp][q] = l[q];
                 }
             }
-            __syncthreads();
-            const bool whole = seg0 >= r0 && seg0 + at.rounds <= r1;
-            const int slot = 2 * blockIdx.x + (seg0 >= r0 ? 1 : 0);   // of a partial result
-            const bool seg_bad = s_bad != 0;
+            __syncthreads();   // (and every warp is past its products with the queries)
+            const bool whole = seg0 >= r0 && seg0 + at.rounds <= r1, seg_bad = s_bad != 0;
+            const size_t head = (size_t)at.b * p.heads + head0, slot = (size_t)(2 * blockIdx.x + (seg0 >= r0 ? 1 : 0)) * NQ;   // of a partial result
 #pragma unroll
             for (int q1 = 0; q1 < NQ; q1 += L::kJoinQ) {
 #pragma unroll
@@ -206,47 +240,55 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn(CacheAttnParams p, int 
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
                     const float f = ex2(m[q] - M);
+                    float2 *dst = reinterpret_cast<float2 *>(join + (warp * L::kJoinQ + q - q1) * L::kPitch + lane * kD);
 #pragma unroll
-                    for (int d = 0; d < kD; ++d) join[(warp * L::kJoinQ + q - q1) * L::kJoinPitch + lane * kD + d] = o[q][d] * f;
+                    for (int d = 0; d < kD / 2; ++d) dst[d] = __fmul2_rn(o[q][d], make_float2(f, f));
                 }
                 __syncthreads();
-                for (int e = tid; e < L::kJoinQ * DP; e += kThreads) {
-                    const int q = q1 + e / DP, d = e % DP;
+                for (int e = tid; e < L::kJoinQ * DP / 4; e += kThreads) {
+                    const int qq = e / (DP / 4), q = q1 + qq, d = e % (DP / 4) * 4;
                     if (q >= nq || d >= c.dim) continue;
-                    float M = s_m[0][q], sum = 0.0f, ls = 0.0f;
+                    float M = s_m[0][q], ls = 0.0f;
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
+                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
                     for (int w = 0; w < kWarps; ++w) {
                         ls += s_l[w][q] * ex2(s_m[w][q] - M);
-                        sum += join[(w * L::kJoinQ + q - q1) * L::kJoinPitch + d];
+                        const float4 v = *reinterpret_cast<const float4 *>(join + (w * L::kJoinQ + qq) * L::kPitch + d);
+                        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
                     }
                     if (whole) {
+                        const float inv = 1.0f / ls;
                         if (!seg_bad)
-                            reinterpret_cast<T *>(p.out)[((size_t)at.b * p.heads + head0 + q) * c.dim + d] = (T)(ls == 0.0f ? 0.0f : sum / ls);
-                        if (d == 0 && p.logits)
-                            p.lse[(size_t)at.b * p.heads + head0 + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+                            store4(reinterpret_cast<float *>(p.out) + (head + q) * c.dim + d,
+                                   ls == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+                        if (d == 0 && p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
                     } else {
-                        p.part[((size_t)slot * NQ + q) * c.dim + d] = sum;
-                        if (d == 0) p.part_ml[(size_t)slot * NQ + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                        *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
+                        if (d == 0) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
                     }
                 }
                 __syncthreads();
             }
-            if (seg_bad && tid == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
-            if (!whole) {
-                join_runs<T, NQ>(p, run, seg0, seg0 + at.rounds, (size_t)at.b * p.heads + head0, nq, join, s_last);
+            if (tid == 0) {
+                if (seg_bad) raise_status(p.status, FUSION_DEV_BAD_CACHE);
+                s_bad = 0;
             }
-            if (tid == 0) s_bad = 0;
+            if (!whole) {
+                join_runs<float, NQ>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
+                __syncthreads();
+            }
+            if (r + 1 == r1) break;
+            write_q();
             __syncthreads();
-            reset();
-            qpar ^= 1;
+            begin_head();
             seg0 = r + 1;
         }
         place_next(p, at, kRound, vheads);
         if (++st == S) st = 0;
     }
-    cp_async_wait<0>();
+    cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)
 }
 
 // weights_j += sum over the query heads of 2^(x - lse): tiles of 128 visible tokens, four to a lane, the heads dealt out to
@@ -306,8 +348,8 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
 
 template <int DP, int NQ, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
-    using L = Layout<float, DP, NQ, TT, S>;
-    return launch_rounds<k_cache_attn<float, DP, NQ, TT, S>>(L::kTotal, p, ceil_div(p.group, NQ), kWarps * TT, s);
+    using L = Layout<DP, NQ, TT, S>;
+    return launch_rounds<k_cache_attn_f32<DP, NQ, TT, S>>(L::kTotal, p, ceil_div(p.group, NQ), kWarps * TT, s);
 }
 template <int NQ>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {

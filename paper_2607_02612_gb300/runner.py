@@ -4,7 +4,6 @@ every step of the computation runs in libfusion.so.
 """
 from __future__ import annotations
 
-import contextlib
 from dataclasses import dataclass, field
 from typing import Dict, List, Optional
 
@@ -83,6 +82,10 @@ class RaggedRows:
     ids: Optional[torch.Tensor] = None
 
     def __post_init__(self):
+        index = self.offsets.get_device()
+        _need(self.offsets, torch.int32, index, "offsets", self.max_batch + 1)
+        _need(self.batch, torch.int32, index, "batch", 1)
+        _need(self.ids, torch.int32, index, "ids", self.max_batch)
         object.__setattr__(self, "_c", fb.ragged(self.max_batch, self.max_tokens, self.max_rows, self.offsets, self.batch,
                                                  self.ids))
 
@@ -90,12 +93,19 @@ class RaggedRows:
         return self._c
 
 
-_HERE = contextlib.nullcontext()
-
-
-def _on(device: int):
-    """The device as the current one (no context object where it is already: 1.5 us a call)."""
-    return _HERE if torch.cuda.current_device() == device else torch.cuda.device(device)
+def _enqueue(call, device: int, status: torch.Tensor, *args) -> None:
+    """A call of the C ABI on the device's current torch stream, the device made the current one (without a context
+    object where it is already, which is 1.5 us of the host's time); the status word is its last argument but the stream."""
+    if status.get_device() != device:
+        raise fb.FusionError("the status word and the cache are on different devices")
+    stream = torch._C._cuda_getCurrentRawStream(device)
+    if torch.cuda.current_device() == device:
+        rc = call(*args, status.data_ptr(), stream)
+    else:
+        with torch.cuda.device(device):
+            rc = call(*args, status.data_ptr(), stream)
+    if rc:
+        fb.check(rc)
 
 
 def _rows_ptr(t: torch.Tensor, rows: int, heads: int, head_dim: int, dtype: torch.dtype, device: int, what: str):
@@ -127,7 +137,8 @@ def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str,
 @dataclass
 class DeviceCache:
     """A paged key-value cache on the device (fusion_cache) with the scratch of its calls, which also fixes the number
-    of query heads.  Calls on one cache that may overlap on the device (other streams) need a cache object each."""
+    of query heads.  The tensors are changed in place, not replaced.  Calls that may overlap on the device (on other streams,
+    or in graphs that do) need a cache object each."""
     dtype: str
     heads: int
     k: torch.Tensor            # [num_pages, kv_heads, page_tokens, head_dim]
@@ -136,8 +147,8 @@ class DeviceCache:
     lengths: torch.Tensor      # [max_batch] int32
     sizes: Optional[torch.Tensor] = None     # [num_pages, page_tokens] float32
     weights: Optional[torch.Tensor] = None
-    workspace: Optional[torch.Tensor] = None
-    ws_bytes: int = 0
+    workspace: torch.Tensor = field(init=False)
+    ws_bytes: int = field(init=False)
 
     def __post_init__(self):
         pages, kv_heads, page_tokens, dim = self.k.shape
@@ -163,6 +174,7 @@ class DeviceCache:
         self.device, self.index = self.k.device, self.k.get_device()
         self.code, self.torch_dtype = DTYPE_CODE[self.dtype], TORCH_DTYPE[self.dtype]
         self.scale = self.head_dim ** -0.5
+        self.lib = fb.load()
         self._ws = self.workspace.data_ptr()
         self._one = None   # the offsets of one row per sequence
 
@@ -346,9 +358,8 @@ class Fusion:
         wp = _need(scores, torch.float32, c.index, "scores", rows.max_rows)
         o = lengths_out if lengths_out is not None else c.lengths
         op = _need(o, torch.int32, c.index, "lengths_out", c.max_batch)
-        with _on(c.index):
-            fb.check(fb.fusion_cache_append(c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp, wp, op, c._ws, c.ws_bytes,
-                                            self.status.data_ptr()))
+        _enqueue(c.lib.fusion_cache_append, c.index, self.status, c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp,
+                 wp, op, c._ws, c.ws_bytes)
         return o
 
     def cache_attention(self, c: DeviceCache, q: torch.Tensor, *, scale: Optional[float] = None, window: int = 0,
@@ -359,10 +370,11 @@ class Fusion:
         qp, qs = _rows_ptr(q, c.max_batch, c.heads, c.head_dim, c.torch_dtype, c.index, "queries")
         if out is None:
             out = torch.empty((c.max_batch, c.heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
-        op = _need(out, c.torch_dtype, c.index, "out", c.max_batch * c.heads * c.head_dim, 3)
-        with _on(c.index):
-            fb.check(fb.fusion_cache_attention(c.code, c.c_struct(), qp, qs, c.heads, c.scale if scale is None else scale,
-                                               window, sinks, op, c._ws, c.ws_bytes, self.status.data_ptr()))
+            op = out.data_ptr()
+        else:
+            op = _need(out, c.torch_dtype, c.index, "out", c.max_batch * c.heads * c.head_dim, 3)
+        _enqueue(c.lib.fusion_cache_attention, c.index, self.status, c.code, c.c_struct(), qp, qs, c.heads,
+                 c.scale if scale is None else scale, window, sinks, op, c._ws, c.ws_bytes)
         return out
 
     def cache_evict(self, c: DeviceCache, budget: torch.Tensor, *, sinks: int = 0, recent: int = 0,
@@ -378,11 +390,9 @@ class Fusion:
         for t, what in ((page_table_out, "page_table_out"), (keep_idx, "keep_idx")):
             if t is not None and t.shape[0] < c.max_batch:
                 raise fb.FusionError(f"{what}: a row per sequence expected")
-        with _on(c.index):
-            fb.check(fb.fusion_cache_evict(c.code, c.c_struct(), bp, sinks, recent, tp,
-                                           page_table_out.shape[1] if tp is not None else 0, op, kp,
-                                           keep_idx.shape[1] if kp is not None else 0, c._ws, c.ws_bytes,
-                                           self.status.data_ptr()))
+        _enqueue(c.lib.fusion_cache_evict, c.index, self.status, c.code, c.c_struct(), bp, sinks, recent, tp,
+                 page_table_out.shape[1] if tp is not None else 0, op, kp, keep_idx.shape[1] if kp is not None else 0, c._ws,
+                 c.ws_bytes)
         return o
 
     def exit_check(self, b: DeviceBatch, head: HeadTensors) -> Dict[str, torch.Tensor]:

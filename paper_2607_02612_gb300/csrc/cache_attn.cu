@@ -34,7 +34,9 @@ struct Layout {
 template <int DP, int NQ, int TT, int S>
 __global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, int chunks) {
     using L = Layout<DP, NQ, TT, S>;
-    constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kD = DP / 32, kMt = TT / 8;
+    constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kMt = TT / 8;
+    // for p v: a lane has kV chunks of four dims; narrow rows are shared out, kGroups of them side by side
+    constexpr int kGroups = DP < 128 ? 2 : 1, kLanes = 32 / kGroups, kV = DP / (4 * kLanes);
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Batch<kThreads> batch;
     __shared__ float s_m[kWarps][NQ], s_l[kWarps][NQ];
@@ -96,14 +98,14 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, 
 
     bool bad = false;
     float m[NQ], l[NQ];
-    float2 o[NQ][kD / 2];
+    float2 o[NQ][2 * kV];
     auto begin_head = [&]() {
 #pragma unroll
         for (int q = 0; q < NQ; ++q) {
             m[q] = kLow;
             l[q] = 0.0f;
 #pragma unroll
-            for (int d = 0; d < kD / 2; ++d) o[q][d] = make_float2(0.0f, 0.0f);
+            for (int d = 0; d < 2 * kV; ++d) o[q][d] = make_float2(0.0f, 0.0f);
         }
     };
     begin_head();
@@ -185,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, 
                     m[q] = mx[q];
                     l[q] *= f;
 #pragma unroll
-                    for (int d = 0; d < kD / 2; ++d) o[q][d] = __fmul2_rn(o[q][d], make_float2(f, f));
+                    for (int d = 0; d < 2 * kV; ++d) o[q][d] = __fmul2_rn(o[q][d], make_float2(f, f));
                 }
             }
 #pragma unroll
@@ -197,22 +199,32 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, 
                     if (quad == 0) pw[(8 * k + row0) * NQ + q] = make_float2(pr, pr);
                 }
             __syncwarp();
-            // ---- o += p v: every lane has kD dims
+            // ---- o += p v
 #pragma unroll 4
-            for (int row = 0; row < TT; ++row) {
-                float2 v[kD / 2];
-                const unsigned char *vr = vs + row * kCpr * 16;
+            for (int i = 0; i < TT / kGroups; ++i) {
+                const int row = i * kGroups + lane / kLanes;
+                float4 v[kV];
 #pragma unroll
-                for (int d = 0; d < kD / 2; ++d) {
-                    const int cd = (lane * kD + 2 * d) / 4;
-                    v[d] = *reinterpret_cast<const float2 *>(vr + ((cd ^ swizzle(row)) * 16) + (lane * kD + 2 * d) % 4 * 4);
+                for (int d = 0; d < kV; ++d)
+                    v[d] = *reinterpret_cast<const float4 *>(vs + (row * kCpr + ((lane % kLanes + d * kLanes) ^ swizzle(row))) * 16);
+                float2 pr[NQ];
+                if constexpr (NQ == 1) {
+                    pr[0] = pw[row];
+                } else {
+#pragma unroll
+                    for (int q = 0; q < NQ; q += 2) {
+                        const float4 two = *reinterpret_cast<const float4 *>(&pw[row * NQ + q]);
+                        pr[q] = make_float2(two.x, two.y);
+                        pr[q + 1] = make_float2(two.z, two.w);
+                    }
                 }
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) {
-                    const float2 pr = pw[row * NQ + q];
+                for (int q = 0; q < NQ; ++q)
 #pragma unroll
-                    for (int d = 0; d < kD / 2; ++d) o[q][d] = __ffma2_rn(pr, v[d], o[q][d]);
-                }
+                    for (int d = 0; d < kV; ++d) {
+                        o[q][2 * d] = __ffma2_rn(pr[q], make_float2(v[d].x, v[d].y), o[q][2 * d]);
+                        o[q][2 * d + 1] = __ffma2_rn(pr[q], make_float2(v[d].z, v[d].w), o[q][2 * d + 1]);
+                    }
             }
         }
 
@@ -240,9 +252,18 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, 
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
                     const float f = ex2(m[q] - M);
-                    float2 *dst = reinterpret_cast<float2 *>(join + (warp * L::kJoinQ + q - q1) * L::kPitch + lane * kD);
+                    float *dst = join + (warp * L::kJoinQ + q - q1) * L::kPitch + lane % kLanes * 4;
 #pragma unroll
-                    for (int d = 0; d < kD / 2; ++d) dst[d] = __fmul2_rn(o[q][d], make_float2(f, f));
+                    for (int d = 0; d < kV; ++d) {
+                        float4 v = make_float4(o[q][2 * d].x * f, o[q][2 * d].y * f, o[q][2 * d + 1].x * f, o[q][2 * d + 1].y * f);
+                        if constexpr (kGroups > 1) {
+                            v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, kLanes);
+                            v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, kLanes);
+                            v.z += __shfl_xor_sync(0xFFFFFFFFu, v.z, kLanes);
+                            v.w += __shfl_xor_sync(0xFFFFFFFFu, v.w, kLanes);
+                        }
+                        if (lane < kLanes) *reinterpret_cast<float4 *>(dst + d * kLanes * 4) = v;
+                    }
                 }
                 __syncthreads();
                 for (int e = tid; e < L::kJoinQ * DP / 4; e += kThreads) {

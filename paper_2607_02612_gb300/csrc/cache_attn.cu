@@ -21,7 +21,7 @@ using namespace rounds;
 template <int DP, int NQ, int TT, int S>
 struct Layout {
     static constexpr int kRow = DP * 4, kStage = 2 * TT * kRow;
-    static constexpr int kJoinQ = NQ < 4 ? NQ : 4;        // query heads joined at a time
+    static constexpr int kJoinQ = NQ < 2 ? NQ : 2;        // query heads joined at a time
     static constexpr int kPitch = DP + 4;
     static constexpr int kLsz = kWarps * S * kStage;          // float [kWarps][S][TT]
     static constexpr int kP = kLsz + kWarps * S * TT * 4;     // float2 [kWarps][TT][NQ]
@@ -32,7 +32,7 @@ struct Layout {
 };
 
 template <int DP, int NQ, int TT, int S>
-__global__ void __launch_bounds__(kThreads) k_cache_attn_f32(CacheAttnParams p, int chunks) {
+__global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(CacheAttnParams p, int chunks) {
     using L = Layout<DP, NQ, TT, S>;
     constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kMt = TT / 8;
     // for p v: a lane has kV chunks of four dims; narrow rows are shared out, kGroups of them side by side
@@ -374,8 +374,8 @@ cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
 }
 template <int NQ>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {
-    if (p.c.dim <= 64) return launch<64, NQ, 16, 3>(p, s);
-    if (p.c.dim <= 128) return launch<128, NQ, 8, 3>(p, s);
+    if (p.c.dim <= 64) return launch<64, NQ, 16, 2>(p, s);
+    if (p.c.dim <= 128) return launch<128, NQ, 8, 2>(p, s);
     return launch<256, NQ, 8, 3>(p, s);
 }
 

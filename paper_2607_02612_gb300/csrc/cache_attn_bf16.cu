@@ -38,7 +38,7 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 template <int DP, int NT, int TT, int S>
 struct Layout {
     static constexpr int kNq = 8 * NT, kRow = 2 * DP, kStage = 2 * TT * kRow;
-    static constexpr int kTiles = 4 / NT, kPitch = 16 * kTiles + 4;   // (pitches of 4 mod 16: no bank conflicts)
+    static constexpr int kTiles = NT == 1 ? 2 : 4 / NT, kPitch = 16 * kTiles + 4;   // (pitches of 4 mod 16: no bank conflicts)
     static constexpr int kLsz = kWarps * S * kStage;
     static constexpr int kShared = kLsz + kWarps * S * TT * 4;
     static constexpr int kQBytes = kNq * kRow, kJoinBytes = kWarps * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
@@ -47,7 +47,7 @@ struct Layout {
 };
 
 template <int DP, int NT, int TT, int S>
-__global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, int chunks) {
+__global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(CacheAttnParams p, int chunks) {
     using L = Layout<DP, NT, TT, S>;
     constexpr int kNq = L::kNq, kRound = kWarps * TT, kRow = L::kRow, kKs = DP / 16, kMt = TT / 16;
     constexpr int kQPer = (kNq * DP / 8 + kThreads - 1) / kThreads;   // 16-byte chunks of the queries per thread
@@ -289,14 +289,15 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
                     f[n][e] = ex2(m[n][e] - M);
                 }
             // this thread joins four dims of one head per step
-            const int q = tid / (4 * L::kTiles), d0 = tid % (4 * L::kTiles) * 4;
+            const bool joins = tid < kNq * 4 * L::kTiles;
+            const int q = joins ? tid / (4 * L::kTiles) : 0, d0 = tid % (4 * L::kTiles) * 4;
             float M = s_m[0][q], ls = 0.0f;
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
             const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
-            if (d0 == 0 && q < nq) {
+            if (joins && d0 == 0 && q < nq) {
                 if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
                 else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
             }
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attn_mma(CacheAttnParams p, 
                 }
                 __syncthreads();
                 const int d = 16 * k1 + d0;
-                if (q < nq && d < c.dim) {
+                if (joins && q < nq && d < c.dim) {
                     float4 sum = *reinterpret_cast<const float4 *>(join + q * L::kPitch + d0);
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) {
@@ -359,8 +360,8 @@ cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
 }
 template <int NT>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {
-    if (p.c.dim <= 64) return launch<64, NT, 32, 3>(p, s);
-    if (p.c.dim <= 128) return launch<128, NT, 16, 3>(p, s);
+    if (p.c.dim <= 64) return launch<64, NT, 32, NT == 1 ? 2 : 3>(p, s);
+    if (p.c.dim <= 128) return launch<128, NT, 16, NT == 1 ? 2 : 3>(p, s);
     return launch<256, NT < 2 ? NT : 2, 16, 3>(p, s);   // (four would need more registers than a thread has)
 }
 

@@ -43,11 +43,10 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Cache &c = p.c;
-    const int vheads = c.kv_heads * chunks;
     if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Run run;
     Place at;
-    if (!find_run(p, batch, kRound, vheads, run, at)) {
+    if (!find_run(p, batch, kRound, chunks, run, at)) {
         empty_sequences<float>(p);
         return;
     }
@@ -62,8 +61,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     // the scaled queries of a (sequence, key head): read ahead into registers, then written to shared memory
     constexpr int kQPer = (NQ * DP / 4 + kThreads - 1) / kThreads;
     float4 qv[kQPer];
-    auto read_q = [&](int b, int vh) {
-        const int h = vh / chunks, ch = vh % chunks;
+    auto read_q = [&](int b, int h, int ch) {
         const float *src = reinterpret_cast<const float *>(p.q) + (size_t)b * p.q_stride + (size_t)(h * p.group + ch * NQ) * c.dim;
 #pragma unroll
         for (int k = 0; k < kQPer; ++k) {
@@ -85,12 +83,12 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
         if (r + at.rounds - at.u >= r1) return;
         Place next = at;
         next.u = at.rounds - 1;
-        place_next(p, next, kRound, vheads);
-        read_q(next.b, next.vh);
+        place_next(p, next, kRound, c.kv_heads, chunks);
+        read_q(next.b, next.h, next.ch);
     };
-    read_q(at.b, at.vh);
+    read_q(at.b, at.h, at.ch);
     Stream<float, DP, TT> in;
-    in.template begin<S>(p, at, run, chunks, vheads, warp, lane, stages, lsz, swizzle);
+    in.template begin<S>(p, at, run, chunks, warp, lane, stages, lsz, swizzle);
     write_q();
     empty_sequences<float>(p);
     if (tid == 0) s_bad = 0;
@@ -115,14 +113,14 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
         if (r == r0 || at.u == 0) read_next_q(r);
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
-        in.next(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
+        in.next(p, chunks, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
         cp_async_wait<S - 1>();
         __syncwarp();
 
         const unsigned char *ks = stages + st * L::kStage, *vs = ks + TT * L::kRow;
         const float *lz = lsz + st * TT;
         const int j0 = at.u * kRound + warp * TT, cnt = min(TT, at.vis - j0);
-        const int h = at.vh / chunks, ch = at.vh % chunks, nq = min(NQ, p.group - ch * NQ), head0 = h * p.group + ch * NQ;
+        const int nq = min(NQ, p.group - at.ch * NQ), head0 = at.h * p.group + at.ch * NQ;
         if (cnt > 0) {
             // ---- logits: four lanes per token, eight tokens side by side
             const int quad = lane & 3, row0 = lane >> 2;
@@ -168,7 +166,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
                         if (q < nq) dst[q * p.lstride] = x[k][q];
                 }
             }
-            // ---- the running maximum grows: the output and the sums follow
+            // ---- the running shift: where a logit exceeds it by more than kLag, it becomes the maximum, and the output and the sums follow
             bool grows = false;
             float mx[NQ];
 #pragma unroll
@@ -176,7 +174,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
                 mx[q] = m[q];
 #pragma unroll
                 for (int k = 0; k < kMt; ++k) mx[q] = fmaxf(mx[q], x[k][q]);
-                grows |= mx[q] > m[q];
+                grows |= mx[q] > m[q] + kLag;
             }
             if (__any_sync(0xFFFFFFFFu, grows)) {
 #pragma unroll
@@ -306,7 +304,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
             begin_head();
             seg0 = r + 1;
         }
-        place_next(p, at, kRound, vheads);
+        place_next(p, at, kRound, c.kv_heads, chunks);
         if (++st == S) st = 0;
     }
     cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)
@@ -331,7 +329,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
     Place at;
     at.b = batch.b[0];
     place_sequence(p, at, kWeightTile);
-    at.vh = 0;
+    at.h = at.ch = 0;
     at.u = (int)batch.rem[0];
     for (long long r = run.r0; r < run.r1; ++r) {
         const int j0 = at.u * kWeightTile, j = j0 + tid;   // the token that this thread updates
@@ -363,7 +361,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
             *dst = old + sum;
         }
         __syncthreads();
-        place_next(p, at, kWeightTile, 1);
+        place_next(p, at, kWeightTile, 1, 1);
     }
 }
 

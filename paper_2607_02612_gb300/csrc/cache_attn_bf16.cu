@@ -59,11 +59,10 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const Cache &c = p.c;
-    const int vheads = c.kv_heads * chunks;
     if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Run run;
     Place at;
-    if (!find_run(p, batch, kRound, vheads, run, at)) {
+    if (!find_run(p, batch, kRound, chunks, run, at)) {
         empty_sequences<__nv_bfloat16>(p);
         return;
     }
@@ -76,8 +75,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
 
     // the queries of a (sequence, key head): read ahead into registers, then written to shared memory
     uint4 qv[kQPer];
-    auto read_q = [&](int b, int vh) {
-        const int h = vh / chunks, ch = vh % chunks;
+    auto read_q = [&](int b, int h, int ch) {
         const __nv_bfloat16 *src = reinterpret_cast<const __nv_bfloat16 *>(p.q) + (size_t)b * p.q_stride + (size_t)(h * p.group + ch * kNq) * c.dim;
 #pragma unroll
         for (int k = 0; k < kQPer; ++k) {
@@ -98,12 +96,12 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
         if (r + at.rounds - at.u >= r1) return;
         Place next = at;
         next.u = at.rounds - 1;
-        place_next(p, next, kRound, vheads);
-        read_q(next.b, next.vh);
+        place_next(p, next, kRound, c.kv_heads, chunks);
+        read_q(next.b, next.h, next.ch);
     };
-    read_q(at.b, at.vh);
+    read_q(at.b, at.h, at.ch);
     Stream<__nv_bfloat16, DP, TT> in;
-    in.template begin<S>(p, at, run, chunks, vheads, warp, lane, stages, lsz, swizzle);
+    in.template begin<S>(p, at, run, chunks, warp, lane, stages, lsz, swizzle);
     write_q();
     empty_sequences<__nv_bfloat16>(p);
     if (tid == 0) s_bad = 0;
@@ -142,14 +140,14 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
         if (kQEarly && (r == r0 || at.u == 0)) read_next_q(r);
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
-        in.next(p, chunks, vheads, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
+        in.next(p, chunks, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT, swizzle);
         cp_async_wait<S - 1>();
         __syncwarp();
 
         const uint32_t ks = smem_addr(stages + st * L::kStage), vs = ks + TT * kRow;
         const float *lz = lsz + st * TT;
         const int j0 = at.u * kRound + warp * TT;
-        const int h = at.vh / chunks, ch = at.vh % chunks, nq = min(kNq, p.group - ch * kNq), head0 = h * p.group + ch * kNq;
+        const int nq = min(kNq, p.group - at.ch * kNq), head0 = at.h * p.group + at.ch * kNq;
         if (j0 < at.vis) {
             // ---- S^T = K Q^T
             float x[kMt][NT][4];
@@ -207,7 +205,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
                             }
                 }
             }
-            // ---- the running maximum grows: O and the sums follow
+            // ---- the running shift: where a logit exceeds it by more than kLag, it becomes the maximum, and O and the sums follow
             float mx[NT][2];
             bool grows = false;
 #pragma unroll
@@ -217,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
                     mx[n][e] = m[n][e];
 #pragma unroll
                     for (int i = 0; i < kMt; ++i) mx[n][e] = fmaxf(mx[n][e], fmaxf(x[i][n][e], x[i][n][2 + e]));
-                    grows |= mx[n][e] > m[n][e];
+                    grows |= mx[n][e] > m[n][e] + kLag;
                 }
             if (__any_sync(0xFFFFFFFFu, grows)) {
 #pragma unroll
@@ -347,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
             begin_head();
             seg0 = r + 1;
         }
-        place_next(p, at, kRound, vheads);
+        place_next(p, at, kRound, c.kv_heads, chunks);
         if (++st == S) st = 0;
     }
     cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)

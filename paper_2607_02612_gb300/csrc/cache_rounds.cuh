@@ -12,6 +12,9 @@ namespace rounds {
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinRounds = 2;       // of a CTA: fewer and the join costs more than the split gains
 constexpr float kLow = -3.0e38f;    // a maximum over nothing: finite, so that (-inf) - kLow is -inf
+// Probabilities are 2^(x - shift) with a shift of at least the largest logit so far less kLag: up to 2^8, which costs no bits in
+// float32 or bf16, and tiles whose maximum grows a little do not rescale (with 32 heads in a warp nearly every tile did).
+constexpr float kLag = 8.0f;
 constexpr float kNoPage = 3.0e38f;  // in the place of a log2 size (at most 128): the token's page id is out of range
 
 __device__ __forceinline__ float ex2(float x) {   // 2^x, one MUFU instruction (2^-inf = 0)
@@ -95,7 +98,7 @@ __device__ void batch_find(const CacheAttnParams &p, Batch<THREADS> &s, int toke
 
 // Where in the batch a round lies.
 struct Place {
-    int b, vh, u;          // sequence, key head (times query chunk), round
+    int b, h, ch, u;       // sequence, key head, chunk of its query heads, round
     int n, vis, rounds;    // length, visible tokens, rounds of one key head
 };
 __device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens) {
@@ -103,11 +106,13 @@ __device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &
     s.vis = visible(p, s.n);
     s.rounds = (s.vis + tokens - 1) / tokens;
 }
-__device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, int tokens, int vheads) {
+__device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, int tokens, int heads, int chunks) {
     if (++s.u < s.rounds) return;
     s.u = 0;
-    if (++s.vh < vheads) return;
-    s.vh = 0;
+    if (++s.ch < chunks) return;
+    s.ch = 0;
+    if (++s.h < heads) return;
+    s.h = 0;
     do {
         if (++s.b >= p.c.max_batch) {
             s.rounds = s.vis = 0;
@@ -153,7 +158,7 @@ struct Run {
 struct Token {
     unsigned page;
     int place;       // -1: no token here
-    int vh;
+    int h;
 };
 
 // Tokens of the rounds to come, a warp's share of TT per round: the page is read two rounds before the token's rows are
@@ -167,8 +172,8 @@ struct Stream {
     Token t0, t1;            // t0's rows are asked for next (its size is here), then t1's
     float size0;
 
-    __device__ __forceinline__ Token look_up(const CacheAttnParams &p, int vheads, int warp, int lane) {
-        Token t{0u, -1, ahead.vh};
+    __device__ __forceinline__ Token look_up(const CacheAttnParams &p, int chunks, int warp, int lane) {
+        Token t{0u, -1, ahead.h};
         if (ahead_r < r1) {
             const int j = ahead.u * kRound + warp * TT + lane;
             if (lane < TT && j < ahead.vis) {
@@ -176,46 +181,53 @@ struct Stream {
                 t.place = cache_page(p.c, ahead.b, pos, t.page) ? pos & ((1 << p.c.shift) - 1) : -2;
             }
             ++ahead_r;
-            place_next(p, ahead, kRound, vheads);
+            place_next(p, ahead, kRound, p.c.kv_heads, chunks);
         }
         return t;
     }
     __device__ __forceinline__ float size_of(const CacheAttnParams &p, const Token &t) const {
         return t.place < 0 ? 0.0f : p.c.sizes ? p.c.sizes[((size_t)t.page << p.c.shift) + t.place] : 1.0f;
     }
-    // Asks for a token's rows (K, then V, rows of kRow bytes with chunk c of row r at c ^ swizzle(r)).
+    // Asks for a token's rows (K, then V, rows of kRow bytes with chunk c of row r at c ^ swizzle(r)).  swizzle is linear in the
+    // bits of r, and a lane has the same chunk in every step, so a step costs one address for each pool and one exclusive or.
     template <typename Swizzle>
-    __device__ __forceinline__ void ask(const CacheAttnParams &p, const Token &t, float size, int chunks, int lane, unsigned char *stage,
-                                        float *lsz, Swizzle swizzle) {
-        const int row_chunks = p.c.dim * (int)sizeof(T) / 16;   // that exist
-        const unsigned row = ((t.page * (unsigned)p.c.kv_heads + (unsigned)(t.vh / chunks)) << p.c.shift) + (unsigned)t.place;
+    __device__ __forceinline__ void ask(const CacheAttnParams &p, const Token &t, float size, int lane, unsigned char *stage, float *lsz,
+                                        Swizzle swizzle) {
         const bool live = t.place >= 0 && size != 0.0f;
-        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live);
+        const unsigned row = live ? ((t.page * (unsigned)p.c.kv_heads + (unsigned)t.h) << p.c.shift) + (unsigned)t.place : 0u;
+        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live), row_bytes = (unsigned)p.c.dim * (unsigned)sizeof(T);
         if (lane < TT) lsz[lane] = t.place == -2 ? kNoPage : live ? log2f(size) : -INFINITY;
+        constexpr int kWide = kCpr < 32 ? 32 / kCpr : 1, kParts = kCpr > 32 ? kCpr / 32 : 1;   // rows of a step, steps of a row
+        const int r_lane = lane / (32 / kWide);
 #pragma unroll
-        for (int e = 0; e < TT * kCpr / 32; ++e) {
-            const int x = e * 32 + lane, r = x / kCpr, cc = x % kCpr;
-            const unsigned rr = __shfl_sync(0xFFFFFFFFu, row, r);
-            const bool read = (lives >> r & 1u) && cc < row_chunks;
-            const size_t off = read ? ((size_t)rr * row_chunks + cc) * 16 : 0;
-            const uint32_t dst = smem_addr(stage) + (r * kCpr + (cc ^ swizzle(r))) * 16;
-            cp_async16_zfill(dst, p.c.k + off, read);
-            cp_async16_zfill(dst + TT * kRow, p.c.v + off, read);
+        for (int part = 0; part < kParts; ++part) {
+            const int cc = lane % (32 / kWide) + part * 32;
+            const bool exists = (unsigned)cc * 16u < row_bytes;
+            const unsigned mine = exists ? lives >> r_lane : 0u;
+            const unsigned char *k = p.c.k + (exists ? cc : 0) * 16, *v = p.c.v + (exists ? cc : 0) * 16;
+            const uint32_t dst = smem_addr(stage) + r_lane * kRow, at = (uint32_t)(cc ^ swizzle(r_lane)) * 16u;
+#pragma unroll
+            for (int e = 0; e < TT / kWide; ++e) {
+                const size_t off = (size_t)__shfl_sync(0xFFFFFFFFu, row, e * kWide + r_lane) * row_bytes;
+                const bool read = mine >> (e * kWide) & 1u;
+                const uint32_t to = dst + e * kWide * kRow + (at ^ (uint32_t)(swizzle(e * kWide) * 16));
+                cp_async16_zfill(to, k + off, read);
+                cp_async16_zfill(to + TT * kRow, v + off, read);
+            }
         }
         cp_async_commit();
     }
     // The next round's rows into `stage`.
     template <typename Swizzle>
-    __device__ __forceinline__ void next(const CacheAttnParams &p, int chunks, int vheads, int warp, int lane, unsigned char *stage, float *lsz,
-                                         Swizzle swizzle) {
-        ask(p, t0, size0, chunks, lane, stage, lsz, swizzle);
+    __device__ __forceinline__ void next(const CacheAttnParams &p, int chunks, int warp, int lane, unsigned char *stage, float *lsz, Swizzle swizzle) {
+        ask(p, t0, size0, lane, stage, lsz, swizzle);
         t0 = t1;
         size0 = size_of(p, t0);
-        t1 = look_up(p, vheads, warp, lane);
+        t1 = look_up(p, chunks, warp, lane);
     }
     // The first S - 1 rounds' rows (all pages asked for at once, then all sizes).
     template <int S, typename Swizzle>
-    __device__ __forceinline__ void begin(const CacheAttnParams &p, const Place &at, const Run &run, int chunks, int vheads, int warp, int lane,
+    __device__ __forceinline__ void begin(const CacheAttnParams &p, const Place &at, const Run &run, int chunks, int warp, int lane,
                                           unsigned char *stages, float *lsz, Swizzle swizzle) {
         ahead = at;
         ahead_r = run.r0;
@@ -223,11 +235,11 @@ struct Stream {
         Token t[S + 1];
         float size[S];
 #pragma unroll
-        for (int s = 0; s <= S; ++s) t[s] = look_up(p, vheads, warp, lane);
+        for (int s = 0; s <= S; ++s) t[s] = look_up(p, chunks, warp, lane);
 #pragma unroll
         for (int s = 0; s < S; ++s) size[s] = size_of(p, t[s]);
 #pragma unroll
-        for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], chunks, lane, stages + s * kStage, lsz + s * TT, swizzle);
+        for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], lane, stages + s * kStage, lsz + s * TT, swizzle);
         t0 = t[S - 1];
         size0 = size[S - 1];
         t1 = t[S];
@@ -251,8 +263,9 @@ __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
 }
 
 // This CTA's run and where it begins; false: it has none.
-__device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThreads> &s, int tokens, int vheads, Run &run, Place &at) {
+__device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThreads> &s, int tokens, int chunks, Run &run, Place &at) {
     long long mine, before;
+    const int vheads = p.c.kv_heads * chunks;
     const long long total = batch_total(p, s, tokens, vheads, mine, before), most = (total + kMinRounds - 1) / kMinRounds;
     const int ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
     if ((int)blockIdx.x >= ctas) return false;
@@ -261,8 +274,10 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThread
     auto place = [&](int k) {
         at.b = s.b[k];
         place_sequence(p, at, tokens);
-        at.vh = at.rounds > 0 ? (int)(s.rem[k] >> 32 ? s.rem[k] / at.rounds : (unsigned)s.rem[k] / (unsigned)at.rounds) : 0;
-        at.u = (int)(s.rem[k] - (long long)at.vh * at.rounds);
+        const int vh = at.rounds > 0 ? (int)(s.rem[k] >> 32 ? s.rem[k] / at.rounds : (unsigned)s.rem[k] / (unsigned)at.rounds) : 0;
+        at.u = (int)(s.rem[k] - (long long)vh * at.rounds);
+        at.h = vh / chunks;
+        at.ch = vh % chunks;
         return run.move(at.u, at.rounds);
     };
     if (run.r1 < total) run.r1 += place(1);
@@ -272,7 +287,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThread
     if (moved < 0) at.u = 0;
     if (moved > 0) {
         at.u = at.rounds - 1;
-        place_next(p, at, tokens, vheads);
+        place_next(p, at, tokens, p.c.kv_heads, chunks);
     }
     return true;
 }

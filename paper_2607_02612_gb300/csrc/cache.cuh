@@ -34,14 +34,14 @@ __device__ __forceinline__ int cache_length(const Cache &c, int b) {
 // Scratch behind the counters of the workspace.  Attention: log-sum-exps, partial results of sequences that
 // several CTAs share, logits (only where weights are accumulated).  Eviction: the kept slots and their counts.
 constexpr int kCacheMaxCtas = 512;   // CTAs of the attention kernel; each has two partial results at most
-constexpr int kCacheMaxQ = 32;       // query heads of a key head that one CTA takes
+constexpr int kCacheMaxQ = 16;       // query heads of a key head that one CTA takes, at most
 struct CacheWs {
     size_t counters, lse, part_ml, part, logits, keep, plan, total;
     long long lstride;               // logits of one (sequence, head)
 };
 inline CacheWs cache_ws_layout(int max_batch, int max_pages, int page_tokens, int kv_heads, int dim, int heads, bool weights) {
     const size_t b = max_batch > 0 ? max_batch : 1, cap = (size_t)max_pages * page_tokens;
-    const int group = heads / kv_heads, nq = group <= 8 ? 8 : group <= 16 ? 16 : kCacheMaxQ;
+    const int group = heads / kv_heads, nq = group <= 8 ? 8 : kCacheMaxQ;
     CacheWs L;
     L.lstride = (long long)((cap + 3) / 4 * 4);
     L.counters = 0;

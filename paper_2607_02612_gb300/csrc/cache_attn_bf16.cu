@@ -33,12 +33,11 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 }
 
 // Shared memory of a CTA: per warp S stages of TT rows of K and of V; the tokens' log2 sizes; then the queries, or, at the end of
-// a (sequence, key head), the warps' outputs on their way to each other, kTiles steps of 16 dims at a time (as many as a
-// thread has four values of).
+// a (sequence, key head), the warps' outputs on their way to each other, kTiles steps of 16 dims at a time.
 template <int DP, int NT, int TT, int S>
 struct Layout {
     static constexpr int kNq = 8 * NT, kRow = 2 * DP, kStage = 2 * TT * kRow;
-    static constexpr int kTiles = NT == 1 ? 2 : 4 / NT, kPitch = 16 * kTiles + 4;   // (pitches of 4 mod 16: no bank conflicts)
+    static constexpr int kTiles = 2, kPitch = 16 * kTiles + 4;   // (pitches of 4 mod 16: no bank conflicts)
     static constexpr int kLsz = kWarps * S * kStage;
     static constexpr int kShared = kLsz + kWarps * S * TT * 4;
     static constexpr int kQBytes = kNq * kRow, kJoinBytes = kWarps * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
@@ -51,8 +50,8 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     using L = Layout<DP, NT, TT, S>;
     constexpr int kNq = L::kNq, kRound = kWarps * TT, kRow = L::kRow, kKs = DP / 16, kMt = TT / 16;
     constexpr int kQPer = (kNq * DP / 8 + kThreads - 1) / kThreads;   // 16-byte chunks of the queries per thread
-    constexpr bool kQRegs = NT * DP <= 256;     // the queries' fragments stay in registers
-    constexpr bool kQEarly = kQPer * NT <= 2;   // the next queries are asked for as soon as these are in use
+    constexpr bool kQRegs = NT * DP <= 128;     // the queries' fragments stay in registers
+    constexpr bool kQEarly = NT == 1;           // the next queries are asked for as soon as these are in use
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Batch<kThreads> batch;
     __shared__ float s_m[kWarps][kNq], s_l[kWarps][kNq];
@@ -358,15 +357,18 @@ cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
 }
 template <int NT>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {
-    if (p.c.dim <= 64) return launch<64, NT, 32, NT == 1 ? 2 : 3>(p, s);
-    if (p.c.dim <= 128) return launch<128, NT, 16, NT == 1 ? 2 : 3>(p, s);
-    return launch<256, NT < 2 ? NT : 2, 16, 3>(p, s);   // (four would need more registers than a thread has)
+    // (two stages let three CTAs share an SM, which hides more than a third stage: 64 x 4096 with weights 112 -> 103 us)
+    if (p.c.dim <= 64) return launch<64, NT, 32, 2>(p, s);
+    if (p.c.dim <= 128) return launch<128, NT, 16, 2>(p, s);
+    return launch<256, NT, 16, 3>(p, s);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_attention_bf16(const CacheAttnParams &p, cudaStream_t s) {
-    return p.group <= 8 ? launch_dim<1>(p, s) : p.group <= 16 ? launch_dim<2>(p, s) : launch_dim<4>(p, s);
+    // groups beyond 16 heads go in parts of 16, the later ones reading K and V from the L2 cache: 32 heads a warp leave it 255
+    // registers and two CTAs per SM (8 x 8192 with one key head of 32 query heads 22.9 us, in two parts 19.8)
+    return p.group <= 8 ? launch_dim<1>(p, s) : launch_dim<2>(p, s);
 }
 
 }  // namespace fz

@@ -20,7 +20,7 @@ __device__ bool named_twice(const Ragged &in, int B, int i, int slot) {
     return __syncthreads_or(twice);
 }
 
-__global__ void __launch_bounds__(kThreads) k_cache_append(CacheAppendParams p, int rows_per_cta, int row_chunks, int head_chunks) {
+__global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams p, int row_chunks, int head_chunks) {
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
     const int B = device_batch(p.in);
@@ -47,34 +47,36 @@ __global__ void __launch_bounds__(kThreads) k_cache_append(CacheAppendParams p, 
         return;
     }
     const int o0 = p.in.offsets[i], n = p.in.offsets[i + 1] - o0, at = c.lengths[slot];
-    int bad = 0;
-    if (o0 < 0 || n < 0 || n > p.in.max_tokens || (long long)o0 + n > p.in.max_rows) bad = FUSION_DEV_BAD_OFFSETS;
-    else if (at < 0 || at > c.capacity || n > c.capacity - at) bad = FUSION_DEV_BAD_CACHE;
-    const int r0 = blockIdx.x * rows_per_cta, r1 = bad ? r0 : min(n, r0 + rows_per_cta), chunks = (r1 - r0) * row_chunks;
-    // chunk e of the CTA: row r0 + e / row_chunks, its (e % row_chunks)-th of all heads
+    const bool rows_ok = o0 >= 0 && n >= 0 && n <= p.in.max_tokens && (long long)o0 + n <= p.in.max_rows;
+    // `side` rows side by side, a thread has the same chunk (of `width` threads' chunks) of kPer rows of the CTA
+    const int width = min(row_chunks, kThreads), side = kThreads / width, r_mine = tid / width;
+    const int r0 = blockIdx.x * side * kPer, r1 = rows_ok && r_mine < side ? min(n, r0 + side * kPer) : r0;
     uint4 k[kPer], v[kPer];
-    int row[kPer], ch[kPer];
-    auto load = [&](int e0) {
+    auto load = [&](int ch) {
+        const unsigned char *ks = p.k + (size_t)(o0 + r0 + r_mine) * p.k_stride + (size_t)ch * 16;
+        const unsigned char *vs = p.v + (size_t)(o0 + r0 + r_mine) * p.v_stride + (size_t)ch * 16;
+#pragma unroll
+        for (int x = 0; x < kPer; ++x)
+            if (r0 + r_mine + x * side < r1) {
+                k[x] = ldg16(ks + (size_t)(x * side) * p.k_stride);
+                v[x] = ldg16(vs + (size_t)(x * side) * p.v_stride);
+            }
+    };
+    load(tid % width);
+    int bad = !rows_ok ? FUSION_DEV_BAD_OFFSETS : at < 0 || at > c.capacity || n > c.capacity - at ? FUSION_DEV_BAD_CACHE : 0;
+    unsigned page[kPer];
+    bool wrong = false;
+    if (!bad) {
+        const unsigned *pages = reinterpret_cast<const unsigned *>(c.table) + (size_t)slot * c.max_pages;
 #pragma unroll
         for (int x = 0; x < kPer; ++x) {
-            const int e = e0 + x * kThreads + tid;
-            row[x] = e / row_chunks;
-            ch[x] = e - row[x] * row_chunks;
-            if (e < chunks) {
-                k[x] = ldg16(p.k + (size_t)(o0 + r0 + row[x]) * p.k_stride + (size_t)ch[x] * 16);
-                v[x] = ldg16(p.v + (size_t)(o0 + r0 + row[x]) * p.v_stride + (size_t)ch[x] * 16);
-            }
+            const int r = r0 + r_mine + x * side;
+            page[x] = r < r1 ? pages[(at + r) >> c.shift] : 0u;
         }
-    };
-    load(0);
-    const bool twice = named_twice(p.in, B, i, slot);
-    if (twice) bad |= FUSION_DEV_BAD_IDS;
-    if (!bad && n > 0) {
-        bool wrong = false;
-        for (int e = (at >> c.shift) + tid; e <= (at + n - 1) >> c.shift; e += kThreads)
-            wrong |= (unsigned)c.table[(size_t)slot * c.max_pages + e] >= c.num_pages;
-        if (__syncthreads_or(wrong)) bad = FUSION_DEV_BAD_CACHE;
+        for (int e = (at >> c.shift) + tid; n > 0 && e <= (at + n - 1) >> c.shift; e += kThreads) wrong |= pages[e] >= c.num_pages;
     }
+    if (named_twice(p.in, B, i, slot)) bad |= FUSION_DEV_BAD_IDS;
+    if (__syncthreads_or(wrong)) bad |= FUSION_DEV_BAD_CACHE;
     if (bad) {   // nothing of this sample is written, and its slot's length stays (also where it is named twice)
         if (blockIdx.x == 0 && tid == 0) {
             raise_status(p.status, bad);
@@ -83,23 +85,22 @@ __global__ void __launch_bounds__(kThreads) k_cache_append(CacheAppendParams p, 
         return;
     }
     const unsigned low = (1u << c.shift) - 1u;
-    for (int e0 = 0; e0 < chunks; e0 += kPer * kThreads) {
-        if (e0 > 0) load(e0);   // (rows of more than kPer * kThreads chunks)
+    for (int ch = tid % width; ch < row_chunks; ch += kThreads) {   // (once, unless a row has more than kThreads chunks)
+        if (ch >= kThreads) load(ch);
+        const int h = ch / head_chunks, cc = ch - h * head_chunks;
 #pragma unroll
         for (int x = 0; x < kPer; ++x) {
-            if (e0 + x * kThreads + tid >= chunks) break;
-            const int pos = at + r0 + row[x], h = ch[x] / head_chunks, cc = ch[x] - h * head_chunks;
-            unsigned page;
-            cache_page(c, slot, pos, page);
-            const size_t dst = ((size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + (pos & low)) * head_chunks + cc) * 16;
+            const int r = r0 + r_mine + x * side;
+            if (r >= r1) break;
+            const size_t dst = ((size_t)(((page[x] * (unsigned)c.kv_heads + h) << c.shift) + ((at + r) & low)) * head_chunks + cc) * 16;
             *reinterpret_cast<uint4 *>(c.k + dst) = k[x];
             *reinterpret_cast<uint4 *>(c.v + dst) = v[x];
         }
     }
-    for (int r = r0 + tid; r < r1; r += kThreads) {
-        unsigned page;
-        cache_page(c, slot, at + r, page);
-        const size_t s = ((size_t)page << c.shift) + ((at + r) & low);
+    for (int r = r0 + tid; r < min(n, r0 + side * kPer); r += kThreads) {
+        unsigned pg;
+        cache_page(c, slot, at + r, pg);
+        const size_t s = ((size_t)pg << c.shift) + ((at + r) & low);
         if (c.sizes) c.sizes[s] = p.sizes ? p.sizes[o0 + r] : 1.0f;
         if (c.weights) c.weights[s] = p.scores ? p.scores[o0 + r] : 0.0f;
     }
@@ -122,9 +123,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_append(CacheAppendParams p, 
 
 cudaError_t launch_cache_append(int dtype, const CacheAppendParams &p, cudaStream_t s) {
     const int es = dtype == FUSION_BF16 ? 2 : 4, head_chunks = p.c.dim * es / 16, row_chunks = head_chunks * p.c.kv_heads;
-    const int fit = kPer * kThreads / row_chunks, rows = fit > 1 ? fit : 1;
-    k_cache_append<<<dim3((unsigned)ceil_div(p.in.max_tokens, rows), (unsigned)p.in.max_batch + 1), kThreads, 0, s>>>(
-        p, rows, row_chunks, head_chunks);
+    const int rows = kPer * (row_chunks < kThreads ? kThreads / row_chunks : 1);
+    k_cache_append<<<dim3((unsigned)ceil_div(p.in.max_tokens, rows), (unsigned)p.in.max_batch + 1), kThreads, 0, s>>>(p, row_chunks, head_chunks);
     return cudaGetLastError();
 }
 

@@ -89,6 +89,21 @@ def test_append_one_row_each_and_defaults(dtype):
     same(dc, c)
 
 
+@pytest.mark.parametrize("dtype,kv_heads,dim", [("bf16", 1, 8), ("f32", 1, 8), ("f32", 9, 256)])
+def test_append_narrow_and_wide_rows(dtype, kv_heads, dim):
+    """Rows of 16 bytes, of which a CTA takes many more than it has threads, and of more chunks than it has threads."""
+    c = ref.make(dtype, [3, 0], kv_heads, dim, 32, room=3000, sizes="whole", weights=True, seed=33)
+    dc, f = on_device(dtype, c, kv_heads), runner.Fusion(2)
+    g = torch.Generator().manual_seed(34)
+    k, v = (torch.randn((4001, kv_heads * dim), generator=g).to(ref.TYPES[dtype]) for _ in range(2))
+    sizes, scores = torch.rand(4001, generator=g), torch.rand(4001, generator=g)
+    offsets = [0, 2500, 4001]
+    f.cache_append(dc, k.to(DEV), v.to(DEV), runner.RaggedRows(2, 2500, 4001, torch.tensor(offsets, dtype=torch.int32, device=DEV)),
+                   sizes=sizes.to(DEV), scores=scores.to(DEV))
+    assert status(f) == 0
+    same(dc, c, ref.append(c, k, v, offsets, sizes=sizes, scores=scores))
+
+
 @pytest.mark.parametrize("in_place", [True, False])
 def test_append_leaves_bad_samples_out(in_place):
     """A sample that is out of range in some way is left out, and the others are appended."""

@@ -38,7 +38,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     // for p v: a lane has kV chunks of four dims; narrow rows are shared out, kGroups of them side by side
     constexpr int kGroups = DP < 128 ? 2 : 1, kLanes = 32 / kGroups, kV = DP / (4 * kLanes);
     extern __shared__ __align__(128) unsigned char sm[];
-    __shared__ Batch<kThreads> batch;
+    __shared__ Finder<kThreads> finder;
     __shared__ float s_m[kWarps][NQ], s_l[kWarps][NQ];
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -46,11 +46,11 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Run run;
     Place at;
-    if (!find_run(p, batch, kRound, chunks, run, at)) {
+    if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
         empty_sequences<float>(p);
         return;
     }
-    const long long r0 = run.r0, r1 = run.r1;
+    const unsigned r0 = run.r0, r1 = run.r1;
 
     unsigned char *stages = sm + warp * S * L::kStage;
     float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
         }
     };
     // those of the (sequence, key head) after the one of round r, if this run has it
-    auto read_next_q = [&](long long r) {
+    auto read_next_q = [&](unsigned r) {
         if (r + at.rounds - at.u >= r1) return;
         Place next = at;
         next.u = at.rounds - 1;
@@ -108,8 +108,8 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     };
     begin_head();
     int st = 0;
-    long long seg0 = r0 - at.u;   // first round of the (sequence, key head)
-    for (long long r = r0;; ++r) {
+    unsigned seg0 = r0 - at.u;   // first round of the (sequence, key head)
+    for (unsigned r = r0;; ++r) {
         if (r == r0 || at.u == 0) read_next_q(r);
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;
@@ -316,22 +316,14 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
 constexpr int kWeightThreads = 256, kWeightTile = 128, kWeightCtas = 608;
 __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParams p) {
     constexpr int kW = kWeightThreads / 32;
-    __shared__ Batch<kWeightThreads> batch;
+    __shared__ Finder<kWeightThreads> finder;
     __shared__ __align__(16) float part[kW][kWeightTile];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Cache &c = p.c;
-    long long mine, before;
-    const long long total = batch_total(p, batch, kWeightTile, 1, mine, before);
     Run run;
-    run.cut(total, (int)gridDim.x);
-    if (run.r0 >= run.r1) return;
-    batch_find(p, batch, kWeightTile, 1, mine, before, run.r0, -1);
     Place at;
-    at.b = batch.b[0];
-    place_sequence(p, at, kWeightTile);
-    at.h = at.ch = 0;
-    at.u = (int)batch.rem[0];
-    for (long long r = run.r0; r < run.r1; ++r) {
+    if (!find_run<kWeightThreads, false>(p, finder, kWeightTile, 1, 1, 1u, run, at)) return;
+    for (unsigned r = run.r0; r < run.r1; ++r) {
         const int j0 = at.u * kWeightTile, j = j0 + tid;   // the token that this thread updates
         unsigned page = 0;
         const int pos = p.window && j >= p.sinks ? j + at.n - at.vis : j;

@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     constexpr bool kQRegs = NT * DP <= 128;     // the queries' fragments stay in registers
     constexpr bool kQEarly = NT == 1;           // the next queries are asked for as soon as these are in use
     extern __shared__ __align__(128) unsigned char sm[];
-    __shared__ Batch<kThreads> batch;
+    __shared__ Finder<kThreads> finder;
     __shared__ float s_m[kWarps][kNq], s_l[kWarps][kNq];
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
@@ -61,11 +61,11 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Run run;
     Place at;
-    if (!find_run(p, batch, kRound, chunks, run, at)) {
+    if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
         empty_sequences<__nv_bfloat16>(p);
         return;
     }
-    const long long r0 = run.r0, r1 = run.r1;
+    const unsigned r0 = run.r0, r1 = run.r1;
 
     unsigned char *stages = sm + warp * S * L::kStage, *qs = sm + L::kShared;
     float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
         }
     };
     // those of the (sequence, key head) after the one of round r, if this run has it
-    auto read_next_q = [&](long long r) {
+    auto read_next_q = [&](unsigned r) {
         if (r + at.rounds - at.u >= r1) return;
         Place next = at;
         next.u = at.rounds - 1;
@@ -134,8 +134,8 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     };
     begin_head();
     int st = 0;
-    long long seg0 = r0 - at.u;   // first round of the (sequence, key head)
-    for (long long r = r0;; ++r) {
+    unsigned seg0 = r0 - at.u;   // first round of the (sequence, key head)
+    for (unsigned r = r0;; ++r) {
         if (kQEarly && (r == r0 || at.u == 0)) read_next_q(r);
         __syncwarp();
         const int next_st = st == 0 ? S - 1 : st - 1;

@@ -32,77 +32,14 @@ __device__ __forceinline__ int visible(const CacheAttnParams &p, int n) {
     return p.window ? min(n, p.window + p.sinks) : n;
 }
 
-// The batch's rounds (or tiles): every thread sums a run of sequences, a scan over the CTA gives the total; then the
-// sequence of the rounds' number `first` is found by the thread whose run holds it.
-template <int THREADS>
-struct Batch {
-    long long excl[THREADS / 32 + 1];
-    long long total;
-    int b[2];             // sequences of the run's first round and of the next run's
-    long long rem[2];     // and the rounds of those sequences before them
-};
-__device__ __forceinline__ long long rounds_of(const CacheAttnParams &p, int b, int tokens, int heads) {
-    const int n = cache_length(p.c, b);
-    return n <= 0 ? 0 : (long long)((visible(p, n) + tokens - 1) / tokens) * heads;
-}
-template <int THREADS>
-__device__ long long batch_total(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long &mine, long long &before) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int per = ceil_div(p.c.max_batch, THREADS), b0 = min(tid * per, p.c.max_batch), b1 = min(b0 + per, p.c.max_batch);
-    mine = 0;
-    for (int b = b0; b < b1; ++b) mine += rounds_of(p, b, tokens, heads);
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
-        if (lane >= o) incl += v;
-    }
-    if (lane == 31) s.excl[warp] = incl;
-    __syncthreads();
-    if (tid == 0) {
-        long long t = 0;
-        for (int w = 0; w < THREADS / 32; ++w) {
-            const long long v = s.excl[w];
-            s.excl[w] = t;
-            t += v;
-        }
-        s.total = t;
-    }
-    __syncthreads();
-    before = s.excl[warp] + incl - mine;
-    return s.total;
-}
-// The sequences of rounds `first` and `next` (the latter may be past the batch: not looked for).
-template <int THREADS>
-__device__ void batch_find(const CacheAttnParams &p, Batch<THREADS> &s, int tokens, int heads, long long mine, long long before, long long first,
-                           long long next) {
-    const int per = ceil_div(p.c.max_batch, THREADS);
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const long long x = k ? next : first;
-        if (x >= before && x < before + mine) {
-            long long at = before;
-            for (int b = threadIdx.x * per;; ++b) {
-                const long long r = rounds_of(p, b, tokens, heads);
-                if (x < at + r) {
-                    s.b[k] = b;
-                    s.rem[k] = x - at;
-                    break;
-                }
-                at += r;
-            }
-        }
-    }
-    __syncthreads();
-}
-
 // Where in the batch a round lies.
 struct Place {
     int b, h, ch, u;       // sequence, key head, chunk of its query heads, round
     int n, vis, rounds;    // length, visible tokens, rounds of one key head
 };
-__device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens) {
-    s.n = max(cache_length(p.c, s.b), 0);
+__device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens, int b) {
+    s.b = b;
+    s.n = max(cache_length(p.c, b), 0);
     s.vis = visible(p, s.n);
     s.rounds = (s.vis + tokens - 1) / tokens;
 }
@@ -118,41 +55,116 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
             s.rounds = s.vis = 0;
             return;
         }
-        place_sequence(p, s, tokens);
+        place_sequence(p, s, tokens, s.b);
     } while (s.rounds == 0);
 }
 
 // The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.  A boundary at most `snap` rounds
 // inside a (sequence, key head) moves to its nearer end (its beginning first): a join costs more time than the few rounds that
-// it would deal out.
+// it would deal out.  (Rounds are counted in 32 bits: the host refuses caches of more.)
 struct Run {
-    long long total, len, more;
-    long long r0, r1;   // this CTA's
+    unsigned total, len, more;
+    unsigned r0, r1;   // this CTA's
     int ctas, snap;
-    __device__ __forceinline__ void cut(long long rounds, int n) {
+    __device__ __forceinline__ void cut(unsigned rounds, int n) {
         total = rounds;
         ctas = n;
-        // (a 64-bit division takes 0.1 us)
-        len = total >> 32 ? total / n : (long long)((unsigned)total / (unsigned)n);
-        more = total - len * n;
+        len = total / (unsigned)n;
+        more = total - len * (unsigned)n;
         r0 = begin(blockIdx.x);
         r1 = begin(blockIdx.x + 1);
         snap = len > 4 ? 4 : (int)len - 1;
     }
-    __device__ __forceinline__ long long begin(long long k) const { return len * k + (k < more ? k : more); }
-    __device__ __forceinline__ int of(long long x) const {   // the last run that begins at round x or before, boundaries not moved
-        const long long big = more * (len + 1);
+    __device__ __forceinline__ unsigned begin(unsigned k) const { return len * k + min(k, more); }
+    __device__ __forceinline__ int of(unsigned x) const {   // the last run that begins at round x or before, boundaries not moved
+        const unsigned big = more * (len + 1);
         return (int)(x < big ? x / (len + 1) : more + (x - big) / len);
     }
     // by how much a boundary moves that lies u rounds inside a (sequence, key head) of n rounds
     __device__ __forceinline__ int move(int u, int n) const { return u <= snap ? -u : n - u <= snap ? n - u : 0; }
     // the runs that share the (sequence, key head) of rounds [s0, s1): the first of them, and their number
-    __device__ __forceinline__ int sharing(long long s0, long long s1, int &first) const {
+    __device__ __forceinline__ int sharing(unsigned s0, unsigned s1, int &first) const {
         const int k0 = of(s0 + snap) + 1, k1 = of(s1 - snap - 1);   // the boundaries inside
         first = k0 - 1;
         return k1 - k0 + 2;
     }
 };
+
+// What a CTA needs to find its run.
+template <int THREADS>
+struct Finder {
+    unsigned sums[THREADS / 32];   // rounds of the warps' sequences
+    Place at[2];                   // of the run's first round and of the next run's
+};
+// This CTA's run and the place where it begins; false: it has none.  Every thread counts the rounds of a few sequences, the
+// warps' sums go through shared memory, and the thread whose sequences hold a boundary looks it up (one barrier before and
+// one after: 2.2 us with 64-bit scans by one thread, 1.2 now, 0.7 of them the reading of the lengths).  min_rounds: of a run.
+// SNAP: the boundaries move to ends of (sequence, key head)s.
+template <int THREADS, bool SNAP>
+__device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREADS> &s, int tokens, int heads, int chunks, unsigned min_rounds,
+                                         Run &run, Place &at) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const unsigned vheads = (unsigned)(heads * chunks);
+    const int per = ceil_div(p.c.max_batch, THREADS), b0 = min(tid * per, p.c.max_batch), b1 = min(b0 + per, p.c.max_batch);
+    unsigned mine = 0;
+    for (int b = b0; b < b1; ++b) {
+        place_sequence(p, at, tokens, b);
+        mine += (unsigned)at.rounds * vheads;
+    }
+    const unsigned sum = __reduce_add_sync(0xFFFFFFFFu, mine);
+    if (lane == 0) s.sums[warp] = sum;
+    if (tid < 2) s.at[tid] = Place{};
+    __syncthreads();
+    unsigned total = 0, base = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) {
+        const unsigned v = s.sums[w];
+        total += v;
+        if (w < warp) base += v;
+    }
+    const unsigned most = (total + min_rounds - 1) / min_rounds;
+    const int ctas = (int)min(most, gridDim.x);
+    if ((int)blockIdx.x >= ctas) return false;
+    run.cut(total, ctas);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const unsigned x = k ? run.r1 : run.r0;
+        if (x < base || x >= base + sum) continue;   // (warp-uniform)
+        unsigned incl = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+            if (lane >= o) incl += v;
+        }
+        unsigned rem = x - base - (incl - mine);   // rounds of this thread's sequences before x (if it is one of theirs)
+        if (x - base >= incl - mine && rem < mine) {
+            for (int b = b0; b < b1; ++b) {
+                if (per > 1) place_sequence(p, at, tokens, b);
+                if (rem < (unsigned)at.rounds * vheads) break;
+                rem -= (unsigned)at.rounds * vheads;
+            }
+            const unsigned vh = at.rounds > 0 ? rem / (unsigned)at.rounds : 0u;
+            at.u = (int)(rem - vh * (unsigned)at.rounds);
+            at.h = chunks == 1 ? (int)vh : (int)vh / chunks;
+            at.ch = (int)vh - at.h * chunks;
+            s.at[k] = at;
+        }
+    }
+    __syncthreads();
+    at = s.at[0];
+    if (SNAP) {
+        const int moved = run.move(at.u, at.rounds);
+        if (run.r1 < total) run.r1 += run.move(s.at[1].u, s.at[1].rounds);
+        run.r0 += moved;
+        if (run.r0 >= run.r1) return false;
+        if (moved < 0) at.u = 0;
+        if (moved > 0) {
+            at.u = at.rounds - 1;
+            place_next(p, at, tokens, heads, chunks);
+        }
+    }
+    return true;
+}
 
 // A token that a warp will load: its page (from the table, a round before its size) and place in it.
 struct Token {
@@ -168,7 +180,7 @@ template <typename T, int DP, int TT>
 struct Stream {
     static constexpr int kRow = DP * (int)sizeof(T), kCpr = kRow / 16, kStage = 2 * TT * kRow, kRound = kWarps * TT;
     Place ahead;             // of the next token to look up
-    long long ahead_r, r1;
+    unsigned ahead_r, r1;
     Token t0, t1;            // t0's rows are asked for next (its size is here), then t1's
     float size0;
 
@@ -260,36 +272,6 @@ __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
         uint4 *o = reinterpret_cast<uint4 *>(p.out) + (size_t)b * row;
         for (int e = threadIdx.x; e < row; e += kThreads) o[e] = make_uint4(0u, 0u, 0u, 0u);
     }
-}
-
-// This CTA's run and where it begins; false: it has none.
-__device__ __forceinline__ bool find_run(const CacheAttnParams &p, Batch<kThreads> &s, int tokens, int chunks, Run &run, Place &at) {
-    long long mine, before;
-    const int vheads = p.c.kv_heads * chunks;
-    const long long total = batch_total(p, s, tokens, vheads, mine, before), most = (total + kMinRounds - 1) / kMinRounds;
-    const int ctas = most < (long long)gridDim.x ? (int)most : (int)gridDim.x;
-    if ((int)blockIdx.x >= ctas) return false;
-    run.cut(total, ctas);
-    batch_find(p, s, tokens, vheads, mine, before, run.r0, run.r1);
-    auto place = [&](int k) {
-        at.b = s.b[k];
-        place_sequence(p, at, tokens);
-        const int vh = at.rounds > 0 ? (int)(s.rem[k] >> 32 ? s.rem[k] / at.rounds : (unsigned)s.rem[k] / (unsigned)at.rounds) : 0;
-        at.u = (int)(s.rem[k] - (long long)vh * at.rounds);
-        at.h = vh / chunks;
-        at.ch = vh % chunks;
-        return run.move(at.u, at.rounds);
-    };
-    if (run.r1 < total) run.r1 += place(1);
-    const int moved = place(0);
-    run.r0 += moved;
-    if (run.r0 >= run.r1) return false;
-    if (moved < 0) at.u = 0;
-    if (moved > 0) {
-        at.u = at.rounds - 1;
-        place_next(p, at, tokens, p.c.kv_heads, chunks);
-    }
-    return true;
 }
 
 // ---- the join of the runs that share a (sequence, key head) ------------------------------------------------------------
@@ -393,7 +375,7 @@ __device__ __forceinline__ bool arrive_last(int *counter, int n, int &s_last) {
 // joins their results.  More than eight are joined in two steps, groups of about the square root of their number first, by the
 // group's last (one CTA reads 16 KB in about 0.3 us, and the results of 38 runs of 32 heads of 128 are 600 KB).
 template <typename T, int NQ>
-__device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, long long seg0, long long seg1, size_t head, int nq,
+__device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, unsigned seg0, unsigned seg1, size_t head, int nq,
                                           float *scratch, int &s_last) {
     int c0;
     const int n = run.sharing(seg0, seg1, c0);

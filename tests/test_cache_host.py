@@ -87,6 +87,9 @@ def test_attention_rejects_bad_arguments():
     for heads in (0, 1, 9, -2, fz.FUSION_CACHE_MAX_HEADS + 2):
         assert attention(heads=heads) == fz.FUSION_ERR_SHAPE, heads
         assert size(heads) == 0
+    big = dict(max_batch=65535, max_pages=1 << 16)   # 2^16 sequences of 2^20 tokens
+    assert attention(cache(**big), heads=2) == fz.FUSION_ERR_SHAPE and size(2, **big) == 0
+    assert size(2, max_batch=1 << 15, max_pages=1 << 16, weights=None) > 0
     for kw in (dict(q=None), dict(out=None), dict(q=FAKE + 2), dict(out=FAKE + 8), dict(q_stride=-8), dict(q_stride=516),
                dict(scale=math.nan), dict(scale=math.inf), dict(window=-1), dict(sinks=-1)):
         assert attention(**kw) == fz.FUSION_ERR_INVALID_ARG, kw

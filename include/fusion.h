@@ -166,7 +166,7 @@ typedef struct fusion_cache {
     int32_t head_dim;          /* width of a head */
     int64_t num_pages;         /* pages in the pools */
     void *k, *v;               /* [num_pages, kv_heads, page_tokens, head_dim], dtype */
-    float *sizes;              /* [num_pages, page_tokens] token sizes (0: a masked token); NULL: all 1 */
+    float *sizes;              /* [num_pages, page_tokens] token sizes >= 0 (0: a masked token); NULL: all 1 */
     float *weights;            /* [num_pages, page_tokens] accumulated attention weights; NULL: not kept */
     const int32_t *page_table; /* [max_batch, max_pages] */
     const int32_t *lengths;    /* [max_batch] tokens held, in [0, max_pages * page_tokens] */
@@ -503,7 +503,7 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
  * q: [max_batch, heads, head_dim], dtype, sequences q_stride elements apart (>= 0, rows 16-byte aligned), 16-byte aligned;
  * out: [max_batch, heads, head_dim], dtype, 16-byte aligned.  heads: a multiple of kv_heads, at most
  * FUSION_CACHE_MAX_HEADS, with max_batch * heads * max_pages * page_tokens <= 2^36.  scale: finite.  window, sinks: >= 0.  Logits, sums and the output are accumulated in float32; in
- * bf16 the probabilities are rounded to bf16 (the operand of the second product) after their sum was taken.
+ * bf16 a probability enters the second product as two bf16 terms, within 2^-16 of itself.  out does not overlap q.
  * Errors: FUSION_ERR_SHAPE, FUSION_ERR_INVALID_ARG, FUSION_ERR_WORKSPACE; device bit BAD_CACHE (a length out of range, or the
  * page id of a visible token: that sequence is not written).
  */

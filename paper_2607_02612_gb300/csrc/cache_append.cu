@@ -124,7 +124,10 @@ __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams 
 cudaError_t launch_cache_append(int dtype, const CacheAppendParams &p, cudaStream_t s) {
     const int es = dtype == FUSION_BF16 ? 2 : 4, head_chunks = p.c.dim * es / 16, row_chunks = head_chunks * p.c.kv_heads;
     const int rows = kPer * (row_chunks < kThreads ? kThreads / row_chunks : 1);
-    k_cache_append<<<dim3((unsigned)ceil_div(p.in.max_tokens, rows), (unsigned)p.in.max_batch + 1), kThreads, 0, s>>>(p, row_chunks, head_chunks);
+    // (samples of more rows than the cache has room for, or than there are, write nothing)
+    long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
+    if (most > p.in.max_rows) most = p.in.max_rows;
+    k_cache_append<<<dim3((unsigned)(most > 0 ? (most + rows - 1) / rows : 1), (unsigned)p.in.max_batch + 1), kThreads, 0, s>>>(p, row_chunks, head_chunks);
     return cudaGetLastError();
 }
 

@@ -4,7 +4,9 @@
 // The tokens are the M rows and the query heads of a key head the N columns, so that a group of up to eight heads fills the
 // instruction's smallest N: S^T = K Q^T (A: 16 tokens x 16 dims of K as it lies, B: the queries), then O^T += V^T P^T (A: 16
 // dims x 16 tokens, V's rows read transposed, B: the probabilities, whose accumulator layout becomes the operand's by one 8 x 8
-// transposition per 8 tokens).  A lane's accumulators of both products belong to the same two heads, so the running maximum
+// transposition per 8 tokens).  A probability is the sum of two bf16 terms there, p and what its rounding lost, so that the
+// products keep 16 bits of it: one term alone made the error against 64 bits 1.3 times that of the output's own rounding, and
+// the second product costs nothing while memory is the bound (64 x 4096: 101.7 and 100.8 us).  A lane's accumulators of both products belong to the same two heads, so the running maximum
 // and the rescaling need no exchange but the maximum over a column's tokens.
 //
 // What bounds it: memory.  A token's K and V of one key head, 4 dim bytes, give 4 dim group flops: for a group of 8, 8 flops
@@ -236,22 +238,28 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
             // ---- O^T += V^T P^T
 #pragma unroll
             for (int i = 0; i < kMt; ++i) {
-                uint32_t b[NT][2];
+                uint32_t b[NT][2], b_lo[NT][2];
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     const float p0 = ex2(x[i][n][0] - m[n][0]), p1 = ex2(x[i][n][1] - m[n][1]);
                     const float p2 = ex2(x[i][n][2] - m[n][0]), p3 = ex2(x[i][n][3] - m[n][1]);
                     l[n][0] += p0 + p2;
                     l[n][1] += p1 + p3;
-                    b[n][0] = transpose8(pack(p0, p1));
-                    b[n][1] = transpose8(pack(p2, p3));
+                    const uint32_t h0 = pack(p0, p1), h1 = pack(p2, p3);
+                    b[n][0] = transpose8(h0);
+                    b[n][1] = transpose8(h1);
+                    b_lo[n][0] = transpose8(pack(p0 - __uint_as_float(h0 << 16), p1 - __uint_as_float(h0 & 0xFFFF0000u)));
+                    b_lo[n][1] = transpose8(pack(p2 - __uint_as_float(h1 << 16), p3 - __uint_as_float(h1 & 0xFFFF0000u)));
                 }
 #pragma unroll
                 for (int k = 0; k < kKs; ++k) {
                     uint32_t a[4];
                     ldsm_x4_t(vs + (16 * i + (lane & 7) + ((lane >> 4) << 3)) * kRow + (((2 * k + (lane >> 3 & 1)) ^ (lane & 7)) << 4), a);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) mma_bf16_16816(o[k][n], a, b[n][0], b[n][1]);
+                    for (int n = 0; n < NT; ++n) {
+                        mma_bf16_16816(o[k][n], a, b[n][0], b[n][1]);
+                        mma_bf16_16816(o[k][n], a, b_lo[n][0], b_lo[n][1]);
+                    }
                 }
             }
         }

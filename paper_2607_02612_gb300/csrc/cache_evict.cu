@@ -114,12 +114,12 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
 #pragma unroll
         for (int i = 0; i < kKeys; ++i) {
             const bool here = at + i * kSelThreads + tid < end;
-            nan |= here && !isfinite(__uint_as_float(key[i]));
+            nan |= here && want > 0 && !isfinite(__uint_as_float(key[i]));
             key[i] = here ? ordered_bits(__uint_as_float(key[i])) : 0u;   // (no finite weight has the key 0)
         }
         for (int j = at + kKeys * kSelThreads + tid; j < end; j += kSelThreads) {
             unsigned page;
-            if (cache_page(c, b, j, page)) nan |= !isfinite(c.weights[(page << c.shift) + (unsigned)(j & ((1 << c.shift) - 1))]);
+            if (cache_page(c, b, j, page)) nan |= want > 0 && !isfinite(c.weights[(page << c.shift) + (unsigned)(j & ((1 << c.shift) - 1))]);
         }
     }
     for (int e = tid; e < kBins; e += kSelThreads) hist[e] = 0;

@@ -261,16 +261,15 @@ struct Stream {
 // Zeros for sequences without tokens (a length out of range is told, its row left), dealt out over the grid.
 template <typename T>
 __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
-    const int row = p.heads * p.c.dim * (int)sizeof(T) / 16;
-    for (int b = blockIdx.x; b < p.c.max_batch; b += gridDim.x) {
-        const int n = cache_length(p.c, b);
-        if (n > 0) continue;
-        if (n < 0) {
-            if (threadIdx.x == 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
-            continue;
+    const int row = p.heads * p.c.dim * (int)sizeof(T) / 16, grid = (int)gridDim.x, lane = threadIdx.x & 31;
+    for (long long b0 = blockIdx.x + (long long)(threadIdx.x >> 5) * 32 * grid; b0 < p.c.max_batch; b0 += (long long)kThreads * grid) {
+        const long long b = b0 + (long long)lane * grid;   // a warp looks at 32 sequences at once
+        const int n = b < p.c.max_batch ? cache_length(p.c, (int)b) : 1;
+        if (n < 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
+        for (unsigned none = __ballot_sync(0xFFFFFFFFu, n == 0); none; none &= none - 1u) {
+            uint4 *o = reinterpret_cast<uint4 *>(p.out) + (size_t)(b0 + (long long)(__ffs(none) - 1) * grid) * row;
+            for (int e = lane; e < row; e += 32) o[e] = make_uint4(0u, 0u, 0u, 0u);
         }
-        uint4 *o = reinterpret_cast<uint4 *>(p.out) + (size_t)b * row;
-        for (int e = threadIdx.x; e < row; e += kThreads) o[e] = make_uint4(0u, 0u, 0u, 0u);
     }
 }
 

@@ -80,7 +80,7 @@ def attention(c, q, dtype, *, scale=None, window=0, sinks=0):
     The tolerances count the roundings.  A logit (base e) is a float32 sum of `dim` products: off by at most
     (dim + 4) 2^-24 scale sum|q k| and a few steps of its own; so a probability is off by a factor 1 + d, d twice that,
     plus 2^-20 for the exponential.  Sums over n tokens in float32, at least four at a time, lose (n / 4 + 64) 2^-24 of the
-    sum of magnitudes.  bf16 adds 2^-8 of sum p |v| (the probabilities as operands) and 2^-8 of the output."""
+    sum of magnitudes.  bf16 adds 2^-16 of sum p |v| (the probabilities, two bf16 terms, as operands) and 2^-8 of the output."""
     batch, heads, dim = q.shape
     kv = c["k"].shape[1]
     group = heads // kv
@@ -111,7 +111,7 @@ def attention(c, q, dtype, *, scale=None, window=0, sinks=0):
         a = torch.einsum("hn,nhd->hd", p, v.abs())
         tol[b] = 2 * d[:, None] * a + 2.0 ** -24 * out[b].abs() + 1e-37
         if dtype == "bf16":
-            tol[b] += 2.0 ** -8 * 1.01 * a + 2.0 ** -8 * out[b].abs()
+            tol[b] += 2.0 ** -16 * a + 2.0 ** -8 * out[b].abs()
         if w is not None:
             w[at] += p.sum(0)
             wtol[at] = 2 * (d[:, None] * p).sum(0) + (heads + 1) * 2.0 ** -24 * w[at].abs()

@@ -216,6 +216,31 @@ def test_attention_many_short_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_thousands_of_sequences(dtype):
+    """More sequences than threads: most of them empty, a few with tokens; and the same batch appended to in one call."""
+    n = [(i % 11) * (i % 3 == 0) for i in range(9000)]
+    c = ref.make(dtype, n, 1, 8, 16, room=1, weights=True, seed=38)
+    _, dc = attend(dtype, c, 2)
+    k, v = (torch.randn((9000, 8), generator=torch.Generator().manual_seed(39)).to(ref.TYPES[dtype]) for _ in range(2))
+    f = runner.Fusion(1)
+    f.cache_append(dc, k.to(DEV), v.to(DEV))
+    c["weights"] = dc.weights.cpu()
+    new = ref.append(c, k, v, range(9001))
+    want = ref.copy(c)
+    for b in range(9000):
+        pg, off = ref.places(want, b, torch.tensor([n[b]]))
+        want["weights"][pg, off] = 0.0
+    assert status(f) == 0
+    same(dc, want, new)
+
+
+@pytest.mark.parametrize("heads,dim", [(1024, 8), (640, 64)])
+def test_attention_many_query_heads(heads, dim):
+    attend("bf16", ref.make("bf16", [130, 17], 1, dim, 16, weights=True, seed=40), heads)
+    attend("f32", ref.make("f32", [130, 17], 1, dim, 16, weights=True, seed=40), heads)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_peaked_and_rising_logits(dtype):
     """Logits of hundreds, rising along the sequence (every tile rescales) or falling; a negative and a zero scale."""
     for sign in (1.0, -1.0):
@@ -412,11 +437,36 @@ def test_evict_ties_go_to_the_lowest_position(outside):
         evicts("bf16", c, [300, 89, 37, 1], sinks=2, recent=3, outside=outside, keep=values != [1.5])
 
 
-@pytest.mark.parametrize("n,budget", [(5000, 2500), (9001, 8999), (20000, 77), (70000, 35000)])
+@pytest.mark.parametrize("n,budget", [(5000, 2500), (9001, 8999), (20000, 77), (40000, 30000), (70000, 35000)])
 @pytest.mark.parametrize("outside", [False, True])
 def test_evict_long_sequences(n, budget, outside):
     c = ref.make("bf16", [n, n // 3], 2, 64, 64, weights=True, sizes="whole", seed=29)
     evicts("bf16", c, [budget, budget // 4], sinks=4, recent=16, outside=outside)
+
+
+@pytest.mark.parametrize("n,budget,values", [(150001, 149000, 0), (150001, 70000, 3), (300000, 5, 0)])
+def test_evict_sequences_longer_than_the_registers(n, budget, values):
+    """More weights than the threads of a cluster hold: the rest are read again; with ties across both parts."""
+    c = ref.make("bf16", [n, 40], 1, 8, 256, weights=True, seed=35)
+    if values:
+        at = ref.places(c, 0, torch.arange(n))
+        c["weights"][at] = torch.randint(0, values, (n,), generator=torch.Generator().manual_seed(36)).float()
+    evicts("bf16", c, [budget, 17], sinks=3, recent=100)
+
+
+def test_evict_compares_nothing_where_all_places_are_given():
+    """Budgets that the sinks and the recent tokens fill, and a budget of nothing: no weight is compared, so NaN is none's
+    concern."""
+    c = ref.make("f32", [50, 60, 70], 2, 16, 16, weights=True, seed=37)
+    c["weights"][:] = math.nan
+    dc, f = on_device("f32", c, 2), runner.Fusion(3)
+    f.cache_evict(dc, torch.tensor([12, 0, 70], dtype=torch.int32, device=DEV), sinks=4, recent=8)
+    assert status(f) == 0
+    for b, keep in ((0, [*range(4), *range(42, 50)]), (1, []), (2, list(range(70)))):
+        src, dst = ref.places(c, b, torch.tensor(keep, dtype=torch.long)), ref.places(c, b, torch.arange(len(keep)))
+        for name in ("k", "v"):
+            c[name][dst[0], :, dst[1]] = c[name][src[0], :, src[1]]
+    same(dc, c, torch.tensor([12, 0, 70], dtype=torch.int32))
 
 
 @pytest.mark.parametrize("outside", [False, True])

@@ -31,6 +31,30 @@ __device__ __forceinline__ int cache_length(const Cache &c, int b) {
     return n >= 0 && n <= c.capacity ? n : -1;
 }
 
+// Every kernel of the cache calls is a programmatic dependent of the one before it on the stream: it is launched while that one
+// still runs, and waits for its end (and its writes) before it touches memory that a kernel may have written.  All of a kernel's
+// CTAs wait, also those without work, so that its end implies the end of the ones before it.
+__device__ __forceinline__ void wait_for_previous() {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename... P, typename... A>
+inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t s, A... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute a[2];
+    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a[0].val.programmaticStreamSerializationAllowed = 1;
+    a[1].id = cudaLaunchAttributeClusterDimension;
+    a[1].val.clusterDim = {(unsigned)cluster, 1, 1};
+    cfg.attrs = a;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 // Scratch behind the counters of the workspace.  Attention: log-sum-exps, partial results of sequences that
 // several CTAs share, logits (only where weights are accumulated).  Eviction: the kept slots and their counts.
 constexpr int kCacheMaxCtas = 512;   // CTAs of the attention kernel; each has two partial results at most

@@ -23,6 +23,7 @@ __device__ bool named_twice(const Ragged &in, int B, int i, int slot) {
 __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams p, int row_chunks, int head_chunks) {
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
+    wait_for_previous();
     const int B = device_batch(p.in);
     if (i == p.in.max_batch) {   // the lengths that no sample raises, where they go elsewhere
         if (blockIdx.x > 0) return;
@@ -127,8 +128,8 @@ cudaError_t launch_cache_append(int dtype, const CacheAppendParams &p, cudaStrea
     // (samples of more rows than the cache has room for, or than there are, write nothing)
     long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
     if (most > p.in.max_rows) most = p.in.max_rows;
-    k_cache_append<<<dim3((unsigned)(most > 0 ? (most + rows - 1) / rows : 1), (unsigned)p.in.max_batch + 1), kThreads, 0, s>>>(p, row_chunks, head_chunks);
-    return cudaGetLastError();
+    return launch_after(k_cache_append, dim3((unsigned)(most > 0 ? (most + rows - 1) / rows : 1), (unsigned)p.in.max_batch + 1), kThreads, 0, 1, s,
+                        p, row_chunks, head_chunks);
 }
 
 }  // namespace fz

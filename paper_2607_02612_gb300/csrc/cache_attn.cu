@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const Cache &c = p.c;
-    if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    wait_for_previous();
     Run run;
     Place at;
     if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
@@ -322,14 +322,22 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
     const Cache &c = p.c;
     Run run;
     Place at;
-    if (!find_run<kWeightThreads, false>(p, finder, kWeightTile, 1, 1, 1u, run, at)) return;
-    for (unsigned r = run.r0; r < run.r1; ++r) {
-        const int j0 = at.u * kWeightTile, j = j0 + tid;   // the token that this thread updates
-        unsigned page = 0;
-        const int pos = p.window && j >= p.sinks ? j + at.n - at.vis : j;
-        const bool here = tid < kWeightTile && j < at.vis && cache_page(c, at.b, pos, page);
-        float *dst = c.weights + ((size_t)page << c.shift) + (pos & ((1 << c.shift) - 1));
-        if (r == run.r0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    const bool works = find_run<kWeightThreads, false>(p, finder, kWeightTile, 1, 1, 1u, run, at);
+    // the token that this thread updates, and its place in its page (-1: none)
+    int j0 = 0, place = -1;
+    unsigned page = 0;
+    auto look_up = [&]() {
+        j0 = at.u * kWeightTile;
+        const int j = j0 + tid, pos = p.window && j >= p.sinks ? j + at.n - at.vis : j;
+        place = tid < kWeightTile && j < at.vis && cache_page(c, at.b, pos, page) ? pos & ((1 << c.shift) - 1) : -1;
+    };
+    // (lengths and pages are complete: the attention kernel let this one start after it had waited for the kernels before)
+    if (works) look_up();
+    wait_for_previous();
+    for (unsigned r = run.r0; works && r < run.r1; ++r) {
+        if (r > run.r0) look_up();
+        const bool here = place >= 0;
+        float *dst = c.weights + ((size_t)page << c.shift) + place;
         const float old = here ? *dst : 0.0f;
         float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (j0 + 4 * lane < at.vis) {   // (up to three logits past the sequence are there, and not used)
@@ -379,16 +387,7 @@ cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStre
                                                : launch_dim<8>(p, s);
     if (e != cudaSuccess || !p.logits) return e;
     const long long tiles = (long long)p.c.max_batch * ceil_div(p.most, kWeightTile);
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)(tiles < kWeightCtas ? tiles : kWeightCtas));
-    cfg.blockDim = dim3(kWeightThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute a[1];
-    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    a[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = a;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, k_cache_weights, p);
+    return launch_after(k_cache_weights, dim3((unsigned)(tiles < kWeightCtas ? tiles : kWeightCtas)), kWeightThreads, 0, 1, s, p);
 }
 
 }  // namespace fz

@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const Cache &c = p.c;
-    if (p.logits) asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    wait_for_previous();
     Run run;
     Place at;
     if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {

@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
     __shared__ int s_warp[kSelWarps], s_digit[3];
     __shared__ int s_scan[kKeys * kSelWarps];
     __shared__ int s_first;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    wait_for_previous();
     int par = 0;
     if constexpr (C > 1) {   // all CTAs of the cluster are here before one writes to another
         cluster_arrive();
@@ -350,7 +350,7 @@ template <bool kInPlace>
 __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, int head_chunks, int parts) {
     const int b = blockIdx.z, job = blockIdx.y / parts, part = blockIdx.y % parts, tid = threadIdx.x, team = gridDim.x, member = blockIdx.x;
     const Cache &c = p.c;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_previous();
     const int2 plan = p.plan[b];
     const int m = plan.x;
     const unsigned *keep = p.keep + (size_t)b * c.capacity;
@@ -415,16 +415,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams
 
 template <int C, int kSelThreads>
 cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(C, (unsigned)p.c.max_batch);
-    cfg.blockDim = dim3(kSelThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute a[1];
-    a[0].id = cudaLaunchAttributeClusterDimension;
-    a[0].val.clusterDim = {C, 1, 1};
-    cfg.attrs = a;
-    cfg.numAttrs = C > 1 ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, k_cache_select<C, kSelThreads>, p);
+    return launch_after(k_cache_select<C, kSelThreads>, dim3(C, (unsigned)p.c.max_batch), kSelThreads, 0, C, s, p);
 }
 
 }  // namespace
@@ -456,18 +447,9 @@ cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_
     if (team > steps) team = steps;
     if (p.in_place) team = team >= 8 ? 8 : team >= 4 ? 4 : team >= 2 ? 2 : 1;
     if (team < 1) team = 1;
-    cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3((unsigned)team, (unsigned)((jobs - 1) * parts + 1), (unsigned)p.c.max_batch);
-    cfg.blockDim = dim3(kMoveThreads);
-    cfg.stream = s;
-    cudaLaunchAttribute a[2];
-    a[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    a[0].val.programmaticStreamSerializationAllowed = 1;
-    a[1].id = cudaLaunchAttributeClusterDimension;
-    a[1].val.clusterDim = {(unsigned)team, 1, 1};
-    cfg.attrs = a;
-    cfg.numAttrs = p.in_place ? 2 : 1;
-    return p.in_place ? cudaLaunchKernelEx(&cfg, k_cache_move<true>, p, head_chunks, parts) : cudaLaunchKernelEx(&cfg, k_cache_move<false>, p, head_chunks, parts);
+    const dim3 grid((unsigned)team, (unsigned)((jobs - 1) * parts + 1), (unsigned)p.c.max_batch);
+    return p.in_place ? launch_after(k_cache_move<true>, grid, kMoveThreads, 0, (int)team, s, p, head_chunks, parts)
+                      : launch_after(k_cache_move<false>, grid, kMoveThreads, 0, 1, s, p, head_chunks, parts);
 }
 
 }  // namespace fz

@@ -419,8 +419,7 @@ cudaError_t launch_rounds(int smem, const CacheAttnParams &p, int chunks, int to
     if (e != cudaSuccess) return e;
     const long long rounds = (long long)p.c.max_batch * p.c.kv_heads * chunks * ceil_div(p.most, tokens);
     if (ctas > kCacheMaxCtas) ctas = kCacheMaxCtas;
-    Kernel<<<(unsigned)(ctas < rounds ? ctas : rounds), kThreads, smem, s>>>(p, chunks);
-    return cudaGetLastError();
+    return launch_after(Kernel, dim3((unsigned)(ctas < rounds ? ctas : rounds)), kThreads, (size_t)smem, 1, s, p, chunks);
 }
 
 }  // namespace rounds

@@ -276,6 +276,7 @@ __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
 // ---- the join of the runs that share a (sequence, key head) ------------------------------------------------------------
 // Run k's result lies in slot 2 k + 1 where the (sequence, key head) begins in run k, else in slot 2 k: per query head a maximum
 // and a sum (below zero: a bad page) and the output before the division.
+constexpr int kJoinAtOnce = 16;     // in one step; more in two
 constexpr int kJoinMost = 23;       // results joined at once: 23 * 23 covers kCacheMaxCtas
 template <int NQ> constexpr int kJoinScratch = (kJoinMost + 2) * NQ * 4;   // bytes
 
@@ -326,7 +327,7 @@ __device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, i
             acc[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
             q[u] = min(e0 + u * kThreads, all - 1) * 4 / dim;
         }
-#pragma unroll 2
+#pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const float4 *src = reinterpret_cast<const float4 *>(p.part + slot(j) * NQ * dim);
 #pragma unroll
@@ -379,7 +380,7 @@ __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &r
     int c0;
     const int n = run.sharing(seg0, seg1, c0);
     int size = n;   // of a group
-    if (n > 8)
+    if (n > kJoinAtOnce)
         for (size = 3; size * size < n;) ++size;
     const int groups = (n + size - 1) / size, g = ((int)blockIdx.x - c0) / size, first = c0 + g * size, members = min(size, n - g * size);
     int *count1 = p.counters, *count2 = p.counters + 2 * kCacheMaxCtas;   // both by the slot of the first run

@@ -13,7 +13,7 @@ constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinRounds = 2;       // of a CTA: fewer and the join costs more than the split gains
 constexpr float kLow = -3.0e38f;    // a maximum over nothing: finite, so that (-inf) - kLow is -inf
 // Probabilities are 2^(x - shift) with a shift of at least the largest logit so far less kLag: up to 2^8, which costs no bits in
-// float32 or bf16, and tiles whose maximum grows a little do not rescale (with 32 heads in a warp nearly every tile did).
+// float32 or bf16, and tiles whose maximum grows a little do not rescale (with 16 heads in a warp nearly every tile does).
 constexpr float kLag = 8.0f;
 constexpr float kNoPage = 3.0e38f;  // in the place of a log2 size (at most 128): the token's page id is out of range
 
@@ -317,7 +317,7 @@ __device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, i
         maxima[tid] = none ? INFINITY : M;
     }
     __syncthreads();
-    constexpr int kU = 4;   // columns of four in flight, for two results at a time
+    constexpr int kU = 4;   // columns of four in flight, for four results at a time
     const int all = nq * dim / 4;
     for (int e0 = tid; e0 < all; e0 += kU * kThreads) {
         float4 acc[kU];
@@ -372,8 +372,8 @@ __device__ __forceinline__ bool arrive_last(int *counter, int n, int &s_last) {
 }
 
 // After a CTA has written its result of the (sequence, key head) of rounds [seg0, seg1): the last of the runs that share it
-// joins their results.  More than eight are joined in two steps, groups of about the square root of their number first, by the
-// group's last (one CTA reads 16 KB in about 0.3 us, and the results of 38 runs of 32 heads of 128 are 600 KB).
+// joins their results.  More than kJoinAtOnce are joined in two steps, groups of about the square root of their number first,
+// by the group's last: one CTA alone reads the results of 38 runs of 16 heads of 128 (300 KB) slower than two in turn a few each.
 template <typename T, int NQ>
 __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, unsigned seg0, unsigned seg1, size_t head, int nq,
                                           float *scratch, int &s_last) {

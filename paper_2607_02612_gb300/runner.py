@@ -351,12 +351,14 @@ class Fusion:
         """Appends the rows of k and v ([rows, kv_heads * head_dim], any stride between rows) to the sequences that `rows`
         (a DeviceBatch or RaggedRows; None: one row per sequence) says; returns the new lengths (the cache's own, raised
         in place, unless lengths_out is given)."""
+        o = lengths_out if lengths_out is not None else c.lengths
+        if c.max_batch == 0:
+            return o
         rows = rows if rows is not None else c.one_row_each()
         kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "keys")
         vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "values")
         zp = _need(sizes, torch.float32, c.index, "sizes", rows.max_rows)
         wp = _need(scores, torch.float32, c.index, "scores", rows.max_rows)
-        o = lengths_out if lengths_out is not None else c.lengths
         op = _need(o, torch.int32, c.index, "lengths_out", c.max_batch)
         _enqueue(c.lib.fusion_cache_append, c.index, self.status, c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp,
                  wp, op, c._ws, c.ws_bytes)
@@ -373,6 +375,8 @@ class Fusion:
             op = out.data_ptr()
         else:
             op = _need(out, c.torch_dtype, c.index, "out", c.max_batch * c.heads * c.head_dim, 3)
+        if c.max_batch == 0:
+            return out
         _enqueue(c.lib.fusion_cache_attention, c.index, self.status, c.code, c.c_struct(), qp, qs, c.heads,
                  c.scale if scale is None else scale, window, sinks, op, c._ws, c.ws_bytes)
         return out
@@ -383,6 +387,8 @@ class Fusion:
         """Prunes each sequence to budget[b] tokens by accumulated weight, in place or into other pages; keep_idx
         [max_batch, n] receives the kept positions.  Returns the new lengths (the cache's own unless lengths_out is given)."""
         o = lengths_out if lengths_out is not None else c.lengths
+        if c.max_batch == 0:
+            return o
         op = _need(o, torch.int32, c.index, "lengths_out", c.max_batch)
         bp = _need(budget, torch.int32, c.index, "budget", c.max_batch)
         tp = _need(page_table_out, torch.int32, c.index, "page_table_out", dim=2)

@@ -232,6 +232,20 @@ def test_attention_thousands_of_sequences(dtype):
         want["weights"][pg, off] = 0.0
     assert status(f) == 0
     same(dc, want, new)
+    want["lengths"] = new
+    budget = [i % 7 for i in range(9000)]
+    f.cache_evict(dc, torch.tensor(budget, dtype=torch.int32, device=DEV), recent=1)
+    want["lengths"], _ = ref.evict(want, budget, recent=1)
+    assert status(f) == 0
+    same(dc, want)
+
+
+def test_a_cache_of_no_sequences():
+    dc, f = runner.device_cache("f32", 0, 64, 4, 2, 16, sizes=True, weights=True), runner.Fusion(1)
+    f.cache_append(dc, torch.zeros((0, 32), device=DEV), torch.zeros((0, 32), device=DEV))
+    assert f.cache_attention(dc, torch.zeros((0, 4, 16), device=DEV)).shape == (0, 4, 16)
+    f.cache_evict(dc, torch.zeros(0, dtype=torch.int32, device=DEV))
+    assert status(f) == 0
 
 
 @pytest.mark.parametrize("heads,dim", [(1024, 8), (640, 64)])

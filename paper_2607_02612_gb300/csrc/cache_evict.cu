@@ -344,11 +344,11 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
 }
 
 constexpr int kMoveThreads = 512, kPer = 8;   // kPer 16-byte chunks of a thread in flight
-// gridDim.x CTAs per (sequence, key head, K or V; the last job: sizes and weights); in place they are a cluster.
-// A row's chunks are dealt out over `parts` teams.
+// gridDim.x CTAs (in place: a cluster) per sequence and `width` columns, a column being one of the 2 kv_heads head_chunks chunks
+// of a token's keys and values; the last group of columns: sizes and weights.  A thread has one column of rows `stride` apart.
 template <bool kInPlace>
-__global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, int head_chunks, int parts) {
-    const int b = blockIdx.z, job = blockIdx.y / parts, part = blockIdx.y % parts, tid = threadIdx.x, team = gridDim.x, member = blockIdx.x;
+__global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, int head_chunks, int width) {
+    const int b = blockIdx.z, tid = threadIdx.x, team = gridDim.x, member = blockIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
     const int2 plan = p.plan[b];
@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams
         const unsigned page = (unsigned)p.table_out[(size_t)b * p.pages_out + (i >> c.shift)];
         return (page << c.shift) + ((unsigned)i & low);
     };
-    if (job == 2 * c.kv_heads) {   // sizes and weights
+    if (blockIdx.y == gridDim.y - 1) {   // sizes and weights
         for (int i0 = plan.y + member * kMoveThreads; i0 - member * kMoveThreads < m; i0 += team * kMoveThreads) {
             const int i = i0 + tid;
             float z = 0.0f, w = 0.0f;
@@ -380,27 +380,27 @@ __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams
         }
         return;
     }
-    unsigned char *pool = job < c.kv_heads ? c.k : c.v;
-    const unsigned h = (unsigned)(job < c.kv_heads ? job : job - c.kv_heads);
+    const int stride = kMoveThreads / width, r0 = tid / width, step = stride * kPer, column = blockIdx.y * width + tid % width;
+    const int h2 = column / head_chunks, chunk = column - h2 * head_chunks;
+    const bool idle = r0 >= stride || h2 >= 2 * c.kv_heads;
+    unsigned char *pool = (h2 < c.kv_heads ? c.k : c.v) + chunk * 16;
+    const unsigned h = (unsigned)(h2 < c.kv_heads ? h2 : h2 - c.kv_heads);
     auto row = [&](unsigned slot) {
         return pool + (size_t)((((slot >> c.shift) * (unsigned)c.kv_heads + h) << c.shift) + (slot & low)) * head_chunks * 16;
     };
-    // rows of a step: as many whole rows as the CTA's chunks give; a thread has the same chunk of rows `stride` apart
-    const int mine = head_chunks / parts, stride = kMoveThreads / mine, chunk = part * mine + tid % mine, r0 = tid / mine, step = stride * kPer;
-    const bool idle = r0 >= stride;
     uint4 v[kPer];
     auto load = [&](int i0) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             const int i = i0 + r0 + k * stride;
-            if (!idle && i < m) v[k] = *reinterpret_cast<const uint4 *>(row(keep[i]) + chunk * 16);
+            if (!idle && i < m) v[k] = *reinterpret_cast<const uint4 *>(row(keep[i]));
         }
     };
     auto store = [&](int i0) {
 #pragma unroll
         for (int k = 0; k < kPer; ++k) {
             const int i = i0 + r0 + k * stride;
-            if (!idle && i < m) *reinterpret_cast<uint4 *>(row(target(i)) + chunk * 16) = v[k];
+            if (!idle && i < m) *reinterpret_cast<uint4 *>(row(target(i))) = v[k];
         }
     };
     for (int s0 = plan.y; s0 < m; s0 += team * step) {   // (the same number of steps for every member)
@@ -433,23 +433,27 @@ cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_
                     : cap <= 4096 * k ? launch_select<8, 512>(p, s)
                                       : launch_select<8, 1024>(p, s);
     if (e != cudaSuccess) return e;
-    // a team per (sequence, job): enough CTAs to fill the GPU a few times, no more than a sequence has steps for
-    const int jobs = 2 * p.c.kv_heads + 1;
+    // Columns of a CTA: a head's, or more where the sequences are too short for a step of kPer rows by all threads (132 x 17 of 16
+    // heads of 80 float32: 33 us with one head a CTA), or half of them (not below 128 bytes) where a team in place would leave SMs
+    // idle.  Then enough CTAs to fill the GPU a few times, no more than a sequence has steps for.
     const long long most = p.in_place ? p.c.capacity : (long long)p.pages_out << p.c.shift;
-    long long team = (p.in_place ? 608ll : 2432ll) / ((long long)jobs * p.c.max_batch);
-    int parts = 1;
-    while (p.in_place && team > 8 && head_chunks / parts >= 16 && head_chunks / parts % 2 == 0) {   // (not below 128 bytes of a row)
-        parts *= 2;
-        team /= 2;
-    }
-    const int step = kMoveThreads / (head_chunks / parts) * kPer;
+    const int columns = 2 * p.c.kv_heads * head_chunks;
+    int width = head_chunks;
+    while (width < kMoveThreads && width < columns && (long long)(kMoveThreads / width) * kPer > most) width *= 2;
+    if (width > columns) width = columns;
+    if (width > kMoveThreads) width = kMoveThreads;
+    auto groups = [&] { return (columns + width - 1) / width; };
+    auto team_of = [&] { return (p.in_place ? 608ll : 2432ll) / ((long long)(groups() + 1) * p.c.max_batch); };
+    while (p.in_place && team_of() > 8 && width <= head_chunks && width >= 16 && width % 2 == 0) width /= 2;
+    const int step = kMoveThreads / width * kPer;
     const long long steps = (most + step - 1) / step;
+    long long team = team_of();
     if (team > steps) team = steps;
     if (p.in_place) team = team >= 8 ? 8 : team >= 4 ? 4 : team >= 2 ? 2 : 1;
     if (team < 1) team = 1;
-    const dim3 grid((unsigned)team, (unsigned)((jobs - 1) * parts + 1), (unsigned)p.c.max_batch);
-    return p.in_place ? launch_after(k_cache_move<true>, grid, kMoveThreads, 0, (int)team, s, p, head_chunks, parts)
-                      : launch_after(k_cache_move<false>, grid, kMoveThreads, 0, 1, s, p, head_chunks, parts);
+    const dim3 grid((unsigned)team, (unsigned)(groups() + 1), (unsigned)p.c.max_batch);
+    return p.in_place ? launch_after(k_cache_move<true>, grid, kMoveThreads, 0, (int)team, s, p, head_chunks, width)
+                      : launch_after(k_cache_move<false>, grid, kMoveThreads, 0, 1, s, p, head_chunks, width);
 }
 
 }  // namespace fz

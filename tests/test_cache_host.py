@@ -127,7 +127,7 @@ def test_runner_refuses_tensors_that_do_not_fit():
     assert rows(packed[:, 16:32], 4) == (packed.data_ptr() + 64, 48)
     assert rows(packed[:, 16:32].unflatten(1, (2, 8)), 4)[1] == 48
     for bad in (t[:3], t.double(), t.bfloat16(), torch.zeros(4, 8), torch.zeros(4, 32)[:, ::2], torch.zeros(4, 8, 2).transpose(1, 2),
-                torch.zeros(64), torch.zeros(4, 2, 16)[:, :, :8]):
+                torch.zeros(64), torch.zeros(4, 2, 16)[:, :, :8], torch.tensor(0.0)):
         with pytest.raises(fz.FusionError):
             rows(bad, 4)
     for bad in (torch.zeros(4), torch.zeros(3, dtype=torch.int32), torch.zeros(8, dtype=torch.int32)[::2],

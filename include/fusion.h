@@ -469,8 +469,8 @@ int fusion_stage_mlp(int dtype, int flags, fusion_ragged in, const void *x, int3
 
 /*
  * Bytes of scratch of the fusion_cache_* calls on this cache (its shape and whether `weights` is NULL are read) with up to
- * `heads` query heads, or 0 for a shape that they refuse; zero-filled before its first use, reusable without clearing, and
- * not to be shared by calls that overlap (as fusion_workspace_size).  With weights it holds a float per query head and token.
+ * `heads` query heads, or 0 for a shape that they refuse.  As with fusion_workspace_size the first 256 KB are zero before its
+ * first use and after every call, and it is not to be shared by calls that overlap.  With weights it holds a float per query head and token.
  */
 size_t fusion_cache_workspace_size(fusion_cache cache, int32_t heads);
 

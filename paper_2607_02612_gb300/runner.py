@@ -175,21 +175,21 @@ class DeviceCache:
         self.ws_bytes = fb.fusion_cache_workspace_size(self._c, self.heads)
         if self.ws_bytes == 0:
             raise fb.FusionError("cache shape or number of heads out of range")
-        self.workspace = torch.zeros(self.ws_bytes, dtype=torch.uint8, device=self.k.device)
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.k.device)
+        self.workspace[:1 << 18].zero_()   # the counters; the rest need not be zero
         self.device, self.index = self.k.device, self.k.get_device()
         self.code, self.torch_dtype = DTYPE_CODE[self.dtype], TORCH_DTYPE[self.dtype]
         self.scale = self.head_dim ** -0.5
         self.lib = fb.load()
         self._ws = self.workspace.data_ptr()
-        self._one = None   # the offsets of one row per sequence
+        self._one = RaggedRows(self.max_batch, 1, self.max_batch,
+                               torch.arange(self.max_batch + 1, dtype=torch.int32, device=self.device))
 
     def c_struct(self) -> fb.fusion_cache:
         return self._c
 
     def one_row_each(self) -> RaggedRows:
-        if self._one is None:
-            self._one = RaggedRows(self.max_batch, 1, self.max_batch,
-                                   torch.arange(self.max_batch + 1, dtype=torch.int32, device=self.k.device))
+        """A row per sequence, in the sequences' order."""
         return self._one
 
 

@@ -57,7 +57,8 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
 
 // Scratch behind the counters of the workspace.  Attention: log-sum-exps, partial results of sequences that
 // several CTAs share, logits (only where weights are accumulated).  Eviction: the kept slots and their counts.
-constexpr int kCacheMaxCtas = 512;   // CTAs of the attention kernel; each has two partial results at most
+constexpr int kCacheMaxCtas = 2048;   // CTAs of the attention kernel; each has two partial results at most
+constexpr int kCacheMaxWide = 512;    // those of four warps
 constexpr int kCacheMaxQ = 16;       // query heads of a key head that one CTA takes, at most
 struct CacheWs {
     size_t counters, lse, part_ml, part, logits, keep, plan, total;
@@ -68,11 +69,12 @@ inline CacheWs cache_ws_layout(int max_batch, int max_pages, int page_tokens, in
     const int group = heads / kv_heads, nq = group <= 8 ? 8 : kCacheMaxQ;
     CacheWs L;
     L.lstride = (long long)((cap + 3) / 4 * 4);
+    const size_t ctas = dim <= 128 ? kCacheMaxCtas : kCacheMaxWide;
     L.counters = 0;
     L.lse = align256(sizeof(int) * (size_t)kWsCounters);
     L.part_ml = L.lse + align256(b * heads * 4);
-    L.part = L.part_ml + align256((size_t)2 * kCacheMaxCtas * nq * 8);
-    L.logits = L.part + align256((size_t)2 * kCacheMaxCtas * nq * dim * 4);
+    L.part = L.part_ml + align256(2 * ctas * nq * 8);
+    L.logits = L.part + align256(2 * ctas * nq * dim * 4);
     const size_t attn = L.logits + (weights ? align256(b * heads * (size_t)L.lstride * 4) : 0);
     L.plan = L.lse;
     L.keep = L.plan + align256(b * 8);

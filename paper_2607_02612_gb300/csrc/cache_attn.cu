@@ -4,7 +4,7 @@
 //   x_aj = scale2 q_a . k_hj + log2 s_j,   out_a = sum_j 2^(x_aj - m) v_hj / sum_j 2^(x_aj - m),   m = max_j x_aj,
 //   weights_j += sum_a 2^(x_aj - lse_a),   lse_a = m + log2 sum_j 2^(x_aj - m).
 //
-// Work is cut into rounds: the next kWarps * TT visible tokens of one (sequence, key head).  Every CTA takes an equal
+// Work is cut into rounds: the next TT visible tokens per warp of a CTA of one (sequence, key head).  Every CTA takes an equal
 // run of the rounds of the whole batch, in the order (sequence, key head, token), whatever the sequences' lengths; a
 // warp takes TT tokens of each round through stages of its own (cp.async) and keeps its own running maximum, sum and
 // output.  Where a run ends with a (sequence, key head) the warps join in shared memory; a (sequence, key head) that
@@ -18,22 +18,24 @@ using namespace rounds;
 
 // The CTA's shared memory: per warp and stage TT rows of K, TT rows of V; the tokens' log2 sizes; their probabilities, each
 // twice (a packed multiplication's operand); then the queries or, at the end of a (sequence, key head), the warps' outputs.
-template <int DP, int NQ, int TT, int S>
+template <int DP, int NQ, int TT, int S, int W>
 struct Layout {
     static constexpr int kRow = DP * 4, kStage = 2 * TT * kRow;
     static constexpr int kJoinQ = NQ < 2 ? NQ : 2;        // query heads joined at a time
     static constexpr int kPitch = DP + 4;
-    static constexpr int kLsz = kWarps * S * kStage;          // float [kWarps][S][TT]
-    static constexpr int kP = kLsz + kWarps * S * TT * 4;     // float2 [kWarps][TT][NQ]
-    static constexpr int kShared = kP + kWarps * TT * NQ * 8;
-    static constexpr int kQBytes = NQ * kRow, kJoinBytes = kWarps * kJoinQ * kPitch * 4, kScratch = kJoinScratch<NQ>;
+    static constexpr int kLsz = W * S * kStage;          // float [W][S][TT]
+    static constexpr int kP = kLsz + W * S * TT * 4;     // float2 [W][TT][NQ]
+    static constexpr int kShared = kP + W * TT * NQ * 8;
+    static constexpr int kQBytes = NQ * kRow, kJoinBytes = W * kJoinQ * kPitch * 4, kScratch = kJoinScratch<NQ>;
     static constexpr int kTotal = kShared + (kQBytes > kJoinBytes ? kQBytes > kScratch ? kQBytes : kScratch
                                              : kJoinBytes > kScratch ? kJoinBytes : kScratch);
 };
 
-template <int DP, int NQ, int TT, int S>
-__global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(CacheAttnParams p, int chunks) {
-    using L = Layout<DP, NQ, TT, S>;
+// W: warps of a CTA.
+template <int DP, int NQ, int TT, int S, int W>
+__global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_attn_f32(CacheAttnParams p, int chunks) {
+    using L = Layout<DP, NQ, TT, S, W>;
+    constexpr int kWarps = W, kThreads = 32 * W;
     constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kMt = TT / 8;
     // for p v: a lane has kV chunks of four dims; narrow rows are shared out, kGroups of them side by side
     constexpr int kGroups = DP < 128 ? 2 : 1, kLanes = 32 / kGroups, kV = DP / (4 * kLanes);
@@ -47,7 +49,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
     Run run;
     Place at;
     if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
-        empty_sequences<float>(p);
+        empty_sequences<float, kThreads>(p);
         return;
     }
     const unsigned r0 = run.r0, r1 = run.r1;
@@ -87,10 +89,10 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
         read_q(next.b, next.h, next.ch);
     };
     read_q(at.b, at.h, at.ch);
-    Stream<float, DP, TT> in;
+    Stream<float, DP, TT, W> in;
     in.template begin<S>(p, at, run, chunks, warp, lane, stages, lsz, swizzle);
     write_q();
-    empty_sequences<float>(p);
+    empty_sequences<float, kThreads>(p);
     if (tid == 0) s_bad = 0;
     __syncthreads();
 
@@ -295,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_f32(Cac
                 s_bad = 0;
             }
             if (!whole) {
-                join_runs<float, NQ>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
+                join_runs<float, NQ, kThreads>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
                 __syncthreads();
             }
             if (r + 1 == r1) break;
@@ -367,8 +369,10 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
 
 template <int DP, int NQ, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
-    using L = Layout<DP, NQ, TT, S>;
-    return launch_rounds<k_cache_attn_f32<DP, NQ, TT, S>>(L::kTotal, p, ceil_div(p.group, NQ), kWarps * TT, s);
+    const int chunks = ceil_div(p.group, NQ);
+    if constexpr (DP <= 128)
+        if (warps_alone(p, chunks)) return launch_rounds<k_cache_attn_f32<DP, NQ, TT, S, 1>, 1>(Layout<DP, NQ, TT, S, 1>::kTotal, p, chunks, TT, s);
+    return launch_rounds<k_cache_attn_f32<DP, NQ, TT, S, 4>, 4>(Layout<DP, NQ, TT, S, 4>::kTotal, p, chunks, 4 * TT, s);
 }
 template <int NQ>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {

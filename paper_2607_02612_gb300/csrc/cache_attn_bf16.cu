@@ -36,20 +36,22 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
 
 // Shared memory of a CTA: per warp S stages of TT rows of K and of V; the tokens' log2 sizes; then the queries, or, at the end of
 // a (sequence, key head), the warps' outputs on their way to each other, kTiles steps of 16 dims at a time.
-template <int DP, int NT, int TT, int S>
+template <int DP, int NT, int TT, int S, int W>
 struct Layout {
     static constexpr int kNq = 8 * NT, kRow = 2 * DP, kStage = 2 * TT * kRow;
     static constexpr int kTiles = 2, kPitch = 16 * kTiles + 4;   // (pitches of 4 mod 16: no bank conflicts)
-    static constexpr int kLsz = kWarps * S * kStage;
-    static constexpr int kShared = kLsz + kWarps * S * TT * 4;
-    static constexpr int kQBytes = kNq * kRow, kJoinBytes = kWarps * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
+    static constexpr int kLsz = W * S * kStage;
+    static constexpr int kShared = kLsz + W * S * TT * 4;
+    static constexpr int kQBytes = kNq * kRow, kJoinBytes = W * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
     static constexpr int kTotal = kShared + (kQBytes > kJoinBytes ? kQBytes > kScratch ? kQBytes : kScratch
                                              : kJoinBytes > kScratch ? kJoinBytes : kScratch);
 };
 
-template <int DP, int NT, int TT, int S>
-__global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(CacheAttnParams p, int chunks) {
-    using L = Layout<DP, NT, TT, S>;
+// W: warps of a CTA.
+template <int DP, int NT, int TT, int S, int W>
+__global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_attn_mma(CacheAttnParams p, int chunks) {
+    using L = Layout<DP, NT, TT, S, W>;
+    constexpr int kWarps = W, kThreads = 32 * W;
     constexpr int kNq = L::kNq, kRound = kWarps * TT, kRow = L::kRow, kKs = DP / 16, kMt = TT / 16;
     constexpr int kQPer = (kNq * DP / 8 + kThreads - 1) / kThreads;   // 16-byte chunks of the queries per thread
     constexpr bool kQRegs = NT * DP <= 128;     // the queries' fragments stay in registers
@@ -64,7 +66,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
     Run run;
     Place at;
     if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
-        empty_sequences<__nv_bfloat16>(p);
+        empty_sequences<__nv_bfloat16, kThreads>(p);
         return;
     }
     const unsigned r0 = run.r0, r1 = run.r1;
@@ -101,10 +103,10 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
         read_q(next.b, next.h, next.ch);
     };
     read_q(at.b, at.h, at.ch);
-    Stream<__nv_bfloat16, DP, TT> in;
+    Stream<__nv_bfloat16, DP, TT, W> in;
     in.template begin<S>(p, at, run, chunks, warp, lane, stages, lsz, swizzle);
     write_q();
-    empty_sequences<__nv_bfloat16>(p);
+    empty_sequences<__nv_bfloat16, kThreads>(p);
     if (tid == 0) s_bad = 0;
     __syncthreads();
 
@@ -293,19 +295,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][8 * n + 2 * t + e]);
                     f[n][e] = ex2(m[n][e] - M);
                 }
-            // this thread joins four dims of one head per step
-            const bool joins = tid < kNq * 4 * L::kTiles;
-            const int q = joins ? tid / (4 * L::kTiles) : 0, d0 = tid % (4 * L::kTiles) * 4;
-            float M = s_m[0][q], ls = 0.0f;
-#pragma unroll
-            for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
-#pragma unroll
-            for (int w = 0; w < kWarps; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
-            const float inv = ls == 0.0f ? 0.0f : 1.0f / ls;
-            if (joins && d0 == 0 && q < nq) {
-                if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
-                else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
-            }
+            // a thread joins four dims of one head per step (of one or two)
 #pragma unroll
             for (int k1 = 0; k1 < kKs; k1 += L::kTiles) {
                 float *dst = join + (warp * kNq + 2 * t) * L::kPitch + g;
@@ -322,14 +312,26 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
                     }
                 }
                 __syncthreads();
-                const int d = 16 * k1 + d0;
-                if (joins && q < nq && d < c.dim) {
+#pragma unroll
+                for (int e0 = 0; e0 < kNq * 4 * L::kTiles; e0 += kThreads) {
+                    const int e = e0 + tid, q = e / (4 * L::kTiles), d0 = e % (4 * L::kTiles) * 4, d = 16 * k1 + d0;
+                    if (q >= nq || d >= c.dim) continue;
+                    float M = s_m[0][q], ls = 0.0f;
+#pragma unroll
+                    for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
+#pragma unroll
+                    for (int w = 0; w < kWarps; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
                     float4 sum = *reinterpret_cast<const float4 *>(join + q * L::kPitch + d0);
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) {
                         const float4 v = *reinterpret_cast<const float4 *>(join + (w * kNq + q) * L::kPitch + d0);
                         sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
                     }
+                    if (d == 0) {
+                        if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                        else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+                    }
+                    const float inv = 1.0f / ls;
                     if (!whole)
                         *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
                     else if (!seg_bad)
@@ -343,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
                 s_bad = 0;
             }
             if (!whole) {
-                join_runs<__nv_bfloat16, kNq>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
+                join_runs<__nv_bfloat16, kNq, kThreads>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
                 __syncthreads();
             }
             if (r + 1 == r1) break;
@@ -360,8 +362,10 @@ __global__ void __launch_bounds__(kThreads, S == 2 ? 3 : 1) k_cache_attn_mma(Cac
 
 template <int DP, int NT, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
-    using L = Layout<DP, NT, TT, S>;
-    return launch_rounds<k_cache_attn_mma<DP, NT, TT, S>>(L::kTotal, p, ceil_div(p.group, 8 * NT), kWarps * TT, s);
+    const int chunks = ceil_div(p.group, 8 * NT);
+    if constexpr (DP <= 128)
+        if (warps_alone(p, chunks)) return launch_rounds<k_cache_attn_mma<DP, NT, TT, S, 1>, 1>(Layout<DP, NT, TT, S, 1>::kTotal, p, chunks, TT, s);
+    return launch_rounds<k_cache_attn_mma<DP, NT, TT, S, 4>, 4>(Layout<DP, NT, TT, S, 4>::kTotal, p, chunks, 4 * TT, s);
 }
 template <int NT>
 cudaError_t launch_dim(const CacheAttnParams &p, cudaStream_t s) {

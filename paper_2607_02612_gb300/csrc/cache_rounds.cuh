@@ -9,8 +9,8 @@
 namespace fz {
 namespace rounds {
 
-constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kMinRounds = 2;       // of a CTA: fewer and the join costs more than the split gains
+constexpr int kAloneMost = 128, kAloneLeast = 256;   // visible tokens at most, (sequence, key head)s at least
 constexpr float kLow = -3.0e38f;    // a maximum over nothing: finite, so that (-inf) - kLow is -inf
 // Probabilities are 2^(x - shift) with a shift of at least the largest logit so far less kLag: up to 2^8, which costs no bits in
 // float32 or bf16, and tiles whose maximum grows a little do not rescale (with 16 heads in a warp nearly every tile does).
@@ -176,9 +176,9 @@ struct Token {
 // Tokens of the rounds to come, a warp's share of TT per round: the page is read two rounds before the token's rows are
 // asked for, the size one round before.  Rows without a token, or of size zero, arrive as zeros and weigh nothing (log2
 // size -inf), whatever the cache holds there.
-template <typename T, int DP, int TT>
+template <typename T, int DP, int TT, int W>
 struct Stream {
-    static constexpr int kRow = DP * (int)sizeof(T), kCpr = kRow / 16, kStage = 2 * TT * kRow, kRound = kWarps * TT;
+    static constexpr int kRow = DP * (int)sizeof(T), kCpr = kRow / 16, kStage = 2 * TT * kRow, kRound = W * TT;
     Place ahead;             // of the next token to look up
     unsigned ahead_r, r1;
     Token t0, t1;            // t0's rows are asked for next (its size is here), then t1's
@@ -259,10 +259,10 @@ struct Stream {
 };
 
 // Zeros for sequences without tokens (a length out of range is told, its row left), dealt out over the grid.
-template <typename T>
+template <typename T, int THREADS>
 __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
     const int row = p.heads * p.c.dim * (int)sizeof(T) / 16, grid = (int)gridDim.x, lane = threadIdx.x & 31;
-    for (long long b0 = blockIdx.x + (long long)(threadIdx.x >> 5) * 32 * grid; b0 < p.c.max_batch; b0 += (long long)kThreads * grid) {
+    for (long long b0 = blockIdx.x + (long long)(threadIdx.x >> 5) * 32 * grid; b0 < p.c.max_batch; b0 += (long long)THREADS * grid) {
         const long long b = b0 + (long long)lane * grid;   // a warp looks at 32 sequences at once
         const int n = b < p.c.max_batch ? cache_length(p.c, (int)b) : 1;
         if (n < 0) raise_status(p.status, FUSION_DEV_BAD_CACHE);
@@ -277,7 +277,7 @@ __device__ __forceinline__ void empty_sequences(const CacheAttnParams &p) {
 // Run k's result lies in slot 2 k + 1 where the (sequence, key head) begins in run k, else in slot 2 k: per query head a maximum
 // and a sum (below zero: a bad page) and the output before the division.
 constexpr int kJoinAtOnce = 16;     // in one step; more in two
-constexpr int kJoinMost = 23;       // results joined at once: 23 * 23 covers kCacheMaxCtas
+constexpr int kJoinMost = 23;       // results joined at once: 23 * 23 covers kCacheMaxWide, and the rounds that short sequences have
 template <int NQ> constexpr int kJoinScratch = (kJoinMost + 2) * NQ * 4;   // bytes
 
 template <typename T> __device__ __forceinline__ void store4(T *dst, float4 v);
@@ -289,7 +289,7 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 
 
 // Joins the results of runs k0, k0 + step, ... (n of them, n <= kJoinMost) in this order, into the output or into the first one's
 // slot.  scratch: kJoinScratch<NQ> bytes of shared memory.
-template <typename T, int NQ>
+template <typename T, int NQ, int THREADS>
 __device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, int k0, int step, int n, bool last, size_t head, int nq,
                                              float *scratch) {
     const int tid = threadIdx.x, dim = p.c.dim;
@@ -319,27 +319,27 @@ __device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, i
     __syncthreads();
     constexpr int kU = 4;   // columns of four in flight, for four results at a time
     const int all = nq * dim / 4;
-    for (int e0 = tid; e0 < all; e0 += kU * kThreads) {
+    for (int e0 = tid; e0 < all; e0 += kU * THREADS) {
         float4 acc[kU];
         int q[kU];
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
             acc[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            q[u] = min(e0 + u * kThreads, all - 1) * 4 / dim;
+            q[u] = min(e0 + u * THREADS, all - 1) * 4 / dim;
         }
 #pragma unroll 4
         for (int j = 0; j < n; ++j) {
             const float4 *src = reinterpret_cast<const float4 *>(p.part + slot(j) * NQ * dim);
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
-                const float4 v = __ldcg(src + min(e0 + u * kThreads, all - 1));
+                const float4 v = __ldcg(src + min(e0 + u * THREADS, all - 1));
                 const float f = weight[j * NQ + q[u]];
                 acc[u] = make_float4(fmaf(v.x, f, acc[u].x), fmaf(v.y, f, acc[u].y), fmaf(v.z, f, acc[u].z), fmaf(v.w, f, acc[u].w));
             }
         }
 #pragma unroll
         for (int u = 0; u < kU; ++u) {
-            const int e = e0 + u * kThreads;
+            const int e = e0 + u * THREADS;
             if (e >= all) break;
             if (!last) {
                 *reinterpret_cast<float4 *>(p.part + slot(0) * NQ * dim + (size_t)e * 4) = acc[u];
@@ -374,7 +374,7 @@ __device__ __forceinline__ bool arrive_last(int *counter, int n, int &s_last) {
 // After a CTA has written its result of the (sequence, key head) of rounds [seg0, seg1): the last of the runs that share it
 // joins their results.  More than kJoinAtOnce are joined in two steps, groups of about the square root of their number first,
 // by the group's last: one CTA alone reads the results of 38 runs of 16 heads of 128 (300 KB) slower than two in turn a few each.
-template <typename T, int NQ>
+template <typename T, int NQ, int THREADS>
 __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &run, unsigned seg0, unsigned seg1, size_t head, int nq,
                                           float *scratch, int &s_last) {
     int c0;
@@ -386,16 +386,23 @@ __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &r
     int *count1 = p.counters, *count2 = p.counters + 2 * kCacheMaxCtas;   // both by the slot of the first run
     if (members > 1 || groups == 1) {
         if (!arrive_last(&count1[2 * first + (first == c0)], members, s_last)) return;
-        join_results<T, NQ>(p, c0, first, 1, members, groups == 1, head, nq, scratch);
+        join_results<T, NQ, THREADS>(p, c0, first, 1, members, groups == 1, head, nq, scratch);
     }
     if (groups == 1) return;
     if (!arrive_last(&count2[2 * c0 + 1], groups, s_last)) return;
-    join_results<T, NQ>(p, c0, c0, size, groups, true, head, nq, scratch);
+    join_results<T, NQ, THREADS>(p, c0, c0, size, groups, true, head, nq, scratch);
+}
+
+// Whether warps work alone (W = 1, CTAs of one warp) instead of four together.  Alone a warp needs no barrier, and sequences of
+// a round or two leave no warp of a CTA idle (alone and together: 200 x 60 tokens of 8 heads 10.6 and 14.9 us, 181 x 87 of 16 heads
+// 33.3 and 38.9); together they share longer ones (60 x 200 of 8 heads 16.8 and 13.8, 64 x 250 19.4 and 17.4).
+inline bool warps_alone(const CacheAttnParams &p, int chunks) {
+    return p.c.dim <= 128 && p.most <= kAloneMost && (long long)p.c.max_batch * p.c.kv_heads * chunks >= kAloneLeast;
 }
 
 // Host: as many CTAs as the GPU holds at once, or as there can be rounds.  What depends on the kernel and the device alone is
 // asked once (asking costs the host 4 us a call).
-template <auto Kernel>
+template <auto Kernel, int THREADS>
 cudaError_t resident_ctas(int smem, int &ctas) {
     constexpr int kDevices = 64;
     static std::atomic<int> known[kDevices];
@@ -407,20 +414,21 @@ cudaError_t resident_ctas(int smem, int &ctas) {
     int sms = 0, occ = 0;
     e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, Kernel, kThreads, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, Kernel, THREADS, smem);
     if (e != cudaSuccess) return e;
     ctas = sms * (occ < 1 ? 1 : occ);
     if (dev < kDevices) known[dev].store(ctas, std::memory_order_release);
     return cudaSuccess;
 }
-template <auto Kernel>
+template <auto Kernel, int W>
 cudaError_t launch_rounds(int smem, const CacheAttnParams &p, int chunks, int tokens, cudaStream_t s) {
     int ctas = 0;
-    const cudaError_t e = resident_ctas<Kernel>(smem, ctas);
+    const cudaError_t e = resident_ctas<Kernel, 32 * W>(smem, ctas);
     if (e != cudaSuccess) return e;
     const long long rounds = (long long)p.c.max_batch * p.c.kv_heads * chunks * ceil_div(p.most, tokens);
-    if (ctas > kCacheMaxCtas) ctas = kCacheMaxCtas;
-    return launch_after(Kernel, dim3((unsigned)(ctas < rounds ? ctas : rounds)), kThreads, (size_t)smem, 1, s, p, chunks);
+    constexpr int kMost = W == 1 ? kCacheMaxCtas : kCacheMaxWide;
+    if (ctas > kMost) ctas = kMost;
+    return launch_after(Kernel, dim3((unsigned)(ctas < rounds ? ctas : rounds)), 32 * W, (size_t)smem, 1, s, p, chunks);
 }
 
 }  // namespace rounds

@@ -216,6 +216,35 @@ def test_attention_many_short_sequences(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads,dim,page", [(1, 1, 64, 16), (8, 2, 128, 16), (16, 1, 64, 8), (21, 1, 128, 4), (4, 4, 80, 32), (3, 1, 8, 128)])
+def test_attention_short_sequences_a_warp_each(dtype, heads, kv_heads, dim, page):
+    """Sequences of at most 128 tokens, enough of them that every warp works alone: masked tokens, weights, a window; and one
+    sequence with a bad page among them."""
+    n = [(29 * i) % 128 for i in range(260)]
+    c = ref.make(dtype, n, kv_heads, dim, page, sizes="masked", weights=True, seed=41)
+    attend(dtype, c, heads)
+    attend(dtype, c, heads, window=40, sinks=3)
+    q = torch.randn((260, heads, dim), generator=torch.Generator().manual_seed(42)).to(ref.TYPES[dtype])
+    want, tol, w, wtol = ref.attention(c, q, dtype)
+    bad = 123
+    assert n[bad] > 0
+    table = c["table"].clone()
+    table[bad, 0] = -1
+    dc, f = on_device(dtype, dict(c, table=table), heads), runner.Fusion(260)
+    out = torch.full((260, heads, dim), 7.0, dtype=ref.TYPES[dtype], device=DEV)
+    f.cache_attention(dc, q.to(DEV), out=out)
+    assert status(f) == fz.FUSION_DEV_BAD_CACHE
+    got, gw, good = out.cpu().double(), dc.weights.cpu().double(), [b for b in range(260) if b != bad]
+    assert ((got[good] - want[good]).abs() <= tol[good]).all() and (got[bad] == 7.0).all()
+    for b in good:
+        at = ref.places(c, b, torch.arange(n[b]))
+        assert ((gw[at] - w[at]).abs() <= wtol[at]).all()
+    at = ref.places(c, bad, torch.arange(n[bad]))
+    assert torch.equal(gw[at], c["weights"][at].double())
+    assert int(dc.workspace[:1 << 18].max()) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_attention_thousands_of_sequences(dtype):
     """More sequences than threads: most of them empty, a few with tokens; and the same batch appended to in one call."""
     n = [(i % 11) * (i % 3 == 0) for i in range(9000)]

@@ -295,7 +295,24 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][8 * n + 2 * t + e]);
                     f[n][e] = ex2(m[n][e] - M);
                 }
-            // a thread joins four dims of one head per step (of one or two)
+            // a thread joins four dims of one head (kMine of them) per step
+            constexpr int kMine = (kNq * 4 * L::kTiles + kThreads - 1) / kThreads;
+            float sums[kMine];
+#pragma unroll
+            for (int x = 0; x < kMine; ++x) {
+                const int q = min((x * kThreads + tid) / (4 * L::kTiles), kNq - 1);
+                float M = s_m[0][q], ls = 0.0f;
+#pragma unroll
+                for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
+                sums[x] = ls;
+                const int e = x * kThreads + tid;
+                if (e < 4 * L::kTiles * nq && e % (4 * L::kTiles) == 0) {
+                    if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                    else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+                }
+            }
 #pragma unroll
             for (int k1 = 0; k1 < kKs; k1 += L::kTiles) {
                 float *dst = join + (warp * kNq + 2 * t) * L::kPitch + g;
@@ -313,30 +330,21 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
                 }
                 __syncthreads();
 #pragma unroll
-                for (int e0 = 0; e0 < kNq * 4 * L::kTiles; e0 += kThreads) {
-                    const int e = e0 + tid, q = e / (4 * L::kTiles), d0 = e % (4 * L::kTiles) * 4, d = 16 * k1 + d0;
+                for (int x = 0; x < kMine; ++x) {
+                    const int e = x * kThreads + tid, q = e / (4 * L::kTiles), d0 = e % (4 * L::kTiles) * 4, d = 16 * k1 + d0;
                     if (q >= nq || d >= c.dim) continue;
-                    float M = s_m[0][q], ls = 0.0f;
-#pragma unroll
-                    for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
-#pragma unroll
-                    for (int w = 0; w < kWarps; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
                     float4 sum = *reinterpret_cast<const float4 *>(join + q * L::kPitch + d0);
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) {
                         const float4 v = *reinterpret_cast<const float4 *>(join + (w * kNq + q) * L::kPitch + d0);
                         sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
                     }
-                    if (d == 0) {
-                        if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
-                        else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
-                    }
-                    const float inv = 1.0f / ls;
+                    const float inv = 1.0f / sums[x];
                     if (!whole)
                         *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
                     else if (!seg_bad)
                         store4(reinterpret_cast<__nv_bfloat16 *>(p.out) + (head + q) * c.dim + d,
-                               ls == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+                               sums[x] == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
                 }
                 __syncthreads();
             }

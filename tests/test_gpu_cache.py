@@ -389,19 +389,24 @@ def test_attention_strided_queries_other_stream_and_graph():
         out = f.cache_attention(dc, p[:, :256])
     side.synchronize()
     assert ((out.cpu().double() - want).abs() <= tol).all()
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph):
+    graph, staged, result = torch.cuda.CUDAGraph(), torch.zeros_like(p), torch.zeros_like(out)
+    with torch.cuda.graph(graph):   # (between kernels of torch's)
+        p.copy_(staged)
+        p.mul_(2.0)
         f.cache_attention(dc, p[:, :256], window=90, sinks=2, out=out)
+        result.copy_(out)
+        p.zero_()
     for seed in (21, 22):
         n = [399 - seed, seed, 0]
         c2 = ref.make("bf16", n, 2, 64, 16, room=400 - max(n), sizes="whole", seed=seed)
         assert c2["table"].shape == c["table"].shape and c2["k"].shape == c["k"].shape
         dc.k.copy_(c2["k"]), dc.v.copy_(c2["v"]), dc.sizes.copy_(c2["sizes"])
         dc.page_table.copy_(c2["table"]), dc.lengths.copy_(c2["lengths"])
-        p.copy_(torch.randn((3, 512), generator=torch.Generator().manual_seed(seed)))
+        staged.copy_(torch.randn((3, 512), generator=torch.Generator().manual_seed(seed)))
         graph.replay()
-        want, tol, _, _ = ref.attention(c2, p.cpu()[:, :256].reshape(3, 4, 64), "bf16", window=90, sinks=2)
-        assert ((out.cpu().double() - want).abs() <= tol).all()
+        q = (staged * 2.0).cpu()[:, :256].reshape(3, 4, 64)
+        want, tol, _, _ = ref.attention(c2, q, "bf16", window=90, sinks=2)
+        assert ((result.cpu().double() - want).abs() <= tol).all()
     assert status(f) == 0
 
 

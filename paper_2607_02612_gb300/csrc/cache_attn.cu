@@ -36,14 +36,22 @@ template <int DP, int NQ, int TT, int S, int W>
 __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_attn_f32(CacheAttnParams p, int chunks) {
     using L = Layout<DP, NQ, TT, S, W>;
     constexpr int kWarps = W, kThreads = 32 * W;
-    constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16, kMt = TT / 8;
-    // for p v: a lane has kV chunks of four dims; narrow rows are shared out, kGroups of them side by side
-    constexpr int kGroups = DP < 128 ? 2 : 1, kLanes = 32 / kGroups, kV = DP / (4 * kLanes);
+    constexpr int kRound = kWarps * TT, kCpr = L::kRow / 16;
+    // What bounds groups of four heads and more is not memory but the reading of operands from shared memory, so a lane's products
+    // are blocked: for q k four lanes per token, a lane has kMt tokens and kHeads heads (eight heads: two halves side by side, 4 x 4
+    // or 2 x 4 a lane; with 32 x 4096 of 8 heads of 64, 128, 256 dims: 65.4, 67.4, 83.6 us with all eight in a lane, 62.1, 60.1, 72.3 so).
+    // Then each lane of the four gets the sums of kMine heads, so that a softmax is computed once (in all four: 72.4 for 64 dims).
+    constexpr int kSides = NQ == 8 ? 2 : 1, kHeads = NQ / kSides, kRows = 8 / kSides, kMt = TT / kRows;
+    constexpr int kMine = kHeads < 4 ? kHeads : kHeads / 4;   // heads whose softmax a lane holds
+    // For p v a lane has kV chunks of four dims of every kGroups-th row (two with eight heads of 64 dims: spills, 71.1).
+    constexpr int kV = NQ == 8 && DP < 256 ? 1 : 2, kLanes = DP / (4 * kV), kGroups = 32 / kLanes;
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Finder<kThreads> finder;
     __shared__ float s_m[kWarps][NQ], s_l[kWarps][NQ];
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int quad = lane & 3, row0 = lane >> 2 & (kRows - 1), h0 = kSides == 1 ? 0 : (lane >> 4) * kHeads;
+    const int my0 = h0 + (kHeads < 4 ? 0 : quad * kMine);
     const Cache &c = p.c;
     wait_for_previous();
     Run run;
@@ -97,16 +105,18 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
     __syncthreads();
 
     bool bad = false;
-    float m[NQ], l[NQ];
+    float m[kMine], l[kMine];
     float2 o[NQ][2 * kV];
     auto begin_head = [&]() {
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) {
-            m[q] = kLow;
-            l[q] = 0.0f;
+        for (int e = 0; e < kMine; ++e) {
+            m[e] = kLow;
+            l[e] = 0.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
 #pragma unroll
             for (int d = 0; d < 2 * kV; ++d) o[q][d] = make_float2(0.0f, 0.0f);
-        }
     };
     begin_head();
     int st = 0;
@@ -124,23 +134,22 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
         const int j0 = at.u * kRound + warp * TT, cnt = min(TT, at.vis - j0);
         const int nq = min(NQ, p.group - at.ch * NQ), head0 = at.h * p.group + at.ch * NQ;
         if (cnt > 0) {
-            // ---- logits: four lanes per token, eight tokens side by side
-            const int quad = lane & 3, row0 = lane >> 2;
-            float2 acc[kMt][NQ];
+            // ---- logits
+            float2 acc[kMt][kHeads];
 #pragma unroll
             for (int k = 0; k < kMt; ++k)
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) acc[k][q] = make_float2(0.0f, 0.0f);
+                for (int q = 0; q < kHeads; ++q) acc[k][q] = make_float2(0.0f, 0.0f);
 #pragma unroll
             for (int i = 0; i < kCpr / 4; ++i) {
                 const int cc = 4 * i + quad;
                 float4 kv[kMt];
 #pragma unroll
                 for (int k = 0; k < kMt; ++k)
-                    kv[k] = *reinterpret_cast<const float4 *>(ks + ((8 * k + row0) * kCpr + (cc ^ swizzle(8 * k + row0))) * 16);
+                    kv[k] = *reinterpret_cast<const float4 *>(ks + ((kRows * k + row0) * kCpr + (cc ^ swizzle(kRows * k + row0))) * 16);
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) {
-                    const float4 qq = *reinterpret_cast<const float4 *>(qs + q * DP + cc * 4);
+                for (int q = 0; q < kHeads; ++q) {
+                    const float4 qq = *reinterpret_cast<const float4 *>(qs + (h0 + q) * DP + cc * 4);
 #pragma unroll
                     for (int k = 0; k < kMt; ++k) {
                         acc[k][q] = __ffma2_rn(make_float2(kv[k].x, kv[k].y), make_float2(qq.x, qq.y), acc[k][q]);
@@ -148,56 +157,80 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
                     }
                 }
             }
-            float x[kMt][NQ];
+            // the four lanes' sums of a token, each to the lane that holds its head (all in every lane below four heads)
+            float x[kMt][kMine];
 #pragma unroll
             for (int k = 0; k < kMt; ++k) {
-                const float z = lz[8 * k + row0];
+                if constexpr (kHeads < 4) {
+#pragma unroll
+                    for (int q = 0; q < kHeads; ++q) {
+                        x[k][q] = acc[k][q].x + acc[k][q].y;
+                        x[k][q] += __shfl_xor_sync(0xFFFFFFFFu, x[k][q], 1);
+                        x[k][q] += __shfl_xor_sync(0xFFFFFFFFu, x[k][q], 2);
+                    }
+                } else {
+                    float half[kHeads / 2];
+#pragma unroll
+                    for (int q = 0; q < kHeads / 2; ++q) {
+                        const float lo = acc[k][q].x + acc[k][q].y, hi = acc[k][q + kHeads / 2].x + acc[k][q + kHeads / 2].y;
+                        half[q] = (quad & 2 ? hi : lo) + __shfl_xor_sync(0xFFFFFFFFu, quad & 2 ? lo : hi, 2);
+                    }
+#pragma unroll
+                    for (int e = 0; e < kMine; ++e)
+                        x[k][e] = (quad & 1 ? half[e + kMine] : half[e]) + __shfl_xor_sync(0xFFFFFFFFu, quad & 1 ? half[e] : half[e + kMine], 1);
+                }
+                const float z = lz[kRows * k + row0];
                 const bool off = z == -INFINITY || z == kNoPage;
                 bad |= z == kNoPage;
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) {
-                    float v = acc[k][q].x + acc[k][q].y;
-                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
-                    v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
-                    x[k][q] = off ? -INFINITY : v + z;
-                }
-                if (p.logits && quad == 0 && 8 * k + row0 < cnt) {
-                    float *dst = p.logits + ((size_t)at.b * p.heads + head0) * p.lstride + j0 + 8 * k + row0;
+                for (int e = 0; e < kMine; ++e) x[k][e] = off ? -INFINITY : x[k][e] + z;
+                if (p.logits && (kHeads >= 4 || quad == 0) && kRows * k + row0 < cnt) {
+                    float *dst = p.logits + ((size_t)at.b * p.heads + head0 + my0) * p.lstride + j0 + kRows * k + row0;
 #pragma unroll
-                    for (int q = 0; q < NQ; ++q)
-                        if (q < nq) dst[q * p.lstride] = x[k][q];
+                    for (int e = 0; e < kMine; ++e)
+                        if (my0 + e < nq) dst[e * p.lstride] = x[k][e];
                 }
             }
             // ---- the running shift: where a logit exceeds it by more than kLag, it becomes the maximum, and the output and the sums follow
             bool grows = false;
-            float mx[NQ];
+            float mx[kMine];
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) {
-                mx[q] = m[q];
+            for (int e = 0; e < kMine; ++e) {
+                mx[e] = m[e];
 #pragma unroll
-                for (int k = 0; k < kMt; ++k) mx[q] = fmaxf(mx[q], x[k][q]);
-                grows |= mx[q] > m[q] + kLag;
+                for (int k = 0; k < kMt; ++k) mx[e] = fmaxf(mx[e], x[k][e]);
+                grows |= mx[e] > m[e] + kLag;
             }
             if (__any_sync(0xFFFFFFFFu, grows)) {
+                float f[kMine];
+#pragma unroll
+                for (int e = 0; e < kMine; ++e) {
+#pragma unroll
+                    for (int s = 4; s < 4 * kRows; s <<= 1) mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xFFFFFFFFu, mx[e], s));
+                    f[e] = ex2(m[e] - mx[e]);
+                    m[e] = mx[e];
+                    l[e] *= f[e];
+                }
 #pragma unroll
                 for (int q = 0; q < NQ; ++q) {
+                    const float fq = kHeads < 4 ? f[q % kMine] : __shfl_sync(0xFFFFFFFFu, f[q % kMine], q / kHeads * 16 + q % kHeads / kMine);
 #pragma unroll
-                    for (int s = 4; s < 32; s <<= 1) mx[q] = fmaxf(mx[q], __shfl_xor_sync(0xFFFFFFFFu, mx[q], s));
-                    const float f = ex2(m[q] - mx[q]);
-                    m[q] = mx[q];
-                    l[q] *= f;
-#pragma unroll
-                    for (int d = 0; d < 2 * kV; ++d) o[q][d] = __fmul2_rn(o[q][d], make_float2(f, f));
+                    for (int d = 0; d < 2 * kV; ++d) o[q][d] = __fmul2_rn(o[q][d], make_float2(fq, fq));
                 }
             }
 #pragma unroll
-            for (int k = 0; k < kMt; ++k)
+            for (int k = 0; k < kMt; ++k) {
+                float pr[kMine];
 #pragma unroll
-                for (int q = 0; q < NQ; ++q) {
-                    const float pr = ex2(x[k][q] - m[q]);
-                    l[q] += pr;
-                    if (quad == 0) pw[(8 * k + row0) * NQ + q] = make_float2(pr, pr);
+                for (int e = 0; e < kMine; ++e) {
+                    pr[e] = ex2(x[k][e] - m[e]);
+                    l[e] += pr[e];
                 }
+                if (kHeads >= 4 || quad == 0) {
+#pragma unroll
+                    for (int e = 0; e < kMine; ++e) pw[(kRows * k + row0) * NQ + my0 + e] = make_float2(pr[e], pr[e]);
+                }
+            }
             __syncwarp();
             // ---- o += p v
 #pragma unroll 4
@@ -233,12 +266,12 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
             if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(&s_bad, 1);
             bad = false;
 #pragma unroll
-            for (int q = 0; q < NQ; ++q) {
+            for (int e = 0; e < kMine; ++e) {
 #pragma unroll
-                for (int s = 4; s < 32; s <<= 1) l[q] += __shfl_xor_sync(0xFFFFFFFFu, l[q], s);
-                if (lane == 0) {
-                    s_m[warp][q] = m[q];
-                    s_l[warp][q] = l[q];
+                for (int s = 4; s < 4 * kRows; s <<= 1) l[e] += __shfl_xor_sync(0xFFFFFFFFu, l[e], s);
+                if (row0 == 0 && (kHeads >= 4 || quad == 0)) {
+                    s_m[warp][my0 + e] = m[e];
+                    s_l[warp][my0 + e] = l[e];
                 }
             }
             __syncthreads();   // (and every warp is past its products with the queries)
@@ -251,18 +284,30 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
                     float M = s_m[0][q];
 #pragma unroll
                     for (int w = 1; w < kWarps; ++w) M = fmaxf(M, s_m[w][q]);
-                    const float f = ex2(m[q] - M);
-                    float *dst = join + (warp * L::kJoinQ + q - q1) * L::kPitch + lane % kLanes * 4;
+                    const float f = ex2(s_m[warp][q] - M);
+                    // the groups' sums: of the lanes with the same columns each ends with its share of them
+                    float v[4 * kV];
 #pragma unroll
-                    for (int d = 0; d < kV; ++d) {
-                        float4 v = make_float4(o[q][2 * d].x * f, o[q][2 * d].y * f, o[q][2 * d + 1].x * f, o[q][2 * d + 1].y * f);
-                        if constexpr (kGroups > 1) {
-                            v.x += __shfl_xor_sync(0xFFFFFFFFu, v.x, kLanes);
-                            v.y += __shfl_xor_sync(0xFFFFFFFFu, v.y, kLanes);
-                            v.z += __shfl_xor_sync(0xFFFFFFFFu, v.z, kLanes);
-                            v.w += __shfl_xor_sync(0xFFFFFFFFu, v.w, kLanes);
-                        }
-                        if (lane < kLanes) *reinterpret_cast<float4 *>(dst + d * kLanes * 4) = v;
+                    for (int d = 0; d < 2 * kV; ++d) {
+                        v[2 * d] = o[q][d].x * f;
+                        v[2 * d + 1] = o[q][d].y * f;
+                    }
+                    constexpr int kShare = 4 * kV / kGroups;
+                    int col = 0;   // of the lane's columns
+#pragma unroll
+                    for (int s = 16, n = 2 * kV; s >= kLanes; s >>= 1, n >>= 1) {
+                        const bool upper = lane & s;
+                        col += upper ? n : 0;
+#pragma unroll
+                        for (int i = 0; i < n; ++i) v[i] = (upper ? v[i + n] : v[i]) + __shfl_xor_sync(0xFFFFFFFFu, upper ? v[i] : v[i + n], s);
+                    }
+                    float *dst = join + (warp * L::kJoinQ + q - q1) * L::kPitch + lane % kLanes * 4 + col / 4 * kLanes * 4 + col % 4;
+                    if constexpr (kShare == 2) {
+                        *reinterpret_cast<float2 *>(dst) = make_float2(v[0], v[1]);
+                    } else {
+#pragma unroll
+                        for (int d = 0; d < kShare / 4; ++d)
+                            *reinterpret_cast<float4 *>(dst + d * kLanes * 4) = make_float4(v[4 * d], v[4 * d + 1], v[4 * d + 2], v[4 * d + 3]);
                     }
                 }
                 __syncthreads();

@@ -6,8 +6,9 @@
 // memory, each warp's in a piece of its own; the smallest kept key is found from its 11 top bits down by three histograms (11
 // bits spread weights, which share a few exponents, over enough bins that their atomics rarely meet; a pass whose bin is kept
 // whole is the last).  Each warp then places its kept tokens behind those of the warps before it.  What bounds it is the chain
-// of its phases, and in that the fetching of instructions that run once: so all loops over keys are rolled (keys in
-// registers, loops unrolled: 8 x 577 6.8 us, the pass over 32768 3.1, the placing of them 4.6).
+// of its phases and, of code that runs once, the fetching of its instructions, so all loops over keys are rolled (keys in
+// registers and loops unrolled: 8 x 577 10.8 us, now 7.8; 157 x 34 11.4, now 8.8).  The CTAs of a cluster exchange sums of 32 bins,
+// then read 32 bins of each other (all 2048 of each: 3000 cycles a pass).
 //
 // k_cache_move copies the rows.  Into other pages: any CTA any rows.  In place: a team of CTAs (a cluster) per (sequence, key
 // head, K or V) takes the rows in ascending position, a step of them at a time, all read before any is written.  That is safe
@@ -284,9 +285,11 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
         }
     }
     unsigned *keep = p.keep + (size_t)b * c.capacity;
+    int *idx = p.keep_idx + (size_t)b * p.keep_stride;
+    const int idx_n = p.keep_idx ? p.keep_stride : 0;
     auto put = [&](int i, int j, unsigned slot) {
         keep[i] = slot;
-        if (p.keep_idx && i < p.keep_stride) p.keep_idx[(size_t)b * p.keep_stride + i] = j;
+        if (i < idx_n) idx[i] = j;
     };
     int evicted = n;   // the first position that goes
     const unsigned lt = (1u << lane) - 1u;
@@ -303,8 +306,9 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
             i += min(before_e, ties);
             ne += __popc(be);
         }
-        if (stays) put(i, j, slot);
-        else if (o != 0u) evicted = min(evicted, j);
+        evicted = stays || o == 0u ? evicted : min(evicted, j);
+        if (stays) keep[i] = slot;
+        if (stays && i < idx_n) idx[i] = j;
     });
     // ---- the tokens that stay anyway
     if (choose) {
@@ -423,13 +427,15 @@ cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
 cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_t s) {
     if (p.c.max_batch == 0) return cudaSuccess;
     const int head_chunks = p.c.dim * (dtype == FUSION_BF16 ? 2 : 4) / 16;
-    // threads that hold a sequence's keys in registers: few where they do, since every warp more costs instructions (selection of
-    // 8 x 577: 1024 threads 16.5 us, 256 threads 9.6), then clusters of up to 8 CTAs (32768: two of 1024 threads 29, four of 512 20)
+    // Threads of a sequence: few where it is short, since every warp more has its share of the phases (8 x 577: 256 threads 7.9 us,
+    // 512 8.1), more where each would have many keys (64 x 1900: 21.4 and 20.8; 64 x 4000: 512 threads 34.2, 1024 32.4; 32 x 8192:
+    // 160.6 and 155.8), then clusters of up to 8 CTAs (8852: two of 1024 threads 18.6, four of 512 18.8; 10973: 16.6 and 14.5; 32768:
+    // four of 1024 85.0, eight of 512 83.7).
     const int cap = p.c.capacity, k = kHeld;
-    cudaError_t e = cap <= 256 * k    ? launch_select<1, 256>(p, s)
-                    : cap <= 512 * k  ? launch_select<1, 512>(p, s)
-                    : cap <= 1024 * k ? launch_select<2, 512>(p, s)
-                    : cap <= 2048 * k ? launch_select<4, 512>(p, s)
+    cudaError_t e = cap <= 64 * k     ? launch_select<1, 256>(p, s)
+                    : cap <= 256 * k  ? launch_select<1, 512>(p, s)
+                    : cap <= 512 * k  ? launch_select<1, 1024>(p, s)
+                    : cap <= 1024 * k ? launch_select<4, 512>(p, s)
                     : cap <= 4096 * k ? launch_select<8, 512>(p, s)
                                       : launch_select<8, 1024>(p, s);
     if (e != cudaSuccess) return e;

@@ -485,7 +485,7 @@ def test_evict_ties_go_to_the_lowest_position(outside):
         evicts("bf16", c, [300, 89, 37, 1], sinks=2, recent=3, outside=outside, keep=values != [1.5])
 
 
-@pytest.mark.parametrize("n,budget", [(5000, 2500), (9001, 8999), (20000, 77), (40000, 30000), (70000, 35000)])
+@pytest.mark.parametrize("n,budget", [(1100, 600), (3000, 1200), (5000, 2500), (9001, 8999), (20000, 77), (40000, 30000), (70000, 35000)])
 @pytest.mark.parametrize("outside", [False, True])
 def test_evict_long_sequences(n, budget, outside):
     c = ref.make("bf16", [n, n // 3], 2, 64, 64, weights=True, sizes="whole", seed=29)

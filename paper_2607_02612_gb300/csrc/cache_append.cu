@@ -52,6 +52,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams 
     // `side` rows side by side, a thread has the same chunk (of `width` threads' chunks) of kPer rows of the CTA
     const int width = min(row_chunks, kThreads), side = kThreads / width, r_mine = tid / width;
     const int r0 = blockIdx.x * side * kPer, r1 = rows_ok && r_mine < side ? min(n, r0 + side * kPer) : r0;
+    // (plain loads: the kernel before may still write the rows while this one is resident, which the read-only path does not allow)
     uint4 k[kPer], v[kPer];
     auto load = [&](int ch) {
         const unsigned char *ks = p.k + (size_t)(o0 + r0 + r_mine) * p.k_stride + (size_t)ch * 16;
@@ -59,8 +60,8 @@ __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams 
 #pragma unroll
         for (int x = 0; x < kPer; ++x)
             if (r0 + r_mine + x * side < r1) {
-                k[x] = ldg16(ks + (size_t)(x * side) * p.k_stride);
-                v[x] = ldg16(vs + (size_t)(x * side) * p.v_stride);
+                k[x] = *reinterpret_cast<const uint4 *>(ks + (size_t)(x * side) * p.k_stride);
+                v[x] = *reinterpret_cast<const uint4 *>(vs + (size_t)(x * side) * p.v_stride);
             }
     };
     load(tid % width);

@@ -3,6 +3,7 @@ checks; and the reference that the GPU tests compare with, against itself (no GP
 import itertools
 import math
 import os
+import re
 import sys
 
 import pytest
@@ -174,3 +175,22 @@ def test_reference_attention_of_merged_tokens():
     assert torch.allclose(a, b, rtol=1e-12, atol=1e-14)
     assert torch.allclose(wa[at], torch.zeros(6, dtype=torch.float64).index_add_(0, rep, wb[to]), rtol=1e-12, atol=1e-14)
     assert abs(float(wb[to].sum()) - 3.0) < 1e-12     # the heads' probabilities
+
+
+# ---- the sources -----------------------------------------------------------------------------------------------------
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2607_02612_gb300", "csrc")
+
+
+def source(name):
+    """A source without its comments."""
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+
+
+@pytest.mark.parametrize("name", ["cache.cuh", "cache_append.cu", "cache_attn.cu", "cache_attn_bf16.cu", "cache_evict.cu", "cache_rounds.cuh"])
+def test_no_read_only_loads_in_kernels_that_start_early(name):
+    """The kernels of the cache calls are resident while the kernel before them still runs, so nothing that they read is
+    read-only for as long as they live, which the non-coherent path asks for."""
+    text = source(name)
+    assert len(text) > 1000, "the sources moved"
+    found = re.findall(r"\bldg16\(|\b__ldg\(|\.nc\b|__restrict__", text)
+    assert not found, found

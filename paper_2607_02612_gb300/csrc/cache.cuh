@@ -20,20 +20,27 @@ struct Cache {
     const int *lengths;
 };
 
+// An entry of the page table or a length; kEarly: past the L1 cache (wait_for_previous).
+template <bool kEarly> __device__ __forceinline__ int cache_entry(const int *p) { return kEarly ? __ldcg(p) : *p; }
 // The page that holds position pos of sequence b; false when its id is out of range.
+template <bool kEarly = false>
 __device__ __forceinline__ bool cache_page(const Cache &c, int b, int pos, unsigned &page) {
-    page = (unsigned)c.table[(size_t)b * c.max_pages + (pos >> c.shift)];
+    page = (unsigned)cache_entry<kEarly>(&c.table[(size_t)b * c.max_pages + (pos >> c.shift)]);
     return page < c.num_pages;
 }
 // Length of sequence b, or -1 when it is out of range.
+template <bool kEarly = false>
 __device__ __forceinline__ int cache_length(const Cache &c, int b) {
-    const int n = c.lengths[b];
+    const int n = cache_entry<kEarly>(&c.lengths[b]);
     return n >= 0 && n <= c.capacity ? n : -1;
 }
 
 // Every kernel of the cache calls is a programmatic dependent of the one before it on the stream: it is launched while that one
 // still runs, and waits for its end (and its writes) before it touches memory that a kernel may have written.  All of a kernel's
-// CTAs wait, also those without work, so that its end implies the end of the ones before it.
+// CTAs wait, also those without work, so that its end implies the end of the ones before it.  k_cache_weights alone reads something
+// before its wait, lengths and pages: it starts when the attention kernel's CTAs have all waited, so the kernels that wrote those
+// have ended and their writes are in the L2 cache, but only the wait would make an SM forget older lines in its L1: it reads them
+// past the L1 (the attention kernel does not, whose pages' other entries the L1 keeps: 16 x 577 float32 19.4 us, past it 20.9).
 __device__ __forceinline__ void wait_for_previous() {
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");

@@ -56,7 +56,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
     wait_for_previous();
     Run run;
     Place at;
-    if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
+    if (!find_run<kThreads, true, false>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
         empty_sequences<float, kThreads>(p);
         return;
     }
@@ -369,16 +369,16 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
     const Cache &c = p.c;
     Run run;
     Place at;
-    const bool works = find_run<kWeightThreads, false>(p, finder, kWeightTile, 1, 1, 1u, run, at);
+    const bool works = find_run<kWeightThreads, false, true>(p, finder, kWeightTile, 1, 1, 1u, run, at);
     // the token that this thread updates, and its place in its page (-1: none)
     int j0 = 0, place = -1;
     unsigned page = 0;
     auto look_up = [&]() {
         j0 = at.u * kWeightTile;
         const int j = j0 + tid, pos = p.window && j >= p.sinks ? j + at.n - at.vis : j;
-        place = tid < kWeightTile && j < at.vis && cache_page(c, at.b, pos, page) ? pos & ((1 << c.shift) - 1) : -1;
+        place = tid < kWeightTile && j < at.vis && cache_page<true>(c, at.b, pos, page) ? pos & ((1 << c.shift) - 1) : -1;
     };
-    // (lengths and pages are complete: the attention kernel let this one start after it had waited for the kernels before)
+    // (lengths and pages are complete in the L2 cache, from where they are read: wait_for_previous)
     if (works) look_up();
     wait_for_previous();
     for (unsigned r = run.r0; works && r < run.r1; ++r) {

@@ -65,7 +65,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
     wait_for_previous();
     Run run;
     Place at;
-    if (!find_run<kThreads, true>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
+    if (!find_run<kThreads, true, false>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
         empty_sequences<__nv_bfloat16, kThreads>(p);
         return;
     }

@@ -37,12 +37,14 @@ struct Place {
     int b, h, ch, u;       // sequence, key head, chunk of its query heads, round
     int n, vis, rounds;    // length, visible tokens, rounds of one key head
 };
+template <bool kEarly = false>
 __device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens, int b) {
     s.b = b;
-    s.n = max(cache_length(p.c, b), 0);
+    s.n = max(cache_length<kEarly>(p.c, b), 0);
     s.vis = visible(p, s.n);
     s.rounds = (s.vis + tokens - 1) / tokens;
 }
+template <bool kEarly = false>
 __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, int tokens, int heads, int chunks) {
     if (++s.u < s.rounds) return;
     s.u = 0;
@@ -55,7 +57,7 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
             s.rounds = s.vis = 0;
             return;
         }
-        place_sequence(p, s, tokens, s.b);
+        place_sequence<kEarly>(p, s, tokens, s.b);
     } while (s.rounds == 0);
 }
 
@@ -99,8 +101,8 @@ struct Finder {
 // This CTA's run and the place where it begins; false: it has none.  Every thread counts the rounds of a few sequences, the
 // warps' sums go through shared memory, and the thread whose sequences hold a boundary looks it up (one barrier before and
 // one after: 2.2 us with 64-bit scans by one thread, 1.2 now, 0.7 of them the reading of the lengths).  min_rounds: of a run.
-// SNAP: the boundaries move to ends of (sequence, key head)s.
-template <int THREADS, bool SNAP>
+// SNAP: the boundaries move to ends of (sequence, key head)s.  kEarly: called before the kernel's wait.
+template <int THREADS, bool SNAP, bool kEarly>
 __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREADS> &s, int tokens, int heads, int chunks, unsigned min_rounds,
                                          Run &run, Place &at) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -108,7 +110,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
     const int per = ceil_div(p.c.max_batch, THREADS), b0 = min(tid * per, p.c.max_batch), b1 = min(b0 + per, p.c.max_batch);
     unsigned mine = 0;
     for (int b = b0; b < b1; ++b) {
-        place_sequence(p, at, tokens, b);
+        place_sequence<kEarly>(p, at, tokens, b);
         mine += (unsigned)at.rounds * vheads;
     }
     const unsigned sum = __reduce_add_sync(0xFFFFFFFFu, mine);
@@ -139,7 +141,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
         unsigned rem = x - base - (incl - mine);   // rounds of this thread's sequences before x (if it is one of theirs)
         if (x - base >= incl - mine && rem < mine) {
             for (int b = b0; b < b1; ++b) {
-                if (per > 1) place_sequence(p, at, tokens, b);
+                if (per > 1) place_sequence<kEarly>(p, at, tokens, b);
                 if (rem < (unsigned)at.rounds * vheads) break;
                 rem -= (unsigned)at.rounds * vheads;
             }
@@ -160,7 +162,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
         if (moved < 0) at.u = 0;
         if (moved > 0) {
             at.u = at.rounds - 1;
-            place_next(p, at, tokens, heads, chunks);
+            place_next<kEarly>(p, at, tokens, heads, chunks);
         }
     }
     return true;

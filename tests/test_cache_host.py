@@ -194,3 +194,17 @@ def test_no_read_only_loads_in_kernels_that_start_early(name):
     assert len(text) > 1000, "the sources moved"
     found = re.findall(r"\bldg16\(|\b__ldg\(|\.nc\b|__restrict__", text)
     assert not found, found
+
+
+def test_what_is_read_before_the_wait_is_read_past_the_l1_cache():
+    """The weights' kernel looks its tokens up before its wait, which alone makes an SM forget older lines in its L1."""
+    shared = source("cache.cuh")
+    assert re.search(r"cache_entry\(const int \*p\) \{ return kEarly \? __ldcg\(p\) : \*p; \}", shared)
+    for name, what in (("cache_page", "table"), ("cache_length", "lengths")):
+        body = re.search(rf"\b{name}\(.*?\n}}\n", shared, re.S).group(0)
+        assert f"cache_entry<kEarly>(&c.{what}[" in body and body.count(f"c.{what}[") == 1, body
+    kernel = re.search(r"\bk_cache_weights\(.*?wait_for_previous\(\)", source("cache_attn.cu"), re.S).group(0)
+    assert re.search(r"find_run<\w+, \w+, true>\(", kernel) and "cache_page<true>(" in kernel
+    assert not re.search(r"c\.(table|lengths|weights|sizes)\[|p\.(logits|lse)\b|cache_(page|length)\(", kernel), kernel
+    run = re.search(r"\bfind_run\(.*?\n}\n", source("cache_rounds.cuh"), re.S).group(0)
+    assert not re.search(r"c\.(table|lengths)\[|\b(place_sequence|place_next|cache_page|cache_length)\(", run), run

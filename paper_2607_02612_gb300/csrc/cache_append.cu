@@ -11,6 +11,7 @@ namespace fz {
 namespace {
 
 constexpr int kThreads = 256, kPer = 4;
+constexpr int kMostY = 65535;   // of a grid's height
 
 // Whether sample i's slot is named by another sample too (all threads; the batch's ids are few).
 __device__ bool named_twice(const Ragged &in, int B, int i, int slot) {
@@ -20,26 +21,30 @@ __device__ bool named_twice(const Ragged &in, int B, int i, int slot) {
     return __syncthreads_or(twice);
 }
 
+// The lengths that no sample raises, where they go elsewhere (all threads; apart from the kernel, whose other CTAs fetch none of it).
+__device__ __noinline__ void copy_other_lengths(const CacheAppendParams &p, int B) {
+    __shared__ unsigned named[(FUSION_CACHE_MAX_BATCH + 32) / 32];
+    const int tid = threadIdx.x, slots = p.c.max_batch;
+    for (int w = tid; w < (slots + 31) / 32; w += kThreads) named[w] = 0u;
+    __syncthreads();
+    for (int j = tid; j < B; j += kThreads) {
+        const int s = p.in.ids ? p.in.ids[j] : j;
+        if (s >= 0 && s < slots) atomicOr(&named[s >> 5], 1u << (s & 31));
+    }
+    __syncthreads();
+    for (int s = tid; s < slots; s += kThreads)
+        if (!(named[s >> 5] >> (s & 31) & 1u)) p.lengths_out[s] = p.c.lengths[s];
+}
+
+// A row of CTAs per sample, and one more for the lengths while the grid has room for it.
 __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams p, int row_chunks, int head_chunks) {
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
     const int B = device_batch(p.in);
-    if (i == p.in.max_batch) {   // the lengths that no sample raises, where they go elsewhere
-        if (blockIdx.x > 0) return;
-        __shared__ unsigned named[2048];
+    if (i == (int)gridDim.y - 1 && blockIdx.x == 0) {   // (with kMostY samples the last sample's first CTA too)
         if (B < 0 && tid == 0) raise_status(p.status, FUSION_DEV_BAD_BATCH);
-        if (p.in_place) return;
-        for (int w = tid; w < 2048; w += kThreads) named[w] = 0u;
-        __syncthreads();
-        for (int j = tid; j < B; j += kThreads) {
-            const int s = p.in.ids ? p.in.ids[j] : j;
-            if (s >= 0 && s < c.max_batch) atomicOr(&named[s >> 5], 1u << (s & 31));
-        }
-        __syncthreads();
-        for (int s = tid; s < c.max_batch; s += kThreads)
-            if (!(named[s >> 5] >> (s & 31) & 1u)) p.lengths_out[s] = c.lengths[s];
-        return;
+        if (!p.in_place) copy_other_lengths(p, B);
     }
     if (B < 0 || i >= B) return;
     const int slot = p.in.ids ? p.in.ids[i] : i;
@@ -129,8 +134,9 @@ cudaError_t launch_cache_append(int dtype, const CacheAppendParams &p, cudaStrea
     // (samples of more rows than the cache has room for, or than there are, write nothing)
     long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
     if (most > p.in.max_rows) most = p.in.max_rows;
-    return launch_after(k_cache_append, dim3((unsigned)(most > 0 ? (most + rows - 1) / rows : 1), (unsigned)p.in.max_batch + 1), kThreads, 0, 1, s,
-                        p, row_chunks, head_chunks);
+    static_assert(FUSION_CACHE_MAX_BATCH <= kMostY, "a row of CTAs per sample");
+    const dim3 grid((unsigned)(most > 0 ? (most + rows - 1) / rows : 1), (unsigned)(p.in.max_batch < kMostY ? p.in.max_batch + 1 : kMostY));
+    return launch_after(k_cache_append, grid, kThreads, 0, 1, s, p, row_chunks, head_chunks);
 }
 
 }  // namespace fz

@@ -620,3 +620,41 @@ def test_a_decoder_over_a_compacted_batch(dtype):
             c["lengths"], _ = ref.evict(c, [20] * b.batch, sinks=1, recent=4)
             same(dc, c)
     assert status(f) == 0
+
+
+# ---- bounds ----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_batch(dtype):
+    """FUSION_CACHE_MAX_BATCH sequences, and one fewer: a row each in place and with the lengths elsewhere, by ids in
+    another order with the last sample left out, attention of one token (its value), eviction of every other one."""
+    for batch in (fz.FUSION_CACHE_MAX_BATCH, fz.FUSION_CACHE_MAX_BATCH - 1):
+        g = torch.Generator(device=DEV).manual_seed(50)
+        dc, f = runner.device_cache(dtype, batch, 2, 1, 1, 8, page_tokens=1, weights=True), runner.Fusion(1)
+        k, v = (torch.randn((batch, 8), generator=g, device=DEV).to(ref.TYPES[dtype]) for _ in range(2))
+        out = torch.full((batch,), -7, dtype=torch.int32, device=DEV)
+        f.cache_append(dc, k, v, lengths_out=out)
+        assert status(f) == 0 and (out == 1).all() and (dc.lengths == 0).all()
+        assert torch.equal(dc.k[::2, 0, 0], k) and torch.equal(dc.v[::2, 0, 0], v)
+        ids = torch.randperm(batch, generator=g, device=DEV).to(torch.int32)
+        last = int(ids[-1])
+        rows = runner.RaggedRows(batch, 1, batch, torch.arange(batch + 1, dtype=torch.int32, device=DEV),
+                                 torch.tensor([batch - 1], dtype=torch.int32, device=DEV), ids)
+        out.fill_(-7)
+        f.cache_append(dc, k, v, rows, lengths_out=out)
+        want = torch.ones_like(out)
+        want[last] = 0
+        assert status(f) == 0 and torch.equal(out, want) and (dc.lengths == 0).all()
+        f.cache_append(dc, k, v, rows)
+        assert status(f) == 0 and torch.equal(dc.lengths, want)
+        held = ids[:-1].long()
+        assert torch.equal(dc.k[::2, 0, 0][held], k[:-1]) and torch.equal(dc.v[::2, 0, 0][held], v[:-1])
+        got = f.cache_attention(dc, k.view(batch, 1, 8))
+        assert status(f) == 0 and torch.equal(got[held, 0], v[:-1]) and (got[last] == 0).all()
+        assert (dc.weights[::2, 0][held] == 1).all()
+        f.cache_evict(dc, (torch.arange(batch, device=DEV) % 2).to(torch.int32))
+        want[::2] = 0
+        assert status(f) == 0 and torch.equal(dc.lengths, want)
+        assert int(dc.workspace[:1 << 18].max()) == 0
+        rows = runner.RaggedRows(batch, 1, batch, rows.offsets, torch.tensor([batch + 1], dtype=torch.int32, device=DEV), ids)
+        f.cache_append(dc, k, v, rows)
+        assert status(f) == fz.FUSION_DEV_BAD_BATCH and torch.equal(dc.lengths, want)

@@ -96,7 +96,7 @@ struct CacheAttnParams {
     long long q_stride;    // elements between the sequences' queries
     int heads, group;      // group: query heads of a key head
     float scale2;          // scale * log2(e)
-    int window, sinks;     // window 0: every token is visible
+    int window, sinks;     // set_visible; window 0: every token is visible
     int most;              // visible tokens of a sequence, at most
     void *out;
     float *lse;            // [max_batch, heads] base 2
@@ -107,6 +107,18 @@ struct CacheAttnParams {
     int *counters;
     int *status;
 };
+// The caller's window and sinks (any numbers from 0) over p.c.capacity positions.  A window over all of them is none, and sinks
+// beyond the positions that a window leaves say nothing more, so their sum is at most the capacity (2^30) and cannot overflow.
+inline void set_visible(CacheAttnParams &p, int window, int sinks) {
+    const int capacity = p.c.capacity;
+    p.window = window < capacity ? window : 0;
+    p.sinks = sinks < capacity - p.window ? sinks : capacity - p.window;
+    p.most = p.window ? p.window + p.sinks : capacity;
+}
+// Visible tokens of a sequence of n tokens: the j-th is position j (j < sinks) or j + n - visible.
+__host__ __device__ __forceinline__ int visible(const CacheAttnParams &p, int n) {
+    return p.window ? min(n, p.window + p.sinks) : n;
+}
 cudaError_t launch_cache_attention_bf16(const CacheAttnParams &p, cudaStream_t s);   // without the weights
 cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStream_t s);
 

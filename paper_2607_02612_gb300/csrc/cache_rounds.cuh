@@ -27,11 +27,6 @@ __device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void *src, 
 }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Visible tokens of a sequence of n tokens: the j-th is position j (j < sinks) or j + n - visible.
-__device__ __forceinline__ int visible(const CacheAttnParams &p, int n) {
-    return p.window ? min(n, p.window + p.sinks) : n;
-}
-
 // Where in the batch a round lies.
 struct Place {
     int b, h, ch, u;       // sequence, key head, chunk of its query heads, round

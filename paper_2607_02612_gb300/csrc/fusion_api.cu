@@ -875,10 +875,7 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
     p.heads = heads;
     p.group = heads / cache.kv_heads;
     p.scale2 = scale * 1.4426950408889634f;   // log2(e)
-    const int capacity = p.c.capacity;
-    p.window = window < capacity ? window : capacity;   // (their sum stays below 2^31)
-    p.sinks = sinks < capacity ? sinks : capacity;
-    p.most = p.window && p.window + p.sinks < capacity ? p.window + p.sinks : capacity;
+    set_visible(p, window, sinks);
     p.out = out;
     p.lse = reinterpret_cast<float *>(wb + L.lse);
     p.part_ml = reinterpret_cast<float2 *>(wb + L.part_ml);

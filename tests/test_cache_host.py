@@ -1,9 +1,11 @@
 """The key-value cache calls on the host: what they refuse before anything is enqueued, the workspace's size, the runner's
 checks; and the reference that the GPU tests compare with, against itself (no GPU needed)."""
+import importlib
 import itertools
 import math
 import os
 import re
+import subprocess
 import sys
 
 import pytest
@@ -208,3 +210,39 @@ def test_what_is_read_before_the_wait_is_read_past_the_l1_cache():
     assert not re.search(r"c\.(table|lengths|weights|sizes)\[|p\.(logits|lse)\b|cache_(page|length)\(", kernel), kernel
     run = re.search(r"\bfind_run\(.*?\n}\n", source("cache_rounds.cuh"), re.S).group(0)
     assert not re.search(r"c\.(table|lengths)\[|\b(place_sequence|place_next|cache_page|cache_length)\(", run), run
+
+
+# ---- arithmetic on the host ------------------------------------------------------------------------------------------
+VISIBLE = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "cache.cuh"
+int main(int argc, char **argv) {   // capacity window sinks length -> most, visible
+    for (int k = 1; k + 3 < argc; k += 4) {
+        fz::CacheAttnParams p{};
+        p.c.capacity = atoi(argv[k]);
+        fz::set_visible(p, atoi(argv[k + 1]), atoi(argv[k + 2]));
+        printf("%d %d %d\n", p.most, fz::visible(p, atoi(argv[k + 3])), p.sinks);
+    }
+}
+"""
+
+
+def test_visible_tokens(tmp_path):
+    """Windows and sinks of any size against capacities up to the largest, in whole numbers without bounds."""
+    B = importlib.import_module("paper_2607_02612_gb300.build")
+    (tmp_path / "v.cu").write_text(VISIBLE)
+    subprocess.run([B._nvcc(), *B.ARCH, "-std=c++17", f"-I{B.INCLUDE}", f"-I{B.CSRC}", "-o", str(tmp_path / "v"), str(tmp_path / "v.cu")],
+                   check=True, capture_output=True)
+    cases = []
+    for cap in (1, 2, 1024, (1 << 30) - 1, 1 << 30):
+        some = sorted({0, 1, 2, 5, cap // 2, cap - 1, cap, cap + 1, (1 << 30) - 1, 1 << 30, (1 << 31) - 1})
+        cases += [(cap, w, s, n) for w in some for s in some for n in {0, 1, 3, cap // 2, cap - 1, cap} if n <= cap]
+    for k in range(0, len(cases), 1000):
+        part = cases[k:k + 1000]
+        out = subprocess.run([str(tmp_path / "v"), *[str(x) for c in part for x in c]], check=True, capture_output=True, text=True)
+        for (cap, w, s, n), line in zip(part, out.stdout.splitlines(), strict=True):
+            most, seen, sinks = map(int, line.split())
+            want = min(n, w + s) if w else n
+            assert seen == want and want <= most <= cap and 0 <= sinks <= cap, (cap, w, s, n, line)
+            assert w == 0 or w >= cap or sinks >= min(s, n - w), (cap, w, s, n, line)   # (the places of those that are visible)

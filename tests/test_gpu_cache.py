@@ -658,3 +658,24 @@ def test_the_largest_batch(dtype):
         rows = runner.RaggedRows(batch, 1, batch, rows.offsets, torch.tensor([batch + 1], dtype=torch.int32, device=DEV), ids)
         f.cache_append(dc, k, v, rows)
         assert status(f) == fz.FUSION_DEV_BAD_BATCH and torch.equal(dc.lengths, want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_capacity(dtype):
+    """A page table with room for 2^30 tokens (of which a few pages are there): windows and sinks of everything, an append,
+    an eviction."""
+    c = ref.make(dtype, [1500], 1, 8, 1024, room=500, weights=True, seed=51)
+    table = torch.full((1, 1 << 20), -1, dtype=torch.int32)
+    table[:, :2] = c["table"]
+    c["table"] = table
+    for window, sinks in ((2 ** 31 - 1, 2 ** 31 - 1), (2 ** 30, 0), (2 ** 30 - 1, 2 ** 31 - 1), (700, 2 ** 31 - 1), (700, 9)):
+        _, dc = attend(dtype, c, 2, window=window, sinks=sinks)
+        c["weights"] = dc.weights.cpu()
+    f = runner.Fusion(1)
+    k, v = (torch.randn((1, 8), generator=torch.Generator().manual_seed(52)).to(ref.TYPES[dtype]) for _ in range(2))
+    f.cache_append(dc, k.to(DEV), v.to(DEV))
+    c["lengths"] = ref.append(c, k, v, [0, 1])
+    f.cache_evict(dc, torch.tensor([601], dtype=torch.int32, device=DEV), sinks=4, recent=2 ** 31 - 1)
+    c["lengths"], _ = ref.evict(c, [601], sinks=4, recent=2 ** 31 - 1)
+    assert status(f) == 0
+    same(dc, c)

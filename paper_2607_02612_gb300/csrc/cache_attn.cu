@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
                         if (!seg_bad)
                             store4(reinterpret_cast<float *>(p.out) + (head + q) * c.dim + d,
                                    ls == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
-                        if (d == 0 && p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+                        if (d == 0 && p.logits) p.lse[head + q] = log_sum(M, seg_bad ? -1.0f : ls);
                     } else {
                         *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
                         if (d == 0) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
@@ -385,7 +385,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
         if (r > run.r0) look_up();
         const bool here = place >= 0;
         float *dst = c.weights + ((size_t)page << c.shift) + place;
-        const float old = here ? *dst : 0.0f;
+        const float old = here ? *dst : 0.0f, first = p.lse[(size_t)at.b * p.heads];
         float4 w = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (j0 + 4 * lane < at.vis) {   // (up to three logits past the sequence are there, and not used)
             const float *x = p.logits + (size_t)at.b * p.heads * p.lstride + j0 + 4 * lane, *lse = p.lse + (size_t)at.b * p.heads;
@@ -405,7 +405,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
             float sum = part[0][tid];
 #pragma unroll
             for (int k = 1; k < kW; ++k) sum += part[k][tid];
-            *dst = old + sum;
+            if (first != kRefused) *dst = old + sum;   // (another sequence may hold a refused one's pages by now)
         }
         __syncthreads();
         place_next(p, at, kWeightTile, 1, 1);

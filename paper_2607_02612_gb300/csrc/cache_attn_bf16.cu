@@ -310,7 +310,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
                 const int e = x * kThreads + tid;
                 if (e < 4 * L::kTiles * nq && e % (4 * L::kTiles) == 0) {
                     if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
-                    else if (p.logits) p.lse[head + q] = seg_bad || ls == 0.0f ? INFINITY : M + log2f(ls);
+                    else if (p.logits) p.lse[head + q] = log_sum(M, seg_bad ? -1.0f : ls);
                 }
             }
 #pragma unroll

@@ -22,6 +22,12 @@ __device__ __forceinline__ float ex2(float x) {   // 2^x, one MUFU instruction (
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+// Log-sum-exp of a row (base 2) for the weights, of its maximum and sum.  No token with a part: +inf, so that 2^(x - lse) is 0 for
+// logits of -inf.  Sum below zero, a bad page: kRefused, which no row has otherwise, and the same in all rows of the sequence.
+constexpr float kRefused = -INFINITY;
+__device__ __forceinline__ float log_sum(float maximum, float sum) {
+    return sum < 0.0f ? kRefused : sum == 0.0f ? INFINITY : maximum + log2f(sum);
+}
 __device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void *src, bool read) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(read ? 16 : 0) : "memory");
 }
@@ -351,7 +357,7 @@ __device__ __forceinline__ void join_results(const CacheAttnParams &p, int c0, i
     if (tid < nq) {
         const float l = sums[tid];
         if (!last) p.part_ml[slot(0) * NQ + tid] = make_float2(maxima[tid], l);
-        else if (p.logits) p.lse[head + tid] = l <= 0.0f ? INFINITY : maxima[tid] + log2f(l);
+        else if (p.logits) p.lse[head + tid] = log_sum(maxima[tid], l);
     }
 }
 

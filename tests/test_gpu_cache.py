@@ -679,3 +679,37 @@ def test_the_largest_capacity(dtype):
     c["lengths"], _ = ref.evict(c, [601], sinks=4, recent=2 ** 31 - 1)
     assert status(f) == 0
     same(dc, c)
+
+
+# ---- sequences that are left out -------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lengths", [[600, 70, 300], [40] * 260])
+def test_attention_leaves_the_weights_of_a_refused_sequence(dtype, lengths):
+    """A bad page, and a NaN or an infinity among the sequence's queries or keys, whose logits are no numbers: its weights
+    keep their bits, -0 among them, and so does every page that it names and another sequence holds."""
+    for what in ("query", "infinite query", "key", "infinite key"):
+        c = ref.make(dtype, lengths, 2, 64, 16, room=16, weights=True, seed=53)
+        good = ref.copy(c)
+        at0 = ref.places(c, 0, torch.arange(lengths[0]))
+        c["weights"][at0[0][::2], at0[1][::2]] = -0.0
+        q = torch.randn((len(lengths), 4, 64), generator=torch.Generator().manual_seed(54)).to(ref.TYPES[dtype])
+        value = math.inf if "infinite" in what else math.nan
+        if "query" in what:
+            q[0, 1:3, 7] = value
+        else:
+            c["k"][at0[0][5:9], :, at0[1][5:9], 3] = value
+        held = c["weights"].clone()
+        c["table"][0, 2] = -1                       # position 32 on
+        c["table"][0, 1] = c["table"][2, 0]         # the third sequence's by now
+        dc, f = on_device(dtype, c, 4), runner.Fusion(len(lengths))
+        out = torch.full((len(lengths), 4, 64), 7.0, dtype=ref.TYPES[dtype], device=DEV)
+        f.cache_attention(dc, q.to(DEV), out=out)
+        assert status(f) == fz.FUSION_DEV_BAD_CACHE, what
+        assert (out[0] == 7.0).all()
+        good["k"], good["lengths"][0] = c["k"], 0
+        want, tol, w, wtol = ref.attention(good, torch.nan_to_num(q), dtype)
+        got, gw = out.cpu().double(), dc.weights.cpu()
+        assert torch.equal(ref.bits(gw[at0]), ref.bits(held[at0])), what
+        for b in range(1, len(lengths)):
+            at = ref.places(good, b, torch.arange(lengths[b]))
+            assert ((got[b] - want[b]).abs() <= tol[b]).all() and ((gw[at].double() - w[at]).abs() <= wtol[at]).all(), (what, b)

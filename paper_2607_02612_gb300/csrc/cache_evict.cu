@@ -291,7 +291,8 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
         keep[i] = slot;
         if (i < idx_n) idx[i] = j;
     };
-    int evicted = n;   // the first position that goes
+    // the first position that goes (where no weight is compared the first between, whatever its weight: a NaN of all ones has the key 0)
+    int evicted = choose && want == 0 ? lo : n;
     const unsigned lt = (1u << lane) - 1u;
     na += first;
     each([&](unsigned o, int j, unsigned slot) {

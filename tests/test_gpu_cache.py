@@ -713,3 +713,20 @@ def test_attention_leaves_the_weights_of_a_refused_sequence(dtype, lengths):
         for b in range(1, len(lengths)):
             at = ref.places(good, b, torch.arange(lengths[b]))
             assert ((got[b] - want[b]).abs() <= tol[b]).all() and ((gw[at].double() - w[at]).abs() <= wtol[at]).all(), (what, b)
+
+
+@pytest.mark.parametrize("n,dtype", [(70, "f32"), (3000, "bf16"), (9000, "bf16"), (150001, "bf16")])
+def test_evict_compares_nothing_whatever_the_weights_hold(n, dtype):
+    """Where the sinks and the recent tokens fill the budget, weights of any bits: NaN of all ones (memory that nobody has
+    written), of either sign, infinities; and a budget of nothing."""
+    for word in (-1, 0x7FFFFFFF, -0x800000, 0x7F800000, 0):
+        c = ref.make(dtype, [n, 60, 45], 1, 8, 16, weights=True, seed=55)
+        c["weights"] = torch.full(c["weights"].shape, word, dtype=torch.int32).view(torch.float32)
+        dc, f = on_device(dtype, c, 1), runner.Fusion(3)
+        f.cache_evict(dc, torch.tensor([n - 20, 0, 12], dtype=torch.int32, device=DEV), sinks=4, recent=n - 24)
+        assert status(f) == 0
+        for b, keep in ((0, [*range(4), *range(24, n)]), (1, []), (2, [*range(4), *range(37, 45)])):
+            src, dst = ref.places(c, b, torch.tensor(keep, dtype=torch.long)), ref.places(c, b, torch.arange(len(keep)))
+            for name in ("k", "v"):
+                c[name][dst[0], :, dst[1]] = c[name][src[0], :, src[1]]
+        same(dc, c, torch.tensor([n - 20, 0, 12], dtype=torch.int32))

@@ -482,7 +482,8 @@ size_t fusion_cache_workspace_size(fusion_cache cache, int32_t heads);
  * lengths_out may be the cache's own lengths.  (Apart from them, the rows are not yet part of the sequences: a caller can
  * take them back by keeping the old lengths.)
  * k, v: [in.max_rows, kv_heads, head_dim] with rows k_stride and v_stride elements apart (a packed projection's slices;
- * any stride >= 0 that keeps rows 16-byte aligned), 16-byte aligned.  in.max_tokens has no upper bound here.
+ * any stride >= 0 that keeps rows 16-byte aligned), 16-byte aligned; NULL where in.max_rows is 0.  in.max_tokens has no upper
+ * bound here.
  * Errors: FUSION_ERR_SHAPE for a cache shape out of range or in.max_batch > cache.max_batch; FUSION_ERR_INVALID_ARG for
  * NULL or misaligned pointers or strides; FUSION_ERR_WORKSPACE.  Device bits, each of which leaves that sample out (and its
  * sequence's length as it is): BAD_OFFSETS, BAD_IDS (an id outside [0, cache.max_batch), or two samples of one id), BAD_CACHE

@@ -830,7 +830,8 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
     if (!in.offsets) return FUSION_ERR_INVALID_ARG;
     if (in.max_batch < 0 || in.max_batch > cache.max_batch || in.max_tokens < 1) return FUSION_ERR_SHAPE;
     if (in.max_rows < 0 || in.max_rows > INT32_MAX) return FUSION_ERR_SHAPE;
-    if (!k || !v || !lengths_out || !aligned16(k) || !aligned16(v)) return FUSION_ERR_INVALID_ARG;
+    if (in.max_rows > 0 && (!k || !v)) return FUSION_ERR_INVALID_ARG;   // (no rows: an empty tensor has no address)
+    if (!lengths_out || !aligned16(k) || !aligned16(v)) return FUSION_ERR_INVALID_ARG;
     if (!good_stride(dtype, k_stride) || !good_stride(dtype, v_stride)) return FUSION_ERR_INVALID_ARG;
     FZ_TRY(check_cache_ws(workspace, workspace_bytes, align256(sizeof(int) * (size_t)kWsCounters)));
     const int es = dtype == FUSION_BF16 ? 2 : 4;

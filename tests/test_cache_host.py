@@ -246,3 +246,9 @@ def test_visible_tokens(tmp_path):
             want = min(n, w + s) if w else n
             assert seen == want and want <= most <= cap and 0 <= sinks <= cap, (cap, w, s, n, line)
             assert w == 0 or w >= cap or sinks >= min(s, n - w), (cap, w, s, n, line)   # (the places of those that are visible)
+
+
+def test_rows_may_be_missing_where_there_are_none():
+    for kw in (dict(k=None), dict(v=None)):
+        assert append(**kw) == fz.FUSION_ERR_INVALID_ARG
+        assert append(in_=fz.ragged(4, 10, 0, FAKE), workspace=None, **kw) == fz.FUSION_ERR_WORKSPACE   # (the next check)

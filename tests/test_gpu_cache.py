@@ -730,3 +730,22 @@ def test_evict_compares_nothing_whatever_the_weights_hold(n, dtype):
             for name in ("k", "v"):
                 c[name][dst[0], :, dst[1]] = c[name][src[0], :, src[1]]
         same(dc, c, torch.tensor([n - 20, 0, 12], dtype=torch.int32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_of_no_rows(dtype):
+    """Batches without rows, whose tensors have no address: samples of no tokens, and no samples; in place and elsewhere."""
+    c = ref.make(dtype, [5, 0, 17], 2, 16, 8, room=4, sizes="whole", weights=True, seed=56)
+    dc, f = on_device(dtype, c, 2), runner.Fusion(3)
+    none = torch.empty((0, 32), dtype=ref.TYPES[dtype], device=DEV)
+    per_row = torch.empty(0, device=DEV)
+    for batch in (3, 1, 0):
+        ids = torch.arange(batch, dtype=torch.int32, device=DEV).flip(0)
+        for rows in (runner.RaggedRows(batch, 1, 0, torch.zeros(batch + 1, dtype=torch.int32, device=DEV)),
+                     runner.RaggedRows(batch, 7, 0, torch.zeros(batch + 1, dtype=torch.int32, device=DEV), ids=ids)):
+            out = torch.full((3,), -7, dtype=torch.int32, device=DEV)
+            assert f.cache_append(dc, none, none, rows, sizes=per_row, scores=per_row, lengths_out=out) is out
+            assert out.tolist() == [5, 0, 17]
+            f.cache_append(dc, none.view(0, 2, 16), none, rows)
+    assert status(f) == 0
+    same(dc, c)

@@ -373,13 +373,15 @@ class Fusion:
                         sinks: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Attention of one new token per sequence, q [max_batch, heads, head_dim] (any stride between sequences), over
         the visible tokens of its cache; accumulates the weights where the cache keeps them.  scale None:
-        head_dim ** -0.5.  Returns [max_batch, heads, head_dim]."""
+        head_dim ** -0.5.  Returns [max_batch, heads, head_dim] (out, where it is given; rows behind the last sequence's stay)."""
         qp, qs = _rows_ptr(q, c.max_batch, c.heads, c.head_dim, c.torch_dtype, c.index, "queries")
         if out is None:
             out = torch.empty((c.max_batch, c.heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
             op = out.data_ptr()
         else:
-            op = _need(out, c.torch_dtype, c.index, "out", c.max_batch * c.heads * c.head_dim, 3)
+            op = _need(out, c.torch_dtype, c.index, "out", dim=3)
+            if out.shape[0] < c.max_batch or out.shape[1] != c.heads or out.shape[2] != c.head_dim:
+                raise fb.FusionError(f"out: [{c.max_batch}, {c.heads}, {c.head_dim}] expected")
         if c.max_batch == 0:
             return out
         _enqueue(c.lib.fusion_cache_attention, c.index, self.status, c.code, c.c_struct(), qp, qs, c.heads,

@@ -7,6 +7,7 @@ import os
 import re
 import subprocess
 import sys
+import types
 
 import pytest
 import torch
@@ -252,3 +253,21 @@ def test_rows_may_be_missing_where_there_are_none():
     for kw in (dict(k=None), dict(v=None)):
         assert append(**kw) == fz.FUSION_ERR_INVALID_ARG
         assert append(in_=fz.ragged(4, 10, 0, FAKE), workspace=None, **kw) == fz.FUSION_ERR_WORKSPACE   # (the next check)
+
+
+def stub_cache(**kw):
+    """What the runner's checks read of a cache, on the host; a call that passes them all reaches `call`."""
+    c = dict(max_batch=3, heads=4, kv_heads=2, head_dim=8, torch_dtype=torch.float32, index=-1, device=torch.device("cpu"), code=fz.FUSION_F32,
+             scale=1.0, _ws=FAKE, ws_bytes=1 << 20, c_struct=lambda: None, lengths=torch.zeros(3, dtype=torch.int32))
+    c.update(kw)
+    return types.SimpleNamespace(**c)
+
+
+def test_runner_refuses_outputs_of_another_shape():
+    c, q = stub_cache(max_batch=0), torch.zeros(0, 4, 8)
+    good = torch.zeros(0, 4, 8)
+    assert runner.Fusion.cache_attention(None, c, q, out=good) is good
+    c, q = stub_cache(), torch.zeros(3, 4, 8)
+    for shape in ((4, 3, 8), (8, 4, 3), (3, 8, 4), (2, 4, 8), (1, 12, 8), (96,), (3, 32), (3, 4, 8, 1), (2, 6, 8)):
+        with pytest.raises(fz.FusionError):
+            runner.Fusion.cache_attention(None, c, q, out=torch.zeros(shape))

@@ -359,7 +359,10 @@ class Fusion:
         o = lengths_out if lengths_out is not None else c.lengths
         if c.max_batch == 0:
             return o
-        rows = rows if rows is not None else c.one_row_each()
+        if rows is None:
+            rows = c.one_row_each()
+        elif any(t is not None and t.get_device() != c.index for t in (rows.offsets, rows.batch, rows.ids)):
+            raise fb.FusionError(f"the rows' offsets, count and ids on the cache's device ({c.index}) expected")
         kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "keys")
         vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "values")
         zp = _need(sizes, torch.float32, c.index, "sizes", rows.max_rows)

@@ -271,3 +271,14 @@ def test_runner_refuses_outputs_of_another_shape():
     for shape in ((4, 3, 8), (8, 4, 3), (3, 8, 4), (2, 4, 8), (1, 12, 8), (96,), (3, 32), (3, 4, 8, 1), (2, 6, 8)):
         with pytest.raises(fz.FusionError):
             runner.Fusion.cache_attention(None, c, q, out=torch.zeros(shape))
+
+
+def test_runner_refuses_rows_described_on_another_device():
+    """A batch whose offsets, count or ids lie on another device than the cache (here: stand-ins that say so)."""
+    elsewhere, here = types.SimpleNamespace(get_device=lambda: 1), types.SimpleNamespace(get_device=lambda: -1)
+    t = torch.zeros(3, 16)
+    for where in ("offsets", "batch", "ids"):
+        rows = types.SimpleNamespace(max_batch=3, max_tokens=1, max_rows=3, offsets=here, batch=None, ids=None, ragged=lambda: None)
+        setattr(rows, where, elsewhere)
+        with pytest.raises(fz.FusionError):
+            runner.Fusion.cache_append(None, stub_cache(), t, t, rows)

@@ -139,6 +139,13 @@ def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str,
     return t.data_ptr()
 
 
+def _tokens(n: int, what: str) -> int:
+    """A number of tokens for the C ABI; one that its 32 bits do not hold is more than any cache has, and means all."""
+    if n < 0:
+        raise fb.FusionError(f"{what}: a number >= 0 expected")
+    return n if n < 1 << 31 else (1 << 31) - 1
+
+
 @dataclass
 class DeviceCache:
     """A paged key-value cache on the device (fusion_cache) with the scratch of its calls, which also fixes the number
@@ -388,7 +395,7 @@ class Fusion:
         if c.max_batch == 0:
             return out
         _enqueue(c.lib.fusion_cache_attention, c.index, self.status, c.code, c.c_struct(), qp, qs, c.heads,
-                 c.scale if scale is None else scale, window, sinks, op, c._ws, c.ws_bytes)
+                 c.scale if scale is None else scale, _tokens(window, "window"), _tokens(sinks, "sinks"), op, c._ws, c.ws_bytes)
         return out
 
     def cache_evict(self, c: DeviceCache, budget: torch.Tensor, *, sinks: int = 0, recent: int = 0,
@@ -406,9 +413,9 @@ class Fusion:
         for t, what in ((page_table_out, "page_table_out"), (keep_idx, "keep_idx")):
             if t is not None and t.shape[0] < c.max_batch:
                 raise fb.FusionError(f"{what}: a row per sequence expected")
-        _enqueue(c.lib.fusion_cache_evict, c.index, self.status, c.code, c.c_struct(), bp, sinks, recent, tp,
-                 page_table_out.shape[1] if tp is not None else 0, op, kp, keep_idx.shape[1] if kp is not None else 0, c._ws,
-                 c.ws_bytes)
+        _enqueue(c.lib.fusion_cache_evict, c.index, self.status, c.code, c.c_struct(), bp, _tokens(sinks, "sinks"),
+                 _tokens(recent, "recent"), tp, page_table_out.shape[1] if tp is not None else 0, op, kp,
+                 keep_idx.shape[1] if kp is not None else 0, c._ws, c.ws_bytes)
         return o
 
     def exit_check(self, b: DeviceBatch, head: HeadTensors) -> Dict[str, torch.Tensor]:

@@ -282,3 +282,24 @@ def test_runner_refuses_rows_described_on_another_device():
         setattr(rows, where, elsewhere)
         with pytest.raises(fz.FusionError):
             runner.Fusion.cache_append(None, stub_cache(), t, t, rows)
+
+
+def test_runner_passes_numbers_of_tokens_of_any_size(monkeypatch):
+    """Numbers beyond 32 bits mean all tokens (their low bits reached the call), negative ones are refused."""
+    seen = []
+    monkeypatch.setattr(runner, "_enqueue", lambda call, device, status, *args: seen.append(args))
+    c = stub_cache(lib=types.SimpleNamespace(fusion_cache_attention=None, fusion_cache_evict=None))
+    f = types.SimpleNamespace(status=None)
+    q, budget, most = torch.zeros(3, 4, 8), torch.zeros(3, dtype=torch.int32), 2 ** 31 - 1
+    for n, want in ((0, 0), (7, 7), (most, most), (1 << 31, most), ((1 << 32) + 5, most), (sys.maxsize, most), (1 << 70, most)):
+        runner.Fusion.cache_attention(f, c, q, window=n, sinks=n)
+        assert seen[-1][6:8] == (want, want)
+        runner.Fusion.cache_evict(f, c, budget, sinks=n, recent=n)
+        assert seen[-1][3:5] == (want, want)
+    for n in (-1, -(1 << 32)):
+        for kw in (dict(window=n), dict(sinks=n)):
+            with pytest.raises(fz.FusionError):
+                runner.Fusion.cache_attention(f, c, q, **kw)
+        for kw in (dict(recent=n), dict(sinks=n)):
+            with pytest.raises(fz.FusionError):
+                runner.Fusion.cache_evict(f, c, budget, **kw)

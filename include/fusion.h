@@ -503,8 +503,9 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
  * weights_j += sum_a softmax_j(x_a) for the visible tokens, summed in float32 in an order that depends on nothing but heads.
  * q: [max_batch, heads, head_dim], dtype, sequences q_stride elements apart (>= 0, rows 16-byte aligned), 16-byte aligned;
  * out: [max_batch, heads, head_dim], dtype, 16-byte aligned.  heads: a multiple of kv_heads, at most
- * FUSION_CACHE_MAX_HEADS, with max_batch * heads * max_pages * page_tokens <= 2^36.  scale: finite.  window, sinks: >= 0.  Logits, sums and the output are accumulated in float32; in
- * bf16 a probability enters the second product as two bf16 terms, within 2^-16 of itself.  out does not overlap q.
+ * FUSION_CACHE_MAX_HEADS, with max_batch * heads * max_pages * page_tokens <= 2^36.  scale: finite, also times log2(e).
+ * window, sinks: >= 0.  Logits, sums and the output are accumulated in float32; in bf16 a probability enters the second
+ * product as two bf16 terms, within 2^-16 of itself.  out does not overlap q.
  * Errors: FUSION_ERR_SHAPE, FUSION_ERR_INVALID_ARG, FUSION_ERR_WORKSPACE; device bit BAD_CACHE (a length out of range, or the
  * page id of a visible token: that sequence is not written).
  */

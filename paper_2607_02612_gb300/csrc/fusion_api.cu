@@ -865,7 +865,8 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
     FZ_TRY(check_heads(cache, heads));
     FZ_TRY(check_cache_pointers(cache));
     if (!q || !out || !aligned16(q) || !aligned16(out) || !good_stride(dtype, q_stride)) return FUSION_ERR_INVALID_ARG;
-    if (!std::isfinite(scale) || window < 0 || sinks < 0) return FUSION_ERR_INVALID_ARG;
+    const float scale2 = scale * 1.4426950408889634f;   // log2(e): logits are in base 2
+    if (!std::isfinite(scale2) || window < 0 || sinks < 0) return FUSION_ERR_INVALID_ARG;
     const CacheWs L = cache_ws(cache, heads);
     FZ_TRY(check_cache_ws(workspace, workspace_bytes, L.total));
     unsigned char *wb = static_cast<unsigned char *>(workspace);
@@ -875,7 +876,7 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
     p.q_stride = q_stride;
     p.heads = heads;
     p.group = heads / cache.kv_heads;
-    p.scale2 = scale * 1.4426950408889634f;   // log2(e)
+    p.scale2 = scale2;
     set_visible(p, window, sinks);
     p.out = out;
     p.lse = reinterpret_cast<float *>(wb + L.lse);

@@ -303,3 +303,11 @@ def test_runner_passes_numbers_of_tokens_of_any_size(monkeypatch):
         for kw in (dict(recent=n), dict(sinks=n)):
             with pytest.raises(fz.FusionError):
                 runner.Fusion.cache_evict(f, c, budget, **kw)
+
+
+def test_attention_refuses_scales_beyond_float32_in_base_2():
+    """2.4e38 log2(e) is infinite in float32, and 0 times that no number."""
+    for scale in (2.4e38, -2.4e38, 3.4e38):
+        assert attention(scale=scale) == fz.FUSION_ERR_INVALID_ARG
+    for scale in (2.3e38, -2.3e38, 0.0, 1e-45):
+        assert attention(scale=scale, workspace=None) == fz.FUSION_ERR_WORKSPACE   # (the next check)

@@ -62,6 +62,9 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
 }
 
+// Query heads times places of a cache, at most (the host refuses more).
+constexpr long long kCacheMaxHeadTokens = 1ll << 36;
+
 // Scratch behind the counters of the workspace.  Attention: log-sum-exps, partial results of sequences that
 // several CTAs share, logits (only where weights are accumulated).  Eviction: the kept slots and their counts.
 constexpr int kCacheMaxCtas = 2048;   // CTAs of the attention kernel; each has two partial results at most

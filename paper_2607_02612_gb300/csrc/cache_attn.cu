@@ -414,6 +414,7 @@ __global__ void __launch_bounds__(kWeightThreads) k_cache_weights(CacheAttnParam
 
 template <int DP, int NQ, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
+    static_assert(counts_fit(TT, 4) && (DP > 128 || counts_fit(TT, 1)), "rounds are counted in 32 bits");
     const int chunks = ceil_div(p.group, NQ);
     if constexpr (DP <= 128)
         if (warps_alone(p, chunks)) return launch_rounds<k_cache_attn_f32<DP, NQ, TT, S, 1>, 1>(Layout<DP, NQ, TT, S, 1>::kTotal, p, chunks, TT, s);

@@ -370,6 +370,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : S == 2 ? 3 : 1) k_cache_
 
 template <int DP, int NT, int TT, int S>
 cudaError_t launch(const CacheAttnParams &p, cudaStream_t s) {
+    static_assert(counts_fit(TT, 4) && (DP > 128 || counts_fit(TT, 1)), "rounds are counted in 32 bits");
     const int chunks = ceil_div(p.group, 8 * NT);
     if constexpr (DP <= 128)
         if (warps_alone(p, chunks)) return launch_rounds<k_cache_attn_mma<DP, NT, TT, S, 1>, 1>(Layout<DP, NT, TT, S, 1>::kTotal, p, chunks, TT, s);

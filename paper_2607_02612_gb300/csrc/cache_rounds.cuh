@@ -64,7 +64,7 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
 
 // The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.  A boundary at most `snap` rounds
 // inside a (sequence, key head) moves to its nearer end (its beginning first): a join costs more time than the few rounds that
-// it would deal out.  (Rounds are counted in 32 bits: the host refuses caches of more.)
+// it would deal out.  (Rounds are counted in 32 bits: counts_fit.)
 struct Run {
     unsigned total, len, more;
     unsigned r0, r1;   // this CTA's
@@ -401,6 +401,14 @@ __device__ __forceinline__ void join_runs(const CacheAttnParams &p, const Run &r
 // 33.3 and 38.9); together they share longer ones (60 x 200 of 8 heads 16.8 and 13.8, 64 x 250 19.4 and 17.4).
 inline bool warps_alone(const CacheAttnParams &p, int chunks) {
     return p.c.dim <= 128 && p.most <= kAloneMost && (long long)p.c.max_batch * p.c.kv_heads * chunks >= kAloneLeast;
+}
+
+// Whether the rounds of any batch that the host lets pass, of TT tokens for each of W warps, are fewer than 2^32.  A (sequence, part
+// of a key head's query heads) has at most its places / round + 1 of them, and there are at most max_batch * heads; warps alone (TT
+// down to 8) take calls of at most kAloneMost visible tokens only.
+constexpr bool counts_fit(long long tt, long long w) {
+    constexpr long long kHeads = (long long)FUSION_CACHE_MAX_BATCH * FUSION_CACHE_MAX_HEADS;
+    return (w == 1 ? kHeads * ((kAloneMost + tt - 1) / tt) : kCacheMaxHeadTokens / (tt * w) + kHeads) < 1ll << 32;
 }
 
 // Host: as many CTAs as the GPU holds at once, or as there can be rounds.  What depends on the kernel and the device alone is

@@ -786,8 +786,8 @@ int check_cache_pointers(const fusion_cache &c) {
 
 int check_heads(const fusion_cache &c, int32_t heads) {
     if (heads < c.kv_heads || heads > FUSION_CACHE_MAX_HEADS || heads % c.kv_heads) return FUSION_ERR_SHAPE;
-    // (the attention counts rounds of at least 32 tokens of a sequence and key head in 32 bits)
-    return (int64_t)c.max_batch * heads <= (1ll << 36) / ((int64_t)c.max_pages * c.page_tokens) ? FUSION_OK : FUSION_ERR_SHAPE;
+    // (the attention counts rounds in 32 bits: rounds::counts_fit)
+    return (int64_t)c.max_batch * heads <= kCacheMaxHeadTokens / ((int64_t)c.max_pages * c.page_tokens) ? FUSION_OK : FUSION_ERR_SHAPE;
 }
 
 CacheWs cache_ws(const fusion_cache &c, int32_t heads) {

@@ -311,3 +311,35 @@ def test_attention_refuses_scales_beyond_float32_in_base_2():
         assert attention(scale=scale) == fz.FUSION_ERR_INVALID_ARG
     for scale in (2.3e38, -2.3e38, 0.0, 1e-45):
         assert attention(scale=scale, workspace=None) == fz.FUSION_ERR_WORKSPACE   # (the next check)
+
+
+ROUNDS = r"""
+#include <cstdio>
+#include <cstdlib>
+#include "cache_rounds.cuh"
+int main(int argc, char **argv) {   // tokens warps -> fits
+    for (int k = 1; k + 1 < argc; k += 2) printf("%d\n", (int)fz::rounds::counts_fit(atoll(argv[k]), atoll(argv[k + 1])));
+    printf("%lld\n", fz::kCacheMaxHeadTokens);
+}
+"""
+
+
+def test_rounds_are_counted_in_32_bits(tmp_path):
+    """The bound that the kernels' rounds are held to, against the largest caches that the calls take, and the cache that the
+    calls refuse just beyond it."""
+    B = importlib.import_module("paper_2607_02612_gb300.build")
+    (tmp_path / "r.cu").write_text(ROUNDS)
+    subprocess.run([B._nvcc(), *B.ARCH, "-std=c++17", f"-I{B.INCLUDE}", f"-I{B.CSRC}", "-o", str(tmp_path / "r"), str(tmp_path / "r.cu")],
+                   check=True, capture_output=True)
+    sizes = [(tt, w) for tt in (1, 2, 4, 8, 16, 32) for w in (1, 4)]
+    out = subprocess.run([str(tmp_path / "r"), *[str(x) for s in sizes for x in s]], check=True, capture_output=True, text=True)
+    *fits, most = map(int, out.stdout.split())
+    places = lambda heads: most // (fz.FUSION_CACHE_MAX_BATCH * heads)   # noqa: E731
+    for (tt, w), ok in zip(sizes, fits, strict=True):
+        worst = max(fz.FUSION_CACHE_MAX_BATCH * heads * -(-(128 if w == 1 else places(heads)) // (tt * w)) for heads in (1, 2, 64, 1024))
+        assert not ok or worst < 1 << 32, (tt, w, worst)
+    assert [s for s, ok in zip(sizes, fits) if ok] == [s for s in sizes if s[0] >= (2 if s[1] == 1 else 8)]   # (65535 * 1024 * 64 < 2^32)
+    heads = 16
+    cap = places(heads) // 16
+    assert size(heads, max_batch=fz.FUSION_CACHE_MAX_BATCH, max_pages=cap, weights=None) > 0
+    assert size(heads, max_batch=fz.FUSION_CACHE_MAX_BATCH, max_pages=cap + 1, weights=None) == 0

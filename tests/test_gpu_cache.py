@@ -749,3 +749,74 @@ def test_append_of_no_rows(dtype):
             f.cache_append(dc, none.view(0, 2, 16), none, rows)
     assert status(f) == 0
     same(dc, c)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_captured_behind_copies_fills_and_other_streams(dtype):
+    """A graph in which each of the three calls follows a copy, a fill or a join with another stream's kernel that writes what
+    it reads, and is followed by a copy of what it wrote; replayed on other rows, lengths and budgets, calls of its own between."""
+    lengths = [100, 37, 0, 64, 300]
+    c = ref.make(dtype, lengths, 2, 64, 16, room=40, sizes="whole", weights=True, seed=57)
+    dc, f = on_device(dtype, c, 4), runner.Fusion(5)
+    t = ref.TYPES[dtype]
+    rows, offsets = 60, torch.tensor([0, 13, 13, 30, 31, 60], dtype=torch.int32)
+    rr = runner.RaggedRows(5, 30, rows, offsets.to(DEV))
+    k, v = (torch.zeros((rows, 2, 64), dtype=t, device=DEV) for _ in range(2))
+    q, out = (torch.zeros((5, 4, 64), dtype=t, device=DEV) for _ in range(2))
+    kept, budget = (torch.zeros(n, dtype=torch.int32, device=DEV) for n in ((5, 64), 5))
+    src = {n: torch.zeros_like(x) for n, x in dict(k=k, v=v, q=q, budget=budget).items()}
+    copies = {n: torch.zeros_like(x) for n, x in dict(lengths=dc.lengths, out=out, weights=dc.weights, kept=kept).items()}
+    side = torch.cuda.Stream()
+    lens = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            v.copy_(src["v"])
+            v.mul_(2.0)                       # another stream's kernel, joined just before the append
+        dc.lengths.copy_(lens)
+        k.copy_(src["k"])
+        main.wait_stream(side)
+        f.cache_append(dc, k, v, rr)
+        copies["lengths"].copy_(dc.lengths)
+        k.zero_()
+        dc.weights.zero_()
+        q.copy_(src["q"])
+        f.cache_attention(dc, q, out=out)
+        q.zero_()
+        copies["out"].copy_(out)
+        copies["weights"].copy_(dc.weights)
+        kept.zero_()
+        side.wait_stream(main)
+        with torch.cuda.stream(side):
+            budget.copy_(src["budget"])
+            budget.add_(1)
+        main.wait_stream(side)
+        f.cache_evict(dc, budget, sinks=2, recent=8, keep_idx=kept)
+        copies["kept"].copy_(kept)
+        budget.zero_()
+    for seed in (58, 59, 60):
+        g = torch.Generator().manual_seed(seed)
+        c = ref.make(dtype, lengths, 2, 64, 16, room=40, sizes="whole", weights=True, seed=seed)
+        for name, x in (("k", dc.k), ("v", dc.v), ("sizes", dc.sizes), ("table", dc.page_table)):
+            x.copy_(c[name])
+        host = {n: torch.randn(x.shape, generator=g).to(t) for n, x in src.items() if n != "budget"}
+        host["budget"] = torch.randint(0, 200, (5,), generator=g).to(torch.int32)
+        for n, x in host.items():
+            src[n].copy_(x)
+        graph.replay()
+        c["lengths"] = ref.append(c, host["k"], host["v"] * 2.0, offsets)
+        assert torch.equal(copies["lengths"].cpu(), c["lengths"])
+        c["weights"] = torch.zeros_like(c["weights"])
+        want, tol, w, wtol = ref.attention(c, host["q"], dtype)
+        assert ((copies["out"].cpu().double() - want).abs() <= tol).all()
+        gw = copies["weights"].cpu()
+        assert ((gw.double() - w).abs() <= wtol + 1e-45).all()
+        c["weights"] = gw
+        c["lengths"], keeps = ref.evict(c, host["budget"] + 1, sinks=2, recent=8)
+        same(dc, c)
+        for b, keep in enumerate(keeps):
+            assert copies["kept"][b].tolist() == (keep + [0] * 64)[:64]
+        f.cache_attention(dc, q)     # (a call of its own between two replays)
+    assert status(f) == 0

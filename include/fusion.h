@@ -157,7 +157,7 @@ typedef struct fusion_mlp_head {
  * Shape.  max_batch in [0, FUSION_CACHE_MAX_BATCH]; page_tokens a power of two up to FUSION_CACHE_MAX_PAGE_TOKENS;
  * head_dim a multiple of 8 up to FUSION_CACHE_MAX_HEAD_DIM; kv_heads in [1, FUSION_CACHE_MAX_HEADS]; max_pages >= 1 with
  * max_pages * page_tokens <= 2^30; num_pages >= 1 with num_pages * kv_heads * page_tokens < 2^32.  k and v are 16-byte
- * aligned. */
+ * aligned, pointers to 32-bit numbers 4-byte aligned (those of the calls too). */
 typedef struct fusion_cache {
     int32_t max_batch;         /* sequences */
     int32_t max_pages;         /* pages of a sequence, at most */

@@ -779,7 +779,11 @@ int check_cache(const fusion_cache &c) {
     return FUSION_OK;
 }
 
+// Pointers to 32-bit numbers (NULL passes): a misaligned one would fault in a kernel.
+template <typename... P> bool aligned4(P... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3u) == 0; }
+
 int check_cache_pointers(const fusion_cache &c) {
+    if (!aligned4(c.sizes, c.weights, c.page_table, c.lengths)) return FUSION_ERR_INVALID_ARG;
     if (!c.k || !c.v || !c.page_table || !c.lengths || !aligned16(c.k) || !aligned16(c.v)) return FUSION_ERR_INVALID_ARG;
     return FUSION_OK;
 }
@@ -832,6 +836,7 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
     if (in.max_rows < 0 || in.max_rows > INT32_MAX) return FUSION_ERR_SHAPE;
     if (in.max_rows > 0 && (!k || !v)) return FUSION_ERR_INVALID_ARG;   // (no rows: an empty tensor has no address)
     if (!lengths_out || !aligned16(k) || !aligned16(v)) return FUSION_ERR_INVALID_ARG;
+    if (!aligned4(in.offsets, in.batch, in.ids, sizes, scores, lengths_out, dev_status)) return FUSION_ERR_INVALID_ARG;
     if (!good_stride(dtype, k_stride) || !good_stride(dtype, v_stride)) return FUSION_ERR_INVALID_ARG;
     FZ_TRY(check_cache_ws(workspace, workspace_bytes, align256(sizeof(int) * (size_t)kWsCounters)));
     const int es = dtype == FUSION_BF16 ? 2 : 4;
@@ -865,6 +870,7 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
     FZ_TRY(check_heads(cache, heads));
     FZ_TRY(check_cache_pointers(cache));
     if (!q || !out || !aligned16(q) || !aligned16(out) || !good_stride(dtype, q_stride)) return FUSION_ERR_INVALID_ARG;
+    if (!aligned4(dev_status)) return FUSION_ERR_INVALID_ARG;
     const float scale2 = scale * 1.4426950408889634f;   // log2(e): logits are in base 2
     if (!std::isfinite(scale2) || window < 0 || sinks < 0) return FUSION_ERR_INVALID_ARG;
     const CacheWs L = cache_ws(cache, heads);
@@ -902,6 +908,7 @@ int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int
     FZ_TRY(check_cache(cache));
     FZ_TRY(check_cache_pointers(cache));
     if (!cache.weights || !budget || !lengths_out || sinks < 0 || recent < 0) return FUSION_ERR_INVALID_ARG;
+    if (!aligned4(budget, page_table_out, lengths_out, keep_idx, dev_status)) return FUSION_ERR_INVALID_ARG;
     if (keep_idx && keep_stride < 1) return FUSION_ERR_INVALID_ARG;
     if (page_table_out && page_table_out != cache.page_table && max_pages_out < 1) return FUSION_ERR_SHAPE;
     const CacheWs L = cache_ws(cache, cache.kv_heads);

@@ -343,3 +343,18 @@ def test_rounds_are_counted_in_32_bits(tmp_path):
     cap = places(heads) // 16
     assert size(heads, max_batch=fz.FUSION_CACHE_MAX_BATCH, max_pages=cap, weights=None) > 0
     assert size(heads, max_batch=fz.FUSION_CACHE_MAX_BATCH, max_pages=cap + 1, weights=None) == 0
+
+
+@pytest.mark.parametrize("off", [1, 2, 3, 6])
+def test_misaligned_numbers_are_refused(off):
+    """Pointers to 32-bit numbers, whose loads would fault."""
+    bad = FAKE + off
+    for call in (append, attention, evict):
+        for kw in (dict(sizes=bad), dict(weights=bad), dict(page_table=bad), dict(lengths=bad)):
+            assert call(cache(**kw)) == fz.FUSION_ERR_INVALID_ARG, kw
+        assert call(dev_status=bad) == fz.FUSION_ERR_INVALID_ARG
+    for kw in (dict(in_=fz.ragged(4, 10, 100, bad)), dict(in_=fz.ragged(4, 10, 100, FAKE, bad)), dict(in_=fz.ragged(4, 10, 100, FAKE, None, bad)),
+               dict(sizes=bad), dict(scores=bad), dict(lengths_out=bad)):
+        assert append(**kw) == fz.FUSION_ERR_INVALID_ARG, kw
+    for kw in (dict(budget=bad), dict(page_table_out=bad, max_pages_out=4), dict(lengths_out=bad), dict(keep_idx=bad, keep_stride=8)):
+        assert evict(**kw) == fz.FUSION_ERR_INVALID_ARG, kw

@@ -499,9 +499,9 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
  *   x_j = scale q_a . k_hj + log s_j,   out[b, a, :] = sum_j softmax_j(x)_j v_hj
  * over the visible tokens j with s_j > 0: all of them for window 0, else the first `sinks` and the last `window`.  A merged
  * token of size s weighs like the s tokens that it replaced (as in fusion_attention); a token of size 0 has no part in the
- * result, whatever its key and value hold.  No token left, or every x_j = -inf (in base 2 below -3e38): the row is 0.  Where the
- * cache keeps weights,
- * weights_j += sum_a softmax_j(x_a) for the visible tokens, summed in float32 in an order that depends on nothing but heads.
+ * result, whatever its key and value hold.  No token left, or every x_j = -inf (in base 2 below -3e38): the row is 0.
+ * Where the cache keeps weights, weights_j += sum_a softmax_j(x_a) for the visible tokens, summed in float32 in an order that
+ * depends on nothing but heads.
  * q: [max_batch, heads, head_dim], dtype, sequences q_stride elements apart (>= 0, rows 16-byte aligned), 16-byte aligned;
  * out: [max_batch, heads, head_dim], dtype, 16-byte aligned.  heads: a multiple of kv_heads, at most
  * FUSION_CACHE_MAX_HEADS, with max_batch * heads * max_pages * page_tokens <= 2^36.  scale: finite, also times log2(e).

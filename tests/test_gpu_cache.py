@@ -820,3 +820,39 @@ def test_captured_behind_copies_fills_and_other_streams(dtype):
             assert copies["kept"][b].tolist() == (keep + [0] * 64)[:64]
         f.cache_attention(dc, q)     # (a call of its own between two replays)
     assert status(f) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_two_streams_at_once(dtype):
+    """Calls that overlap on two streams, a cache object each over the same pools (other sequences' pages): steps of append,
+    attention with weights and, at the end, an eviction give the bits that they give one after the other."""
+    lengths = [700, 33, 2500, 64, 5, 900]
+    c = ref.make(dtype, lengths, 2, 64, 16, room=40, sizes="whole", weights=True, seed=61)
+    g = torch.Generator().manual_seed(62)
+    rows = [torch.randn((20, 3, 8 * 64), generator=g).to(ref.TYPES[dtype]).to(DEV) for _ in range(2)]   # queries, keys, values
+    budget = torch.tensor([300, 40, 1100], dtype=torch.int32, device=DEV)
+
+    def run(streams):
+        d = {k: None if t is None else t.to(DEV) for k, t in c.items()}
+        halves = [runner.cache_of(dtype, d["k"], d["v"], d["table"][3 * s:3 * s + 3].contiguous(), d["lengths"][3 * s:3 * s + 3].contiguous(), heads=4,
+                                  sizes=d["sizes"], weights=d["weights"]) for s in range(2)]
+        f, outs = runner.Fusion(6), [[], []]
+        torch.cuda.synchronize()
+        for step in range(21):
+            for s, dc in enumerate(halves):
+                with torch.cuda.stream(streams[s]):
+                    if step == 20:
+                        f.cache_evict(dc, budget, sinks=2, recent=16)
+                        continue
+                    x = rows[s][step]
+                    f.cache_append(dc, x[:, 256:384], x[:, 384:])
+                    outs[s].append(f.cache_attention(dc, x[:, :256]))
+        assert status(f) == 0
+        bits = [ref.bits(t.cpu()) for t in (d["k"], d["v"], d["sizes"], d["weights"], *outs[0], *outs[1])]
+        return [*bits, halves[0].lengths.cpu(), halves[1].lengths.cpu()]
+
+    main = torch.cuda.current_stream()
+    want = run([main, main])
+    for _ in range(3):
+        got = run([torch.cuda.Stream(), torch.cuda.Stream()])
+        assert all(torch.equal(a, b) for a, b in zip(got, want, strict=True))

@@ -428,11 +428,11 @@ cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
 cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_t s) {
     if (p.c.max_batch == 0) return cudaSuccess;
     const int head_chunks = p.c.dim * (dtype == FUSION_BF16 ? 2 : 4) / 16;
-    // Threads of a sequence, by the room of a row of the page table, since its length is known on the device alone (64 sequences of 500
-    // with room for 512, 4096, 32768, in place to half: 16.9, 17.8, 43.4 us): few where it is short, since every warp more has its share of the phases (8 x 577: 256 threads 7.9 us,
-    // 512 8.1), more where each would have many keys (64 x 1900: 21.4 and 20.8; 64 x 4000: 512 threads 34.2, 1024 32.4; 32 x 8192:
-    // 160.6 and 155.8), then clusters of up to 8 CTAs (8852: two of 1024 threads 18.6, four of 512 18.8; 10973: 16.6 and 14.5; 32768:
-    // four of 1024 85.0, eight of 512 83.7).
+    // Threads of a sequence, by the room of a row of the page table, since its length is known on the device alone (64 sequences of
+    // 500 with room for 512, 4096, 32768, in place to half: 16.9, 17.8, 43.4 us).  Few where it is short, since every warp more has its
+    // share of the phases (8 x 577: 256 threads 7.9 us, 512 8.1), more where each would have many keys (64 x 1900: 21.4 and 20.8;
+    // 64 x 4000: 512 threads 34.2, 1024 32.4; 32 x 8192: 160.6 and 155.8), then clusters of up to 8 CTAs (8852: two of 1024 threads
+    // 18.6, four of 512 18.8; 10973: 16.6 and 14.5; 32768: four of 1024 85.0, eight of 512 83.7).
     const int cap = p.c.capacity, k = kHeld;
     cudaError_t e = cap <= 64 * k     ? launch_select<1, 256>(p, s)
                     : cap <= 256 * k  ? launch_select<1, 512>(p, s)

@@ -1,6 +1,6 @@
 """Position rotation on the way into the key-value cache, and the cache in 4 bits, on work of their whole range:
 `Fusion.cache_append_rotated`, and `Fusion.cache_append`, `Fusion.cache_read`, `Fusion.cache_attention` and
-`Fusion.cache_evict` on a `DeviceCache4`; and the same in elementary torch operations.
+`Fusion.cache_evict` on a `DevicePackedCache`; and the same in elementary torch operations.
 
 A cache holds the keys and values of up to `batch` sequences in pages of `page` tokens, a size and an accumulated
 attention weight per token, a page table and lengths.  Its pages lie in random order, as in a pool that has been in use.
@@ -203,7 +203,7 @@ def _handles(s):
     def cache(table, lengths):
         if s["kind"] == "rotate":
             return runner.cache_of(s["dtype"], s["k"], s["v"], table, lengths, sizes=s["sizes"], weights=s["weights"], heads=heads)
-        return runner.cache4_of(s["dtype"], s["k"], s["v"], s["k_scales"], s["v_scales"], table, lengths, sizes=s["sizes"],
+        return runner.packed_cache_of(s["dtype"], s["k"], s["v"], s["k_scales"], s["v_scales"], table, lengths, sizes=s["sizes"],
                                 weights=s["weights"], heads=heads)
 
     s["cache"] = cache(s["table"], s["lengths"])

@@ -79,6 +79,7 @@ extern "C" {
 #define FUSION_DEV_BAD_IDS 16    /* a sample id outside [0, max_batch) */
 #define FUSION_DEV_TIMEOUT 32    /* a bounded wait inside a kernel gave up (outputs of that sample skipped) */
 #define FUSION_DEV_BAD_CACHE 64  /* a cache length or page id out of range, or no room for the appended rows */
+#define FUSION_DEV_BAD_POSITION 128 /* a position that the rotation's table does not have */
 
 /* ---- storage types and stage flags --------------------------------------- */
 #define FUSION_F32 0
@@ -104,6 +105,10 @@ extern "C" {
 #define FUSION_CACHE_MAX_PAGE_TOKENS 1024
 #define FUSION_CACHE_MAX_HEAD_DIM 256
 #define FUSION_CACHE_MAX_HEADS 1024
+
+/* Which dims a rotation turns together (fusion_rotation.pairs). */
+#define FUSION_PAIRS_HALVES 0   /* i and i + dims / 2 */
+#define FUSION_PAIRS_ADJACENT 1 /* 2 i and 2 i + 1 */
 
 /* Pooling of an MLP exit head (fusion_mlp_head.pool). */
 #define FUSION_POOL_CLS 0     /* the CLS row (the paper's CLS-only head, block 10) */
@@ -171,6 +176,31 @@ typedef struct fusion_cache {
     const int32_t *page_table; /* [max_batch, max_pages] */
     const int32_t *lengths;    /* [max_batch] tokens held, in [0, max_pages * page_tokens] */
 } fusion_cache;
+
+/* The same cache with keys and values in 4 bits (4.5 with their scales).  A row of a head is held in groups of 16 dims: a scale,
+ * of type e4m3 (a sign, 4 bits of exponent, 3 of mantissa), and 16 codes of type e2m1 (a sign and one of 0, 0.5, 1, 1.5, 2, 3,
+ * 4, 6 by the code's lower three bits).  A dim's value is its code's times the scale: at most 6 significant bits, exact in bf16.
+ * cache.k, cache.v: [num_pages, kv_heads, page_tokens, head_dim / 2] bytes, dim 2 i in the lower four bits of byte i, 2 i + 1
+ * in the upper ones.  k_scales, v_scales: [num_pages, kv_heads, page_tokens, FUSION_PACKED_SCALE_BYTES(head_dim)] bytes, the
+ * scale of dims 16 i .. 16 i + 15 in byte i; bytes behind the last scale are not read (fusion_packed_append writes zeros there).
+ * All 16-byte aligned.  head_dim is a multiple of 32; everything else as in fusion_cache. */
+#define FUSION_PACKED_SCALE_BYTES(head_dim) (((head_dim) / 16 + 3) / 4 * 4)
+typedef struct fusion_packed_cache {
+    fusion_cache cache;
+    void *k_scales, *v_scales;
+} fusion_packed_cache;
+
+/* Rotation of keys and queries by their positions.  With a row of the table for each position, c_i and s_i (i < dims / 2) its
+ * cosines and sines, the dims (a, b) of pair i (FUSION_PAIRS_*) become (a c_i - b s_i, b c_i + a s_i), each product and the
+ * difference or sum rounded to float32 (no fused multiply-add); dims from `dims` on stay.  What the angles are is the
+ * caller's: any frequencies, positions in a plane, a factor on all of them. */
+typedef struct fusion_rotation {
+    const float *table;       /* [table_rows, dims]: dims / 2 cosines, then as many sines; 16-byte aligned */
+    int32_t table_rows;       /* positions 0 .. table_rows - 1 */
+    int32_t dims;             /* a multiple of 16 (of 32 for a cache in 4 bits) up to head_dim */
+    int32_t pairs;            /* FUSION_PAIRS_HALVES or FUSION_PAIRS_ADJACENT */
+    const int32_t *positions; /* [max_rows], of every row; NULL: the row's place in its sequence */
+} fusion_rotation;
 
 /* Human-readable name of a return code or of a single FUSION_DEV_* bit. */
 const char *fusion_status_string(int code);
@@ -531,6 +561,69 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
 int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int32_t sinks, int32_t recent,
                        const int32_t *page_table_out, int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx,
                        int32_t keep_stride, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * fusion_cache_append_rotated: fusion_cache_append with the keys rotated on the way (fusion_rotation), and with them the
+ * queries of the same rows: q_out[row] is q[row] rotated by the row's position.  Keys and queries are rounded once, to the
+ * dtype; values are copied.  q: [in.max_rows, heads, head_dim] with rows q_stride elements apart (>= 0, rows 16-byte
+ * aligned), NULL: none; q_out: [in.max_rows, heads, head_dim], may be q where its rows lie that way and overlaps nothing else.
+ * heads: in [1, FUSION_CACHE_MAX_HEADS], read only with q; any number beside the cache's.  Rows of no sample are left in q_out.
+ * Errors: those of fusion_cache_append; FUSION_ERR_INVALID_ARG for a NULL or misaligned table, bad pairs, q without q_out;
+ * FUSION_ERR_SHAPE for table_rows < 1 or dims or heads out of range.  Device bits: those of fusion_cache_append (which leave that
+ * sample's rows of q_out unwritten too) and BAD_POSITION, which leaves the sequence's length as it is; places past its end, and
+ * the sample's rows of q_out, may have been written.
+ */
+int fusion_cache_append_rotated(int dtype, fusion_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                                int64_t v_stride, const float *sizes, const float *scores, fusion_rotation rotation,
+                                const void *q, int64_t q_stride, int32_t heads, void *q_out, int32_t *lengths_out,
+                                void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/* As fusion_cache_workspace_size, for the fusion_packed_* calls. */
+size_t fusion_packed_workspace_size(fusion_packed_cache cache, int32_t heads);
+
+/*
+ * fusion_packed_append, fusion_packed_append_rotated: rows of `dtype` to a cache in 4 bits.  For every group of 16 dims (of
+ * rotated keys in float32, not rounded to the dtype before) with largest magnitude m:
+ *   scale = m * fl(1/6) in float32, rounded to the nearest e4m3 number, 448 at most;
+ *   code  = the e2m1 number nearest to x / scale (exactly; ties to the even code), 6 at most, with the sign of x.
+ * Where the scale is 0 all codes are 0.  A group with a NaN or an infinity holds NaN (scale 0x7F, codes 0).
+ * Arguments and errors as fusion_cache_append and fusion_cache_append_rotated.
+ */
+int fusion_packed_append(int dtype, fusion_packed_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
+                         size_t workspace_bytes, int32_t *dev_status, void *stream);
+int fusion_packed_append_rotated(int dtype, fusion_packed_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                                 int64_t v_stride, const float *sizes, const float *scores, fusion_rotation rotation,
+                                 const void *q, int64_t q_stride, int32_t heads, void *q_out, int32_t *lengths_out,
+                                 void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * fusion_packed_attention: fusion_cache_attention over a cache in 4 bits, q and out of type dtype.  Keys and values enter the
+ * products as the values that the cache holds, exactly; a query as a float16 (for FUSION_F32 the sum of two) times a power of
+ * two of its head's own; a probability as a float16 (two), within 2^-11 (2^-21) of itself or of 2^-21 (2^-31) of the largest.
+ */
+int fusion_packed_attention(int dtype, fusion_packed_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
+                            int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
+                            int32_t *dev_status, void *stream);
+
+/* fusion_packed_evict: fusion_cache_evict of a cache in 4 bits (codes and scales move as they are). */
+int fusion_packed_evict(fusion_packed_cache cache, const int32_t *budget, int32_t sinks, int32_t recent, const int32_t *page_table_out,
+                        int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx, int32_t keep_stride, void *workspace,
+                        size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * fusion_cache_read, fusion_packed_read: the rows that a cache holds, back in a ragged batch (the counterpart of the appends).
+ * Row r of sample i is position start + r of sequence t, where t = in.ids[i], or i when in.ids is NULL, and start = starts[i],
+ * or 0 when starts is NULL.  k_out, v_out: [in.max_rows, kv_heads, head_dim], dtype, 16-byte aligned; sizes_out (1 where the
+ * cache keeps no sizes), weights_out (0 where it keeps no weights): [in.max_rows]; any of the four may be NULL.  A value of a
+ * cache in 4 bits is exact in either dtype.  Samples may name a sequence several times; rows of no sample are left.
+ * Errors: FUSION_ERR_SHAPE, FUSION_ERR_INVALID_ARG, FUSION_ERR_DTYPE; device bits, each of which leaves that sample's rows:
+ * BAD_OFFSETS, BAD_IDS, BAD_CACHE (a length or page id out of range, rows beyond the length); BAD_BATCH leaves all.  No workspace.
+ */
+int fusion_cache_read(int dtype, fusion_cache cache, fusion_ragged in, const int32_t *starts, void *k_out, void *v_out,
+                      float *sizes_out, float *weights_out, int32_t *dev_status, void *stream);
+int fusion_packed_read(int dtype, fusion_packed_cache cache, fusion_ragged in, const int32_t *starts, void *k_out, void *v_out,
+                       float *sizes_out, float *weights_out, int32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -30,6 +30,7 @@ FUSION_DEV_INTERNAL = 8
 FUSION_DEV_BAD_IDS = 16
 FUSION_DEV_TIMEOUT = 32
 FUSION_DEV_BAD_CACHE = 64
+FUSION_DEV_BAD_POSITION = 128
 FUSION_F32 = 0
 FUSION_BF16 = 1
 FUSION_STAGE_MERGE = 1
@@ -44,6 +45,8 @@ FUSION_CACHE_MAX_BATCH = 65535
 FUSION_CACHE_MAX_PAGE_TOKENS = 1024
 FUSION_CACHE_MAX_HEAD_DIM = 256
 FUSION_CACHE_MAX_HEADS = 1024
+FUSION_PAIRS_HALVES = 0
+FUSION_PAIRS_ADJACENT = 1
 FUSION_POOL_CLS = 0
 FUSION_POOL_SPATIAL = 1
 
@@ -52,7 +55,9 @@ EXPORTED = ("fusion_status_string", "fusion_version", "fusion_profile_next", "fu
             "fusion_stage", "fusion_merge_router", "fusion_token_scores", "fusion_exit_mlp_workspace_size",
             "fusion_exit_check_mlp", "fusion_attention", "fusion_stage_mlp",
             "fusion_stage_mlp_workspace_size", "fusion_set_launch_gate", "fusion_cache_workspace_size",
-            "fusion_cache_append", "fusion_cache_attention", "fusion_cache_evict")
+            "fusion_cache_append", "fusion_cache_attention", "fusion_cache_evict", "fusion_cache_append_rotated",
+            "fusion_cache_read", "fusion_packed_workspace_size", "fusion_packed_append", "fusion_packed_append_rotated",
+            "fusion_packed_attention", "fusion_packed_evict", "fusion_packed_read")
 
 
 class FusionError(RuntimeError):
@@ -83,6 +88,15 @@ class fusion_cache(ctypes.Structure):
                 ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("num_pages", ctypes.c_int64),
                 ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("sizes", ctypes.c_void_p),
                 ("weights", ctypes.c_void_p), ("page_table", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
+
+
+class fusion_packed_cache(ctypes.Structure):
+    _fields_ = [("cache", fusion_cache), ("k_scales", ctypes.c_void_p), ("v_scales", ctypes.c_void_p)]
+
+
+class fusion_rotation(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_rows", ctypes.c_int32), ("dims", ctypes.c_int32),
+                ("pairs", ctypes.c_int32), ("positions", ctypes.c_void_p)]
 
 
 _lib = None
@@ -139,7 +153,19 @@ def load(path: Optional[str] = None):
     lib.fusion_cache_append.argtypes = [ctypes.c_int, C, R, V, I64, V, I64, V, V, V, V, SZ, V, V]
     lib.fusion_cache_attention.argtypes = [ctypes.c_int, C, V, I64, I32, F, I32, I32, V, V, SZ, V, V]
     lib.fusion_cache_evict.argtypes = [ctypes.c_int, C, V, I32, I32, V, I32, V, V, I32, V, SZ, V, V]
-    for name in ("fusion_cache_append", "fusion_cache_attention", "fusion_cache_evict"):
+    C4, T = fusion_packed_cache, fusion_rotation
+    lib.fusion_cache_append_rotated.argtypes = [ctypes.c_int, C, R, V, I64, V, I64, V, V, T, V, I64, I32, V, V, V, SZ, V, V]
+    lib.fusion_cache_read.argtypes = [ctypes.c_int, C, R, V, V, V, V, V, V, V]
+    lib.fusion_packed_workspace_size.argtypes = [C4, I32]
+    lib.fusion_packed_workspace_size.restype = SZ
+    lib.fusion_packed_append.argtypes = [ctypes.c_int, C4, R, V, I64, V, I64, V, V, V, V, SZ, V, V]
+    lib.fusion_packed_append_rotated.argtypes = [ctypes.c_int, C4, R, V, I64, V, I64, V, V, T, V, I64, I32, V, V, V, SZ, V, V]
+    lib.fusion_packed_attention.argtypes = [ctypes.c_int, C4, V, I64, I32, F, I32, I32, V, V, SZ, V, V]
+    lib.fusion_packed_evict.argtypes = [C4, V, I32, I32, V, I32, V, V, I32, V, SZ, V, V]
+    lib.fusion_packed_read.argtypes = [ctypes.c_int, C4, R, V, V, V, V, V, V, V]
+    for name in ("fusion_cache_append", "fusion_cache_attention", "fusion_cache_evict", "fusion_cache_append_rotated",
+                 "fusion_cache_read", "fusion_packed_append", "fusion_packed_append_rotated", "fusion_packed_attention",
+                 "fusion_packed_evict", "fusion_packed_read"):
         getattr(lib, name).restype = ctypes.c_int
     for name in ("fusion_merge", "fusion_exit_check", "fusion_exit_check_noalloc", "fusion_prune",
                  "fusion_compact", "fusion_stage", "fusion_merge_router", "fusion_token_scores",
@@ -194,6 +220,19 @@ def cache(max_batch: int, max_pages: int, page_tokens: int, kv_heads: int, head_
           sizes, weights, page_table, lengths) -> fusion_cache:
     return fusion_cache(int(max_batch), int(max_pages), int(page_tokens), int(kv_heads), int(head_dim), int(num_pages),
                         _ptr(k), _ptr(v), _ptr(sizes), _ptr(weights), _ptr(page_table), _ptr(lengths))
+
+
+def packed_cache(cache: fusion_cache, k_scales, v_scales) -> fusion_packed_cache:
+    return fusion_packed_cache(cache, _ptr(k_scales), _ptr(v_scales))
+
+
+def packed_scale_bytes(head_dim: int) -> int:
+    """Bytes of a row's scales (FUSION_PACKED_SCALE_BYTES)."""
+    return (head_dim // 16 + 3) // 4 * 4
+
+
+def rotation(table, table_rows: int, dims: int, pairs: int, positions=None) -> fusion_rotation:
+    return fusion_rotation(_ptr(table), int(table_rows), int(dims), int(pairs), _ptr(positions))
 
 
 def check(rc: int) -> None:
@@ -364,3 +403,61 @@ def fusion_cache_evict(dtype, cache, budget, sinks, recent, page_table_out, max_
     return load().fusion_cache_evict(int(dtype), cache, _ptr(budget), int(sinks), int(recent), _ptr(page_table_out),
                                      int(max_pages_out), _ptr(lengths_out), _ptr(keep_idx), int(keep_stride),
                                      _ptr(workspace), int(workspace_bytes), _ptr(dev_status), _stream(stream))
+
+
+def fusion_cache_append_rotated(dtype, cache, in_, k, k_stride, v, v_stride, sizes, scores, rotation, q, q_stride, heads,
+                                q_out, lengths_out, workspace, workspace_bytes, dev_status, stream=None) -> int:
+    """fusion_cache_append with the keys, and the queries of the same rows, rotated by their positions."""
+    return load().fusion_cache_append_rotated(int(dtype), cache, in_, _ptr(k), int(k_stride), _ptr(v), int(v_stride),
+                                              _ptr(sizes), _ptr(scores), rotation, _ptr(q), int(q_stride), int(heads),
+                                              _ptr(q_out), _ptr(lengths_out), _ptr(workspace), int(workspace_bytes),
+                                              _ptr(dev_status), _stream(stream))
+
+
+def fusion_cache_read(dtype, cache, in_, starts, k_out, v_out, sizes_out, weights_out, dev_status, stream=None) -> int:
+    """Rows of cached sequences back into a ragged batch."""
+    return load().fusion_cache_read(int(dtype), cache, in_, _ptr(starts), _ptr(k_out), _ptr(v_out), _ptr(sizes_out),
+                                    _ptr(weights_out), _ptr(dev_status), _stream(stream))
+
+
+def fusion_packed_workspace_size(cache, heads: int) -> int:
+    return int(load().fusion_packed_workspace_size(cache, int(heads)))
+
+
+def fusion_packed_append(dtype, cache, in_, k, k_stride, v, v_stride, sizes, scores, lengths_out, workspace,
+                         workspace_bytes, dev_status, stream=None) -> int:
+    """fusion_cache_append to a cache in 4 bits."""
+    return load().fusion_packed_append(int(dtype), cache, in_, _ptr(k), int(k_stride), _ptr(v), int(v_stride), _ptr(sizes),
+                                       _ptr(scores), _ptr(lengths_out), _ptr(workspace), int(workspace_bytes),
+                                       _ptr(dev_status), _stream(stream))
+
+
+def fusion_packed_append_rotated(dtype, cache, in_, k, k_stride, v, v_stride, sizes, scores, rotation, q, q_stride, heads,
+                                 q_out, lengths_out, workspace, workspace_bytes, dev_status, stream=None) -> int:
+    """fusion_cache_append_rotated to a cache in 4 bits."""
+    return load().fusion_packed_append_rotated(int(dtype), cache, in_, _ptr(k), int(k_stride), _ptr(v), int(v_stride),
+                                               _ptr(sizes), _ptr(scores), rotation, _ptr(q), int(q_stride), int(heads),
+                                               _ptr(q_out), _ptr(lengths_out), _ptr(workspace), int(workspace_bytes),
+                                               _ptr(dev_status), _stream(stream))
+
+
+def fusion_packed_attention(dtype, cache, q, q_stride, heads, scale, window, sinks, out, workspace, workspace_bytes,
+                            dev_status, stream=None) -> int:
+    """fusion_cache_attention over a cache in 4 bits."""
+    return load().fusion_packed_attention(int(dtype), cache, _ptr(q), int(q_stride), int(heads), float(scale), int(window),
+                                          int(sinks), _ptr(out), _ptr(workspace), int(workspace_bytes), _ptr(dev_status),
+                                          _stream(stream))
+
+
+def fusion_packed_evict(cache, budget, sinks, recent, page_table_out, max_pages_out, lengths_out, keep_idx, keep_stride,
+                        workspace, workspace_bytes, dev_status, stream=None) -> int:
+    """fusion_cache_evict of a cache in 4 bits."""
+    return load().fusion_packed_evict(cache, _ptr(budget), int(sinks), int(recent), _ptr(page_table_out), int(max_pages_out),
+                                      _ptr(lengths_out), _ptr(keep_idx), int(keep_stride), _ptr(workspace),
+                                      int(workspace_bytes), _ptr(dev_status), _stream(stream))
+
+
+def fusion_packed_read(dtype, cache, in_, starts, k_out, v_out, sizes_out, weights_out, dev_status, stream=None) -> int:
+    """fusion_cache_read of a cache in 4 bits."""
+    return load().fusion_packed_read(int(dtype), cache, in_, _ptr(starts), _ptr(k_out), _ptr(v_out), _ptr(sizes_out),
+                                     _ptr(weights_out), _ptr(dev_status), _stream(stream))

@@ -20,7 +20,7 @@ OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(OUT_DIR, "libfusion.so")
 
 SOURCES = ["fusion_api.cu", "exit.cu", "image.cu", "image_f32.cu", "image_tc.cu", "router.cu", "scores.cu", "pool.cu", "attn.cu", "noalloc.cu",
-           "cache_append.cu", "cache_attn.cu", "cache_attn_bf16.cu", "cache_evict.cu"]
+           "cache_append.cu", "cache_attn.cu", "cache_attn_bf16.cu", "cache_evict.cu", "cache_store.cu", "cache_read.cu", "packed_attn.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
          "--expt-relaxed-constexpr", f"-I{INCLUDE}", f"-I{CSRC}"]

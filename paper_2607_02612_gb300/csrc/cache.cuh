@@ -124,6 +124,17 @@ __host__ __device__ __forceinline__ int visible(const CacheAttnParams &p, int n)
 }
 cudaError_t launch_cache_attention_bf16(const CacheAttnParams &p, cudaStream_t s);   // without the weights
 cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStream_t s);
+cudaError_t launch_cache_weights(const CacheAttnParams &p, cudaStream_t s);           // after the attention
+
+// The scales of a cache in 4 bits: `bytes` of a row, a multiple of 4.
+struct PackedScales {
+    unsigned char *k, *v;
+    int bytes;
+};
+struct PackedAttnParams : CacheAttnParams {
+    PackedScales s;
+};
+cudaError_t launch_packed_attention(int dtype, const PackedAttnParams &p, cudaStream_t s);
 
 struct CacheAppendParams {
     Cache c;
@@ -138,6 +149,30 @@ struct CacheAppendParams {
 };
 cudaError_t launch_cache_append(int dtype, const CacheAppendParams &p, cudaStream_t s);
 
+// Keys and queries rotated on the way (turned > 0), or a cache in 4 bits (s.k), or both.
+struct CacheStoreParams : CacheAppendParams {
+    PackedScales s;
+    const float *table;
+    int table_rows, turned;         // turned: dims that are rotated
+    const int *positions;
+    const unsigned char *q;         // NULL: none
+    long long q_stride;             // bytes between rows
+    int heads;
+    unsigned char *q_out;
+};
+cudaError_t launch_cache_store(int dtype, int pairs, const CacheStoreParams &p, cudaStream_t s);
+
+struct CacheReadParams {
+    Cache c;
+    PackedScales s;                      // s.k NULL: not in 4 bits
+    Ragged in;
+    const int *starts;
+    unsigned char *k_out, *v_out;
+    float *sizes_out, *weights_out;
+    int *status;
+};
+cudaError_t launch_cache_read(int dtype, const CacheReadParams &p, cudaStream_t s);
+
 struct CacheEvictParams {
     Cache c;
     const int *budget;
@@ -148,10 +183,11 @@ struct CacheEvictParams {
     int *lengths_out;
     int *keep_idx;
     int keep_stride;
+    PackedScales s;                      // s.k NULL: not in 4 bits
     int2 *plan;                     // [max_batch]: kept tokens (-1: leave the sequence), the first one that moves
     unsigned *keep;                 // [max_batch, capacity] slots of the kept tokens
     int *status;
 };
-cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_t s);
+cudaError_t launch_cache_evict(int row_bytes, const CacheEvictParams &p, cudaStream_t s);   // row_bytes: of a head of K or V
 
 }  // namespace fz

@@ -5,37 +5,12 @@
 // sample's ids and pages have been checked (256 samples of 100 to 197 tokens of 6 x 64 dims 23.4 us, 74 % of the copy's rate; before
 // the checks, in registers meanwhile, 23.9).  All CTAs of a sample read its length before the last of them to finish raises it (a
 // counter per sample, zero between calls), where the length is raised in place.
-#include "cache.cuh"
+#include "cache_rows.cuh"
 
 namespace fz {
 namespace {
 
 constexpr int kThreads = 256, kPer = 4;
-constexpr int kMostY = 65535;   // of a grid's height
-
-// Whether sample i's slot is named by another sample too (all threads).  Every CTA reads all ids: 1 us for 256 samples, but the work
-// grows with the square of the batch (1 to 65 tokens of 6 x 64 dims with and without ids: 1024 samples 21 and 20 us, 8192 197 and 163).
-__device__ bool named_twice(const Ragged &in, int B, int i, int slot) {
-    if (!in.ids) return false;
-    bool twice = false;
-    for (int j = threadIdx.x; j < B; j += kThreads) twice |= j != i && in.ids[j] == slot;
-    return __syncthreads_or(twice);
-}
-
-// The lengths that no sample raises, where they go elsewhere (all threads; apart from the kernel, whose other CTAs fetch none of it).
-__device__ __noinline__ void copy_other_lengths(const CacheAppendParams &p, int B) {
-    __shared__ unsigned named[(FUSION_CACHE_MAX_BATCH + 32) / 32];
-    const int tid = threadIdx.x, slots = p.c.max_batch;
-    for (int w = tid; w < (slots + 31) / 32; w += kThreads) named[w] = 0u;
-    __syncthreads();
-    for (int j = tid; j < B; j += kThreads) {
-        const int s = p.in.ids ? p.in.ids[j] : j;
-        if (s >= 0 && s < slots) atomicOr(&named[s >> 5], 1u << (s & 31));
-    }
-    __syncthreads();
-    for (int s = tid; s < slots; s += kThreads)
-        if (!(named[s >> 5] >> (s & 31) & 1u)) p.lengths_out[s] = p.c.lengths[s];
-}
 
 // A row of CTAs per sample, and one more for the lengths while the grid has room for it.
 __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams p, int row_chunks, int head_chunks) {
@@ -45,7 +20,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams 
     const int B = device_batch(p.in);
     if (i == (int)gridDim.y - 1 && blockIdx.x == 0) {   // (with kMostY samples the last sample's first CTA too)
         if (B < 0 && tid == 0) raise_status(p.status, FUSION_DEV_BAD_BATCH);
-        if (!p.in_place) copy_other_lengths(p, B);
+        if (!p.in_place) copy_other_lengths<kThreads>(p, B);
     }
     if (B < 0 || i >= B) return;
     const int slot = p.in.ids ? p.in.ids[i] : i;
@@ -82,7 +57,7 @@ __global__ void __launch_bounds__(kThreads, 4) k_cache_append(CacheAppendParams 
         }
         for (int e = (at >> c.shift) + tid; n > 0 && e <= (at + n - 1) >> c.shift; e += kThreads) wrong |= pages[e] >= c.num_pages;
     }
-    if (named_twice(p.in, B, i, slot)) bad |= FUSION_DEV_BAD_IDS;
+    if (named_twice<kThreads>(p.in, B, i, slot)) bad |= FUSION_DEV_BAD_IDS;
     if (__syncthreads_or(wrong)) bad |= FUSION_DEV_BAD_CACHE;
     if (bad) {   // nothing of this sample is written, and its slot's length stays (also where it is named twice)
         if (blockIdx.x == 0 && tid == 0) {

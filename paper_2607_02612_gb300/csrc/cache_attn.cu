@@ -435,7 +435,10 @@ cudaError_t launch_cache_attention(int dtype, const CacheAttnParams &p, cudaStre
                           : p.group == 1       ? launch_dim<1>(p, s)
                           : p.group <= 4       ? launch_dim<4>(p, s)
                                                : launch_dim<8>(p, s);
-    if (e != cudaSuccess || !p.logits) return e;
+    return e != cudaSuccess || !p.logits ? e : launch_cache_weights(p, s);
+}
+
+cudaError_t launch_cache_weights(const CacheAttnParams &p, cudaStream_t s) {
     const long long tiles = (long long)p.c.max_batch * ceil_div(p.most, kWeightTile);
     return launch_after(k_cache_weights, dim3((unsigned)(tiles < kWeightCtas ? tiles : kWeightCtas)), kWeightThreads, 0, 1, s, p);
 }

@@ -333,11 +333,57 @@ __global__ void __launch_bounds__(kSelThreads) k_cache_select(CacheEvictParams p
     }
 }
 
-constexpr int kMoveThreads = 512, kPer = 8;   // kPer 16-byte chunks of a thread in flight
-// gridDim.x CTAs (in place: a cluster) per sequence and `width` columns, a column being one of the 2 kv_heads head_chunks chunks
-// of a token's keys and values; the last group of columns: sizes and weights.  A thread has one column of rows `stride` apart.
+constexpr int kMoveThreads = 512, kPer = 8;   // kPer units of a thread in flight
+// `width` columns of a sequence's kept rows by a team of CTAs, a column being one of the 2 kv_heads * units units (16 bytes of keys
+// and values, 4 of scales) of a token.  A thread has one column of rows `stride` apart.
+template <bool kInPlace, typename U, typename Target>
+__device__ __forceinline__ void move_columns(const CacheEvictParams &p, const int2 plan, const unsigned *keep, Target target,
+                                             unsigned char *k, unsigned char *v, int units, int width, int group) {
+    const int tid = threadIdx.x, team = gridDim.x, member = blockIdx.x, m = plan.x;
+    const Cache &c = p.c;
+    const unsigned low = (1u << c.shift) - 1u;
+    const int stride = kMoveThreads / width, r0 = tid / width, step = stride * kPer, column = group * width + tid % width;
+    const int h2 = column / units, unit = column - h2 * units;
+    const bool idle = r0 >= stride || h2 >= 2 * c.kv_heads;
+    unsigned char *pool = (h2 < c.kv_heads ? k : v) + unit * sizeof(U);
+    const unsigned h = (unsigned)(h2 < c.kv_heads ? h2 : h2 - c.kv_heads);
+    auto row = [&](unsigned slot) {
+        return pool + (size_t)((((slot >> c.shift) * (unsigned)c.kv_heads + h) << c.shift) + (slot & low)) * units * sizeof(U);
+    };
+    U held[kPer];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int x = 0; x < kPer; ++x) {
+            const int i = i0 + r0 + x * stride;
+            if (!idle && i < m) held[x] = *reinterpret_cast<const U *>(row(keep[i]));
+        }
+    };
+    auto store = [&](int i0) {
+#pragma unroll
+        for (int x = 0; x < kPer; ++x) {
+            const int i = i0 + r0 + x * stride;
+            if (!idle && i < m) *reinterpret_cast<U *>(row(target(i))) = held[x];
+        }
+    };
+    for (int s0 = plan.y; s0 < m; s0 += team * step) {   // (the same number of steps for every member)
+        load(s0 + member * step);
+        if (kInPlace) {
+            cluster_arrive();
+            cluster_wait();
+        }
+        store(s0 + member * step);
+    }
+}
+
+// How the columns of one kind are dealt out: `width` of them a CTA, `groups` CTAs.
+struct Columns {
+    int units, width, groups;
+};
+
+// gridDim.x CTAs (in place: a cluster) per sequence and group of columns: the groups of keys and values, those of their scales, then
+// one for sizes and weights.
 template <bool kInPlace>
-__global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, int head_chunks, int width) {
+__global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams p, Columns rows, Columns scales) {
     const int b = blockIdx.z, tid = threadIdx.x, team = gridDim.x, member = blockIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
@@ -370,37 +416,8 @@ __global__ void __launch_bounds__(kMoveThreads, 2) k_cache_move(CacheEvictParams
         }
         return;
     }
-    const int stride = kMoveThreads / width, r0 = tid / width, step = stride * kPer, column = blockIdx.y * width + tid % width;
-    const int h2 = column / head_chunks, chunk = column - h2 * head_chunks;
-    const bool idle = r0 >= stride || h2 >= 2 * c.kv_heads;
-    unsigned char *pool = (h2 < c.kv_heads ? c.k : c.v) + chunk * 16;
-    const unsigned h = (unsigned)(h2 < c.kv_heads ? h2 : h2 - c.kv_heads);
-    auto row = [&](unsigned slot) {
-        return pool + (size_t)((((slot >> c.shift) * (unsigned)c.kv_heads + h) << c.shift) + (slot & low)) * head_chunks * 16;
-    };
-    uint4 v[kPer];
-    auto load = [&](int i0) {
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int i = i0 + r0 + k * stride;
-            if (!idle && i < m) v[k] = *reinterpret_cast<const uint4 *>(row(keep[i]));
-        }
-    };
-    auto store = [&](int i0) {
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int i = i0 + r0 + k * stride;
-            if (!idle && i < m) *reinterpret_cast<uint4 *>(row(target(i))) = v[k];
-        }
-    };
-    for (int s0 = plan.y; s0 < m; s0 += team * step) {   // (the same number of steps for every member)
-        load(s0 + member * step);
-        if (kInPlace) {
-            cluster_arrive();
-            cluster_wait();
-        }
-        store(s0 + member * step);
-    }
+    if ((int)blockIdx.y < rows.groups) move_columns<kInPlace, uint4>(p, plan, keep, target, c.k, c.v, rows.units, rows.width, blockIdx.y);
+    else move_columns<kInPlace, uint32_t>(p, plan, keep, target, p.s.k, p.s.v, scales.units, scales.width, (int)blockIdx.y - rows.groups);
 }
 
 // Lets a kernel have `smem` bytes of dynamic shared memory, asked for once per device.
@@ -425,9 +442,9 @@ cudaError_t launch_select(const CacheEvictParams &p, cudaStream_t s) {
 
 }  // namespace
 
-cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_t s) {
+cudaError_t launch_cache_evict(int row_bytes, const CacheEvictParams &p, cudaStream_t s) {
     if (p.c.max_batch == 0) return cudaSuccess;
-    const int head_chunks = p.c.dim * (dtype == FUSION_BF16 ? 2 : 4) / 16;
+    const int head_chunks = row_bytes / 16;
     // Threads of a sequence, by the room of a row of the page table, since its length is known on the device alone (64 sequences of
     // 500 with room for 512, 4096, 32768, in place to half: 16.9, 17.8, 43.4 us).  Few where it is short, since every warp more has its
     // share of the phases (8 x 577: 256 threads 7.9 us, 512 8.1), more where each would have many keys (64 x 1900: 21.4 and 20.8;
@@ -445,23 +462,30 @@ cudaError_t launch_cache_evict(int dtype, const CacheEvictParams &p, cudaStream_
     // heads of 80 float32: 33 us with one head a CTA), or half of them (not below 128 bytes) where a team in place would leave SMs
     // idle.  Then enough CTAs to fill the GPU a few times, no more than a sequence has steps for.
     const long long most = p.in_place ? p.c.capacity : (long long)p.pages_out << p.c.shift;
-    const int columns = 2 * p.c.kv_heads * head_chunks;
-    int width = head_chunks;
-    while (width < kMoveThreads && width < columns && (long long)(kMoveThreads / width) * kPer > most) width *= 2;
-    if (width > columns) width = columns;
-    if (width > kMoveThreads) width = kMoveThreads;
-    auto groups = [&] { return (columns + width - 1) / width; };
-    auto team_of = [&] { return (p.in_place ? 608ll : 2432ll) / ((long long)(groups() + 1) * p.c.max_batch); };
-    while (p.in_place && team_of() > 8 && width <= head_chunks && width >= 16 && width % 2 == 0) width /= 2;
-    const int step = kMoveThreads / width * kPer;
+    auto columns_of = [&](int units) {
+        Columns k{units, units, 0};
+        const int columns = 2 * p.c.kv_heads * units;
+        while (k.width < kMoveThreads && k.width < columns && (long long)(kMoveThreads / k.width) * kPer > most) k.width *= 2;
+        if (k.width > columns) k.width = columns;
+        if (k.width > kMoveThreads) k.width = kMoveThreads;
+        k.groups = (columns + k.width - 1) / k.width;
+        return k;
+    };
+    Columns rows = columns_of(head_chunks), scales = p.s.k ? columns_of(p.s.bytes / 4) : Columns{1, 1, 0};
+    auto team_of = [&] { return (p.in_place ? 608ll : 2432ll) / ((long long)(rows.groups + scales.groups + 1) * p.c.max_batch); };
+    while (p.in_place && team_of() > 8 && rows.width <= head_chunks && rows.width >= 16 && rows.width % 2 == 0) {
+        rows.width /= 2;
+        rows.groups = (2 * p.c.kv_heads * head_chunks + rows.width - 1) / rows.width;
+    }
+    const int step = kMoveThreads / rows.width * kPer;
     const long long steps = (most + step - 1) / step;
     long long team = team_of();
     if (team > steps) team = steps;
     if (p.in_place) team = team >= 8 ? 8 : team >= 4 ? 4 : team >= 2 ? 2 : 1;
     if (team < 1) team = 1;
-    const dim3 grid((unsigned)team, (unsigned)(groups() + 1), (unsigned)p.c.max_batch);
-    return p.in_place ? launch_after(k_cache_move<true>, grid, kMoveThreads, 0, (int)team, s, p, head_chunks, width)
-                      : launch_after(k_cache_move<false>, grid, kMoveThreads, 0, 1, s, p, head_chunks, width);
+    const dim3 grid((unsigned)team, (unsigned)(rows.groups + scales.groups + 1), (unsigned)p.c.max_batch);
+    return p.in_place ? launch_after(k_cache_move<true>, grid, kMoveThreads, 0, (int)team, s, p, rows, scales)
+                      : launch_after(k_cache_move<false>, grid, kMoveThreads, 0, 1, s, p, rows, scales);
 }
 
 }  // namespace fz

@@ -431,8 +431,8 @@ cudaError_t resident_ctas(int smem, int &ctas) {
     if (dev < kDevices) known[dev].store(ctas, std::memory_order_release);
     return cudaSuccess;
 }
-template <auto Kernel, int W>
-cudaError_t launch_rounds(int smem, const CacheAttnParams &p, int chunks, int tokens, cudaStream_t s) {
+template <auto Kernel, int W, typename P>
+cudaError_t launch_rounds(int smem, const P &p, int chunks, int tokens, cudaStream_t s) {
     int ctas = 0;
     const cudaError_t e = resident_ctas<Kernel, 32 * W>(smem, ctas);
     if (e != cudaSuccess) return e;

@@ -1,0 +1,76 @@
+// Numbers of the cache in 4 bits: e2m1 codes (a sign, two bits of exponent, one of mantissa: 0, 0.5, 1, 1.5, 2, 3, 4, 6), eight to
+// a word, and an e4m3 scale for 16 of them.  A product of the two has 6 significant bits and lies in 2^-10 .. 2688, so float16
+// holds it exactly.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace fz {
+
+// Bytes 0 .. 3 of w, each two codes, as two float16 each (the lower four bits in the lower half).
+__device__ __forceinline__ void codes_to_half(uint32_t w, uint32_t (&r)[4]) {
+    asm("{ .reg .b8 b0, b1, b2, b3;\n"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n"
+        "cvt.rn.f16x2.e2m1x2 %3, b3; }"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+        : "r"(w));
+}
+// The two scales in the lower bytes of w as float16.
+__device__ __forceinline__ uint32_t scales_to_half(uint32_t w) {
+    uint32_t r;
+    asm("{ .reg .b16 lo, hi; mov.b32 {lo, hi}, %1; cvt.rn.f16x2.e4m3x2 %0, lo; }" : "=r"(r) : "r"(w));
+    return r;
+}
+__device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float half_low(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
+__device__ __forceinline__ float half_high(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
+
+// A group of 16 numbers: its codes, eight to a word, and its scale's byte.
+//
+// A code is the e2m1 number nearest to x / scale, ties to the even code, which is what the conversion makes of the quotient if
+// the division's rounding neither leaves a tie nor makes one.  A scale has 4 significant bits and a tie lies at one of 3, so
+// scale * tie is exact, and where x is not equal to it the quotient is further from the tie than its own rounding: correctly
+// rounded it serves.  It comes of y = x / scale but for a few roundings and one correction by the exact remainder x - y scale.
+__device__ __forceinline__ uint2 quantise(const float (&x)[16], uint32_t &scale) {
+    uint32_t top = 0u;   // (as whole numbers magnitudes order NaN above infinity above the rest)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    const float want = __uint_as_float(top) * (1.0f / 6.0f);
+    uint16_t s;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(0.0f), "f"(want));
+    const float z = half_low(scales_to_half(s));
+    const bool fine = top < 0x7F800000u, some = fine && s != 0;
+    scale = fine ? (uint32_t)s : 0x7Fu;
+    const float inv = some ? __frcp_rn(z) : 0.0f;
+    float y[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float y0 = x[i] * inv;
+        const float y1 = fmaf(fmaf(-y0, z, x[i]), inv, y0);
+        y[i] = __uint_as_float((__float_as_uint(y1) & 0x7FFFFFFFu) | (__float_as_uint(x[i]) & 0x80000000u));   // (-0 stays -0)
+    }
+    uint32_t w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+        asm("{ .reg .b8 b0, b1, b2, b3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
+            "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
+            "mov.b32 %0, {b0, b1, b2, b3}; }"
+            : "=r"(w[h])
+            : "f"(y[8 * h]), "f"(y[8 * h + 1]), "f"(y[8 * h + 2]), "f"(y[8 * h + 3]), "f"(y[8 * h + 4]), "f"(y[8 * h + 5]),
+              "f"(y[8 * h + 6]), "f"(y[8 * h + 7]));
+    return make_uint2(some ? w[0] : 0u, some ? w[1] : 0u);
+}
+
+}  // namespace fz

@@ -212,6 +212,7 @@ const char *fusion_status_string(int code) {
         case FUSION_DEV_BAD_IDS: return "device: sample id out of range";
         case FUSION_DEV_TIMEOUT: return "device: a bounded wait timed out";
         case FUSION_DEV_BAD_CACHE: return "device: cache length or page id out of range, or no room";
+        case FUSION_DEV_BAD_POSITION: return "device: position outside the rotation's table";
         default: return "unknown status";
     }
 }
@@ -816,21 +817,24 @@ Cache dev(const fusion_cache &c) {
 
 // Rows `stride` elements apart, 16-byte aligned.
 bool good_stride(int dtype, int64_t stride) { return stride >= 0 && stride % (dtype == FUSION_BF16 ? 8 : 4) == 0; }
-}  // namespace
 
-extern "C" {
-
-size_t fusion_cache_workspace_size(fusion_cache cache, int32_t heads) {
-    if (check_cache(cache) != FUSION_OK || check_heads(cache, heads) != FUSION_OK) return 0;
-    return cache_ws(cache, heads).total;
+// ---- a cache in 4 bits
+int check_packed(const fusion_packed_cache &c) {
+    FZ_TRY(check_cache(c.cache));
+    return c.cache.head_dim % 32 ? FUSION_ERR_SHAPE : FUSION_OK;
+}
+int check_packed_pointers(const fusion_packed_cache &c) {
+    FZ_TRY(check_cache_pointers(c.cache));
+    return c.k_scales && c.v_scales && aligned16(c.k_scales) && aligned16(c.v_scales) ? FUSION_OK : FUSION_ERR_INVALID_ARG;
+}
+PackedScales scales(const fusion_packed_cache &c) {
+    return PackedScales{static_cast<unsigned char *>(c.k_scales), static_cast<unsigned char *>(c.v_scales), FUSION_PACKED_SCALE_BYTES(c.cache.head_dim)};
 }
 
-int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
-                        int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
-                        size_t workspace_bytes, int32_t *dev_status, void *stream) {
-    FZ_TRY(check_dtype(dtype));
-    FZ_TRY(check_cache(cache));
-    FZ_TRY(check_cache_pointers(cache));
+// ---- what the calls on either cache have in common, the cache's shape and pointers checked before
+int append_params(int dtype, const fusion_cache &cache, const fusion_ragged &in, const void *k, int64_t k_stride, const void *v,
+                  int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
+                  size_t workspace_bytes, int32_t *dev_status, CacheAppendParams &p) {
     if (!in.offsets) return FUSION_ERR_INVALID_ARG;
     if (in.max_batch < 0 || in.max_batch > cache.max_batch || in.max_tokens < 1) return FUSION_ERR_SHAPE;
     if (in.max_rows < 0 || in.max_rows > INT32_MAX) return FUSION_ERR_SHAPE;
@@ -840,7 +844,6 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
     if (!good_stride(dtype, k_stride) || !good_stride(dtype, v_stride)) return FUSION_ERR_INVALID_ARG;
     FZ_TRY(check_cache_ws(workspace, workspace_bytes, align256(sizeof(int) * (size_t)kWsCounters)));
     const int es = dtype == FUSION_BF16 ? 2 : 4;
-    CacheAppendParams p{};
     p.c = dev(cache);
     p.in = dev(in);
     p.k = static_cast<const unsigned char *>(k);
@@ -853,22 +856,31 @@ int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const v
     p.in_place = lengths_out == cache.lengths;
     p.counters = static_cast<int *>(workspace);
     p.status = dev_status;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const ProfileEvents ev = take_profile();
-    record(ev.start, s);
-    record(ev.mid, s);
-    const int rc = cuda_rc(launch_cache_append(dtype, p, s));
-    record(ev.end, s);
-    return rc;
+    return FUSION_OK;
 }
 
-int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
-                           int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
-                           int32_t *dev_status, void *stream) {
-    FZ_TRY(check_dtype(dtype));
-    FZ_TRY(check_cache(cache));
-    FZ_TRY(check_heads(cache, heads));
-    FZ_TRY(check_cache_pointers(cache));
+int rotation_params(int dtype, const fusion_cache &cache, const fusion_ragged &in, const fusion_rotation &r, const void *q,
+                    int64_t q_stride, int32_t heads, void *q_out, int unit, CacheStoreParams &p) {
+    if (!r.table || !aligned16(r.table) || !aligned4(r.positions)) return FUSION_ERR_INVALID_ARG;
+    if (r.pairs != FUSION_PAIRS_HALVES && r.pairs != FUSION_PAIRS_ADJACENT) return FUSION_ERR_INVALID_ARG;
+    if (r.table_rows < 1 || r.dims < unit || r.dims > cache.head_dim || r.dims % unit) return FUSION_ERR_SHAPE;
+    p.table = r.table;
+    p.table_rows = r.table_rows;
+    p.turned = r.dims;
+    p.positions = r.positions;
+    if (!q) return FUSION_OK;
+    if (heads < 1 || heads > FUSION_CACHE_MAX_HEADS) return FUSION_ERR_SHAPE;
+    if (!q_out || !aligned16(q) || !aligned16(q_out) || !good_stride(dtype, q_stride)) return FUSION_ERR_INVALID_ARG;
+    if (q_out == q && in.max_rows > 1 && q_stride != (int64_t)heads * cache.head_dim) return FUSION_ERR_INVALID_ARG;
+    p.q = static_cast<const unsigned char *>(q);
+    p.q_stride = q_stride * (dtype == FUSION_BF16 ? 2 : 4);
+    p.heads = heads;
+    p.q_out = static_cast<unsigned char *>(q_out);
+    return FUSION_OK;
+}
+
+int attention_params(int dtype, const fusion_cache &cache, const void *q, int64_t q_stride, int32_t heads, float scale, int32_t window,
+                     int32_t sinks, void *out, void *workspace, size_t workspace_bytes, int32_t *dev_status, CacheAttnParams &p) {
     if (!q || !out || !aligned16(q) || !aligned16(out) || !good_stride(dtype, q_stride)) return FUSION_ERR_INVALID_ARG;
     if (!aligned4(dev_status)) return FUSION_ERR_INVALID_ARG;
     const float scale2 = scale * 1.4426950408889634f;   // log2(e): logits are in base 2
@@ -876,7 +888,6 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
     const CacheWs L = cache_ws(cache, heads);
     FZ_TRY(check_cache_ws(workspace, workspace_bytes, L.total));
     unsigned char *wb = static_cast<unsigned char *>(workspace);
-    CacheAttnParams p{};
     p.c = dev(cache);
     p.q = q;
     p.q_stride = q_stride;
@@ -892,21 +903,12 @@ int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t
     p.lstride = L.lstride;
     p.counters = reinterpret_cast<int *>(wb + L.counters);
     p.status = dev_status;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const ProfileEvents ev = take_profile();
-    record(ev.start, s);
-    record(ev.mid, s);
-    const int rc = cuda_rc(launch_cache_attention(dtype, p, s));
-    record(ev.end, s);
-    return rc;
+    return FUSION_OK;
 }
 
-int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int32_t sinks, int32_t recent,
-                       const int32_t *page_table_out, int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx,
-                       int32_t keep_stride, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream) {
-    FZ_TRY(check_dtype(dtype));
-    FZ_TRY(check_cache(cache));
-    FZ_TRY(check_cache_pointers(cache));
+int evict_params(const fusion_cache &cache, const int32_t *budget, int32_t sinks, int32_t recent, const int32_t *page_table_out,
+                 int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx, int32_t keep_stride, void *workspace,
+                 size_t workspace_bytes, int32_t *dev_status, CacheEvictParams &p) {
     if (!cache.weights || !budget || !lengths_out || sinks < 0 || recent < 0) return FUSION_ERR_INVALID_ARG;
     if (!aligned4(budget, page_table_out, lengths_out, keep_idx, dev_status)) return FUSION_ERR_INVALID_ARG;
     if (keep_idx && keep_stride < 1) return FUSION_ERR_INVALID_ARG;
@@ -914,7 +916,6 @@ int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int
     const CacheWs L = cache_ws(cache, cache.kv_heads);
     FZ_TRY(check_cache_ws(workspace, workspace_bytes, L.total));
     unsigned char *wb = static_cast<unsigned char *>(workspace);
-    CacheEvictParams p{};
     p.c = dev(cache);
     p.budget = budget;
     p.sinks = sinks;
@@ -928,13 +929,169 @@ int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int
     p.plan = reinterpret_cast<int2 *>(wb + L.plan);
     p.keep = reinterpret_cast<unsigned *>(wb + L.keep);
     p.status = dev_status;
+    return FUSION_OK;
+}
+
+int read_params(const fusion_cache &cache, const fusion_ragged &in, const int32_t *starts, void *k_out, void *v_out, float *sizes_out,
+                float *weights_out, int32_t *dev_status, CacheReadParams &p) {
+    if (!in.offsets) return FUSION_ERR_INVALID_ARG;
+    if (in.max_batch < 0 || in.max_batch > FUSION_CACHE_MAX_BATCH || in.max_tokens < 1) return FUSION_ERR_SHAPE;
+    if (in.max_rows < 0 || in.max_rows > INT32_MAX) return FUSION_ERR_SHAPE;
+    if (!aligned16(k_out) || !aligned16(v_out)) return FUSION_ERR_INVALID_ARG;
+    if (!aligned4(in.offsets, in.batch, in.ids, starts, sizes_out, weights_out, dev_status)) return FUSION_ERR_INVALID_ARG;
+    p.c = dev(cache);
+    p.in = dev(in);
+    p.starts = starts;
+    p.k_out = static_cast<unsigned char *>(k_out);
+    p.v_out = static_cast<unsigned char *>(v_out);
+    p.sizes_out = sizes_out;
+    p.weights_out = weights_out;
+    p.status = dev_status;
+    return FUSION_OK;
+}
+
+// A launch between the events that a caller asked for.
+template <typename F> int launched(void *stream, F launch) {
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const ProfileEvents ev = take_profile();
     record(ev.start, s);
     record(ev.mid, s);
-    const int rc = cuda_rc(launch_cache_evict(dtype, p, s));
+    const int rc = cuda_rc(launch(s));
     record(ev.end, s);
     return rc;
+}
+}  // namespace
+
+extern "C" {
+
+size_t fusion_cache_workspace_size(fusion_cache cache, int32_t heads) {
+    if (check_cache(cache) != FUSION_OK || check_heads(cache, heads) != FUSION_OK) return 0;
+    return cache_ws(cache, heads).total;
+}
+
+int fusion_cache_append(int dtype, fusion_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                        int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
+                        size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_cache_pointers(cache));
+    CacheAppendParams p{};
+    FZ_TRY(append_params(dtype, cache, in, k, k_stride, v, v_stride, sizes, scores, lengths_out, workspace, workspace_bytes, dev_status, p));
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_append(dtype, p, s); });
+}
+
+int fusion_cache_append_rotated(int dtype, fusion_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                                int64_t v_stride, const float *sizes, const float *scores, fusion_rotation rotation,
+                                const void *q, int64_t q_stride, int32_t heads, void *q_out, int32_t *lengths_out,
+                                void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_cache_pointers(cache));
+    CacheStoreParams p{};
+    FZ_TRY(append_params(dtype, cache, in, k, k_stride, v, v_stride, sizes, scores, lengths_out, workspace, workspace_bytes, dev_status, p));
+    FZ_TRY(rotation_params(dtype, cache, in, rotation, q, q_stride, heads, q_out, 16, p));
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_store(dtype, rotation.pairs, p, s); });
+}
+
+int fusion_cache_attention(int dtype, fusion_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
+                           int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
+                           int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_heads(cache, heads));
+    FZ_TRY(check_cache_pointers(cache));
+    CacheAttnParams p{};
+    FZ_TRY(attention_params(dtype, cache, q, q_stride, heads, scale, window, sinks, out, workspace, workspace_bytes, dev_status, p));
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_attention(dtype, p, s); });
+}
+
+int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int32_t sinks, int32_t recent,
+                       const int32_t *page_table_out, int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx,
+                       int32_t keep_stride, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_cache_pointers(cache));
+    CacheEvictParams p{};
+    FZ_TRY(evict_params(cache, budget, sinks, recent, page_table_out, max_pages_out, lengths_out, keep_idx, keep_stride, workspace,
+                        workspace_bytes, dev_status, p));
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_evict(cache.head_dim * (dtype == FUSION_BF16 ? 2 : 4), p, s); });
+}
+
+int fusion_cache_read(int dtype, fusion_cache cache, fusion_ragged in, const int32_t *starts, void *k_out, void *v_out,
+                      float *sizes_out, float *weights_out, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_cache(cache));
+    FZ_TRY(check_cache_pointers(cache));
+    CacheReadParams p{};
+    FZ_TRY(read_params(cache, in, starts, k_out, v_out, sizes_out, weights_out, dev_status, p));
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_read(dtype, p, s); });
+}
+
+// ---- in 4 bits
+size_t fusion_packed_workspace_size(fusion_packed_cache cache, int32_t heads) {
+    return check_packed(cache) == FUSION_OK ? fusion_cache_workspace_size(cache.cache, heads) : 0;
+}
+
+int fusion_packed_append(int dtype, fusion_packed_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                         int64_t v_stride, const float *sizes, const float *scores, int32_t *lengths_out, void *workspace,
+                         size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_packed(cache));
+    FZ_TRY(check_packed_pointers(cache));
+    CacheStoreParams p{};
+    FZ_TRY(append_params(dtype, cache.cache, in, k, k_stride, v, v_stride, sizes, scores, lengths_out, workspace, workspace_bytes, dev_status, p));
+    p.s = scales(cache);
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_store(dtype, FUSION_PAIRS_HALVES, p, s); });
+}
+
+int fusion_packed_append_rotated(int dtype, fusion_packed_cache cache, fusion_ragged in, const void *k, int64_t k_stride, const void *v,
+                                 int64_t v_stride, const float *sizes, const float *scores, fusion_rotation rotation,
+                                 const void *q, int64_t q_stride, int32_t heads, void *q_out, int32_t *lengths_out,
+                                 void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_packed(cache));
+    FZ_TRY(check_packed_pointers(cache));
+    CacheStoreParams p{};
+    FZ_TRY(append_params(dtype, cache.cache, in, k, k_stride, v, v_stride, sizes, scores, lengths_out, workspace, workspace_bytes, dev_status, p));
+    FZ_TRY(rotation_params(dtype, cache.cache, in, rotation, q, q_stride, heads, q_out, 32, p));
+    p.s = scales(cache);
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_store(dtype, rotation.pairs, p, s); });
+}
+
+int fusion_packed_attention(int dtype, fusion_packed_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
+                            int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
+                            int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_packed(cache));
+    FZ_TRY(check_heads(cache.cache, heads));
+    FZ_TRY(check_packed_pointers(cache));
+    PackedAttnParams p{};
+    FZ_TRY(attention_params(dtype, cache.cache, q, q_stride, heads, scale, window, sinks, out, workspace, workspace_bytes, dev_status, p));
+    p.s = scales(cache);
+    return launched(stream, [&](cudaStream_t s) { return launch_packed_attention(dtype, p, s); });
+}
+
+int fusion_packed_evict(fusion_packed_cache cache, const int32_t *budget, int32_t sinks, int32_t recent, const int32_t *page_table_out,
+                        int32_t max_pages_out, int32_t *lengths_out, int32_t *keep_idx, int32_t keep_stride, void *workspace,
+                        size_t workspace_bytes, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_packed(cache));
+    FZ_TRY(check_packed_pointers(cache));
+    CacheEvictParams p{};
+    FZ_TRY(evict_params(cache.cache, budget, sinks, recent, page_table_out, max_pages_out, lengths_out, keep_idx, keep_stride, workspace,
+                        workspace_bytes, dev_status, p));
+    p.s = scales(cache);
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_evict(cache.cache.head_dim / 2, p, s); });
+}
+
+int fusion_packed_read(int dtype, fusion_packed_cache cache, fusion_ragged in, const int32_t *starts, void *k_out, void *v_out,
+                       float *sizes_out, float *weights_out, int32_t *dev_status, void *stream) {
+    FZ_TRY(check_dtype(dtype));
+    FZ_TRY(check_packed(cache));
+    FZ_TRY(check_packed_pointers(cache));
+    CacheReadParams p{};
+    FZ_TRY(read_params(cache.cache, in, starts, k_out, v_out, sizes_out, weights_out, dev_status, p));
+    p.s = scales(cache);
+    return launched(stream, [&](cudaStream_t s) { return launch_cache_read(dtype, p, s); });
 }
 
 }  // extern "C"

@@ -1,0 +1,554 @@
+// Attention of one new token per sequence over the paged cache in 4 bits (the formulas and the cut into rounds: cache_attn.cu, the
+// numbers: fp4.cuh), both products on the warp's matrix instruction m16n8k16 with float16 operands and float32 sums.
+//
+// As in bf16 the tokens are the M rows and the query heads the N columns: S^T = K Q^T, then O^T += V^T P^T.  What differs is how the
+// operands come about.  Codes and scales lie in shared memory as in the cache; a lane reads words of eight codes and makes its
+// own fragments: the conversion gives two dims of one token, which is what K's fragment needs, and a product with their scale.
+// V's fragment pairs the same dim of two tokens, so two tokens' words are interleaved by halves of a byte first.  Which
+// dims and tokens a fragment's rows and columns stand for is free as long as both operands agree:
+//   K: lane (g, t) has dims t DP/4 .. (t + 1) DP/4 - 1 of a row, and reads the same dims of head g's query, straight from memory;
+//   V: lane (g, t) has words g, g + 8, ..., of its four tokens, so its sums are of 8 dims in a row;
+//   tokens: row i of a tile is token order(i), so that the lanes' reads of both spread over the banks.
+// Values of the cache are exact in float16.  A query is not, so it enters times a power of two that brings its largest dim to
+// 2^14 .. 2^15 (float32 queries as the sum of two float16).  Probabilities are 2^(x - shift), at most 2^(kLag + kUp) = 2^15: kUp
+// keeps the small ones out of float16's subnormal numbers.  One float16 term (two for float32): its 11 bits lie 3 below the output's.
+//
+// What bounds it: memory (a token and key head: 9/8 dim bytes), closely followed by the issue of instructions: 6 for eight codes.
+#include <float.h>
+
+#include "cache_rounds.cuh"
+#include "fp4.cuh"
+
+namespace fz {
+namespace {
+
+using namespace rounds;
+
+constexpr float kUp = 7.0f;
+
+__device__ __forceinline__ uint32_t transpose8(uint32_t v) {   // an 8 x 8 matrix of b16, a row per four lanes
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_half(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t *>(&v);
+}
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void *src, bool read) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(read ? 4 : 0) : "memory");
+}
+__device__ __forceinline__ void cp_async8_zfill(uint32_t dst, const void *src, bool read) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(read ? 8 : 0) : "memory");
+}
+
+// The token of row i of a tile's half, and the place of 16-byte chunk c of row r: c ^ swizzle(r), linear in the bits of r.  A row of
+// codes is a quarter, a half or all of the banks wide; tokens and places are such that eight lanes that read K (two rows of
+// a half, 16 bytes each; four rows of a quarter) and all lanes that read V (a word of eight lanes of every other row) meet no bank twice.
+template <int DP> __device__ __forceinline__ int order(int i) {
+    if constexpr (DP == 64) {
+        const int high = i >> 2, two = (i & 1) << 1 | (i >> 1 & 1);
+        return high << 2 | (two ^ (high << 1));              // 0 2 1 3 6 4 7 5
+    } else {
+        return i & 1 ? 4 + (i >> 1 ^ 1) : i >> 1;            // 0 5 1 4 2 7 3 6
+    }
+}
+template <int DP> __device__ __forceinline__ int swizzle(int r) {
+    return DP == 64 ? 0 : DP == 128 ? r & 2 : (r & 3) << 1 | (r >> 2 & 1);
+}
+
+// Shared memory of a CTA: per warp S stages of TT rows of K's and of V's codes and of their scales; the tokens' log2 sizes; then,
+// at the end of a (sequence, key head), the warps' outputs on their way to each other, 64 dims at a time.
+template <int DP, int NT, int TT, int S, int W>
+struct Layout {
+    static constexpr int kNq = 8 * NT, kRow = DP / 2, kScales = DP / 16, kStage = 2 * TT * (kRow + kScales);
+    static constexpr int kPitch = 64 + 8;
+    static constexpr int kLsz = W * S * kStage;
+    static constexpr int kShared = kLsz + W * S * TT * 4;
+    static constexpr int kJoinBytes = W * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
+    static constexpr int kTotal = kShared + (kJoinBytes > kScratch ? kJoinBytes : kScratch);
+};
+
+// The tokens of the rounds to come (rounds::Stream), their rows in 4 bits.
+template <int DP, int TT, int W>
+struct PackedStream : Stream<unsigned char, DP / 2, TT, W> {
+    using Base = Stream<unsigned char, DP / 2, TT, W>;
+    static constexpr int kRow = DP / 2, kScales = DP / 16, kCpr = kRow / 16, kStage = 2 * TT * (kRow + kScales);
+
+    __device__ __forceinline__ void ask(const PackedAttnParams &p, const Token &t, float size, int lane, unsigned char *stage, float *lsz) {
+        const bool live = t.place >= 0 && size != 0.0f;
+        const unsigned row = live ? ((t.page * (unsigned)p.c.kv_heads + (unsigned)t.h) << p.c.shift) + (unsigned)t.place : 0u;
+        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live), row_bytes = (unsigned)p.c.dim / 2;
+        if (lane < TT) lsz[lane] = t.place == -2 ? kNoPage : live ? log2f(size) : -INFINITY;
+        constexpr int kWide = 32 / kCpr;   // rows of a step
+        const int r_lane = lane / kCpr, cc = lane % kCpr;
+        const bool exists = (unsigned)cc * 16u < row_bytes;
+        const unsigned mine = exists ? lives >> r_lane : 0u;
+        const unsigned char *k = p.c.k + (exists ? cc : 0) * 16, *v = p.c.v + (exists ? cc : 0) * 16;
+        const uint32_t dst = smem_addr(stage) + r_lane * kRow, at = (uint32_t)(cc ^ swizzle<DP>(r_lane)) * 16u;
+#pragma unroll
+        for (int e = 0; e < TT / kWide; ++e) {
+            const size_t off = (size_t)__shfl_sync(0xFFFFFFFFu, row, e * kWide + r_lane) * row_bytes;
+            const bool read = mine >> (e * kWide) & 1u;
+            const uint32_t to = dst + e * kWide * kRow + (at ^ (uint32_t)(swizzle<DP>(e * kWide) * 16));
+            cp_async16_zfill(to, k + off, read);
+            cp_async16_zfill(to + TT * kRow, v + off, read);
+        }
+        if (lane < TT) {
+            const uint32_t ks = smem_addr(stage) + 2 * TT * kRow + lane * kScales, vs = ks + TT * kScales;
+            const size_t off = (size_t)row * (unsigned)p.s.bytes;
+            if constexpr (kScales == 4) {
+                cp_async4_zfill(ks, p.s.k + off, live);
+                cp_async4_zfill(vs, p.s.v + off, live);
+            } else if constexpr (kScales == 8) {
+                cp_async8_zfill(ks, p.s.k + off, live);
+                cp_async8_zfill(vs, p.s.v + off, live);
+            } else {   // rows of 12 or 16 bytes
+#pragma unroll
+                for (int e = 0; e < kScales; e += 4) {
+                    const bool read = live && e < p.s.bytes;
+                    cp_async4_zfill(ks + e, p.s.k + (read ? off + e : 0), read);
+                    cp_async4_zfill(vs + e, p.s.v + (read ? off + e : 0), read);
+                }
+            }
+        }
+        cp_async_commit();
+    }
+    __device__ __forceinline__ void next(const PackedAttnParams &p, int chunks, int warp, int lane, unsigned char *stage, float *lsz) {
+        ask(p, this->t0, this->size0, lane, stage, lsz);
+        this->t0 = this->t1;
+        this->size0 = this->size_of(p, this->t0);
+        this->t1 = this->look_up(p, chunks, warp, lane);
+    }
+    template <int S>
+    __device__ __forceinline__ void begin(const PackedAttnParams &p, const Place &at, const Run &run, int chunks, int warp, int lane,
+                                          unsigned char *stages, float *lsz) {
+        this->ahead = at;
+        this->ahead_r = run.r0;
+        this->r1 = run.r1;
+        Token t[S + 1];
+        float size[S];
+#pragma unroll
+        for (int s = 0; s <= S; ++s) t[s] = this->look_up(p, chunks, warp, lane);
+#pragma unroll
+        for (int s = 0; s < S; ++s) size[s] = this->size_of(p, t[s]);
+#pragma unroll
+        for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], lane, stages + s * kStage, lsz + s * TT);
+        this->t0 = t[S - 1];
+        this->size0 = size[S - 1];
+        this->t1 = t[S];
+    }
+};
+
+template <int N> __device__ __forceinline__ void load_words(const unsigned char *src, uint32_t (&w)[N]) {   // aligned to their size, or 16
+    if constexpr (N == 1) {
+        w[0] = *reinterpret_cast<const uint32_t *>(src);
+    } else if constexpr (N == 2) {
+        const uint2 v = *reinterpret_cast<const uint2 *>(src);
+        w[0] = v.x, w[1] = v.y;
+    } else {
+        static_assert(N == 4, "up to 16 bytes");
+        const uint4 v = *reinterpret_cast<const uint4 *>(src);
+        w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    }
+}
+// Two numbers of a row.
+__device__ __forceinline__ float2 load2(const __nv_bfloat16 *src, int i) {
+    const uint32_t w = reinterpret_cast<const uint32_t *>(src)[i];
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+}
+__device__ __forceinline__ float2 load2(const float *src, int i) { return reinterpret_cast<const float2 *>(src)[i]; }
+
+// T: type of queries and output.  W: warps of a CTA.
+template <typename T, int DP, int NT, int TT, int S, int W>
+__global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4 : 2) k_packed_attn(PackedAttnParams p, int chunks) {
+    using L = Layout<DP, NT, TT, S, W>;
+    constexpr int kThreads = 32 * W, kTerms = sizeof(T) == 4 ? 2 : 1;
+    constexpr int kNq = L::kNq, kRound = W * TT, kRow = L::kRow, kScales = L::kScales, kKs = DP / 16, kMt = TT / 16;
+    constexpr int kKw = DP / 32, kVw = DP / 64;   // words of a K row and of a V row that a lane has
+    extern __shared__ __align__(128) unsigned char sm[];
+    __shared__ Finder<kThreads> finder;
+    __shared__ float s_m[W][kNq], s_l[W][kNq];
+    __shared__ int s_bad, s_last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const Cache &c = p.c;
+    wait_for_previous();
+    Run run;
+    Place at;
+    if (!find_run<kThreads, true, false>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
+        empty_sequences<T, kThreads>(p);
+        return;
+    }
+    const unsigned r0 = run.r0, r1 = run.r1;
+
+    unsigned char *stages = sm + warp * S * L::kStage;
+    float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
+    float *join = reinterpret_cast<float *>(sm + L::kShared);
+    PackedStream<DP, TT, W> in;
+    in.template begin<S>(p, at, run, chunks, warp, lane, stages, lsz);
+    empty_sequences<T, kThreads>(p);
+    if (tid == 0) s_bad = 0;
+    __syncthreads();
+
+    // scales behind the last dim: zero, whatever the cache holds there
+    uint32_t k_mask = 0u, v_mask[kVw];
+#pragma unroll
+    for (int i = 0; i < kVw; ++i) {
+        if ((t * kVw + i) * 16 < c.dim) k_mask |= 0xFFu << (8 * i);
+        v_mask[i] = (g / 2 + 4 * i) * 16 < c.dim ? 0xFFFFu : 0u;
+    }
+    const uint32_t v_pick = (uint32_t)(g / 2) | (uint32_t)(4 + g / 2) << 4;   // a byte of each of two words
+
+    float m[NT][2], l[NT][2], factor[NT][2], o[kKs][NT][4];
+    uint32_t qf[kTerms][kKs][NT][2];
+    bool bad = false;
+    auto begin_head = [&]() {
+        const int heads = min(kNq, p.group - at.ch * kNq);
+        const T *src = reinterpret_cast<const T *>(p.q) + (size_t)at.b * p.q_stride + (size_t)(at.h * p.group + at.ch * kNq) * c.dim;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float2 q[2 * kKs];
+            uint32_t top = 0u;
+#pragma unroll
+            for (int i = 0; i < 2 * kKs; ++i) {
+                const int d = t * (DP / 4) + 2 * i;
+                q[i] = 8 * n + g < heads && d < c.dim ? load2(src + (size_t)(8 * n + g) * c.dim, d / 2) : make_float2(0.0f, 0.0f);
+                top = max(top, max(__float_as_uint(q[i].x) & 0x7FFFFFFFu, __float_as_uint(q[i].y) & 0x7FFFFFFFu));
+            }
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+            top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+            // the largest dim to 2^14 .. 2^15; queries below 2^-99 stay small, and their logits nothing
+            const int up = min(14 + 127 - (int)(top >> 23), 113);
+            const float f = __int_as_float((127 + up) << 23);
+#pragma unroll
+            for (int i = 0; i < 2 * kKs; ++i) {
+                const float x = q[i].x * f, y = q[i].y * f;
+                const uint32_t h = pack_half(x, y);
+                qf[0][i / 2][n][i & 1] = h;
+                if constexpr (kTerms == 2) qf[kTerms - 1][i / 2][n][i & 1] = pack_half(x - half_low(h), y - half_high(h));
+            }
+            const float back = fminf(fmaxf(p.scale2 * __int_as_float((127 - up) << 23), -FLT_MAX), FLT_MAX);   // (infinity times 0 is NaN)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                factor[n][e] = __shfl_sync(0xFFFFFFFFu, back, (2 * t + e) * 4);
+                m[n][e] = kLow;
+                l[n][e] = 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < kKs; ++k) o[k][n][0] = o[k][n][1] = o[k][n][2] = o[k][n][3] = 0.0f;
+        }
+    };
+    begin_head();
+    int st = 0;
+    unsigned seg0 = r0 - at.u;   // first round of the (sequence, key head)
+    for (unsigned r = r0;; ++r) {
+        __syncwarp();
+        const int next_st = st == 0 ? S - 1 : st - 1;
+        in.next(p, chunks, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT);
+        cp_async_wait<S - 1>();
+        __syncwarp();
+
+        const unsigned char *ks = stages + st * L::kStage, *vs = ks + TT * kRow, *kz = vs + TT * kRow, *vz = kz + TT * kScales;
+        const float *lz = lsz + st * TT;
+        const int j0 = at.u * kRound + warp * TT;
+        const int nq = min(kNq, p.group - at.ch * kNq), head0 = at.h * p.group + at.ch * kNq;
+        if (j0 < at.vis) {
+            // ---- S^T = K Q^T
+            float x[kMt][NT][4];
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) x[i][n][0] = x[i][n][1] = x[i][n][2] = x[i][n][3] = 0.0f;
+                uint32_t kw[2][kKw], sc[2][kVw];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int row = 16 * i + 8 * h + order<DP>(g);
+                    const unsigned char *from = ks + row * kRow;
+                    if constexpr (DP == 64) {
+                        load_words<2>(from + 8 * t, kw[h]);
+                    } else if constexpr (DP == 128) {
+                        load_words<4>(from + ((t ^ swizzle<DP>(row)) << 4), kw[h]);
+                    } else {
+                        uint32_t a[4], b[4];
+                        load_words<4>(from + (((2 * t) ^ swizzle<DP>(row)) << 4), a);
+                        load_words<4>(from + (((2 * t + 1) ^ swizzle<DP>(row)) << 4), b);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) kw[h][j] = a[j], kw[h][kKw - 4 + j] = b[j];
+                    }
+                    const unsigned char *scales = kz + row * kScales + t * kVw;
+                    if constexpr (DP == 64) {
+                        sc[h][0] = scales_to_half((*scales & k_mask) * 0x0101u);
+                    } else if constexpr (DP == 128) {
+                        const uint32_t two = scales_to_half(*reinterpret_cast<const unsigned short *>(scales) & k_mask);
+                        sc[h][0] = __byte_perm(two, two, 0x1010);
+                        sc[h][1] = __byte_perm(two, two, 0x3232);
+                    } else {
+                        const uint32_t four = *reinterpret_cast<const uint32_t *>(scales) & k_mask;
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t two = scales_to_half(four >> (16 * j));
+                            sc[h][2 * j] = __byte_perm(two, two, 0x1010);
+                            sc[h][2 * j + 1] = __byte_perm(two, two, 0x3232);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kKw; ++j) {
+                    uint32_t a[2][4];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        codes_to_half(kw[h][j], a[h]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) a[h][e] = mul_half2(a[h][e], sc[h][j / 2]);
+                    }
+#pragma unroll
+                    for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int term = 0; term < kTerms; ++term)
+                                mma_f16_16816(x[i][n], a[0][2 * kk], a[1][2 * kk], a[0][2 * kk + 1], a[1][2 * kk + 1],
+                                              qf[term][2 * j + kk][n][0], qf[term][2 * j + kk][n][1]);
+                }
+            }
+            // ---- logits in base 2; a masked token's are -inf
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+                const int at0 = 16 * i + order<DP>(g), at1 = at0 + 8;
+                const float z0 = lz[at0], z1 = lz[at1];
+                const bool off0 = z0 == -INFINITY || z0 == kNoPage, off1 = z1 == -INFINITY || z1 == kNoPage;
+                bad |= z0 == kNoPage || z1 == kNoPage;
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    x[i][n][0] = off0 ? -INFINITY : fmaf(x[i][n][0], factor[n][0], z0);
+                    x[i][n][1] = off0 ? -INFINITY : fmaf(x[i][n][1], factor[n][1], z0);
+                    x[i][n][2] = off1 ? -INFINITY : fmaf(x[i][n][2], factor[n][0], z1);
+                    x[i][n][3] = off1 ? -INFINITY : fmaf(x[i][n][3], factor[n][1], z1);
+                }
+                if (p.logits) {
+                    float *dst = p.logits + ((size_t)at.b * p.heads + head0) * p.lstride + j0;
+                    const bool in0 = j0 + at0 < at.vis, in1 = j0 + at1 < at.vis;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (8 * n + 2 * t + e < nq) {
+                                if (in0) dst[(8 * n + 2 * t + e) * p.lstride + at0] = x[i][n][e];
+                                if (in1) dst[(8 * n + 2 * t + e) * p.lstride + at1] = x[i][n][2 + e];
+                            }
+                }
+            }
+            // ---- the running shift: kUp below the largest logit when it was set; where a logit exceeds that by kLag, it moves, and O
+            // and the sums follow
+            float mx[NT][2];
+            bool grows = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    mx[n][e] = fmaxf(x[0][n][e], x[0][n][2 + e]);
+#pragma unroll
+                    for (int i = 1; i < kMt; ++i) mx[n][e] = fmaxf(mx[n][e], fmaxf(x[i][n][e], x[i][n][2 + e]));
+                    grows |= mx[n][e] > m[n][e] + (kUp + kLag);
+                }
+            if (__any_sync(0xFFFFFFFFu, grows)) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int s = 4; s < 32; s <<= 1) mx[n][e] = fmaxf(mx[n][e], __shfl_xor_sync(0xFFFFFFFFu, mx[n][e], s));
+                        const float to = fmaxf(m[n][e], mx[n][e] - kUp), f = ex2(m[n][e] - to);
+                        m[n][e] = to;
+                        l[n][e] *= f;
+#pragma unroll
+                        for (int k = 0; k < kKs; ++k) {
+                            o[k][n][e] *= f;
+                            o[k][n][2 + e] *= f;
+                        }
+                    }
+            }
+            // ---- O^T += V^T P^T
+#pragma unroll
+            for (int i = 0; i < kMt; ++i) {
+                uint32_t b[kTerms][NT][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float p0 = ex2(x[i][n][0] - m[n][0]), p1 = ex2(x[i][n][1] - m[n][1]);
+                    const float p2 = ex2(x[i][n][2] - m[n][0]), p3 = ex2(x[i][n][3] - m[n][1]);
+                    l[n][0] += p0 + p2;
+                    l[n][1] += p1 + p3;
+                    const uint32_t h0 = pack_half(p0, p1), h1 = pack_half(p2, p3);
+                    b[0][n][0] = transpose8(h0);
+                    b[0][n][1] = transpose8(h1);
+                    if constexpr (kTerms == 2) {
+                        b[kTerms - 1][n][0] = transpose8(pack_half(p0 - half_low(h0), p1 - half_high(h0)));
+                        b[kTerms - 1][n][1] = transpose8(pack_half(p2 - half_low(h1), p3 - half_high(h1)));
+                    }
+                }
+                uint32_t vw[4][kVw], sz[4][kVw];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int row = 16 * i + 8 * (j >> 1) + order<DP>(2 * t + (j & 1));
+#pragma unroll
+                    for (int w = 0; w < kVw; ++w)
+                        vw[j][w] = *reinterpret_cast<const uint32_t *>(vs + row * kRow + (((g / 4 + 2 * w) ^ swizzle<DP>(row)) << 4) + (g & 3) * 4);
+                    load_words<kVw>(vz + row * kScales, sz[j]);
+                }
+#pragma unroll
+                for (int w = 0; w < kVw; ++w) {
+                    uint32_t a[4][4];   // fragment registers of four steps of 16 dims
+#pragma unroll
+                    for (int pair = 0; pair < 2; ++pair) {
+                        const uint32_t u = vw[2 * pair][w], v = vw[2 * pair + 1][w];
+                        const uint32_t s = scales_to_half(__byte_perm(sz[2 * pair][w], sz[2 * pair + 1][w], v_pick) & v_mask[w]);
+                        codes_to_half((u & 0x0F0F0F0Fu) | (v << 4 & 0xF0F0F0F0u), a[2 * pair]);       // even dims
+                        codes_to_half((u >> 4 & 0x0F0F0F0Fu) | (v & 0xF0F0F0F0u), a[2 * pair + 1]);   // odd dims
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            a[2 * pair][e] = mul_half2(a[2 * pair][e], s);
+                            a[2 * pair + 1][e] = mul_half2(a[2 * pair + 1][e], s);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int term = 0; term < kTerms; ++term)
+                                mma_f16_16816(o[4 * w + e][n], a[0][e], a[1][e], a[2][e], a[3][e], b[term][n][0], b[term][n][1]);
+                }
+            }
+        }
+
+        // ---- the end of a (sequence, key head), or of the run: the warps' results together
+        if (at.u + 1 == at.rounds || r + 1 == r1) {
+            if (__any_sync(0xFFFFFFFFu, bad) && lane == 0) atomicOr(&s_bad, 1);
+            bad = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                    for (int s = 4; s < 32; s <<= 1) l[n][e] += __shfl_xor_sync(0xFFFFFFFFu, l[n][e], s);
+                    if (g == 0) {
+                        s_m[warp][8 * n + 2 * t + e] = m[n][e];
+                        s_l[warp][8 * n + 2 * t + e] = l[n][e];
+                    }
+                }
+            __syncthreads();
+            const bool whole = seg0 >= r0 && seg0 + at.rounds <= r1, seg_bad = s_bad != 0;
+            const size_t head = (size_t)at.b * p.heads + head0, slot = (size_t)(2 * blockIdx.x + (seg0 >= r0 ? 1 : 0)) * kNq;   // of a partial result
+            float f[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float M = s_m[0][8 * n + 2 * t + e];
+#pragma unroll
+                    for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][8 * n + 2 * t + e]);
+                    f[n][e] = ex2(m[n][e] - M);
+                }
+            // a thread joins four dims of kMine heads per step of 64 dims
+            constexpr int kMine = (kNq * 16 + kThreads - 1) / kThreads;
+            float sums[kMine];
+#pragma unroll
+            for (int y = 0; y < kMine; ++y) {
+                const int e = y * kThreads + tid, q = min(e / 16, kNq - 1);
+                float M = s_m[0][q], ls = 0.0f;
+#pragma unroll
+                for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][q]);
+#pragma unroll
+                for (int w = 0; w < W; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
+                sums[y] = ls;
+                if (e < 16 * nq && e % 16 == 0) {
+                    if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                    else if (p.logits) p.lse[head + q] = log_sum(M, seg_bad ? -1.0f : ls);
+                }
+            }
+#pragma unroll
+            for (int w0 = 0; w0 < kVw; ++w0) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        if (8 * n + 2 * t + e >= nq) break;
+                        float *to = join + (warp * kNq + 8 * n + 2 * t + e) * L::kPitch + 8 * g;
+#pragma unroll
+                        for (int k = 0; k < 4; k += 2)
+                            *reinterpret_cast<float4 *>(to + 2 * k) =
+                                make_float4(o[4 * w0 + k][n][e] * f[n][e], o[4 * w0 + k][n][2 + e] * f[n][e],
+                                            o[4 * w0 + k + 1][n][e] * f[n][e], o[4 * w0 + k + 1][n][2 + e] * f[n][e]);
+                    }
+                __syncthreads();
+#pragma unroll
+                for (int y = 0; y < kMine; ++y) {
+                    const int e = y * kThreads + tid, q = e / 16, d0 = e % 16 * 4, d = 64 * w0 + d0;
+                    if (q >= nq || d >= c.dim) continue;
+                    float4 sum = *reinterpret_cast<const float4 *>(join + q * L::kPitch + d0);
+#pragma unroll
+                    for (int w = 1; w < W; ++w) {
+                        const float4 v = *reinterpret_cast<const float4 *>(join + (w * kNq + q) * L::kPitch + d0);
+                        sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
+                    }
+                    const float inv = 1.0f / sums[y];
+                    if (!whole)
+                        *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
+                    else if (!seg_bad)
+                        store4(reinterpret_cast<T *>(p.out) + (head + q) * c.dim + d,
+                               sums[y] == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+                }
+                __syncthreads();
+            }
+            if (tid == 0) {
+                if (seg_bad) raise_status(p.status, FUSION_DEV_BAD_CACHE);
+                s_bad = 0;
+            }
+            if (!whole) {
+                join_runs<T, kNq, kThreads>(p, run, seg0, seg0 + at.rounds, head, nq, join, s_last);
+                __syncthreads();
+            }
+            if (r + 1 == r1) break;
+            place_next(p, at, kRound, c.kv_heads, chunks);
+            __syncthreads();
+            begin_head();
+            seg0 = r + 1;
+        } else {
+            place_next(p, at, kRound, c.kv_heads, chunks);
+        }
+        if (++st == S) st = 0;
+    }
+    cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)
+}
+
+template <typename T, int DP, int NT, int TT, int S>
+cudaError_t launch(const PackedAttnParams &p, cudaStream_t s) {
+    static_assert(counts_fit(TT, 4) && (DP > 128 || counts_fit(TT, 1)), "rounds are counted in 32 bits");
+    const int chunks = ceil_div(p.group, 8 * NT);
+    if constexpr (DP <= 128)
+        if (warps_alone(p, chunks)) return launch_rounds<k_packed_attn<T, DP, NT, TT, S, 1>, 1>(Layout<DP, NT, TT, S, 1>::kTotal, p, chunks, TT, s);
+    return launch_rounds<k_packed_attn<T, DP, NT, TT, S, 4>, 4>(Layout<DP, NT, TT, S, 4>::kTotal, p, chunks, 4 * TT, s);
+}
+template <typename T, int NT>
+cudaError_t launch_dim(const PackedAttnParams &p, cudaStream_t s) {
+    if (p.c.dim <= 64) return launch<T, 64, NT, 32, 3>(p, s);
+    if (p.c.dim <= 128) return launch<T, 128, NT, 32, 3>(p, s);
+    return launch<T, 256, NT, 16, 3>(p, s);
+}
+
+}  // namespace
+
+cudaError_t launch_packed_attention(int dtype, const PackedAttnParams &p, cudaStream_t s) {
+    if (p.c.max_batch == 0) return cudaSuccess;
+    const cudaError_t e = dtype == FUSION_BF16 ? (p.group <= 8 ? launch_dim<__nv_bfloat16, 1>(p, s) : launch_dim<__nv_bfloat16, 2>(p, s))
+                                               : launch_dim<float, 1>(p, s);
+    return e != cudaSuccess || !p.logits ? e : launch_cache_weights(p, s);
+}
+
+}  // namespace fz

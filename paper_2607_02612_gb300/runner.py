@@ -5,6 +5,7 @@ every step of the computation runs in libfusion.so.
 from __future__ import annotations
 
 from dataclasses import dataclass, field
+from types import SimpleNamespace
 from typing import Dict, List, Optional
 
 import numpy as np
@@ -139,6 +140,25 @@ def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str,
     return t.data_ptr()
 
 
+def _rows_here(c, rows) -> None:
+    if any(t is not None and t.get_device() != c.index for t in (rows.offsets, rows.batch, rows.ids)):
+        raise fb.FusionError(f"the rows' offsets, count and ids on the cache's device ({c.index}) expected")
+
+
+def _append_args(c, k, v, rows, sizes, scores, lengths_out):
+    """The rows of an append, checked, and their addresses and strides."""
+    if rows is None:
+        rows = c.one_row_each()
+    else:
+        _rows_here(c, rows)
+    kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "keys")
+    vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "values")
+    zp = _need(sizes, torch.float32, c.index, "sizes", rows.max_rows)
+    wp = _need(scores, torch.float32, c.index, "scores", rows.max_rows)
+    op = _need(lengths_out, torch.int32, c.index, "lengths_out", c.max_batch)
+    return rows, kp, ks, vp, vs, zp, wp, op
+
+
 def _tokens(n: int, what: str) -> int:
     """A number of tokens for the C ABI; one that its 32 bits do not hold is more than any cache has, and means all."""
     if n < 0:
@@ -163,8 +183,15 @@ class DeviceCache:
     ws_bytes: int = field(init=False)
 
     def __post_init__(self):
-        pages, kv_heads, page_tokens, dim = self.k.shape
-        ok = self.k.dtype == self.v.dtype == TORCH_DTYPE[self.dtype] and self.v.shape == self.k.shape
+        self._check_and_fill(TORCH_DTYPE[self.dtype], 1)
+        self.ws_bytes = fb.fusion_cache_workspace_size(self._c, self.heads)
+        self._scratch()
+
+    def _check_and_fill(self, stored: torch.dtype, per: int):
+        """Checks the tensors, whose rows have `per` dims to an element of type `stored`; the C struct and what calls need."""
+        pages, kv_heads, page_tokens, row = self.k.shape
+        dim = row * per
+        ok = self.k.dtype == self.v.dtype == stored and self.v.shape == self.k.shape
         ok = ok and self.page_table.dim() == 2 and self.page_table.dtype == torch.int32
         ok = ok and self.lengths.shape == self.page_table.shape[:1] and self.lengths.dtype == torch.int32
         for t in (self.sizes, self.weights):
@@ -179,25 +206,77 @@ class DeviceCache:
             raise fb.FusionError("device tensors expected")
         self._c = fb.cache(self.max_batch, self.max_pages, page_tokens, kv_heads, dim, pages, self.k, self.v, self.sizes,
                            self.weights, self.page_table, self.lengths)
-        self.ws_bytes = fb.fusion_cache_workspace_size(self._c, self.heads)
-        if self.ws_bytes == 0:
-            raise fb.FusionError("cache shape or number of heads out of range")
-        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.k.device)
-        self.workspace[:1 << 18].zero_()   # the counters; the rest need not be zero
         self.device, self.index = self.k.device, self.k.get_device()
         self.code, self.torch_dtype = DTYPE_CODE[self.dtype], TORCH_DTYPE[self.dtype]
         self.scale = self.head_dim ** -0.5
         self.lib = fb.load()
+
+    def _scratch(self):
+        if self.ws_bytes == 0:
+            raise fb.FusionError("cache shape or number of heads out of range")
+        self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.k.device)
+        self.workspace[:1 << 18].zero_()   # the counters; the rest need not be zero
         self._ws = self.workspace.data_ptr()
         self._one = RaggedRows(self.max_batch, 1, self.max_batch,
                                torch.arange(self.max_batch + 1, dtype=torch.int32, device=self.device))
 
-    def c_struct(self) -> fb.fusion_cache:
+    def c_struct(self):
         return self._c
 
     def one_row_each(self) -> RaggedRows:
         """A row per sequence, in the sequences' order."""
         return self._one
+
+
+@dataclass
+class DevicePackedCache(DeviceCache):
+    """The same with keys and values in 4 bits (fusion_packed_cache): k and v [num_pages, kv_heads, page_tokens, head_dim / 2]
+    bytes of two codes each, and the scales of 16 dims each.  dtype: the type of the rows, queries and results of the calls.
+    All of Fusion's cache calls take either cache."""
+    k_scales: Optional[torch.Tensor] = None   # [num_pages, kv_heads, page_tokens, scale bytes of a row] uint8
+    v_scales: Optional[torch.Tensor] = None
+
+    def __post_init__(self):
+        self._check_and_fill(torch.uint8, 2)
+        shape = (*self.k.shape[:3], fb.packed_scale_bytes(self.head_dim))
+        for t in (self.k_scales, self.v_scales):
+            if t is None or t.dtype != torch.uint8 or t.shape != shape or t.device != self.k.device:
+                raise fb.FusionError(f"scales: uint8 tensors of shape {shape} on the cache's device expected")
+        self._c = fb.packed_cache(self._c, self.k_scales, self.v_scales)
+        self.ws_bytes = fb.fusion_packed_workspace_size(self._c, self.heads)
+        lib = fb.load()
+        self.lib = SimpleNamespace(   # the calls on this cache under the names of the others'
+            fusion_cache_append=lib.fusion_packed_append, fusion_cache_append_rotated=lib.fusion_packed_append_rotated,
+            fusion_cache_attention=lib.fusion_packed_attention, fusion_cache_read=lib.fusion_packed_read,
+            fusion_cache_evict=lambda dtype, *args: lib.fusion_packed_evict(*args))
+        self._scratch()
+
+
+@dataclass(frozen=True)
+class Rotation:
+    """Rotation of keys and queries (fusion_rotation): the table [positions, dims] float32 of each position's dims / 2 cosines,
+    then as many sines, and which dims turn together: "halves" (i and i + dims / 2) or "adjacent" (2 i and 2 i + 1)."""
+    table: torch.Tensor
+    pairs: str = "halves"
+
+    def __post_init__(self):
+        if self.pairs not in ("halves", "adjacent"):
+            raise fb.FusionError('pairs: "halves" or "adjacent" expected')
+        if not self.table.is_cuda:
+            raise fb.FusionError("device tensors expected")
+        _need(self.table, torch.float32, self.table.get_device(), "table", dim=2)
+
+    def c_struct(self, positions: Optional[int]) -> fb.fusion_rotation:
+        rows, dims = self.table.shape
+        code = fb.FUSION_PAIRS_HALVES if self.pairs == "halves" else fb.FUSION_PAIRS_ADJACENT
+        return fb.fusion_rotation(self.table.data_ptr(), rows, dims, code, positions)
+
+
+def rotation_table(positions: int, dims: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """The usual table of a Rotation: angles position * base ** (-2 i / dims), in 64 bits, their cosines and sines rounded once."""
+    i = torch.arange(dims // 2, dtype=torch.float64, device=device)
+    a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * float(base) ** (-2.0 * i / dims)
+    return torch.cat([a.cos(), a.sin()], dim=1).float()
 
 
 def cache_of(dtype: str, k: torch.Tensor, v: torch.Tensor, page_table: torch.Tensor, lengths: torch.Tensor, *, heads: int,
@@ -216,6 +295,27 @@ def device_cache(dtype: str, max_batch: int, max_tokens: int, heads: int, kv_hea
     table = torch.arange(max_batch * per, dtype=torch.int32, device=device).view(max_batch, per)
     return DeviceCache(dtype, heads, pool(), pool(), table, torch.zeros(max_batch, dtype=torch.int32, device=device),
                        per_token(sizes), per_token(weights))
+
+
+def packed_cache_of(dtype: str, k: torch.Tensor, v: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+              page_table: torch.Tensor, lengths: torch.Tensor, *, heads: int, sizes: Optional[torch.Tensor] = None,
+              weights: Optional[torch.Tensor] = None) -> DevicePackedCache:
+    """A cache in 4 bits over the caller's pools of codes and scales, page table and lengths."""
+    return DevicePackedCache(dtype, int(heads), k, v, page_table, lengths, sizes, weights, k_scales, v_scales)
+
+
+def device_packed_cache(dtype: str, max_batch: int, max_tokens: int, heads: int, kv_heads: int, head_dim: int, *,
+                  page_tokens: int = 16, sizes: bool = False, weights: bool = False, device="cuda") -> DevicePackedCache:
+    """An empty cache in 4 bits (device_cache)."""
+    per = -(-max_tokens // page_tokens)
+    pages = max(1, max_batch * per)
+    pool = lambda row: torch.zeros((pages, kv_heads, page_tokens, row), dtype=torch.uint8, device=device)   # noqa: E731
+    per_token = lambda on: torch.zeros((pages, page_tokens), dtype=torch.float32, device=device) if on else None   # noqa: E731
+    table = torch.arange(max_batch * per, dtype=torch.int32, device=device).view(max_batch, per)
+    scale = fb.packed_scale_bytes(head_dim)
+    return DevicePackedCache(dtype, heads, pool(head_dim // 2), pool(head_dim // 2), table,
+                        torch.zeros(max_batch, dtype=torch.int32, device=device), per_token(sizes), per_token(weights),
+                        pool(scale), pool(scale))
 
 
 @dataclass
@@ -366,18 +466,70 @@ class Fusion:
         o = lengths_out if lengths_out is not None else c.lengths
         if c.max_batch == 0:
             return o
+        rows, kp, ks, vp, vs, zp, wp, op = _append_args(c, k, v, rows, sizes, scores, o)
+        _enqueue(c.lib.fusion_cache_append, c.index, self.status, c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp, wp, op, c._ws,
+                 c.ws_bytes)
+        return o
+
+    def cache_append_rotated(self, c: DeviceCache, k: torch.Tensor, v: torch.Tensor, rotation: Rotation, rows=None, *,
+                             positions: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None,
+                             q_out: Optional[torch.Tensor] = None, sizes: Optional[torch.Tensor] = None,
+                             scores: Optional[torch.Tensor] = None, lengths_out: Optional[torch.Tensor] = None):
+        """cache_append with the keys rotated on the way, by `positions` ([rows] int32; None: the rows' places in their
+        sequences), and with them the queries of the same rows, q [rows, heads, head_dim] (any stride between rows, any number
+        of heads).  The new lengths go to the cache's own unless lengths_out is given; returns the rotated queries (q_out, where
+        it is given, which may be a contiguous q; rows of no sample stay; None without q)."""
+        if q is not None and (q.dim() != 3 or q.shape[2] != c.head_dim):
+            raise fb.FusionError(f"queries: [rows, heads, {c.head_dim}] expected")
+        if q is None and q_out is not None:
+            raise fb.FusionError("q_out without q")
+        o = lengths_out if lengths_out is not None else c.lengths
         if rows is None:
             rows = c.one_row_each()
-        elif any(t is not None and t.get_device() != c.index for t in (rows.offsets, rows.batch, rows.ids)):
-            raise fb.FusionError(f"the rows' offsets, count and ids on the cache's device ({c.index}) expected")
-        kp, ks = _rows_ptr(k, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "keys")
-        vp, vs = _rows_ptr(v, rows.max_rows, c.kv_heads, c.head_dim, c.torch_dtype, c.index, "values")
-        zp = _need(sizes, torch.float32, c.index, "sizes", rows.max_rows)
-        wp = _need(scores, torch.float32, c.index, "scores", rows.max_rows)
-        op = _need(o, torch.int32, c.index, "lengths_out", c.max_batch)
-        _enqueue(c.lib.fusion_cache_append, c.index, self.status, c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp,
-                 wp, op, c._ws, c.ws_bytes)
-        return o
+        heads, qp, qs, qo = 0, None, 0, None
+        if q is not None:
+            heads = q.shape[1]
+            qp, qs = _rows_ptr(q, rows.max_rows, heads, c.head_dim, c.torch_dtype, c.index, "queries")
+            if q_out is None:
+                q_out = torch.empty((rows.max_rows, heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
+            qo = _need(q_out, c.torch_dtype, c.index, "q_out", dim=3)
+            if q_out.shape[0] < rows.max_rows or q_out.shape[1] != heads or q_out.shape[2] != c.head_dim:
+                raise fb.FusionError(f"q_out: [{rows.max_rows}, {heads}, {c.head_dim}] expected")
+            if rows.max_rows == 0:   # (an empty tensor has no address)
+                qp = qo = None
+        if c.max_batch == 0:
+            return q_out
+        rows, kp, ks, vp, vs, zp, wp, op = _append_args(c, k, v, rows, sizes, scores, o)
+        pp = _need(positions, torch.int32, c.index, "positions", rows.max_rows)
+        if rotation.table.get_device() != c.index:
+            raise fb.FusionError(f"the rotation's table on the cache's device ({c.index}) expected")
+        _enqueue(c.lib.fusion_cache_append_rotated, c.index, self.status, c.code, c.c_struct(), rows.ragged(), kp, ks, vp, vs, zp, wp,
+                 rotation.c_struct(pp), qp, qs, heads, qo, op, c._ws, c.ws_bytes)
+        return q_out
+
+    def cache_read(self, c: DeviceCache, rows, *, starts: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                   v_out: Optional[torch.Tensor] = None, sizes_out: Optional[torch.Tensor] = None,
+                   weights_out: Optional[torch.Tensor] = None):
+        """The rows that `rows` (a DeviceBatch or RaggedRows) names, back from the cache: row r of sample i is position
+        starts[i] + r (starts [max_batch] int32; None: 0) of its sequence.  Returns keys and values [rows, kv_heads,
+        head_dim] (k_out and v_out, where they are given; rows of no sample stay); sizes_out and weights_out [rows] get the
+        tokens' sizes and weights."""
+        _rows_here(c, rows)
+        outs = []
+        for t, what in ((k_out, "k_out"), (v_out, "v_out")):
+            if t is None:
+                t = torch.empty((rows.max_rows, c.kv_heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
+            _need(t, c.torch_dtype, c.index, what, dim=3)
+            if t.shape[0] < rows.max_rows or t.shape[1] != c.kv_heads or t.shape[2] != c.head_dim:
+                raise fb.FusionError(f"{what}: [{rows.max_rows}, {c.kv_heads}, {c.head_dim}] expected")
+            outs.append(t)
+        sp = _need(starts, torch.int32, c.index, "starts", rows.max_batch)
+        zp = _need(sizes_out, torch.float32, c.index, "sizes_out", rows.max_rows)
+        wp = _need(weights_out, torch.float32, c.index, "weights_out", rows.max_rows)
+        if rows.max_batch and rows.max_rows and c.max_batch:
+            _enqueue(c.lib.fusion_cache_read, c.index, self.status, c.code, c.c_struct(), rows.ragged(), sp, outs[0].data_ptr(),
+                     outs[1].data_ptr(), zp, wp)
+        return outs[0], outs[1]
 
     def cache_attention(self, c: DeviceCache, q: torch.Tensor, *, scale: Optional[float] = None, window: int = 0,
                         sinks: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -41,6 +41,20 @@ __device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// d += A B, B the sum of kTerms terms.  With two, for float32 results, the lower term comes first and the sum is added by itself: the
+// matrix instruction cuts its sums off instead of rounding them (16 x 577 float32: off by 6.3e-7 of the result when it adds to d).
+template <int kTerms, typename B>
+__device__ __forceinline__ void products(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, B b) {
+    if constexpr (kTerms == 1) {
+        mma_f16_16816(d, a0, a1, a2, a3, b(0, 0), b(0, 1));
+    } else {
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int term = kTerms - 1; term >= 0; --term) mma_f16_16816(s, a0, a1, a2, a3, b(term, 0), b(term, 1));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) d[e] += s[e];
+    }
+}
 __device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void *src, bool read) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(read ? 4 : 0) : "memory");
 }
@@ -223,17 +237,21 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
             }
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-            // the largest dim to 2^14 .. 2^15; queries below 2^-99 stay small, and their logits nothing
-            const int up = min(14 + 127 - (int)(top >> 23), 113);
+            // the largest dim to 2^14 .. 2^15, small ones by way of 2^64 times it, so that no factor is out of range
+            const bool low = top < 64u << 23;
+            const float lift = low ? 0x1p64f : 1.0f;
+            top = __float_as_uint(__uint_as_float(top) * lift);
+            const int up = min(14 + 127 - (int)(top >> 23), 113);   // (113: a query of zeros)
             const float f = __int_as_float((127 + up) << 23);
 #pragma unroll
             for (int i = 0; i < 2 * kKs; ++i) {
-                const float x = q[i].x * f, y = q[i].y * f;
+                const float x = q[i].x * lift * f, y = q[i].y * lift * f;
                 const uint32_t h = pack_half(x, y);
                 qf[0][i / 2][n][i & 1] = h;
                 if constexpr (kTerms == 2) qf[kTerms - 1][i / 2][n][i & 1] = pack_half(x - half_low(h), y - half_high(h));
             }
-            const float back = fminf(fmaxf(p.scale2 * __int_as_float((127 - up) << 23), -FLT_MAX), FLT_MAX);   // (infinity times 0 is NaN)
+            float back = p.scale2 * __int_as_float((127 - up) << 23) * (low ? 0x1p-64f : 1.0f);
+            back = fminf(fmaxf(back, -FLT_MAX), FLT_MAX);   // (infinity times 0 is NaN)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 factor[n][e] = __shfl_sync(0xFFFFFFFFu, back, (2 * t + e) * 4);
@@ -311,10 +329,8 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                     for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int term = 0; term < kTerms; ++term)
-                                mma_f16_16816(x[i][n], a[0][2 * kk], a[1][2 * kk], a[0][2 * kk + 1], a[1][2 * kk + 1],
-                                              qf[term][2 * j + kk][n][0], qf[term][2 * j + kk][n][1]);
+                            products<kTerms>(x[i][n], a[0][2 * kk], a[1][2 * kk], a[0][2 * kk + 1], a[1][2 * kk + 1],
+                                             [&](int term, int e) { return qf[term][2 * j + kk][n][e]; });
                 }
             }
             // ---- logits in base 2; a masked token's are -inf
@@ -420,9 +436,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int n = 0; n < NT; ++n)
-#pragma unroll
-                            for (int term = 0; term < kTerms; ++term)
-                                mma_f16_16816(o[4 * w + e][n], a[0][e], a[1][e], a[2][e], a[3][e], b[term][n][0], b[term][n][1]);
+                            products<kTerms>(o[4 * w + e][n], a[0][e], a[1][e], a[2][e], a[3][e], [&](int term, int i) { return b[term][n][i]; });
                 }
             }
         }

@@ -62,21 +62,22 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
     } while (s.rounds == 0);
 }
 
-// The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.  A boundary at most `snap` rounds
+// The batch's rounds in `ctas` runs: the first `more` of len + 1 rounds, the others of len.  A boundary at most `snap` (kSnap) rounds
 // inside a (sequence, key head) moves to its nearer end (its beginning first): a join costs more time than the few rounds that
 // it would deal out.  (Rounds are counted in 32 bits: counts_fit.)
+constexpr int kSnap = 4;
 struct Run {
     unsigned total, len, more;
     unsigned r0, r1;   // this CTA's
     int ctas, snap;
-    __device__ __forceinline__ void cut(unsigned rounds, int n) {
+    __device__ __forceinline__ void cut(unsigned rounds, int n, int most) {
         total = rounds;
         ctas = n;
         len = total / (unsigned)n;
         more = total - len * (unsigned)n;
         r0 = begin(blockIdx.x);
         r1 = begin(blockIdx.x + 1);
-        snap = len > 4 ? 4 : (int)len - 1;
+        snap = (int)len > most ? most : (int)len - 1;
     }
     __device__ __forceinline__ unsigned begin(unsigned k) const { return len * k + min(k, more); }
     __device__ __forceinline__ int of(unsigned x) const {   // the last run that begins at round x or before, boundaries not moved
@@ -103,7 +104,7 @@ struct Finder {
 // warps' sums go through shared memory, and the thread whose sequences hold a boundary looks it up (one barrier before and
 // one after: 2.2 us with 64-bit scans by one thread, 1.2 now, 0.7 of them the reading of the lengths).  min_rounds: of a run.
 // SNAP: the boundaries move to ends of (sequence, key head)s.  kEarly: called before the kernel's wait.
-template <int THREADS, bool SNAP, bool kEarly>
+template <int THREADS, bool SNAP, bool kEarly, int MOST = kSnap>
 __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREADS> &s, int tokens, int heads, int chunks, unsigned min_rounds,
                                          Run &run, Place &at) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -128,7 +129,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
     const unsigned most = (total + min_rounds - 1) / min_rounds;
     const int ctas = (int)min(most, gridDim.x);
     if ((int)blockIdx.x >= ctas) return false;
-    run.cut(total, ctas);
+    run.cut(total, ctas, MOST);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const unsigned x = k ? run.r1 : run.r0;

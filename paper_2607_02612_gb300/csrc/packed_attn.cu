@@ -25,6 +25,8 @@ namespace {
 using namespace rounds;
 
 constexpr float kUp = 7.0f;
+constexpr int kSnap = 2;      // rounds: of 128 tokens, twice bf16's
+constexpr int kTokens = 32;   // of a warp and round
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {   // an 8 x 8 matrix of b16, a row per four lanes
     uint32_t r;
@@ -55,11 +57,25 @@ __device__ __forceinline__ void products(float (&d)[4], uint32_t a0, uint32_t a1
         for (int e = 0; e < 4; ++e) d[e] += s[e];
     }
 }
-__device__ __forceinline__ void cp_async4_zfill(uint32_t dst, const void *src, bool read) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(read ? 4 : 0) : "memory");
+// BYTES from src, or zeros.  (A predicate, not a number of bytes to read, which would cost instructions at every copy.)
+template <int BYTES> __device__ __forceinline__ void copy_or_zero(uint32_t dst, unsigned long long src, bool read) {
+    if constexpr (BYTES == 16)
+        asm volatile("{ .reg .pred p; setp.eq.u32 p, %2, 0; cp.async.cg.shared.global [%0], [%1], 16, p; }" ::"r"(dst), "l"(src), "r"((int)read) : "memory");
+    else
+        asm volatile("{ .reg .pred p; setp.eq.u32 p, %2, 0; cp.async.ca.shared.global [%0], [%1], %3, p; }" ::"r"(dst), "l"(src), "r"((int)read), "n"(BYTES)
+                     : "memory");
 }
-__device__ __forceinline__ void cp_async8_zfill(uint32_t dst, const void *src, bool read) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(read ? 8 : 0) : "memory");
+// base + a b, in one instruction
+__device__ __forceinline__ unsigned long long at_row(const unsigned char *base, unsigned a, unsigned b) {
+    unsigned long long r;
+    asm("mad.wide.u32 %0, %1, %2, %3;" : "=l"(r) : "r"(a), "r"(b), "l"(base));
+    return r;
+}
+// The bits of a where m has ones, those of b elsewhere.
+__device__ __forceinline__ uint32_t pick_bits(uint32_t a, uint32_t b, uint32_t m) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xE4;" : "=r"(r) : "r"(a), "r"(b), "r"(m));
+    return r;
 }
 
 // The token of row i of a tile's half, and the place of 16-byte chunk c of row r: c ^ swizzle(r), linear in the bits of r.  A row of
@@ -77,86 +93,109 @@ template <int DP> __device__ __forceinline__ int swizzle(int r) {
     return DP == 64 ? 0 : DP == 128 ? r & 2 : (r & 3) << 1 | (r >> 2 & 1);
 }
 
-// Shared memory of a CTA: per warp S stages of TT rows of K's and of V's codes and of their scales; the tokens' log2 sizes; then,
-// at the end of a (sequence, key head), the warps' outputs on their way to each other, 64 dims at a time.
-template <int DP, int NT, int TT, int S, int W>
+// Shared memory of a CTA: per warp S stages of kTokens rows of K's and of V's codes and of their scales; the tokens' log2 sizes; the queries of this (sequence, key head) and the next; the warps' outputs on their way to each other, at the
+// end of a (sequence, key head), kJoinDims dims at a time.
+template <typename T, int DP, int NT, int S, int W>
 struct Layout {
-    static constexpr int kNq = 8 * NT, kRow = DP / 2, kScales = DP / 16, kStage = 2 * TT * (kRow + kScales);
-    static constexpr int kPitch = 64 + 8;
+    static constexpr int kNq = 8 * NT, kRow = DP / 2, kScales = DP / 16, kStage = 2 * kTokens * (kRow + kScales);
+    static constexpr int kQPitch = DP * (int)sizeof(T) + 16, kQ = kNq * kQPitch;
+    static constexpr int kJoinDims = DP < 128 ? DP : 128, kPitch = kJoinDims + 8;
     static constexpr int kLsz = W * S * kStage;
-    static constexpr int kShared = kLsz + W * S * TT * 4;
+    static constexpr int kQueries = kLsz + W * S * kTokens * 4;
+    static constexpr int kJoin = kQueries + 2 * kQ;
     static constexpr int kJoinBytes = W * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
-    static constexpr int kTotal = kShared + (kJoinBytes > kScratch ? kJoinBytes : kScratch);
+    static constexpr int kTotal = kJoin + (kJoinBytes > kScratch ? kJoinBytes : kScratch);
 };
 
-// The tokens of the rounds to come (rounds::Stream), their rows in 4 bits.
-template <int DP, int TT, int W>
-struct PackedStream : Stream<unsigned char, DP / 2, TT, W> {
-    using Base = Stream<unsigned char, DP / 2, TT, W>;
-    static constexpr int kRow = DP / 2, kScales = DP / 16, kCpr = kRow / 16, kStage = 2 * TT * (kRow + kScales);
+// The tokens of the rounds to come, one to a lane (rounds::Stream with rows in 4 bits).
+template <int DP, int W>
+struct PackedStream {
+    static constexpr int kRow = DP / 2, kScales = DP / 16, kCpr = kRow / 16, kStage = 2 * kTokens * (kRow + kScales), kRound = W * kTokens;
+    Place ahead;             // of the next round to look up
+    unsigned ahead_r, r1;
+    Token t0, t1;            // t0's rows are asked for next (its size is here), then t1's
+    float size0;
+    unsigned plain;          // a bit per stage: all of its tokens are there, of size 1
 
-    __device__ __forceinline__ void ask(const PackedAttnParams &p, const Token &t, float size, int lane, unsigned char *stage, float *lsz) {
+    __device__ __forceinline__ Token look_up(const PackedAttnParams &p, int chunks, int warp, int lane) {
+        Token r{0u, -1, ahead.h};
+        if (ahead_r < r1) {
+            const int j = ahead.u * kRound + warp * kTokens + lane;
+            if (j < ahead.vis) {
+                const int pos = p.window && j >= p.sinks ? j + ahead.n - ahead.vis : j;
+                r.place = cache_page(p.c, ahead.b, pos, r.page) ? pos & ((1 << p.c.shift) - 1) : -2;
+            }
+            ++ahead_r;
+            place_next(p, ahead, kRound, p.c.kv_heads, chunks);
+        }
+        return r;
+    }
+    __device__ __forceinline__ float size_of(const PackedAttnParams &p, const Token &t) const {
+        return t.place < 0 ? 0.0f : p.c.sizes ? p.c.sizes[((size_t)t.page << p.c.shift) + t.place] : 1.0f;
+    }
+    // Asks for the rows of a round's tokens, and notes their log2 sizes unless all are 0.
+    __device__ __forceinline__ void ask(const PackedAttnParams &p, const Token &t, float size, int lane, int st, unsigned char *stages, float *lsz) {
+        const unsigned row_bytes = (unsigned)p.c.dim / 2;
         const bool live = t.place >= 0 && size != 0.0f;
         const unsigned row = live ? ((t.page * (unsigned)p.c.kv_heads + (unsigned)t.h) << p.c.shift) + (unsigned)t.place : 0u;
-        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live), row_bytes = (unsigned)p.c.dim / 2;
-        if (lane < TT) lsz[lane] = t.place == -2 ? kNoPage : live ? log2f(size) : -INFINITY;
+        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live);
+        const bool all_plain = __all_sync(0xFFFFFFFFu, live && size == 1.0f);
+        plain = (plain & ~(1u << st)) | (unsigned)all_plain << st;
+        if (!all_plain) lsz[st * kTokens + lane] = t.place == -2 ? kNoPage : live ? log2f(size) : -INFINITY;
         constexpr int kWide = 32 / kCpr;   // rows of a step
         const int r_lane = lane / kCpr, cc = lane % kCpr;
         const bool exists = (unsigned)cc * 16u < row_bytes;
-        const unsigned mine = exists ? lives >> r_lane : 0u;
         const unsigned char *k = p.c.k + (exists ? cc : 0) * 16, *v = p.c.v + (exists ? cc : 0) * 16;
-        const uint32_t dst = smem_addr(stage) + r_lane * kRow, at = (uint32_t)(cc ^ swizzle<DP>(r_lane)) * 16u;
+        const uint32_t stage = smem_addr(stages) + st * kStage, dst = stage + r_lane * kRow, at = (uint32_t)(cc ^ swizzle<DP>(r_lane)) * 16u;
+        const unsigned mine = exists ? lives >> r_lane : 0u;
 #pragma unroll
-        for (int e = 0; e < TT / kWide; ++e) {
-            const size_t off = (size_t)__shfl_sync(0xFFFFFFFFu, row, e * kWide + r_lane) * row_bytes;
+        for (int e = 0; e < kTokens / kWide; ++e) {
+            const unsigned theirs = __shfl_sync(0xFFFFFFFFu, row, e * kWide + r_lane);
             const bool read = mine >> (e * kWide) & 1u;
             const uint32_t to = dst + e * kWide * kRow + (at ^ (uint32_t)(swizzle<DP>(e * kWide) * 16));
-            cp_async16_zfill(to, k + off, read);
-            cp_async16_zfill(to + TT * kRow, v + off, read);
+            copy_or_zero<16>(to, at_row(k, theirs, row_bytes), read);
+            copy_or_zero<16>(to + kTokens * kRow, at_row(v, theirs, row_bytes), read);
         }
-        if (lane < TT) {
-            const uint32_t ks = smem_addr(stage) + 2 * TT * kRow + lane * kScales, vs = ks + TT * kScales;
-            const size_t off = (size_t)row * (unsigned)p.s.bytes;
-            if constexpr (kScales == 4) {
-                cp_async4_zfill(ks, p.s.k + off, live);
-                cp_async4_zfill(vs, p.s.v + off, live);
-            } else if constexpr (kScales == 8) {
-                cp_async8_zfill(ks, p.s.k + off, live);
-                cp_async8_zfill(vs, p.s.v + off, live);
-            } else {   // rows of 12 or 16 bytes
+        const uint32_t ks = stage + 2 * kTokens * kRow + lane * kScales, vs = ks + kTokens * kScales;
+        const unsigned long long kz = at_row(p.s.k, row, (unsigned)p.s.bytes), vz = at_row(p.s.v, row, (unsigned)p.s.bytes);
+        if constexpr (kScales <= 8) {
+            copy_or_zero<kScales>(ks, kz, live);
+            copy_or_zero<kScales>(vs, vz, live);
+        } else {   // rows of 12 or 16 bytes
 #pragma unroll
-                for (int e = 0; e < kScales; e += 4) {
-                    const bool read = live && e < p.s.bytes;
-                    cp_async4_zfill(ks + e, p.s.k + (read ? off + e : 0), read);
-                    cp_async4_zfill(vs + e, p.s.v + (read ? off + e : 0), read);
-                }
+            for (int e = 0; e < kScales; e += 4) {
+                const bool read = live && e < p.s.bytes;
+                copy_or_zero<4>(ks + e, kz + (read ? e : 0), read);
+                copy_or_zero<4>(vs + e, vz + (read ? e : 0), read);
             }
         }
         cp_async_commit();
     }
-    __device__ __forceinline__ void next(const PackedAttnParams &p, int chunks, int warp, int lane, unsigned char *stage, float *lsz) {
-        ask(p, this->t0, this->size0, lane, stage, lsz);
-        this->t0 = this->t1;
-        this->size0 = this->size_of(p, this->t0);
-        this->t1 = this->look_up(p, chunks, warp, lane);
+    __device__ __forceinline__ void next(const PackedAttnParams &p, int chunks, int warp, int lane, int st, unsigned char *stages, float *lsz) {
+        ask(p, t0, size0, lane, st, stages, lsz);
+        t0 = t1;
+        size0 = size_of(p, t0);
+        t1 = look_up(p, chunks, warp, lane);
     }
+    // The first S - 1 rounds' rows (all pages asked for at once, then all sizes).
     template <int S>
     __device__ __forceinline__ void begin(const PackedAttnParams &p, const Place &at, const Run &run, int chunks, int warp, int lane,
                                           unsigned char *stages, float *lsz) {
-        this->ahead = at;
-        this->ahead_r = run.r0;
-        this->r1 = run.r1;
+        ahead = at;
+        ahead_r = run.r0;
+        r1 = run.r1;
+        plain = 0u;
         Token t[S + 1];
         float size[S];
 #pragma unroll
-        for (int s = 0; s <= S; ++s) t[s] = this->look_up(p, chunks, warp, lane);
+        for (int s = 0; s <= S; ++s) t[s] = look_up(p, chunks, warp, lane);
 #pragma unroll
-        for (int s = 0; s < S; ++s) size[s] = this->size_of(p, t[s]);
+        for (int s = 0; s < S; ++s) size[s] = size_of(p, t[s]);
 #pragma unroll
-        for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], lane, stages + s * kStage, lsz + s * TT);
-        this->t0 = t[S - 1];
-        this->size0 = size[S - 1];
-        this->t1 = t[S];
+        for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], lane, s, stages, lsz);
+        t0 = t[S - 1];
+        size0 = size[S - 1];
+        t1 = t[S];
     }
 };
 
@@ -180,11 +219,11 @@ __device__ __forceinline__ float2 load2(const __nv_bfloat16 *src, int i) {
 __device__ __forceinline__ float2 load2(const float *src, int i) { return reinterpret_cast<const float2 *>(src)[i]; }
 
 // T: type of queries and output.  W: warps of a CTA.
-template <typename T, int DP, int NT, int TT, int S, int W>
-__global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4 : 2) k_packed_attn(PackedAttnParams p, int chunks) {
-    using L = Layout<DP, NT, TT, S, W>;
+template <typename T, int DP, int NT, int S, int W>
+__global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3 : 2) k_packed_attn(PackedAttnParams p, int chunks) {
+    using L = Layout<T, DP, NT, S, W>;
     constexpr int kThreads = 32 * W, kTerms = sizeof(T) == 4 ? 2 : 1;
-    constexpr int kNq = L::kNq, kRound = W * TT, kRow = L::kRow, kScales = L::kScales, kKs = DP / 16, kMt = TT / 16;
+    constexpr int kNq = L::kNq, kRound = W * kTokens, kRow = L::kRow, kScales = L::kScales, kKs = DP / 16, kMt = kTokens / 16;
     constexpr int kKw = DP / 32, kVw = DP / 64;   // words of a K row and of a V row that a lane has
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Finder<kThreads> finder;
@@ -192,47 +231,70 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const Cache &c = p.c;
+
+    unsigned char *stages = sm + warp * S * L::kStage;
+    float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * kTokens;
+    float *join = reinterpret_cast<float *>(sm + L::kJoin);
+    PackedStream<DP, W> in;
     wait_for_previous();
     Run run;
     Place at;
-    if (!find_run<kThreads, true, false>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
+    if (!find_run<kThreads, true, false, kSnap>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
         empty_sequences<T, kThreads>(p);
         return;
     }
     const unsigned r0 = run.r0, r1 = run.r1;
 
-    unsigned char *stages = sm + warp * S * L::kStage;
-    float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
-    float *join = reinterpret_cast<float *>(sm + L::kShared);
-    PackedStream<DP, TT, W> in;
+    // asks for the queries of a (sequence, key head), into one of two places in turn (with the next group of copies)
+    int q_at = 0;
+    auto ask_q = [&](const Place &s, int where) {
+        const int heads = min(kNq, p.group - s.ch * kNq);
+        const unsigned char *src = reinterpret_cast<const unsigned char *>(
+            reinterpret_cast<const T *>(p.q) + (size_t)s.b * p.q_stride + (size_t)(s.h * p.group + s.ch * kNq) * c.dim);
+        constexpr int kChunks = DP * (int)sizeof(T) / 16;
+        const int row = c.dim * (int)sizeof(T);
+        for (int e = tid; e < kNq * kChunks; e += kThreads) {
+            const int q = e / kChunks, cc = e % kChunks * 16;
+            const bool read = q < heads && cc < row;
+            copy_or_zero<16>(smem_addr(sm + L::kQueries + where * L::kQ + q * L::kQPitch + cc),
+                             reinterpret_cast<unsigned long long>(src + (read ? (size_t)q * row + cc : 0)), read);
+        }
+    };
+    // those of the (sequence, key head) after this one, if this run has it
+    auto ask_next_q = [&](unsigned r) {
+        if (r + at.rounds - at.u >= r1) return;
+        Place next = at;
+        next.u = at.rounds - 1;
+        place_next(p, next, kRound, c.kv_heads, chunks);
+        ask_q(next, q_at ^ 1);
+    };
+    ask_q(at, q_at);
+    cp_async_commit();
     in.template begin<S>(p, at, run, chunks, warp, lane, stages, lsz);
     empty_sequences<T, kThreads>(p);
     if (tid == 0) s_bad = 0;
+    cp_async_wait<S - 1>();   // (all but the first rounds)
     __syncthreads();
 
-    // scales behind the last dim: zero, whatever the cache holds there
-    uint32_t k_mask = 0u, v_mask[kVw];
+    // scales behind the last dim: zero for K, whose dims are summed, whatever the cache holds there (V's give sums of their own)
+    uint32_t k_mask = 0u;
 #pragma unroll
-    for (int i = 0; i < kVw; ++i) {
+    for (int i = 0; i < kVw; ++i)
         if ((t * kVw + i) * 16 < c.dim) k_mask |= 0xFFu << (8 * i);
-        v_mask[i] = (g / 2 + 4 * i) * 16 < c.dim ? 0xFFFFu : 0u;
-    }
     const uint32_t v_pick = (uint32_t)(g / 2) | (uint32_t)(4 + g / 2) << 4;   // a byte of each of two words
 
     float m[NT][2], l[NT][2], factor[NT][2], o[kKs][NT][4];
     uint32_t qf[kTerms][kKs][NT][2];
     bool bad = false;
     auto begin_head = [&]() {
-        const int heads = min(kNq, p.group - at.ch * kNq);
-        const T *src = reinterpret_cast<const T *>(p.q) + (size_t)at.b * p.q_stride + (size_t)(at.h * p.group + at.ch * kNq) * c.dim;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
+            const T *src = reinterpret_cast<const T *>(sm + L::kQueries + q_at * L::kQ + (8 * n + g) * L::kQPitch) + t * (DP / 4);
             float2 q[2 * kKs];
             uint32_t top = 0u;
 #pragma unroll
             for (int i = 0; i < 2 * kKs; ++i) {
-                const int d = t * (DP / 4) + 2 * i;
-                q[i] = 8 * n + g < heads && d < c.dim ? load2(src + (size_t)(8 * n + g) * c.dim, d / 2) : make_float2(0.0f, 0.0f);
+                q[i] = load2(src, i);
                 top = max(top, max(__float_as_uint(q[i].x) & 0x7FFFFFFFu, __float_as_uint(q[i].y) & 0x7FFFFFFFu));
             }
             top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
@@ -266,39 +328,33 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
     int st = 0;
     unsigned seg0 = r0 - at.u;   // first round of the (sequence, key head)
     for (unsigned r = r0;; ++r) {
+        if (r == r0 || at.u == 0) ask_next_q(r);
         __syncwarp();
-        const int next_st = st == 0 ? S - 1 : st - 1;
-        in.next(p, chunks, warp, lane, stages + next_st * L::kStage, lsz + next_st * TT);
+        in.next(p, chunks, warp, lane, st == 0 ? S - 1 : st - 1, stages, lsz);
         cp_async_wait<S - 1>();
         __syncwarp();
 
-        const unsigned char *ks = stages + st * L::kStage, *vs = ks + TT * kRow, *kz = vs + TT * kRow, *vz = kz + TT * kScales;
-        const float *lz = lsz + st * TT;
-        const int j0 = at.u * kRound + warp * TT;
+        const bool plain = in.plain >> st & 1u;
         const int nq = min(kNq, p.group - at.ch * kNq), head0 = at.h * p.group + at.ch * kNq;
+        const unsigned char *ks = stages + st * L::kStage, *vs = ks + kTokens * kRow, *kz = vs + kTokens * kRow, *vz = kz + kTokens * kScales;
+        const float *lz = lsz + st * kTokens;
+        const int j0 = at.u * kRound + warp * kTokens;
         if (j0 < at.vis) {
             // ---- S^T = K Q^T
             float x[kMt][NT][4];
 #pragma unroll
             for (int i = 0; i < kMt; ++i) {
+                float y[NT][4];   // every other step's sums
 #pragma unroll
-                for (int n = 0; n < NT; ++n) x[i][n][0] = x[i][n][1] = x[i][n][2] = x[i][n][3] = 0.0f;
-                uint32_t kw[2][kKw], sc[2][kVw];
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][n][e] = y[n][e] = 0.0f;
+                uint32_t sc[2][kVw];
+                const unsigned char *from[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const int row = 16 * i + 8 * h + order<DP>(g);
-                    const unsigned char *from = ks + row * kRow;
-                    if constexpr (DP == 64) {
-                        load_words<2>(from + 8 * t, kw[h]);
-                    } else if constexpr (DP == 128) {
-                        load_words<4>(from + ((t ^ swizzle<DP>(row)) << 4), kw[h]);
-                    } else {
-                        uint32_t a[4], b[4];
-                        load_words<4>(from + (((2 * t) ^ swizzle<DP>(row)) << 4), a);
-                        load_words<4>(from + (((2 * t + 1) ^ swizzle<DP>(row)) << 4), b);
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) kw[h][j] = a[j], kw[h][kKw - 4 + j] = b[j];
-                    }
+                    from[h] = ks + row * kRow;
                     const unsigned char *scales = kz + row * kScales + t * kVw;
                     if constexpr (DP == 64) {
                         sc[h][0] = scales_to_half((*scales & k_mask) * 0x0101u);
@@ -316,49 +372,76 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                         }
                     }
                 }
+                constexpr int kAtOnce = DP == 64 ? 2 : 4;   // words of a load
 #pragma unroll
-                for (int j = 0; j < kKw; ++j) {
-                    uint32_t a[2][4];
+                for (int j0w = 0; j0w < kKw; j0w += kAtOnce) {
+                    uint32_t kw[2][kAtOnce];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        codes_to_half(kw[h][j], a[h]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) a[h][e] = mul_half2(a[h][e], sc[h][j / 2]);
+                        const int chunk = DP == 64 ? 0 : DP == 128 ? t : 2 * t + j0w / 4;
+                        load_words<kAtOnce>(from[h] + (DP == 64 ? 8 * t : (chunk ^ swizzle<DP>(order<DP>(g))) << 4), kw[h]);
                     }
 #pragma unroll
-                    for (int kk = 0; kk < 2; ++kk)
+                    for (int jj = 0; jj < kAtOnce; ++jj) {
+                        const int j = j0w + jj;
+                        uint32_t a[2][4];
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            products<kTerms>(x[i][n], a[0][2 * kk], a[1][2 * kk], a[0][2 * kk + 1], a[1][2 * kk + 1],
-                                             [&](int term, int e) { return qf[term][2 * j + kk][n][e]; });
+                        for (int h = 0; h < 2; ++h) {
+                            codes_to_half(kw[h][jj], a[h]);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) a[h][e] = mul_half2(a[h][e], sc[h][j / 2]);
+                        }
+#pragma unroll
+                        for (int kk = 0; kk < 2; ++kk)
+#pragma unroll
+                            for (int n = 0; n < NT; ++n)
+                                products<kTerms>(x[i][n], a[0][2 * kk], a[1][2 * kk], a[0][2 * kk + 1], a[1][2 * kk + 1],
+                                                 [&](int term, int e) { return qf[term][2 * j + kk][n][e]; });
+                    }
                 }
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][n][e] += y[n][e];
             }
             // ---- logits in base 2; a masked token's are -inf
+            if (plain) {
 #pragma unroll
-            for (int i = 0; i < kMt; ++i) {
-                const int at0 = 16 * i + order<DP>(g), at1 = at0 + 8;
-                const float z0 = lz[at0], z1 = lz[at1];
-                const bool off0 = z0 == -INFINITY || z0 == kNoPage, off1 = z1 == -INFINITY || z1 == kNoPage;
-                bad |= z0 == kNoPage || z1 == kNoPage;
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    x[i][n][0] = off0 ? -INFINITY : fmaf(x[i][n][0], factor[n][0], z0);
-                    x[i][n][1] = off0 ? -INFINITY : fmaf(x[i][n][1], factor[n][1], z0);
-                    x[i][n][2] = off1 ? -INFINITY : fmaf(x[i][n][2], factor[n][0], z1);
-                    x[i][n][3] = off1 ? -INFINITY : fmaf(x[i][n][3], factor[n][1], z1);
-                }
-                if (p.logits) {
-                    float *dst = p.logits + ((size_t)at.b * p.heads + head0) * p.lstride + j0;
-                    const bool in0 = j0 + at0 < at.vis, in1 = j0 + at1 < at.vis;
+                for (int i = 0; i < kMt; ++i)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (8 * n + 2 * t + e < nq) {
-                                if (in0) dst[(8 * n + 2 * t + e) * p.lstride + at0] = x[i][n][e];
-                                if (in1) dst[(8 * n + 2 * t + e) * p.lstride + at1] = x[i][n][2 + e];
-                            }
+                        for (int e = 0; e < 4; ++e) x[i][n][e] *= factor[n][e & 1];
+            } else {
+#pragma unroll
+                for (int i = 0; i < kMt; ++i) {
+                    const float z0 = lz[16 * i + order<DP>(g)], z1 = lz[16 * i + order<DP>(g) + 8];
+                    const bool off0 = z0 == -INFINITY || z0 == kNoPage, off1 = z1 == -INFINITY || z1 == kNoPage;
+                    bad |= z0 == kNoPage || z1 == kNoPage;
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            x[i][n][e] = off0 ? -INFINITY : fmaf(x[i][n][e], factor[n][e], z0);
+                            x[i][n][2 + e] = off1 ? -INFINITY : fmaf(x[i][n][2 + e], factor[n][e], z1);
+                        }
                 }
+            }
+            if (p.logits) {
+                float *dst = p.logits + ((size_t)at.b * p.heads + head0 + 2 * t) * p.lstride + (j0 + order<DP>(g));
+                const int left = at.vis - j0 - order<DP>(g);
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (8 * n + 2 * t + e < nq) {
+                            float *to = dst + (8 * n + e) * p.lstride;
+#pragma unroll
+                            for (int i = 0; i < kMt; ++i) {
+                                if (16 * i < left) to[16 * i] = x[i][n][e];
+                                if (16 * i + 8 < left) to[16 * i + 8] = x[i][n][2 + e];
+                            }
+                        }
             }
             // ---- the running shift: kUp below the largest logit when it was set; where a logit exceeds that by kLag, it moves, and O
             // and the sums follow
@@ -408,24 +491,25 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                         b[kTerms - 1][n][1] = transpose8(pack_half(p2 - half_low(h1), p3 - half_high(h1)));
                     }
                 }
-                uint32_t vw[4][kVw], sz[4][kVw];
+                uint32_t sz[4][kVw];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int row = 16 * i + 8 * (j >> 1) + order<DP>(2 * t + (j & 1));
-#pragma unroll
-                    for (int w = 0; w < kVw; ++w)
-                        vw[j][w] = *reinterpret_cast<const uint32_t *>(vs + row * kRow + (((g / 4 + 2 * w) ^ swizzle<DP>(row)) << 4) + (g & 3) * 4);
-                    load_words<kVw>(vz + row * kScales, sz[j]);
-                }
+                for (int j = 0; j < 4; ++j) load_words<kVw>(vz + (16 * i + 8 * (j >> 1) + order<DP>(2 * t + (j & 1))) * kScales, sz[j]);
 #pragma unroll
                 for (int w = 0; w < kVw; ++w) {
+                    uint32_t vw[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int token = order<DP>(2 * t + (j & 1));
+                        vw[j] = *reinterpret_cast<const uint32_t *>(vs + (16 * i + 8 * (j >> 1) + token) * kRow + (((g / 4 + 2 * w) ^ swizzle<DP>(token)) << 4) +
+                                                                    (g & 3) * 4);
+                    }
                     uint32_t a[4][4];   // fragment registers of four steps of 16 dims
 #pragma unroll
                     for (int pair = 0; pair < 2; ++pair) {
-                        const uint32_t u = vw[2 * pair][w], v = vw[2 * pair + 1][w];
-                        const uint32_t s = scales_to_half(__byte_perm(sz[2 * pair][w], sz[2 * pair + 1][w], v_pick) & v_mask[w]);
-                        codes_to_half((u & 0x0F0F0F0Fu) | (v << 4 & 0xF0F0F0F0u), a[2 * pair]);       // even dims
-                        codes_to_half((u >> 4 & 0x0F0F0F0Fu) | (v & 0xF0F0F0F0u), a[2 * pair + 1]);   // odd dims
+                        const uint32_t u = vw[2 * pair], v = vw[2 * pair + 1];
+                        const uint32_t s = scales_to_half(__byte_perm(sz[2 * pair][w], sz[2 * pair + 1][w], v_pick));
+                        codes_to_half(pick_bits(u, v * 16u, 0x0F0F0F0Fu), a[2 * pair]);      // even dims
+                        codes_to_half(pick_bits(u >> 4, v, 0x0F0F0F0Fu), a[2 * pair + 1]);   // odd dims
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             a[2 * pair][e] = mul_half2(a[2 * pair][e], s);
@@ -469,25 +553,10 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                     for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][8 * n + 2 * t + e]);
                     f[n][e] = ex2(m[n][e] - M);
                 }
-            // a thread joins four dims of kMine heads per step of 64 dims
-            constexpr int kMine = (kNq * 16 + kThreads - 1) / kThreads;
-            float sums[kMine];
+            // a thread joins four dims of kMine heads per step of kJoinDims dims
+            constexpr int kAcross = L::kJoinDims / 4, kMine = (kNq * kAcross + kThreads - 1) / kThreads;
 #pragma unroll
-            for (int y = 0; y < kMine; ++y) {
-                const int e = y * kThreads + tid, q = min(e / 16, kNq - 1);
-                float M = s_m[0][q], ls = 0.0f;
-#pragma unroll
-                for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][q]);
-#pragma unroll
-                for (int w = 0; w < W; ++w) ls += s_l[w][q] * ex2(s_m[w][q] - M);
-                sums[y] = ls;
-                if (e < 16 * nq && e % 16 == 0) {
-                    if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
-                    else if (p.logits) p.lse[head + q] = log_sum(M, seg_bad ? -1.0f : ls);
-                }
-            }
-#pragma unroll
-            for (int w0 = 0; w0 < kVw; ++w0) {
+            for (int w0 = 0; w0 < kVw; w0 += L::kJoinDims / 64) {
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -495,28 +564,36 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                         if (8 * n + 2 * t + e >= nq) break;
                         float *to = join + (warp * kNq + 8 * n + 2 * t + e) * L::kPitch + 8 * g;
 #pragma unroll
-                        for (int k = 0; k < 4; k += 2)
-                            *reinterpret_cast<float4 *>(to + 2 * k) =
+                        for (int k = 0; k < L::kJoinDims / 16; k += 2)
+                            *reinterpret_cast<float4 *>(to + k / 4 * 64 + 2 * (k % 4)) =
                                 make_float4(o[4 * w0 + k][n][e] * f[n][e], o[4 * w0 + k][n][2 + e] * f[n][e],
                                             o[4 * w0 + k + 1][n][e] * f[n][e], o[4 * w0 + k + 1][n][2 + e] * f[n][e]);
                     }
                 __syncthreads();
 #pragma unroll
                 for (int y = 0; y < kMine; ++y) {
-                    const int e = y * kThreads + tid, q = e / 16, d0 = e % 16 * 4, d = 64 * w0 + d0;
+                    const int e = y * kThreads + tid, q = e / kAcross, d0 = e % kAcross * 4, d = 64 * w0 + d0;
                     if (q >= nq || d >= c.dim) continue;
-                    float4 sum = *reinterpret_cast<const float4 *>(join + q * L::kPitch + d0);
+                    float M = s_m[0][q], ls = 0.0f;
 #pragma unroll
-                    for (int w = 1; w < W; ++w) {
+                    for (int w = 1; w < W; ++w) M = fmaxf(M, s_m[w][q]);
+                    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int w = 0; w < W; ++w) {
+                        ls += s_l[w][q] * ex2(s_m[w][q] - M);
                         const float4 v = *reinterpret_cast<const float4 *>(join + (w * kNq + q) * L::kPitch + d0);
                         sum = make_float4(sum.x + v.x, sum.y + v.y, sum.z + v.z, sum.w + v.w);
                     }
-                    const float inv = 1.0f / sums[y];
+                    const float inv = 1.0f / ls;
                     if (!whole)
                         *reinterpret_cast<float4 *>(p.part + (slot + q) * c.dim + d) = sum;
                     else if (!seg_bad)
                         store4(reinterpret_cast<T *>(p.out) + (head + q) * c.dim + d,
-                               sums[y] == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+                               ls == 0.0f ? make_float4(0.0f, 0.0f, 0.0f, 0.0f) : make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv));
+                    if (d == 0) {
+                        if (!whole) p.part_ml[slot + q] = make_float2(seg_bad ? INFINITY : M, seg_bad ? -1.0f : ls);
+                        else if (p.logits) p.lse[head + q] = log_sum(M, seg_bad ? -1.0f : ls);
+                    }
                 }
                 __syncthreads();
             }
@@ -529,7 +606,11 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
                 __syncthreads();
             }
             if (r + 1 == r1) break;
+            const int had = at.u;
+            const bool first = seg0 < r0 && r - r0 < (unsigned)S;   // (the run began inside)
             place_next(p, at, kRound, c.kv_heads, chunks);
+            if (had + 1 < S || first) cp_async_wait<0>();   // the next queries were asked for fewer rounds ago than wait() waits for
+            q_at ^= 1;
             __syncthreads();
             begin_head();
             seg0 = r + 1;
@@ -541,19 +622,24 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 4
     cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)
 }
 
-template <typename T, int DP, int NT, int TT, int S>
+template <typename T, int DP, int NT, int S, int W>
+cudaError_t launch_warps(const PackedAttnParams &p, int chunks, cudaStream_t s) {
+    static_assert(counts_fit(kTokens, W), "rounds are counted in 32 bits");
+    return launch_rounds<k_packed_attn<T, DP, NT, S, W>, W>(Layout<T, DP, NT, S, W>::kTotal, p, chunks, W * kTokens, s);
+}
+template <typename T, int DP, int NT>
 cudaError_t launch(const PackedAttnParams &p, cudaStream_t s) {
-    static_assert(counts_fit(TT, 4) && (DP > 128 || counts_fit(TT, 1)), "rounds are counted in 32 bits");
+    constexpr int kStages = 2;
     const int chunks = ceil_div(p.group, 8 * NT);
     if constexpr (DP <= 128)
-        if (warps_alone(p, chunks)) return launch_rounds<k_packed_attn<T, DP, NT, TT, S, 1>, 1>(Layout<DP, NT, TT, S, 1>::kTotal, p, chunks, TT, s);
-    return launch_rounds<k_packed_attn<T, DP, NT, TT, S, 4>, 4>(Layout<DP, NT, TT, S, 4>::kTotal, p, chunks, 4 * TT, s);
+        if (warps_alone(p, chunks)) return launch_warps<T, DP, NT, kStages, 1>(p, chunks, s);
+    return launch_warps<T, DP, NT, kStages, 4>(p, chunks, s);
 }
 template <typename T, int NT>
 cudaError_t launch_dim(const PackedAttnParams &p, cudaStream_t s) {
-    if (p.c.dim <= 64) return launch<T, 64, NT, 32, 3>(p, s);
-    if (p.c.dim <= 128) return launch<T, 128, NT, 32, 3>(p, s);
-    return launch<T, 256, NT, 16, 3>(p, s);
+    if (p.c.dim <= 64) return launch<T, 64, NT>(p, s);
+    if (p.c.dim <= 128) return launch<T, 128, NT>(p, s);
+    return launch<T, 256, NT>(p, s);
 }
 
 }  // namespace

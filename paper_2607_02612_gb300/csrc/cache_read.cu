@@ -1,8 +1,8 @@
 // Rows of cached sequences back into a ragged batch: a copy, or the values of a cache in 4 bits (a code's times its group's
 // scale, exact in bf16 and in float32: fp4.cuh).  Bound by memory: every row is read once and written once.
 //
-// A CTA takes as many rows of one sample as give each thread kPer pieces of K and of V, all asked for at once: 16 bytes, or the 8
-// codes of a word, which are 16 bytes of bf16.
+// A CTA takes as many rows of one sample as give each thread kPer pieces of K and of V, all asked for at once; a piece is what gives
+// 16 bytes of a row.
 #include "cache_rows.cuh"
 #include "fp4.cuh"
 
@@ -16,28 +16,26 @@ __device__ __forceinline__ uint32_t to_bf16(uint32_t h) {   // two float16 whose
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// The 8 values of a word of codes and a scale's byte, in order.
-template <typename T> __device__ __forceinline__ void store_values(T *dst, uint32_t codes, uint32_t scale) {
+// What gives 16 bytes of a row: a word of codes (8 dims) as bf16, half of one as float32, 16 bytes as they are.
+template <typename T> struct Piece;
+template <> struct Piece<__nv_bfloat16> { using Held = uint32_t; };
+template <> struct Piece<float> { using Held = uint16_t; };
+template <> struct Piece<uint4> { using Held = uint4; };
+template <typename T> __device__ __forceinline__ uint4 values(uint32_t codes, uint32_t scale) {
     uint32_t v[4];
     codes_to_half(codes, v);
     const uint32_t s = scales_to_half(scale * 0x0101u);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = mul_half2(v[i], s);
-    uint4 *to = reinterpret_cast<uint4 *>(dst);
-    if constexpr (sizeof(T) == 2) {
-        *to = make_uint4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            to[i] = make_uint4(__float_as_uint(half_low(v[2 * i])), __float_as_uint(half_high(v[2 * i])),
-                               __float_as_uint(half_low(v[2 * i + 1])), __float_as_uint(half_high(v[2 * i + 1])));
-    }
+    for (int i = 0; i < (sizeof(T) == 2 ? 4 : 2); ++i) v[i] = mul_half2(v[i], s);
+    if constexpr (sizeof(T) == 2) return make_uint4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
+    else return make_uint4(__float_as_uint(half_low(v[0])), __float_as_uint(half_high(v[0])), __float_as_uint(half_low(v[1])), __float_as_uint(half_high(v[1])));
 }
 
 // T: the type of a cache in 4 bits' values; uint4: a copy of pieces of 16 bytes.  pieces: of a head's row.
 template <typename T>
 __global__ void __launch_bounds__(kThreads) k_cache_read(CacheReadParams p, int row_pieces, int pieces) {
     constexpr bool kFour = sizeof(T) != 16;
+    using Held = typename Piece<T>::Held;
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
@@ -79,41 +77,29 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(CacheReadParams p, int 
             return (size_t)(((page[x] * (unsigned)c.kv_heads + h) << c.shift) + ((unsigned)(at + r0 + r_mine + x * side) & low));
         };
         auto given = [&](int x) { return ((size_t)(o0 + r0 + r_mine + x * side) * row_pieces + ch); };
-        if constexpr (kFour) {
-            uint32_t k[kPer], v[kPer], ks[kPer], vs[kPer];
+        Held k[kPer], v[kPer];
+        uint32_t ks[kPer], vs[kPer];
 #pragma unroll
-            for (int x = 0; x < kPer; ++x) {
-                if (r0 + r_mine + x * side >= r1) break;
-                const size_t row = held_row(x), code = row * pieces + cc, scale = row * p.s.bytes + cc / 2;
-                if (p.k_out) {
-                    k[x] = reinterpret_cast<const uint32_t *>(c.k)[code];
-                    ks[x] = p.s.k[scale];
-                }
-                if (p.v_out) {
-                    v[x] = reinterpret_cast<const uint32_t *>(c.v)[code];
-                    vs[x] = p.s.v[scale];
-                }
+        for (int x = 0; x < kPer; ++x) {
+            if (r0 + r_mine + x * side >= r1) break;
+            const size_t row = held_row(x), from = row * pieces + cc, scale = row * p.s.bytes + cc * (int)sizeof(Held) / 8;
+            if (p.k_out) {
+                k[x] = reinterpret_cast<const Held *>(c.k)[from];
+                if (kFour) ks[x] = p.s.k[scale];
             }
-#pragma unroll
-            for (int x = 0; x < kPer; ++x) {
-                if (r0 + r_mine + x * side >= r1) break;
-                const size_t to = given(x) * 8;
-                if (p.k_out) store_values(reinterpret_cast<T *>(p.k_out) + to, k[x], ks[x]);
-                if (p.v_out) store_values(reinterpret_cast<T *>(p.v_out) + to, v[x], vs[x]);
+            if (p.v_out) {
+                v[x] = reinterpret_cast<const Held *>(c.v)[from];
+                if (kFour) vs[x] = p.s.v[scale];
             }
-        } else {
-            uint4 k[kPer], v[kPer];
+        }
 #pragma unroll
-            for (int x = 0; x < kPer; ++x) {
-                if (r0 + r_mine + x * side >= r1) break;
-                const size_t from = held_row(x) * pieces + cc;
-                if (p.k_out) k[x] = reinterpret_cast<const uint4 *>(c.k)[from];
-                if (p.v_out) v[x] = reinterpret_cast<const uint4 *>(c.v)[from];
-            }
-#pragma unroll
-            for (int x = 0; x < kPer; ++x) {
-                if (r0 + r_mine + x * side >= r1) break;
-                const size_t to = given(x);
+        for (int x = 0; x < kPer; ++x) {
+            if (r0 + r_mine + x * side >= r1) break;
+            const size_t to = given(x);
+            if constexpr (kFour) {
+                if (p.k_out) reinterpret_cast<uint4 *>(p.k_out)[to] = values<T>(k[x], ks[x]);
+                if (p.v_out) reinterpret_cast<uint4 *>(p.v_out)[to] = values<T>(v[x], vs[x]);
+            } else {
                 if (p.k_out) reinterpret_cast<uint4 *>(p.k_out)[to] = k[x];
                 if (p.v_out) reinterpret_cast<uint4 *>(p.v_out)[to] = v[x];
             }
@@ -142,7 +128,7 @@ template <typename T> cudaError_t launch(const CacheReadParams &p, int pieces, c
 
 cudaError_t launch_cache_read(int dtype, const CacheReadParams &p, cudaStream_t s) {
     if (!p.s.k) return launch<uint4>(p, p.c.dim * (dtype == FUSION_BF16 ? 2 : 4) / 16, s);
-    return dtype == FUSION_BF16 ? launch<__nv_bfloat16>(p, p.c.dim / 8, s) : launch<float>(p, p.c.dim / 8, s);
+    return dtype == FUSION_BF16 ? launch<__nv_bfloat16>(p, p.c.dim / 8, s) : launch<float>(p, p.c.dim / 4, s);
 }
 
 }  // namespace fz

@@ -5,9 +5,15 @@
 // 4 bits: fp4.cuh.  Bound by memory: every row is read once and written once, a row of the table is read once per row and
 // comes mostly from the caches.
 //
-// A thread has one unit of a row, two segments of S dims (8, or a group of 16 in 4 bits) that a rotation by halves turns with
-// one another, and in turn that unit of several heads of keys, queries and values, kPer of them asked for at once: the cosines
-// and sines stay in registers.  Units lie next to each other in the lanes, then heads, then rows.
+// A thread has one unit of a row, two segments of S dims (16 bytes, or a group of 16 dims in 4 bits) that a rotation by halves turns
+// with one another: that unit of several heads of keys, queries and values in turn, then of its next row.  The cosines and sines
+// stay in registers for a row.  Units lie next to each other in the lanes, then heads, then rows; a unit's segments lie half of the
+// dims apart in any case, so that the lanes' first segments are next to each other (one behind the other in a thread they are
+// half sectors to each access: 64 x 577 float32 158 us).  What a thread will need it asks for
+// itself, up to kDepth units ahead into a ring of its own in shared memory (cp.async, no barriers), so that about 190 KB per SM
+// are on their way.
+#include <atomic>
+
 #include "cache_rows.cuh"
 #include "fp4.cuh"
 
@@ -16,12 +22,20 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kBadShift = 16;   // a sample's counter: its CTAs that are done, and from this bit on those with a bad position
-constexpr int kMostX = 2432;    // CTAs of a sample, at most (four waves of four on each of 152 SMs)
+constexpr int kMostX = 2432;    // CTAs of a sample, at most
 static_assert(kMostX < 1 << kBadShift, "a sample's CTAs are counted below the bad ones");
 
+constexpr int kTurns = 4;
+
 enum Pairs { kNone, kHalves, kAdjacent };
-// Heads of a thread in flight: as many as registers hold without spills.
-template <typename T, bool kFour> constexpr int per_thread() { return kFour ? (sizeof(T) == 2 ? 2 : 1) : (sizeof(T) == 2 ? 4 : 2); }
+
+// CTAs of an SM, by the registers that a unit's dims and angles take, and units of a thread's ring.
+template <typename T, bool kFour, int P>
+struct Shape {
+    static constexpr int S = kFour ? 16 : 16 / (int)sizeof(T), kChunks = S * (int)sizeof(T) / 16;   // 16 bytes of a segment
+    static constexpr int kCtas = kFour && P != kNone ? 2 : 3;
+    static constexpr int kDepth = (kCtas == 2 ? 24 : 16) / (2 * kChunks), kSmem = kDepth * 2 * kChunks * kThreads * 16;
+};
 
 template <typename T> __device__ __forceinline__ void to_float(const uint4 &w, float *x);
 template <> __device__ __forceinline__ void to_float<float>(const uint4 &w, float *x) {
@@ -49,16 +63,30 @@ template <> __device__ __forceinline__ uint4 from_float<__nv_bfloat16>(const flo
     return make_uint4(v[0], v[1], v[2], v[3]);
 }
 
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Two segments of S numbers, as they lie in memory.
 template <typename T, int S>
 struct Unit {
     static constexpr int kChunk = 16 / (int)sizeof(T), kChunks = S / kChunk;   // numbers of 16 bytes; 16 bytes of a segment
     uint4 w[2][kChunks];
-    __device__ __forceinline__ void load(const T *a, const T *b, bool second) {
+    // From a thread's place in the ring, where its chunks lie kThreads apart; and their copy to there.
+    __device__ __forceinline__ void load(const uint4 *ring) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < kChunks; ++i) w[s][i] = ring[(s * kChunks + i) * kThreads];
+    }
+    // (segments of more than 16 bytes are asked for in half sectors, whose other half the L1 keeps)
+    static __device__ __forceinline__ void ask16(uint4 *dst, const T *src) {
+        if constexpr (kChunks == 1) cp_async16(dst, src);
+        else asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+    }
+    static __device__ __forceinline__ void ask(uint4 *ring, const T *a, const T *b, bool second) {
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
-            w[0][i] = reinterpret_cast<const uint4 *>(a)[i];
-            if (second) w[1][i] = reinterpret_cast<const uint4 *>(b)[i];
+            ask16(ring + i * kThreads, a + i * kChunk);
+            if (second) ask16(ring + (kChunks + i) * kThreads, b + i * kChunk);
         }
     }
     __device__ __forceinline__ void store(T *a, T *b, bool second) const {
@@ -78,16 +106,36 @@ struct Unit {
     }
 };
 
-// Cosines and sines of a unit's S pairs.
-template <int S>
+// N floats, 16- or 8-byte aligned.
+template <int N> __device__ __forceinline__ void load_floats(const float *src, float *x) {
+    if constexpr (N == 2) {
+        const float2 v = *reinterpret_cast<const float2 *>(src);
+        x[0] = v.x, x[1] = v.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4) {
+            const float4 v = *reinterpret_cast<const float4 *>(src + i);
+            x[i] = v.x, x[i + 1] = v.y, x[i + 2] = v.z, x[i + 3] = v.w;
+        }
+    }
+}
+// Cosines and sines of a unit's S pairs: those of the first segment's dims with the second's, or of neighbours in each.
+template <int S, int P>
 struct Angles {
     float c[S], s[S];
-    __device__ __forceinline__ void load(const float *row, int half, int pair) {
-#pragma unroll
-        for (int i = 0; i < S; i += 4) {
-            const float4 v = *reinterpret_cast<const float4 *>(row + pair + i), w = *reinterpret_cast<const float4 *>(row + half + pair + i);
-            c[i] = v.x, c[i + 1] = v.y, c[i + 2] = v.z, c[i + 3] = v.w;
-            s[i] = w.x, s[i + 1] = w.y, s[i + 2] = w.z, s[i + 3] = w.w;
+    __device__ __forceinline__ void load(const float *row, int half, int a, int b, bool first, bool second) {
+        if constexpr (P == kHalves) {
+            load_floats<S>(row + a, c);
+            load_floats<S>(row + half + a, s);
+        } else {
+            if (first) {
+                load_floats<S / 2>(row + a / 2, c);
+                load_floats<S / 2>(row + half + a / 2, s);
+            }
+            if (second) {
+                load_floats<S / 2>(row + b / 2, c + S / 2);
+                load_floats<S / 2>(row + half + b / 2, s + S / 2);
+            }
         }
     }
     static __device__ __forceinline__ void turn(float &a, float &b, float c, float s) {
@@ -95,15 +143,19 @@ struct Angles {
         b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
         a = x;
     }
-    template <int P> __device__ __forceinline__ void turn(float (&a)[S], float (&b)[S]) const {
+    __device__ __forceinline__ void turn(float (&a)[S], float (&b)[S], bool first, bool second) const {
         if constexpr (P == kHalves) {
 #pragma unroll
             for (int i = 0; i < S; ++i) turn(a[i], b[i], c[i], s[i]);
         } else {
+            if (first) {
 #pragma unroll
-            for (int i = 0; i < S / 2; ++i) turn(a[2 * i], a[2 * i + 1], c[i], s[i]);
+                for (int i = 0; i < S / 2; ++i) turn(a[2 * i], a[2 * i + 1], c[i], s[i]);
+            }
+            if (second) {
 #pragma unroll
-            for (int i = 0; i < S / 2; ++i) turn(b[2 * i], b[2 * i + 1], c[S / 2 + i], s[S / 2 + i]);
+                for (int i = 0; i < S / 2; ++i) turn(b[2 * i], b[2 * i + 1], c[S / 2 + i], s[S / 2 + i]);
+            }
         }
     }
 };
@@ -111,8 +163,10 @@ struct Angles {
 // Rows of CTAs as in k_cache_append: one per sample, and one more for the lengths while the grid has room for it.  `lanes`:
 // threads that share the heads of a unit.
 template <typename T, bool kFour, int P>
-__global__ void __launch_bounds__(kThreads, 2) k_cache_store(CacheStoreParams p, int units, int lanes) {
-    constexpr int S = kFour ? 16 : 8, kPer = per_thread<T, kFour>();
+__global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_store(CacheStoreParams p, int units, int lanes) {
+    using X = Shape<T, kFour, P>;
+    constexpr int S = X::S, kDepth = X::kDepth, kSlot = 2 * X::kChunks * kThreads;
+    extern __shared__ __align__(16) uint4 ring[];   // [kDepth][2 kChunks][kThreads]
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
@@ -129,6 +183,40 @@ __global__ void __launch_bounds__(kThreads, 2) k_cache_store(CacheStoreParams p,
     }
     const int o0 = p.in.offsets[i], n = p.in.offsets[i + 1] - o0, at = c.lengths[slot];
     const bool rows_ok = o0 >= 0 && n >= 0 && n <= p.in.max_tokens && (long long)o0 + n <= p.in.max_rows;
+
+    // this thread's unit: its dims, whether they are rotated, and its first head and row
+    const int per_row = units * lanes, side = kThreads / per_row, mine = tid / per_row, u = tid % units, lane = tid / units % lanes;
+    // where values (and keys and queries but for a rotation by halves) have its segments, and where keys and queries have them
+    const int plain_a = S * u, plain_b = S * (u + units);
+    const int turning = P == kHalves ? p.turned / (2 * S) : 0;   // units that a rotation by halves turns, the first ones
+    const int a = P == kHalves && u >= turning ? p.turned + S * (u - turning) : plain_a;
+    const int b = P != kHalves ? plain_b : u < turning ? a + p.turned / 2 : a + S * (units - turning);
+    const bool turn_a = P == kHalves ? u < turning : P == kAdjacent && a < p.turned, turn_b = P == kHalves ? turn_a : P == kAdjacent && b < p.turned;
+    const bool second = b < c.dim, plain_second = plain_b < c.dim;   // (where S divides the dims an odd number of times)
+    const int heads = p.q ? p.heads : 0, all = 2 * c.kv_heads + heads;   // keys, queries, values
+    const int r_first = mine < side && rows_ok ? (int)blockIdx.x * side + mine : n, r_step = (int)gridDim.x * side;
+    int ask_r = r_first, ask_x = lane, ask_at = 0;   // the next unit to ask for, and its place in the ring
+    auto ask = [&]() {
+        if (ask_r < n) {
+            const bool value = ask_x >= c.kv_heads + heads;
+            const size_t row = (size_t)(o0 + ask_r);
+            const unsigned char *base = ask_x < c.kv_heads ? p.k + row * p.k_stride : value ? p.v + row * p.v_stride : p.q + row * p.q_stride;
+            const int h = ask_x < c.kv_heads ? ask_x : value ? ask_x - c.kv_heads - heads : ask_x - c.kv_heads;
+            const T *src = reinterpret_cast<const T *>(base) + (size_t)h * c.dim;
+            if (value) Unit<T, S>::ask(ring + ask_at * kSlot + tid, src + plain_a, src + plain_b, plain_second);
+            else Unit<T, S>::ask(ring + ask_at * kSlot + tid, src + a, src + b, second);
+            ask_x += lanes;
+            if (ask_x >= all) {
+                ask_x = lane;
+                ask_r += r_step;
+            }
+        }
+        cp_async_commit();
+        ask_at = ask_at + 1 == kDepth ? 0 : ask_at + 1;
+    };
+#pragma unroll 1
+    for (int d = 0; d < kDepth - 1; ++d) ask();
+
     int bad = !rows_ok ? FUSION_DEV_BAD_OFFSETS : at < 0 || at > c.capacity || n > c.capacity - at ? FUSION_DEV_BAD_CACHE : 0;
     const unsigned *pages = reinterpret_cast<const unsigned *>(c.table) + (size_t)slot * c.max_pages;
     bool wrong = false;
@@ -141,97 +229,76 @@ __global__ void __launch_bounds__(kThreads, 2) k_cache_store(CacheStoreParams p,
             raise_status(p.status, bad);
             if (!p.in_place) p.lengths_out[slot] = at;
         }
+        cp_async_wait<0>();
         return;
     }
-    // this thread's unit: its dims, whether they are rotated, and its first head
-    const int per_row = units * lanes, side = kThreads / per_row, mine = tid / per_row, u = tid % units, lane = tid / units % lanes;
-    const int turning = p.turned / (2 * S);   // units that a rotation turns, the first ones
-    const bool turned = P != kNone && u < turning;
-    const int plain_a = 2 * S * u;
-    const int a = P == kHalves ? (u < turning ? S * u : p.turned + 2 * S * (u - turning)) : plain_a;
-    const int b = P == kHalves && u < turning ? a + p.turned / 2 : a + S;
-    const bool second = b < c.dim, plain_second = plain_a + S < c.dim;   // (of 8 dims, a row's last unit may have one segment)
-    const int heads = p.q ? p.heads : 0, all = 2 * c.kv_heads + heads;   // keys, queries, values
     const unsigned low = (1u << c.shift) - 1u;
+    // page and position of a row, read a row ahead (0 and 0 behind the last)
+    auto page_of = [&](int r) { return r < n ? pages[(at + r) >> c.shift] : 0u; };
+    auto position_of = [&](int r) { return P == kNone ? 0u : r >= n ? 0u : (unsigned)(p.positions ? p.positions[o0 + r] : at + r); };
+    unsigned next_page = page_of(r_first), next_pos = position_of(r_first);
     bool bad_position = false;
-    for (int r0 = blockIdx.x * side; r0 < n; r0 += gridDim.x * side) {
-        const int r = r0 + mine;
-        if (mine >= side || r >= n) continue;
-        unsigned page;
-        if (!cache_page(c, slot, at + r, page)) continue;   // (checked)
-        const unsigned place = (unsigned)(at + r) & low;
+    int have_at = 0;
+    for (int r = r_first; r < n; r += r_step) {
+        const unsigned page = next_page, pos = next_pos, place = (unsigned)(at + r) & low;
+        const bool known = P == kNone || pos < (unsigned)p.table_rows;   // a row without a position in the table is left out
+        bad_position |= !known;
+        Angles<S, P> w;
+        if constexpr (P != kNone)
+            if (known && (turn_a || turn_b)) w.load(p.table + (size_t)pos * p.turned, p.turned / 2, a, b, turn_a, turn_b);
+        next_page = page_of(r + r_step);
+        next_pos = position_of(r + r_step);
         const size_t row = (size_t)(o0 + r);
-        Angles<S> w;
-        if constexpr (P != kNone) {
-            const unsigned pos = (unsigned)(p.positions ? p.positions[row] : at + r);
-            if (pos >= (unsigned)p.table_rows) {
-                bad_position = true;
-                continue;
-            }
-            if (turned) w.load(p.table + (size_t)pos * p.turned, p.turned / 2, S * u);
-        }
-        for (int x0 = lane; x0 < all; x0 += lanes * kPer) {
-            Unit<T, S> v[kPer];
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                const int x = x0 + k * lanes;
-                if (x >= all) break;
-                const bool value = x >= c.kv_heads + heads;
-                const unsigned char *base = x < c.kv_heads ? p.k + row * p.k_stride
-                                            : value        ? p.v + row * p.v_stride
-                                                           : p.q + row * p.q_stride;
-                const int h = x < c.kv_heads ? x : value ? x - c.kv_heads - heads : x - c.kv_heads;
-                const T *src = reinterpret_cast<const T *>(base) + (size_t)h * c.dim;
-                if (value) v[k].load(src + plain_a, src + plain_a + S, plain_second);
-                else v[k].load(src + a, src + b, second);
-            }
-#pragma unroll
-            for (int k = 0; k < kPer; ++k) {
-                const int x = x0 + k * lanes;
-                if (x >= all) break;
-                const bool value = x >= c.kv_heads + heads, query = !value && x >= c.kv_heads;
-                const int h = x < c.kv_heads ? x : value ? x - c.kv_heads - heads : x - c.kv_heads;
-                const int da = value ? plain_a : a, db = value ? plain_a + S : b;
-                const bool two = value ? plain_second : second;
-                if (!kFour || query) {
-                    if constexpr (P != kNone)
-                        if (turned && !value) {
-                            float xa[S], xb[S];
-                            v[k].floats(0, xa);
-                            v[k].floats(1, xb);
-                            w.template turn<P>(xa, xb);
-                            v[k].set(0, xa);
-                            v[k].set(1, xb);
-                        }
-                    unsigned char *pool = value ? c.v : c.k;
-                    T *dst = query ? reinterpret_cast<T *>(p.q_out) + (row * heads + h) * c.dim
-                                   : reinterpret_cast<T *>(pool) + (size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + place) * c.dim;
-                    v[k].store(dst + da, dst + db, two);
-                } else if constexpr (kFour) {
-                    float xa[S], xb[S];
-                    v[k].floats(0, xa);
-                    v[k].floats(1, xb);
-                    if constexpr (P != kNone)
-                        if (turned && !value) w.template turn<P>(xa, xb);
-                    const size_t to = (size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + place);
-                    unsigned char *codes = (value ? c.v : c.k) + to * (c.dim / 2), *scales = (value ? p.s.v : p.s.k) + to * p.s.bytes;
-                    uint32_t sa, sb;
-                    const uint2 ca = quantise(xa, sa), cb = quantise(xb, sb);
-                    *reinterpret_cast<uint2 *>(codes + da / 2) = ca;
-                    *reinterpret_cast<uint2 *>(codes + db / 2) = cb;
-                    scales[da / 16] = (unsigned char)sa;
-                    scales[db / 16] = (unsigned char)sb;
-                    if (u == 0)   // (the bytes behind the last scale)
-                        for (int e = c.dim / 16; e < p.s.bytes; ++e) scales[e] = 0;
-                }
+#pragma unroll 1
+        for (int x = lane; x < all; x += lanes) {
+            ask();
+            cp_async_wait<kDepth - 1>();
+            Unit<T, S> v;
+            v.load(ring + have_at * kSlot + tid);
+            have_at = have_at + 1 == kDepth ? 0 : have_at + 1;
+            if (!known) continue;
+            const bool value = x >= c.kv_heads + heads, query = !value && x >= c.kv_heads;
+            const int h = x < c.kv_heads ? x : value ? x - c.kv_heads - heads : x - c.kv_heads;
+            const int da = value ? plain_a : a, db = value ? plain_b : b;
+            if (!kFour || query) {
+                if constexpr (P != kNone)
+                    if ((turn_a || turn_b) && !value) {
+                        float xa[S], xb[S];
+                        v.floats(0, xa);
+                        v.floats(1, xb);
+                        w.turn(xa, xb, turn_a, turn_b);
+                        if (turn_a) v.set(0, xa);
+                        if (turn_b) v.set(1, xb);
+                    }
+                unsigned char *pool = value ? c.v : c.k;
+                T *dst = query ? reinterpret_cast<T *>(p.q_out) + (row * heads + h) * c.dim
+                               : reinterpret_cast<T *>(pool) + (size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + place) * c.dim;
+                v.store(dst + da, dst + db, value ? plain_second : second);
+            } else if constexpr (kFour) {
+                float xa[S], xb[S];
+                v.floats(0, xa);
+                v.floats(1, xb);
+                if constexpr (P != kNone)
+                    if ((turn_a || turn_b) && !value) w.turn(xa, xb, turn_a, turn_b);
+                const size_t to = (size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + place);
+                unsigned char *codes = (value ? c.v : c.k) + to * (c.dim / 2), *scales = (value ? p.s.v : p.s.k) + to * p.s.bytes;
+                uint32_t sa, sb;
+                const uint2 ca = quantise(xa, sa), cb = quantise(xb, sb);
+                *reinterpret_cast<uint2 *>(codes + da / 2) = ca;
+                *reinterpret_cast<uint2 *>(codes + db / 2) = cb;
+                scales[da / 16] = (unsigned char)sa;
+                scales[db / 16] = (unsigned char)sb;
+                if (u == 0)   // (the bytes behind the last scale)
+                    for (int e = c.dim / 16; e < p.s.bytes; ++e) scales[e] = 0;
             }
         }
-        if (u == 0 && lane == 0) {
+        if (u == 0 && lane == 0 && known) {
             const size_t s = ((size_t)page << c.shift) + place;
             if (c.sizes) c.sizes[s] = p.sizes ? p.sizes[row] : 1.0f;
             if (c.weights) c.weights[s] = p.scores ? p.scores[row] : 0.0f;
         }
     }
+    cp_async_wait<0>();
     // every CTA of the sample has read its length before the last one raises it
     const bool any = __syncthreads_or(bad_position);
     if (tid == 0) {
@@ -249,21 +316,53 @@ __global__ void __launch_bounds__(kThreads, 2) k_cache_store(CacheStoreParams p,
     }
 }
 
+// How many threads share a unit's heads: of the numbers that let no more rows lie side by side than there are, one that leaves the
+// fewest threads idle, a small one, since a thread reads the angles of its unit once per row.
+int lanes_of(int units, int all, long long rows) {
+    const int most = all < kThreads / units ? all : kThreads / units;
+    int best = most;
+    double best_used = 0.0;
+    for (int lanes = most; lanes >= 1; --lanes) {
+        const int side = kThreads / (units * lanes);
+        if (side > rows && lanes < most) break;
+        const double used = (double)side * units * lanes / kThreads * all / (double)(ceil_div(all, lanes) * lanes);
+        if (used >= best_used) {
+            best = lanes;
+            best_used = used;
+        }
+    }
+    return best;
+}
+
 template <typename T, bool kFour, int P>
 cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
-    constexpr int S = kFour ? 16 : 8, kPer = per_thread<T, kFour>();
-    const int units = ceil_div(p.c.dim, 2 * S), all = 2 * p.c.kv_heads + (p.q ? p.heads : 0);
-    int lanes = ceil_div(all, kPer);
-    if (lanes > kThreads / units) lanes = kThreads / units;
-    const int rows = kThreads / (units * lanes);
+    using X = Shape<T, kFour, P>;
+    constexpr int kDevices = 64;
+    static std::atomic<bool> allowed[kDevices];   // the kernel's shared memory, asked for once per device
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e == cudaSuccess && !(device < kDevices && allowed[device].load(std::memory_order_acquire))) {
+        e = cudaFuncSetAttribute(k_cache_store<T, kFour, P>, cudaFuncAttributeMaxDynamicSharedMemorySize, X::kSmem);
+        if (e == cudaSuccess && device < kDevices) allowed[device].store(true, std::memory_order_release);
+    }
+    if (e != cudaSuccess) return e;
+    const int units = ceil_div(p.c.dim, 2 * X::S), all = 2 * p.c.kv_heads + (p.q ? p.heads : 0);
     // (samples of more rows than the cache has room for, or than there are, write nothing)
     long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
     if (most > p.in.max_rows) most = p.in.max_rows;
-    long long x = most > 0 ? (most + rows - 1) / rows : 1;
+    if (most < 1) most = 1;
+    const int lanes = lanes_of(units, all, most), side = kThreads / (units * lanes);
+    // as many rows a CTA as make its start worth while (kTurns rings), unless that leaves SMs without two rounds of CTAs
+    const long long steps = (most + side - 1) / side, per_step = ceil_div(all, lanes);
+    long long turns = (kTurns * X::kDepth + per_step - 1) / per_step;
+    const long long least = (2ll * 152 * X::kCtas + p.in.max_batch) / (p.in.max_batch + 1);   // CTAs of a sample
+    if (turns > steps / least) turns = steps / least;
+    if (turns < 1) turns = 1;
+    long long x = (steps + turns - 1) / turns;
     if (x > kMostX) x = kMostX;
     static_assert(FUSION_CACHE_MAX_BATCH <= kMostY, "a row of CTAs per sample");
     const dim3 grid((unsigned)x, (unsigned)(p.in.max_batch < kMostY ? p.in.max_batch + 1 : kMostY));
-    return launch_after(k_cache_store<T, kFour, P>, grid, kThreads, 0, 1, s, p, units, lanes);
+    return launch_after(k_cache_store<T, kFour, P>, grid, kThreads, X::kSmem, 1, s, p, units, lanes);
 }
 template <typename T, bool kFour>
 cudaError_t launch_pairs(int pairs, const CacheStoreParams &p, cudaStream_t s) {

@@ -37,35 +37,38 @@ struct Shape {
     static constexpr int kDepth = (kCtas == 2 ? 24 : 16) / (2 * kChunks), kSmem = kDepth * 2 * kChunks * kThreads * 16;
 };
 
-template <typename T> __device__ __forceinline__ void to_float(const uint4 &w, float *x);
-template <> __device__ __forceinline__ void to_float<float>(const uint4 &w, float *x) {
-    x[0] = __uint_as_float(w.x), x[1] = __uint_as_float(w.y), x[2] = __uint_as_float(w.z), x[3] = __uint_as_float(w.w);
-}
-template <> __device__ __forceinline__ void to_float<__nv_bfloat16>(const uint4 &w, float *x) {
-    const uint32_t v[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        x[2 * i] = __uint_as_float(v[i] << 16);
-        x[2 * i + 1] = __uint_as_float(v[i] & 0xFFFF0000u);
-    }
-}
-template <typename T> __device__ __forceinline__ uint4 from_float(const float *x);
-template <> __device__ __forceinline__ uint4 from_float<float>(const float *x) {
-    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
-}
-template <> __device__ __forceinline__ uint4 from_float<__nv_bfloat16>(const float *x) {
-    uint32_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-        v[i] = *reinterpret_cast<const uint32_t *>(&p);
-    }
-    return make_uint4(v[0], v[1], v[2], v[3]);
-}
-
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Two segments of S numbers, as they lie in memory.
+// S dims, the even ones in e, the odd ones in o, two to a register pair.
+template <int S> struct Segment {
+    float2 e[S / 4], o[S / 4];
+};
+// 16 bytes as they lie in memory, at dim i of a segment.
+template <int S> __device__ __forceinline__ void unpack(const uint4 &w, const float *, Segment<S> &x, int i) {
+    x.e[i / 4] = make_float2(__uint_as_float(w.x), __uint_as_float(w.z));
+    x.o[i / 4] = make_float2(__uint_as_float(w.y), __uint_as_float(w.w));
+}
+template <int S> __device__ __forceinline__ void unpack(const uint4 &w, const __nv_bfloat16 *, Segment<S> &x, int i) {
+    auto low = [](uint32_t v) { return __uint_as_float(v << 16); };
+    auto high = [](uint32_t v) { return __uint_as_float(v & 0xFFFF0000u); };
+    x.e[i / 4] = make_float2(low(w.x), low(w.y));
+    x.o[i / 4] = make_float2(high(w.x), high(w.y));
+    x.e[i / 4 + 1] = make_float2(low(w.z), low(w.w));
+    x.o[i / 4 + 1] = make_float2(high(w.z), high(w.w));
+}
+template <int S> __device__ __forceinline__ void pack(const Segment<S> &x, int i, float *, uint4 &w) {
+    w = make_uint4(__float_as_uint(x.e[i / 4].x), __float_as_uint(x.o[i / 4].x), __float_as_uint(x.e[i / 4].y), __float_as_uint(x.o[i / 4].y));
+}
+template <int S> __device__ __forceinline__ void pack(const Segment<S> &x, int i, __nv_bfloat16 *, uint4 &w) {
+    auto both = [](float a, float b) {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+        return *reinterpret_cast<const uint32_t *>(&p);
+    };
+    w = make_uint4(both(x.e[i / 4].x, x.o[i / 4].x), both(x.e[i / 4].y, x.o[i / 4].y), both(x.e[i / 4 + 1].x, x.o[i / 4 + 1].x),
+                   both(x.e[i / 4 + 1].y, x.o[i / 4 + 1].y));
+}
+
+// Two segments of S dims, as they lie in memory.
 template <typename T, int S>
 struct Unit {
     static constexpr int kChunk = 16 / (int)sizeof(T), kChunks = S / kChunk;   // numbers of 16 bytes; 16 bytes of a segment
@@ -96,13 +99,13 @@ struct Unit {
             if (second) reinterpret_cast<uint4 *>(b)[i] = w[1][i];
         }
     }
-    __device__ __forceinline__ void floats(int s, float (&x)[S]) const {
+    __device__ __forceinline__ void get(int s, Segment<S> &x) const {
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) to_float<T>(w[s][i], x + i * kChunk);
+        for (int i = 0; i < kChunks; ++i) unpack<S>(w[s][i], (const T *)nullptr, x, i * kChunk);
     }
-    __device__ __forceinline__ void set(int s, const float (&x)[S]) {
+    __device__ __forceinline__ void set(int s, const Segment<S> &x) {
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) w[s][i] = from_float<T>(x + i * kChunk);
+        for (int i = 0; i < kChunks; ++i) pack<S>(x, i * kChunk, (T *)nullptr, w[s][i]);
     }
 };
 
@@ -119,42 +122,58 @@ template <int N> __device__ __forceinline__ void load_floats(const float *src, f
         }
     }
 }
-// Cosines and sines of a unit's S pairs: those of the first segment's dims with the second's, or of neighbours in each.
+// Every product is rounded by itself: the sums go one by one, since the assembler makes mul2 and add2 one operation with one rounding.
+__device__ __forceinline__ void turn(float2 &a, float2 &b, float2 c, float2 s) {
+    const float2 ac = mul2(a, c), bs = mul2(b, s), bc = mul2(b, c), as = mul2(a, s);
+    a = make_float2(__fadd_rn(ac.x, -bs.x), __fadd_rn(ac.y, -bs.y));
+    b = make_float2(__fadd_rn(bc.x, as.x), __fadd_rn(bc.y, as.y));
+}
+// Cosines and sines of a unit's S pairs: those of the first segment's dims with the second's (even ones, odd ones), or of
+// neighbours, that is of an even dim with the next, in each.
 template <int S, int P>
 struct Angles {
-    float c[S], s[S];
+    float2 c[S / 2], s[S / 2];
     __device__ __forceinline__ void load(const float *row, int half, int a, int b, bool first, bool second) {
+        float x[S], y[S];
         if constexpr (P == kHalves) {
-            load_floats<S>(row + a, c);
-            load_floats<S>(row + half + a, s);
+            load_floats<S>(row + a, x);
+            load_floats<S>(row + half + a, y);
+#pragma unroll
+            for (int i = 0; i < S / 4; ++i) {
+                c[i] = make_float2(x[4 * i], x[4 * i + 2]), c[S / 4 + i] = make_float2(x[4 * i + 1], x[4 * i + 3]);
+                s[i] = make_float2(y[4 * i], y[4 * i + 2]), s[S / 4 + i] = make_float2(y[4 * i + 1], y[4 * i + 3]);
+            }
         } else {
             if (first) {
-                load_floats<S / 2>(row + a / 2, c);
-                load_floats<S / 2>(row + half + a / 2, s);
+                load_floats<S / 2>(row + a / 2, x);
+                load_floats<S / 2>(row + half + a / 2, y);
             }
             if (second) {
-                load_floats<S / 2>(row + b / 2, c + S / 2);
-                load_floats<S / 2>(row + half + b / 2, s + S / 2);
+                load_floats<S / 2>(row + b / 2, x + S / 2);
+                load_floats<S / 2>(row + half + b / 2, y + S / 2);
+            }
+#pragma unroll
+            for (int i = 0; i < S / 2; ++i) {
+                c[i] = make_float2(x[2 * i], x[2 * i + 1]);
+                s[i] = make_float2(y[2 * i], y[2 * i + 1]);
             }
         }
     }
-    static __device__ __forceinline__ void turn(float &a, float &b, float c, float s) {
-        const float x = __fadd_rn(__fmul_rn(a, c), -__fmul_rn(b, s));
-        b = __fadd_rn(__fmul_rn(b, c), __fmul_rn(a, s));
-        a = x;
-    }
-    __device__ __forceinline__ void turn(float (&a)[S], float (&b)[S], bool first, bool second) const {
+    __device__ __forceinline__ void turn_unit(Segment<S> &a, Segment<S> &b, bool first, bool second) const {
         if constexpr (P == kHalves) {
 #pragma unroll
-            for (int i = 0; i < S; ++i) turn(a[i], b[i], c[i], s[i]);
+            for (int i = 0; i < S / 4; ++i) {
+                turn(a.e[i], b.e[i], c[i], s[i]);
+                turn(a.o[i], b.o[i], c[S / 4 + i], s[S / 4 + i]);
+            }
         } else {
             if (first) {
 #pragma unroll
-                for (int i = 0; i < S / 2; ++i) turn(a[2 * i], a[2 * i + 1], c[i], s[i]);
+                for (int i = 0; i < S / 4; ++i) turn(a.e[i], a.o[i], c[i], s[i]);
             }
             if (second) {
 #pragma unroll
-                for (int i = 0; i < S / 2; ++i) turn(b[2 * i], b[2 * i + 1], c[S / 2 + i], s[S / 2 + i]);
+                for (int i = 0; i < S / 4; ++i) turn(b.e[i], b.o[i], c[S / 4 + i], s[S / 4 + i]);
             }
         }
     }
@@ -193,22 +212,35 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
     const int b = P != kHalves ? plain_b : u < turning ? a + p.turned / 2 : a + S * (units - turning);
     const bool turn_a = P == kHalves ? u < turning : P == kAdjacent && a < p.turned, turn_b = P == kHalves ? turn_a : P == kAdjacent && b < p.turned;
     const bool second = b < c.dim, plain_second = plain_b < c.dim;   // (where S divides the dims an odd number of times)
-    const int heads = p.q ? p.heads : 0, all = 2 * c.kv_heads + heads;   // keys, queries, values
+    const int heads = p.q ? p.heads : 0;
     const int r_first = mine < side && rows_ok ? (int)blockIdx.x * side + mine : n, r_step = (int)gridDim.x * side;
-    int ask_r = r_first, ask_x = lane, ask_at = 0;   // the next unit to ask for, and its place in the ring
+    // the next unit to ask for: keys, queries and values of a row (kinds 0, 1, 2), a thread's heads in turn; its place in the ring
+    int ask_r = r_first, ask_kind = 0, ask_h = lane, ask_at = 0;
+    const T *ask_src = nullptr;
+    auto find = [&]() {   // the first head of this thread from (ask_r, ask_kind) on
+        for (;;) {
+            if (ask_kind == 3) {
+                ask_kind = 0;
+                ask_r += r_step;
+            }
+            if (ask_r >= n || lane < (ask_kind == 1 ? heads : c.kv_heads)) break;
+            ++ask_kind;
+        }
+        const unsigned char *base = ask_kind == 0 ? p.k : ask_kind == 1 ? p.q : p.v;
+        const long long stride = ask_kind == 0 ? p.k_stride : ask_kind == 1 ? p.q_stride : p.v_stride;
+        ask_src = reinterpret_cast<const T *>(base + (size_t)(o0 + ask_r) * stride) + (size_t)lane * c.dim;
+        ask_h = lane;
+    };
+    find();
     auto ask = [&]() {
         if (ask_r < n) {
-            const bool value = ask_x >= c.kv_heads + heads;
-            const size_t row = (size_t)(o0 + ask_r);
-            const unsigned char *base = ask_x < c.kv_heads ? p.k + row * p.k_stride : value ? p.v + row * p.v_stride : p.q + row * p.q_stride;
-            const int h = ask_x < c.kv_heads ? ask_x : value ? ask_x - c.kv_heads - heads : ask_x - c.kv_heads;
-            const T *src = reinterpret_cast<const T *>(base) + (size_t)h * c.dim;
-            if (value) Unit<T, S>::ask(ring + ask_at * kSlot + tid, src + plain_a, src + plain_b, plain_second);
-            else Unit<T, S>::ask(ring + ask_at * kSlot + tid, src + a, src + b, second);
-            ask_x += lanes;
-            if (ask_x >= all) {
-                ask_x = lane;
-                ask_r += r_step;
+            const bool value = ask_kind == 2;
+            Unit<T, S>::ask(ring + ask_at * kSlot + tid, ask_src + (value ? plain_a : a), ask_src + (value ? plain_b : b), value ? plain_second : second);
+            ask_h += lanes;
+            ask_src += (size_t)lanes * c.dim;
+            if (ask_h >= (ask_kind == 1 ? heads : c.kv_heads)) {
+                ++ask_kind;
+                find();
             }
         }
         cp_async_commit();
@@ -244,53 +276,78 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
         const bool known = P == kNone || pos < (unsigned)p.table_rows;   // a row without a position in the table is left out
         bad_position |= !known;
         Angles<S, P> w;
+        const bool turned = turn_a || turn_b;
         if constexpr (P != kNone)
-            if (known && (turn_a || turn_b)) w.load(p.table + (size_t)pos * p.turned, p.turned / 2, a, b, turn_a, turn_b);
+            if (known && turned) w.load(p.table + (size_t)pos * p.turned, p.turned / 2, a, b, turn_a, turn_b);
         next_page = page_of(r + r_step);
         next_pos = position_of(r + r_step);
-        const size_t row = (size_t)(o0 + r);
-#pragma unroll 1
-        for (int x = lane; x < all; x += lanes) {
+        const size_t row = (size_t)(o0 + r), first_row = (size_t)((page * (unsigned)c.kv_heads) << c.shift) + place;   // of key head 0 in the pools
+        auto next_unit = [&](Unit<T, S> &v) {
             ask();
             cp_async_wait<kDepth - 1>();
-            Unit<T, S> v;
             v.load(ring + have_at * kSlot + tid);
             have_at = have_at + 1 == kDepth ? 0 : have_at + 1;
-            if (!known) continue;
-            const bool value = x >= c.kv_heads + heads, query = !value && x >= c.kv_heads;
-            const int h = x < c.kv_heads ? x : value ? x - c.kv_heads - heads : x - c.kv_heads;
-            const int da = value ? plain_a : a, db = value ? plain_b : b;
-            if (!kFour || query) {
+        };
+        auto put_codes = [&](const Unit<T, S> &v, bool turns, unsigned char *codes, unsigned char *scales, int da, int db, int h) {
+            if constexpr (kFour) {
+                Segment<S> xa, xb;
+                v.get(0, xa);
+                v.get(1, xb);
                 if constexpr (P != kNone)
-                    if ((turn_a || turn_b) && !value) {
-                        float xa[S], xb[S];
-                        v.floats(0, xa);
-                        v.floats(1, xb);
-                        w.turn(xa, xb, turn_a, turn_b);
-                        if (turn_a) v.set(0, xa);
-                        if (turn_b) v.set(1, xb);
-                    }
-                unsigned char *pool = value ? c.v : c.k;
-                T *dst = query ? reinterpret_cast<T *>(p.q_out) + (row * heads + h) * c.dim
-                               : reinterpret_cast<T *>(pool) + (size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + place) * c.dim;
-                v.store(dst + da, dst + db, value ? plain_second : second);
-            } else if constexpr (kFour) {
-                float xa[S], xb[S];
-                v.floats(0, xa);
-                v.floats(1, xb);
-                if constexpr (P != kNone)
-                    if ((turn_a || turn_b) && !value) w.turn(xa, xb, turn_a, turn_b);
-                const size_t to = (size_t)(((page * (unsigned)c.kv_heads + h) << c.shift) + place);
-                unsigned char *codes = (value ? c.v : c.k) + to * (c.dim / 2), *scales = (value ? p.s.v : p.s.k) + to * p.s.bytes;
+                    if (turns) w.turn_unit(xa, xb, turn_a, turn_b);
+                const size_t to = first_row + ((size_t)h << c.shift);
+                codes += to * (c.dim / 2);
+                scales += to * p.s.bytes;
                 uint32_t sa, sb;
-                const uint2 ca = quantise(xa, sa), cb = quantise(xb, sb);
+                const uint2 ca = quantise(xa.e, xa.o, sa), cb = quantise(xb.e, xb.o, sb);
                 *reinterpret_cast<uint2 *>(codes + da / 2) = ca;
                 *reinterpret_cast<uint2 *>(codes + db / 2) = cb;
                 scales[da / 16] = (unsigned char)sa;
                 scales[db / 16] = (unsigned char)sb;
                 if (u == 0)   // (the bytes behind the last scale)
-                    for (int e = c.dim / 16; e < p.s.bytes; ++e) scales[e] = 0;
+                    for (int x = c.dim / 16; x < p.s.bytes; ++x) scales[x] = 0;
             }
+        };
+        auto turn_in_place = [&](Unit<T, S> &v) {
+            if constexpr (P != kNone)
+                if (turned) {
+                    Segment<S> xa, xb;
+                    v.get(0, xa);
+                    v.get(1, xb);
+                    w.turn_unit(xa, xb, turn_a, turn_b);
+                    if (turn_a) v.set(0, xa);
+                    if (turn_b) v.set(1, xb);
+                }
+        };
+        const auto in_pool = [&](unsigned char *pool, int h) { return reinterpret_cast<T *>(pool) + (first_row + ((size_t)h << c.shift)) * c.dim; };
+#pragma unroll 1
+        for (int h = lane; h < c.kv_heads; h += lanes) {
+            Unit<T, S> v;
+            next_unit(v);
+            if (!known) continue;
+            if constexpr (kFour) {
+                put_codes(v, turned, c.k, p.s.k, a, b, h);
+            } else {
+                turn_in_place(v);
+                v.store(in_pool(c.k, h) + a, in_pool(c.k, h) + b, second);
+            }
+        }
+#pragma unroll 1
+        for (int h = lane; P != kNone && h < heads; h += lanes) {
+            Unit<T, S> v;
+            next_unit(v);
+            if (!known) continue;
+            turn_in_place(v);
+            T *dst = reinterpret_cast<T *>(p.q_out) + (row * heads + h) * c.dim;
+            v.store(dst + a, dst + b, second);
+        }
+#pragma unroll 1
+        for (int h = lane; h < c.kv_heads; h += lanes) {
+            Unit<T, S> v;
+            next_unit(v);
+            if (!known) continue;
+            if constexpr (kFour) put_codes(v, false, c.v, p.s.v, plain_a, plain_b, h);
+            else v.store(in_pool(c.v, h) + plain_a, in_pool(c.v, h) + plain_b, plain_second);
         }
         if (u == 0 && lane == 0 && known) {
             const size_t s = ((size_t)page << c.shift) + place;
@@ -316,16 +373,18 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
     }
 }
 
+// Units of a row that a thread has, if `lanes` threads share a unit's heads.
+int units_of(int lanes, int kv_heads, int heads) { return 2 * ceil_div(kv_heads, lanes) + ceil_div(heads, lanes); }
 // How many threads share a unit's heads: of the numbers that let no more rows lie side by side than there are, one that leaves the
 // fewest threads idle, a small one, since a thread reads the angles of its unit once per row.
-int lanes_of(int units, int all, long long rows) {
-    const int most = all < kThreads / units ? all : kThreads / units;
+int lanes_of(int units, int kv_heads, int heads, long long rows) {
+    const int more = heads > kv_heads ? heads : kv_heads, most = more < kThreads / units ? more : kThreads / units;
     int best = most;
     double best_used = 0.0;
     for (int lanes = most; lanes >= 1; --lanes) {
         const int side = kThreads / (units * lanes);
         if (side > rows && lanes < most) break;
-        const double used = (double)side * units * lanes / kThreads * all / (double)(ceil_div(all, lanes) * lanes);
+        const double used = (double)side * units * (2 * kv_heads + heads) / units_of(lanes, kv_heads, heads);
         if (used >= best_used) {
             best = lanes;
             best_used = used;
@@ -346,14 +405,14 @@ cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
         if (e == cudaSuccess && device < kDevices) allowed[device].store(true, std::memory_order_release);
     }
     if (e != cudaSuccess) return e;
-    const int units = ceil_div(p.c.dim, 2 * X::S), all = 2 * p.c.kv_heads + (p.q ? p.heads : 0);
+    const int units = ceil_div(p.c.dim, 2 * X::S), heads = p.q ? p.heads : 0;
     // (samples of more rows than the cache has room for, or than there are, write nothing)
     long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
     if (most > p.in.max_rows) most = p.in.max_rows;
     if (most < 1) most = 1;
-    const int lanes = lanes_of(units, all, most), side = kThreads / (units * lanes);
+    const int lanes = lanes_of(units, p.c.kv_heads, heads, most), side = kThreads / (units * lanes);
     // as many rows a CTA as make its start worth while (kTurns rings), unless that leaves SMs without two rounds of CTAs
-    const long long steps = (most + side - 1) / side, per_step = ceil_div(all, lanes);
+    const long long steps = (most + side - 1) / side, per_step = units_of(lanes, p.c.kv_heads, heads);
     long long turns = (kTurns * X::kDepth + per_step - 1) / per_step;
     const long long least = (2ll * 152 * X::kCtas + p.in.max_batch) / (p.in.max_batch + 1);   // CTAs of a sample
     if (turns > steps / least) turns = steps / least;

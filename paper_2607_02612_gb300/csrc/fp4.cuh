@@ -5,7 +5,7 @@
 
 #include <cuda_fp16.h>
 
-#include "common.cuh"
+#include "ln.cuh"
 
 namespace fz {
 
@@ -34,29 +34,43 @@ __device__ __forceinline__ uint32_t mul_half2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ float half_low(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)w)); }
 __device__ __forceinline__ float half_high(uint32_t w) { return __half2float(__ushort_as_half((unsigned short)(w >> 16))); }
 
-// A group of 16 numbers: its codes, eight to a word, and its scale's byte.
+// The largest magnitude of three numbers; NaN if one is.
+__device__ __forceinline__ float max_magnitude(float a, float b, float c) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
+    return r;
+}
+// A group of 16 numbers, the even ones in e and the odd ones in o: its codes, eight to a word, and its scale's byte.
 //
 // A code is the e2m1 number nearest to x / scale, ties to the even code, which is what the conversion makes of the quotient if
 // the division's rounding neither leaves a tie nor makes one.  A scale has 4 significant bits and a tie lies at one of 3, so
 // scale * tie is exact, and where x is not equal to it the quotient is further from the tie than its own rounding: correctly
-// rounded it serves.  It comes of y = x / scale but for a few roundings and one correction by the exact remainder x - y scale.
-__device__ __forceinline__ uint2 quantise(const float (&x)[16], uint32_t &scale) {
-    uint32_t top = 0u;   // (as whole numbers magnitudes order NaN above infinity above the rest)
+// rounded it serves.  It comes of y = -x / scale but for a few roundings and one correction by the exact remainder x + y scale
+// (of the negative quotient, so that -0 stays -0: the codes' signs are turned at the end).
+__device__ __forceinline__ uint2 quantise(const float2 (&e)[4], const float2 (&o)[4], uint32_t &scale) {
+    float top = fabsf(e[0].x);
+    top = max_magnitude(top, e[0].y, o[0].x);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) top = max(top, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    const float want = __uint_as_float(top) * (1.0f / 6.0f);
+    for (int i = 1; i < 4; ++i) {
+        top = max_magnitude(top, o[i - 1].y, e[i].x);
+        top = max_magnitude(top, e[i].y, o[i].x);
+    }
+    top = max_magnitude(top, o[3].y, o[3].y);
+    const float want = top * (1.0f / 6.0f);
     uint16_t s;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(0.0f), "f"(want));
     const float z = half_low(scales_to_half(s));
-    const bool fine = top < 0x7F800000u, some = fine && s != 0;
+    const bool fine = top < INFINITY, some = fine && s != 0;
     scale = fine ? (uint32_t)s : 0x7Fu;
-    const float inv = some ? __frcp_rn(z) : 0.0f;
-    float y[16];
+    const float inv = some ? -__frcp_rn(z) : 0.0f;
+    const float2 zz = make_float2(z, z), ii = make_float2(inv, inv);
+    float2 ye[4], yo[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float y0 = x[i] * inv;
-        const float y1 = fmaf(fmaf(-y0, z, x[i]), inv, y0);
-        y[i] = __uint_as_float((__float_as_uint(y1) & 0x7FFFFFFFu) | (__float_as_uint(x[i]) & 0x80000000u));   // (-0 stays -0)
+    for (int i = 0; i < 4; ++i) {
+        ye[i] = mul2(e[i], ii);
+        ye[i] = fma2(fma2(ye[i], zz, e[i]), ii, ye[i]);
+        yo[i] = mul2(o[i], ii);
+        yo[i] = fma2(fma2(yo[i], zz, o[i]), ii, yo[i]);
     }
     uint32_t w[2];
 #pragma unroll
@@ -68,9 +82,9 @@ __device__ __forceinline__ uint2 quantise(const float (&x)[16], uint32_t &scale)
             "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
             "mov.b32 %0, {b0, b1, b2, b3}; }"
             : "=r"(w[h])
-            : "f"(y[8 * h]), "f"(y[8 * h + 1]), "f"(y[8 * h + 2]), "f"(y[8 * h + 3]), "f"(y[8 * h + 4]), "f"(y[8 * h + 5]),
-              "f"(y[8 * h + 6]), "f"(y[8 * h + 7]));
-    return make_uint2(some ? w[0] : 0u, some ? w[1] : 0u);
+            : "f"(ye[2 * h].x), "f"(yo[2 * h].x), "f"(ye[2 * h].y), "f"(yo[2 * h].y), "f"(ye[2 * h + 1].x), "f"(yo[2 * h + 1].x),
+              "f"(ye[2 * h + 1].y), "f"(yo[2 * h + 1].y));
+    return make_uint2(some ? w[0] ^ 0x88888888u : 0u, some ? w[1] ^ 0x88888888u : 0u);
 }
 
 }  // namespace fz

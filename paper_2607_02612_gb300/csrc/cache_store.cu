@@ -5,13 +5,14 @@
 // 4 bits: fp4.cuh.  Bound by memory: every row is read once and written once, a row of the table is read once per row and
 // comes mostly from the caches.
 //
-// A thread has one unit of a row, two segments of S dims (16 bytes, or a group of 16 dims in 4 bits) that a rotation by halves turns
-// with one another: that unit of several heads of keys, queries and values in turn, then of its next row.  The cosines and sines
-// stay in registers for a row.  Units lie next to each other in the lanes, then heads, then rows; a unit's segments lie half of the
-// dims apart in any case, so that the lanes' first segments are next to each other (one behind the other in a thread they are
-// half sectors to each access: 64 x 577 float32 158 us).  What a thread will need it asks for
-// itself, up to kDepth units ahead into a ring of its own in shared memory (cp.async, no barriers), so that about 190 KB per SM
-// are on their way.
+// A thread has one unit of a row, two segments of S dims (16 bytes) that a rotation by halves turns with one another: that unit of
+// several heads of keys, queries and values in turn, then of its next row.  The cosines and sines stay in registers for a row.
+// Units lie next to each other in the lanes, then heads, then rows; a unit's segments lie half of the dims apart in any case, so that
+// the lanes' segments make whole lines (one behind the other in a thread, 64 x 577 float32 took 158 us, now 100; a whole group of
+// 16 dims in a thread, a prompt of 32768 to 4 bits 88, now 55: the copies' pieces of 16 bytes were written to shared memory one by
+// one).  A group of 16 dims is the segments of two lanes (four in float32), which find its largest magnitude together.
+// What a thread will need it asks for itself, up to kDepth units ahead into a ring of its own in shared memory (cp.async, no
+// barriers), so that about 190 KB per SM are on their way.
 #include <atomic>
 
 #include "cache_rows.cuh"
@@ -25,15 +26,17 @@ constexpr int kBadShift = 16;   // a sample's counter: its CTAs that are done, a
 constexpr int kMostX = 2432;    // CTAs of a sample, at most
 static_assert(kMostX < 1 << kBadShift, "a sample's CTAs are counted below the bad ones");
 
-constexpr int kTurns = 4;
+constexpr int kTurns = 2;
 
 enum Pairs { kNone, kHalves, kAdjacent };
 
-// CTAs of an SM, by the registers that a unit's dims and angles take, and units of a thread's ring.
+// Dims of a segment: 16 bytes, or a group that is bf16 to be rounded to 4 bits, which saves more instructions than its half sectors
+// cost (256 samples of 100 to 197 tokens of 6 x 64: 42 us with groups of two lanes, 33 so; float32, four lanes or one: 107, 131).
+// CTAs of an SM, and units of a thread's ring.
 template <typename T, bool kFour, int P>
 struct Shape {
-    static constexpr int S = kFour ? 16 : 16 / (int)sizeof(T), kChunks = S * (int)sizeof(T) / 16;   // 16 bytes of a segment
-    static constexpr int kCtas = kFour && P != kNone ? 2 : 3;
+    static constexpr int S = kFour && sizeof(T) == 2 ? 16 : 16 / (int)sizeof(T), kChunks = S * (int)sizeof(T) / 16;   // 16 bytes of a segment
+    static constexpr int kCtas = S == 16 && P != kNone ? 2 : 3;
     static constexpr int kDepth = (kCtas == 2 ? 24 : 16) / (2 * kChunks), kSmem = kDepth * 2 * kChunks * kThreads * 16;
 };
 
@@ -67,6 +70,11 @@ template <int S> __device__ __forceinline__ void pack(const Segment<S> &x, int i
     w = make_uint4(both(x.e[i / 4].x, x.o[i / 4].x), both(x.e[i / 4].y, x.o[i / 4].y), both(x.e[i / 4 + 1].x, x.o[i / 4 + 1].x),
                    both(x.e[i / 4 + 1].y, x.o[i / 4 + 1].y));
 }
+
+template <int S> struct CodesOf;   // the codes of a segment
+template <> struct CodesOf<16> { using Type = unsigned long long; };
+template <> struct CodesOf<8> { using Type = uint32_t; };
+template <> struct CodesOf<4> { using Type = uint16_t; };
 
 // Two segments of S dims, as they lie in memory.
 template <typename T, int S>
@@ -184,7 +192,7 @@ struct Angles {
 template <typename T, bool kFour, int P>
 __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_store(CacheStoreParams p, int units, int lanes) {
     using X = Shape<T, kFour, P>;
-    constexpr int S = X::S, kDepth = X::kDepth, kSlot = 2 * X::kChunks * kThreads;
+    constexpr int S = X::S, kDepth = X::kDepth, kSlot = 2 * X::kChunks * kThreads, kShare = 16 / S;   // kShare: lanes of a group of 16 dims
     extern __shared__ __align__(16) uint4 ring[];   // [kDepth][2 kChunks][kThreads]
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
@@ -215,30 +223,35 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
     const int heads = p.q ? p.heads : 0;
     const int r_first = mine < side && rows_ok ? (int)blockIdx.x * side + mine : n, r_step = (int)gridDim.x * side;
     // the next unit to ask for: keys, queries and values of a row (kinds 0, 1, 2), a thread's heads in turn; its place in the ring
-    int ask_r = r_first, ask_kind = 0, ask_h = lane, ask_at = 0;
-    const T *ask_src = nullptr;
+    int ask_r = r_first, ask_kind = 0, ask_left = 0, ask_at = 0;
+    const T *ask_a = nullptr, *ask_b = nullptr;
+    bool ask_second = false;
     auto find = [&]() {   // the first head of this thread from (ask_r, ask_kind) on
         for (;;) {
             if (ask_kind == 3) {
                 ask_kind = 0;
                 ask_r += r_step;
             }
-            if (ask_r >= n || lane < (ask_kind == 1 ? heads : c.kv_heads)) break;
+            ask_left = (ask_kind == 1 ? heads : c.kv_heads) - lane;
+            if (ask_r >= n || ask_left > 0) break;
             ++ask_kind;
         }
         const unsigned char *base = ask_kind == 0 ? p.k : ask_kind == 1 ? p.q : p.v;
         const long long stride = ask_kind == 0 ? p.k_stride : ask_kind == 1 ? p.q_stride : p.v_stride;
-        ask_src = reinterpret_cast<const T *>(base + (size_t)(o0 + ask_r) * stride) + (size_t)lane * c.dim;
-        ask_h = lane;
+        const T *src = reinterpret_cast<const T *>(base + (size_t)(o0 + ask_r) * stride) + (size_t)lane * c.dim;
+        ask_a = src + (ask_kind == 2 ? plain_a : a);
+        ask_b = src + (ask_kind == 2 ? plain_b : b);
+        ask_second = ask_kind == 2 ? plain_second : second;
     };
     find();
+    const int ask_step = lanes * c.dim;
     auto ask = [&]() {
         if (ask_r < n) {
-            const bool value = ask_kind == 2;
-            Unit<T, S>::ask(ring + ask_at * kSlot + tid, ask_src + (value ? plain_a : a), ask_src + (value ? plain_b : b), value ? plain_second : second);
-            ask_h += lanes;
-            ask_src += (size_t)lanes * c.dim;
-            if (ask_h >= (ask_kind == 1 ? heads : c.kv_heads)) {
+            Unit<T, S>::ask(ring + ask_at * kSlot + tid, ask_a, ask_b, ask_second);
+            ask_a += ask_step;
+            ask_b += ask_step;
+            ask_left -= lanes;
+            if (ask_left <= 0) {
                 ++ask_kind;
                 find();
             }
@@ -288,26 +301,6 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
             v.load(ring + have_at * kSlot + tid);
             have_at = have_at + 1 == kDepth ? 0 : have_at + 1;
         };
-        auto put_codes = [&](const Unit<T, S> &v, bool turns, unsigned char *codes, unsigned char *scales, int da, int db, int h) {
-            if constexpr (kFour) {
-                Segment<S> xa, xb;
-                v.get(0, xa);
-                v.get(1, xb);
-                if constexpr (P != kNone)
-                    if (turns) w.turn_unit(xa, xb, turn_a, turn_b);
-                const size_t to = first_row + ((size_t)h << c.shift);
-                codes += to * (c.dim / 2);
-                scales += to * p.s.bytes;
-                uint32_t sa, sb;
-                const uint2 ca = quantise(xa.e, xa.o, sa), cb = quantise(xb.e, xb.o, sb);
-                *reinterpret_cast<uint2 *>(codes + da / 2) = ca;
-                *reinterpret_cast<uint2 *>(codes + db / 2) = cb;
-                scales[da / 16] = (unsigned char)sa;
-                scales[db / 16] = (unsigned char)sb;
-                if (u == 0)   // (the bytes behind the last scale)
-                    for (int x = c.dim / 16; x < p.s.bytes; ++x) scales[x] = 0;
-            }
-        };
         auto turn_in_place = [&](Unit<T, S> &v) {
             if constexpr (P != kNone)
                 if (turned) {
@@ -319,19 +312,48 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
                     if (turn_b) v.set(1, xb);
                 }
         };
-        const auto in_pool = [&](unsigned char *pool, int h) { return reinterpret_cast<T *>(pool) + (first_row + ((size_t)h << c.shift)) * c.dim; };
-#pragma unroll 1
-        for (int h = lane; h < c.kv_heads; h += lanes) {
-            Unit<T, S> v;
-            next_unit(v);
-            if (!known) continue;
+        // keys or values, from this thread's first head on
+        auto to_pool = [&](unsigned char *pool, unsigned char *scales, int da, int db, bool two, bool turns) {
+            const size_t row0 = first_row + ((size_t)lane << c.shift), step = (size_t)lanes << c.shift;
             if constexpr (kFour) {
-                put_codes(v, turned, c.k, p.s.k, a, b, h);
+                using Codes = typename CodesOf<S>::Type;
+                const unsigned mask = kShare == 1 ? 0u : ((1u << kShare) - 1u) << (tid & 31 & ~(kShare - 1));
+                unsigned char *codes = pool + row0 * (c.dim / 2) + da / 2, *z = scales + row0 * p.s.bytes;
+                const int apart = (db - da) / 2, za = da / 16, zb = db / 16;
+#pragma unroll 1
+                for (int h = lane; h < c.kv_heads; h += lanes, codes += step * (c.dim / 2), z += step * p.s.bytes) {
+                    Unit<T, S> v;
+                    next_unit(v);
+                    if (!known) continue;
+                    Segment<S> xa, xb;
+                    v.get(0, xa);
+                    v.get(1, xb);
+                    if constexpr (P != kNone)
+                        if (turns) w.turn_unit(xa, xb, turn_a, turn_b);
+                    uint32_t sa, sb;
+                    const Codes ca = (Codes)quantise<S>(xa.e, xa.o, mask, sa), cb = (Codes)quantise<S>(xb.e, xb.o, mask, sb);
+                    *reinterpret_cast<Codes *>(codes) = ca;
+                    *reinterpret_cast<Codes *>(codes + apart) = cb;
+                    if (u % kShare == 0) {
+                        z[za] = (unsigned char)sa;
+                        z[zb] = (unsigned char)sb;
+                    }
+                    if (u == 0)   // (the bytes behind the last scale)
+                        for (int x = c.dim / 16; x < p.s.bytes; ++x) z[x] = 0;
+                }
             } else {
-                turn_in_place(v);
-                v.store(in_pool(c.k, h) + a, in_pool(c.k, h) + b, second);
+                T *dst = reinterpret_cast<T *>(pool) + row0 * c.dim + da;
+#pragma unroll 1
+                for (int h = lane; h < c.kv_heads; h += lanes, dst += step * c.dim) {
+                    Unit<T, S> v;
+                    next_unit(v);
+                    if (!known) continue;
+                    if (turns) turn_in_place(v);
+                    v.store(dst, dst + (db - da), two);
+                }
             }
-        }
+        };
+        to_pool(c.k, p.s.k, a, b, second, turned);
 #pragma unroll 1
         for (int h = lane; P != kNone && h < heads; h += lanes) {
             Unit<T, S> v;
@@ -341,14 +363,7 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
             T *dst = reinterpret_cast<T *>(p.q_out) + (row * heads + h) * c.dim;
             v.store(dst + a, dst + b, second);
         }
-#pragma unroll 1
-        for (int h = lane; h < c.kv_heads; h += lanes) {
-            Unit<T, S> v;
-            next_unit(v);
-            if (!known) continue;
-            if constexpr (kFour) put_codes(v, false, c.v, p.s.v, plain_a, plain_b, h);
-            else v.store(in_pool(c.v, h) + plain_a, in_pool(c.v, h) + plain_b, plain_second);
-        }
+        to_pool(c.v, p.s.v, plain_a, plain_b, plain_second, false);
         if (u == 0 && lane == 0 && known) {
             const size_t s = ((size_t)page << c.shift) + place;
             if (c.sizes) c.sizes[s] = p.sizes ? p.sizes[row] : 1.0f;
@@ -376,16 +391,17 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
 // Units of a row that a thread has, if `lanes` threads share a unit's heads.
 int units_of(int lanes, int kv_heads, int heads) { return 2 * ceil_div(kv_heads, lanes) + ceil_div(heads, lanes); }
 // How many threads share a unit's heads: of the numbers that let no more rows lie side by side than there are, one that leaves the
-// fewest threads idle, a small one, since a thread reads the angles of its unit once per row.
+// fewest threads idle; of those a small one, since a thread reads the angles of its unit once per row, but not below kUnits units.
+constexpr int kUnits = 8;
 int lanes_of(int units, int kv_heads, int heads, long long rows) {
     const int more = heads > kv_heads ? heads : kv_heads, most = more < kThreads / units ? more : kThreads / units;
     int best = most;
     double best_used = 0.0;
     for (int lanes = most; lanes >= 1; --lanes) {
-        const int side = kThreads / (units * lanes);
+        const int side = kThreads / (units * lanes), mine = units_of(lanes, kv_heads, heads);
         if (side > rows && lanes < most) break;
-        const double used = (double)side * units * (2 * kv_heads + heads) / units_of(lanes, kv_heads, heads);
-        if (used >= best_used) {
+        const double used = (double)side * units * (2 * kv_heads + heads) / mine;
+        if (used > best_used * 1.02 || (used >= best_used * 0.999 && mine <= kUnits)) {
             best = lanes;
             best_used = used;
         }
@@ -396,6 +412,7 @@ int lanes_of(int units, int kv_heads, int heads, long long rows) {
 template <typename T, bool kFour, int P>
 cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
     using X = Shape<T, kFour, P>;
+    constexpr int S = X::S, kDepth = X::kDepth;
     constexpr int kDevices = 64;
     static std::atomic<bool> allowed[kDevices];   // the kernel's shared memory, asked for once per device
     int device = 0;
@@ -405,7 +422,7 @@ cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
         if (e == cudaSuccess && device < kDevices) allowed[device].store(true, std::memory_order_release);
     }
     if (e != cudaSuccess) return e;
-    const int units = ceil_div(p.c.dim, 2 * X::S), heads = p.q ? p.heads : 0;
+    const int units = ceil_div(p.c.dim, 2 * S), heads = p.q ? p.heads : 0;
     // (samples of more rows than the cache has room for, or than there are, write nothing)
     long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
     if (most > p.in.max_rows) most = p.in.max_rows;
@@ -413,7 +430,7 @@ cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
     const int lanes = lanes_of(units, p.c.kv_heads, heads, most), side = kThreads / (units * lanes);
     // as many rows a CTA as make its start worth while (kTurns rings), unless that leaves SMs without two rounds of CTAs
     const long long steps = (most + side - 1) / side, per_step = units_of(lanes, p.c.kv_heads, heads);
-    long long turns = (kTurns * X::kDepth + per_step - 1) / per_step;
+    long long turns = (kTurns * kDepth + per_step - 1) / per_step;
     const long long least = (2ll * 152 * X::kCtas + p.in.max_batch) / (p.in.max_batch + 1);   // CTAs of a sample
     if (turns > steps / least) turns = steps / least;
     if (turns < 1) turns = 1;

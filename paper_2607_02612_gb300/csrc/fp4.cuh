@@ -40,22 +40,27 @@ __device__ __forceinline__ float max_magnitude(float a, float b, float c) {
     asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(fabsf(a)), "f"(fabsf(b)), "f"(fabsf(c)));
     return r;
 }
-// A group of 16 numbers, the even ones in e and the odd ones in o: its codes, eight to a word, and its scale's byte.
+// S numbers of a group of 16, the even ones in e and the odd ones in o, the rest in the 16 / S lanes of `mask` around this one: their
+// codes, four bits each, and the group's scale's byte.
 //
 // A code is the e2m1 number nearest to x / scale, ties to the even code, which is what the conversion makes of the quotient if
 // the division's rounding neither leaves a tie nor makes one.  A scale has 4 significant bits and a tie lies at one of 3, so
 // scale * tie is exact, and where x is not equal to it the quotient is further from the tie than its own rounding: correctly
 // rounded it serves.  It comes of y = -x / scale but for a few roundings and one correction by the exact remainder x + y scale
 // (of the negative quotient, so that -0 stays -0: the codes' signs are turned at the end).
-__device__ __forceinline__ uint2 quantise(const float2 (&e)[4], const float2 (&o)[4], uint32_t &scale) {
-    float top = fabsf(e[0].x);
-    top = max_magnitude(top, e[0].y, o[0].x);
+template <int S> __device__ __forceinline__ unsigned long long quantise(const float2 (&e)[S / 4], const float2 (&o)[S / 4], unsigned mask, uint32_t &scale) {
+    float top = max_magnitude(e[0].x, e[0].y, o[0].x);
 #pragma unroll
-    for (int i = 1; i < 4; ++i) {
+    for (int i = 1; i < S / 4; ++i) {
         top = max_magnitude(top, o[i - 1].y, e[i].x);
         top = max_magnitude(top, e[i].y, o[i].x);
     }
-    top = max_magnitude(top, o[3].y, o[3].y);
+    top = max_magnitude(top, o[S / 4 - 1].y, o[S / 4 - 1].y);
+#pragma unroll
+    for (int d = 1; d < 16 / S; d <<= 1) {
+        const float other = __shfl_xor_sync(mask, top, d);
+        top = max_magnitude(top, other, other);
+    }
     const float want = top * (1.0f / 6.0f);
     uint16_t s;
     asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(s) : "f"(0.0f), "f"(want));
@@ -64,27 +69,25 @@ __device__ __forceinline__ uint2 quantise(const float2 (&e)[4], const float2 (&o
     scale = fine ? (uint32_t)s : 0x7Fu;
     const float inv = some ? -__frcp_rn(z) : 0.0f;
     const float2 zz = make_float2(z, z), ii = make_float2(inv, inv);
-    float2 ye[4], yo[4];
+    uint32_t codes[S > 8 ? 2 : 1] = {0u};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        ye[i] = mul2(e[i], ii);
-        ye[i] = fma2(fma2(ye[i], zz, e[i]), ii, ye[i]);
-        yo[i] = mul2(o[i], ii);
-        yo[i] = fma2(fma2(yo[i], zz, o[i]), ii, yo[i]);
-    }
-    uint32_t w[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-        asm("{ .reg .b8 b0, b1, b2, b3;\n"
+    for (int i = 0; i < S / 4; ++i) {
+        float2 ye = mul2(e[i], ii), yo = mul2(o[i], ii);
+        ye = fma2(fma2(ye, zz, e[i]), ii, ye);
+        yo = fma2(fma2(yo, zz, o[i]), ii, yo);
+        uint16_t w;
+        asm("{ .reg .b8 b0, b1;\n"
             "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n"
             "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n"
-            "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n"
-            "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n"
-            "mov.b32 %0, {b0, b1, b2, b3}; }"
-            : "=r"(w[h])
-            : "f"(ye[2 * h].x), "f"(yo[2 * h].x), "f"(ye[2 * h].y), "f"(yo[2 * h].y), "f"(ye[2 * h + 1].x), "f"(yo[2 * h + 1].x),
-              "f"(ye[2 * h + 1].y), "f"(yo[2 * h + 1].y));
-    return make_uint2(some ? w[0] ^ 0x88888888u : 0u, some ? w[1] ^ 0x88888888u : 0u);
+            "mov.b16 %0, {b0, b1}; }"
+            : "=h"(w)
+            : "f"(ye.x), "f"(yo.x), "f"(ye.y), "f"(yo.y));
+        codes[i / 2] |= (uint32_t)w << (i % 2 * 16);
+    }
+    const uint32_t flip = some ? 0xFFFFFFFFu : 0u;
+    const uint32_t low = (codes[0] ^ (S == 4 ? 0x8888u : 0x88888888u)) & flip;
+    if constexpr (S > 8) return low | (unsigned long long)((codes[1] ^ 0x88888888u) & flip) << 32;
+    else return low;
 }
 
 }  // namespace fz

@@ -1,8 +1,8 @@
 // Rows of cached sequences back into a ragged batch: a copy, or the values of a cache in 4 bits (a code's times its group's
 // scale, exact in bf16 and in float32: fp4.cuh).  Bound by memory: every row is read once and written once.
 //
-// A CTA takes as many rows of one sample as give each thread kPer pieces of K and of V, all asked for at once; a piece is what gives
-// 16 bytes of a row.
+// A CTA takes as many rows of one sample as give each thread kPer pieces of K and of V, all asked for at once; a piece of a packed row
+// is what gives 32 bytes, which go out in one store (in pieces of 16: 48000 rows of 8 x 128 bf16 51 us).
 #include "cache_rows.cuh"
 #include "fp4.cuh"
 
@@ -16,26 +16,53 @@ __device__ __forceinline__ uint32_t to_bf16(uint32_t h) {   // two float16 whose
     return *reinterpret_cast<const uint32_t *>(&v);
 }
 
-// What gives 16 bytes of a row: a word of codes (8 dims) as bf16, half of one as float32, 16 bytes as they are.
+// What a thread reads at a time, kBytes of a row: 16 codes as bf16, 8 as float32, 16 bytes as they are.
 template <typename T> struct Piece;
-template <> struct Piece<__nv_bfloat16> { using Held = uint32_t; };
-template <> struct Piece<float> { using Held = uint16_t; };
-template <> struct Piece<uint4> { using Held = uint4; };
-template <typename T> __device__ __forceinline__ uint4 values(uint32_t codes, uint32_t scale) {
-    uint32_t v[4];
-    codes_to_half(codes, v);
-    const uint32_t s = scales_to_half(scale * 0x0101u);
-#pragma unroll
-    for (int i = 0; i < (sizeof(T) == 2 ? 4 : 2); ++i) v[i] = mul_half2(v[i], s);
-    if constexpr (sizeof(T) == 2) return make_uint4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
-    else return make_uint4(__float_as_uint(half_low(v[0])), __float_as_uint(half_high(v[0])), __float_as_uint(half_low(v[1])), __float_as_uint(half_high(v[1])));
+template <> struct Piece<__nv_bfloat16> { using Held = uint2; static constexpr int kBytes = 32; };
+template <> struct Piece<float> { using Held = uint32_t; static constexpr int kBytes = 32; };
+template <> struct Piece<uint4> { using Held = uint4; static constexpr int kBytes = 16; };
+// 32 bytes at once, or in two halves where they are not aligned to that.
+__device__ __forceinline__ void store32(unsigned char *to, const uint32_t (&v)[8], bool aligned) {
+    if (aligned) {
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]),
+                     "r"(v[5]), "r"(v[6]), "r"(v[7])
+                     : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(to)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+        reinterpret_cast<uint4 *>(to)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+    }
 }
+__device__ __forceinline__ void values_of(uint32_t codes, uint32_t scale, uint32_t (&v)[4]) {   // of eight codes
+    codes_to_half(codes, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = mul_half2(v[i], scale);
+}
+__device__ __forceinline__ void put(unsigned char *to, uint2 codes, uint32_t scale, bool aligned) {   // as bf16
+    const uint32_t s = scales_to_half(scale * 0x0101u);
+    uint32_t a[4], b[4];
+    values_of(codes.x, s, a);
+    values_of(codes.y, s, b);
+    const uint32_t v[8] = {to_bf16(a[0]), to_bf16(a[1]), to_bf16(a[2]), to_bf16(a[3]), to_bf16(b[0]), to_bf16(b[1]), to_bf16(b[2]), to_bf16(b[3])};
+    store32(to, v, aligned);
+}
+__device__ __forceinline__ void put(unsigned char *to, uint32_t codes, uint32_t scale, bool aligned) {   // as float32
+    uint32_t a[4], v[8];
+    values_of(codes, scales_to_half(scale * 0x0101u), a);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __float_as_uint(half_low(a[i]));
+        v[2 * i + 1] = __float_as_uint(half_high(a[i]));
+    }
+    store32(to, v, aligned);
+}
+__device__ __forceinline__ void put(unsigned char *to, uint4 v, uint32_t, bool) { *reinterpret_cast<uint4 *>(to) = v; }
 
 // T: the type of a cache in 4 bits' values; uint4: a copy of pieces of 16 bytes.  pieces: of a head's row.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) k_cache_read(CacheReadParams p, int row_pieces, int pieces) {
+__global__ void __launch_bounds__(kThreads, 4) k_cache_read(CacheReadParams p, int row_pieces, int pieces) {
     constexpr bool kFour = sizeof(T) != 16;
     using Held = typename Piece<T>::Held;
+    constexpr int kBytes = Piece<T>::kBytes;
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
@@ -71,6 +98,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(CacheReadParams p, int 
         return;
     }
     const unsigned low = (1u << c.shift) - 1u;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p.k_out) | reinterpret_cast<uintptr_t>(p.v_out)) & 31u) == 0;
     for (int ch = tid % width; ch < row_pieces; ch += kThreads) {   // (once, unless a row has more than kThreads pieces)
         const int h = ch / pieces, cc = ch - h * pieces;
         auto held_row = [&](int x) {
@@ -95,14 +123,9 @@ __global__ void __launch_bounds__(kThreads) k_cache_read(CacheReadParams p, int 
 #pragma unroll
         for (int x = 0; x < kPer; ++x) {
             if (r0 + r_mine + x * side >= r1) break;
-            const size_t to = given(x);
-            if constexpr (kFour) {
-                if (p.k_out) reinterpret_cast<uint4 *>(p.k_out)[to] = values<T>(k[x], ks[x]);
-                if (p.v_out) reinterpret_cast<uint4 *>(p.v_out)[to] = values<T>(v[x], vs[x]);
-            } else {
-                if (p.k_out) reinterpret_cast<uint4 *>(p.k_out)[to] = k[x];
-                if (p.v_out) reinterpret_cast<uint4 *>(p.v_out)[to] = v[x];
-            }
+            const size_t to = given(x) * kBytes;
+            if (p.k_out) put(p.k_out + to, k[x], ks[x], aligned);
+            if (p.v_out) put(p.v_out + to, v[x], vs[x], aligned);
         }
     }
     for (int r = r0 + tid; r < min(n, r0 + side * kPer); r += kThreads) {
@@ -128,7 +151,7 @@ template <typename T> cudaError_t launch(const CacheReadParams &p, int pieces, c
 
 cudaError_t launch_cache_read(int dtype, const CacheReadParams &p, cudaStream_t s) {
     if (!p.s.k) return launch<uint4>(p, p.c.dim * (dtype == FUSION_BF16 ? 2 : 4) / 16, s);
-    return dtype == FUSION_BF16 ? launch<__nv_bfloat16>(p, p.c.dim / 8, s) : launch<float>(p, p.c.dim / 4, s);
+    return dtype == FUSION_BF16 ? launch<__nv_bfloat16>(p, p.c.dim / 16, s) : launch<float>(p, p.c.dim / 8, s);
 }
 
 }  // namespace fz

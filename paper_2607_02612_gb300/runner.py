@@ -89,6 +89,7 @@ class RaggedRows:
         _need(self.ids, torch.int32, index, "ids", self.max_batch)
         object.__setattr__(self, "_c", fb.ragged(self.max_batch, self.max_tokens, self.max_rows, self.offsets, self.batch,
                                                  self.ids))
+        object.__setattr__(self, "_index", index)   # of the device that all of them are on
 
     def ragged(self) -> fb.fusion_ragged:
         return self._c
@@ -141,8 +142,23 @@ def _need(t: Optional[torch.Tensor], dtype: torch.dtype, device: int, what: str,
 
 
 def _rows_here(c, rows) -> None:
-    if any(t is not None and t.get_device() != c.index for t in (rows.offsets, rows.batch, rows.ids)):
+    if type(rows) is RaggedRows:
+        ok = rows._index == c.index
+    else:
+        ok = not any(t is not None and t.get_device() != c.index for t in (rows.offsets, rows.batch, rows.ids))
+    if not ok:
         raise fb.FusionError(f"the rows' offsets, count and ids on the cache's device ({c.index}) expected")
+
+
+def _heads_out(c, t: Optional[torch.Tensor], rows: int, heads: int, what: str):
+    """An output [rows, heads, head_dim] of the cache's type and device: t, checked, or a new one; and its address."""
+    if t is None:
+        t = torch.empty((rows, heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
+        return t, t.data_ptr()
+    shape = t.shape
+    if len(shape) != 3 or shape[0] < rows or shape[1] != heads or shape[2] != c.head_dim:
+        raise fb.FusionError(f"{what}: [{rows}, {heads}, {c.head_dim}] expected")
+    return t, _need(t, c.torch_dtype, c.index, what, dim=3)
 
 
 def _append_args(c, k, v, rows, sizes, scores, lengths_out):
@@ -264,12 +280,12 @@ class Rotation:
             raise fb.FusionError('pairs: "halves" or "adjacent" expected')
         if not self.table.is_cuda:
             raise fb.FusionError("device tensors expected")
-        _need(self.table, torch.float32, self.table.get_device(), "table", dim=2)
+        address = _need(self.table, torch.float32, self.table.get_device(), "table", dim=2)
+        code = fb.FUSION_PAIRS_HALVES if self.pairs == "halves" else fb.FUSION_PAIRS_ADJACENT
+        object.__setattr__(self, "_args", (address, *self.table.shape, code))
 
     def c_struct(self, positions: Optional[int]) -> fb.fusion_rotation:
-        rows, dims = self.table.shape
-        code = fb.FUSION_PAIRS_HALVES if self.pairs == "halves" else fb.FUSION_PAIRS_ADJACENT
-        return fb.fusion_rotation(self.table.data_ptr(), rows, dims, code, positions)
+        return fb.fusion_rotation(*self._args, positions)
 
 
 def rotation_table(positions: int, dims: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -479,24 +495,21 @@ class Fusion:
         sequences), and with them the queries of the same rows, q [rows, heads, head_dim] (any stride between rows, any number
         of heads).  The new lengths go to the cache's own unless lengths_out is given; returns the rotated queries (q_out, where
         it is given, which may be a contiguous q; rows of no sample stay; None without q)."""
-        if q is not None and (q.dim() != 3 or q.shape[2] != c.head_dim):
-            raise fb.FusionError(f"queries: [rows, heads, {c.head_dim}] expected")
-        if q is None and q_out is not None:
-            raise fb.FusionError("q_out without q")
         o = lengths_out if lengths_out is not None else c.lengths
         if rows is None:
             rows = c.one_row_each()
         heads, qp, qs, qo = 0, None, 0, None
         if q is not None:
-            heads = q.shape[1]
+            shape = q.shape
+            if len(shape) != 3 or shape[2] != c.head_dim:
+                raise fb.FusionError(f"queries: [rows, heads, {c.head_dim}] expected")
+            heads = shape[1]
             qp, qs = _rows_ptr(q, rows.max_rows, heads, c.head_dim, c.torch_dtype, c.index, "queries")
-            if q_out is None:
-                q_out = torch.empty((rows.max_rows, heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
-            qo = _need(q_out, c.torch_dtype, c.index, "q_out", dim=3)
-            if q_out.shape[0] < rows.max_rows or q_out.shape[1] != heads or q_out.shape[2] != c.head_dim:
-                raise fb.FusionError(f"q_out: [{rows.max_rows}, {heads}, {c.head_dim}] expected")
+            q_out, qo = _heads_out(c, q_out, rows.max_rows, heads, "q_out")
             if rows.max_rows == 0:   # (an empty tensor has no address)
                 qp = qo = None
+        elif q_out is not None:
+            raise fb.FusionError("q_out without q")
         if c.max_batch == 0:
             return q_out
         rows, kp, ks, vp, vs, zp, wp, op = _append_args(c, k, v, rows, sizes, scores, o)
@@ -515,21 +528,14 @@ class Fusion:
         head_dim] (k_out and v_out, where they are given; rows of no sample stay); sizes_out and weights_out [rows] get the
         tokens' sizes and weights."""
         _rows_here(c, rows)
-        outs = []
-        for t, what in ((k_out, "k_out"), (v_out, "v_out")):
-            if t is None:
-                t = torch.empty((rows.max_rows, c.kv_heads, c.head_dim), dtype=c.torch_dtype, device=c.device)
-            _need(t, c.torch_dtype, c.index, what, dim=3)
-            if t.shape[0] < rows.max_rows or t.shape[1] != c.kv_heads or t.shape[2] != c.head_dim:
-                raise fb.FusionError(f"{what}: [{rows.max_rows}, {c.kv_heads}, {c.head_dim}] expected")
-            outs.append(t)
+        k_out, kp = _heads_out(c, k_out, rows.max_rows, c.kv_heads, "k_out")
+        v_out, vp = _heads_out(c, v_out, rows.max_rows, c.kv_heads, "v_out")
         sp = _need(starts, torch.int32, c.index, "starts", rows.max_batch)
         zp = _need(sizes_out, torch.float32, c.index, "sizes_out", rows.max_rows)
         wp = _need(weights_out, torch.float32, c.index, "weights_out", rows.max_rows)
         if rows.max_batch and rows.max_rows and c.max_batch:
-            _enqueue(c.lib.fusion_cache_read, c.index, self.status, c.code, c.c_struct(), rows.ragged(), sp, outs[0].data_ptr(),
-                     outs[1].data_ptr(), zp, wp)
-        return outs[0], outs[1]
+            _enqueue(c.lib.fusion_cache_read, c.index, self.status, c.code, c.c_struct(), rows.ragged(), sp, kp, vp, zp, wp)
+        return k_out, v_out
 
     def cache_attention(self, c: DeviceCache, q: torch.Tensor, *, scale: Optional[float] = None, window: int = 0,
                         sinks: int = 0, out: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -32,12 +32,14 @@ enum Pairs { kNone, kHalves, kAdjacent };
 
 // Dims of a segment: 16 bytes, or a group that is bf16 to be rounded to 4 bits, which saves more instructions than its half sectors
 // cost (256 samples of 100 to 197 tokens of 6 x 64: 42 us with groups of two lanes, 33 so; float32, four lanes or one: 107, 131).
+// Those of 32 bytes are not asked for through the ring, but one unit ahead in registers, 32 bytes a load.
 // CTAs of an SM, and units of a thread's ring.
 template <typename T, bool kFour, int P>
 struct Shape {
     static constexpr int S = kFour && sizeof(T) == 2 ? 16 : 16 / (int)sizeof(T), kChunks = S * (int)sizeof(T) / 16;   // 16 bytes of a segment
+    static constexpr bool kRing = kChunks == 1;
     static constexpr int kCtas = S == 16 && P != kNone ? 2 : 3;
-    static constexpr int kDepth = (kCtas == 2 ? 24 : 16) / (2 * kChunks), kSmem = kDepth * 2 * kChunks * kThreads * 16;
+    static constexpr int kDepth = kRing ? 8 : 2, kSmem = kRing ? kDepth * 2 * kThreads * 16 : 0;
 };
 
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -81,23 +83,31 @@ template <typename T, int S>
 struct Unit {
     static constexpr int kChunk = 16 / (int)sizeof(T), kChunks = S / kChunk;   // numbers of 16 bytes; 16 bytes of a segment
     uint4 w[2][kChunks];
-    // From a thread's place in the ring, where its chunks lie kThreads apart; and their copy to there.
+    // From a thread's place in the ring, where its segments lie kThreads apart; and their copy to there.
     __device__ __forceinline__ void load(const uint4 *ring) {
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 0; i < kChunks; ++i) w[s][i] = ring[(s * kChunks + i) * kThreads];
-    }
-    // (segments of more than 16 bytes are asked for in half sectors, whose other half the L1 keeps)
-    static __device__ __forceinline__ void ask16(uint4 *dst, const T *src) {
-        if constexpr (kChunks == 1) cp_async16(dst, src);
-        else asm volatile("cp.async.ca.shared.global [%0], [%1], 16;" ::"r"(smem_addr(dst)), "l"(src) : "memory");
+        w[0][0] = ring[0];
+        w[1][0] = ring[kThreads];
     }
     static __device__ __forceinline__ void ask(uint4 *ring, const T *a, const T *b, bool second) {
-#pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-            ask16(ring + i * kThreads, a + i * kChunk);
-            if (second) ask16(ring + (kChunks + i) * kThreads, b + i * kChunk);
+        cp_async16(ring, a);
+        if (second) cp_async16(ring + kThreads, b);
+    }
+    // From memory: segments of 32 bytes, aligned to that or in two halves.
+    __device__ __forceinline__ void load(const T *a, const T *b, bool aligned) {
+        if constexpr (kChunks == 2) {
+            load32(a, w[0], aligned);
+            load32(b, w[1], aligned);
+        }
+    }
+    static __device__ __forceinline__ void load32(const T *src, uint4 (&w)[kChunks], bool aligned) {
+        if (aligned) {
+            asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                         : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[kChunks - 1].x), "=r"(w[kChunks - 1].y),
+                           "=r"(w[kChunks - 1].z), "=r"(w[kChunks - 1].w)
+                         : "l"(src));
+        } else {
+            w[0] = reinterpret_cast<const uint4 *>(src)[0];
+            w[kChunks - 1] = reinterpret_cast<const uint4 *>(src)[1];
         }
     }
     __device__ __forceinline__ void store(T *a, T *b, bool second) const {
@@ -192,8 +202,8 @@ struct Angles {
 template <typename T, bool kFour, int P>
 __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_store(CacheStoreParams p, int units, int lanes) {
     using X = Shape<T, kFour, P>;
-    constexpr int S = X::S, kDepth = X::kDepth, kSlot = 2 * X::kChunks * kThreads, kShare = 16 / S;   // kShare: lanes of a group of 16 dims
-    extern __shared__ __align__(16) uint4 ring[];   // [kDepth][2 kChunks][kThreads]
+    constexpr int S = X::S, kDepth = X::kDepth, kSlot = 2 * kThreads, kShare = 16 / S;   // kShare: lanes of a group of 16 dims
+    extern __shared__ __align__(16) uint4 ring[];   // [kDepth][2][kThreads]
     const int i = blockIdx.y, tid = threadIdx.x;
     const Cache &c = p.c;
     wait_for_previous();
@@ -245,9 +255,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
     };
     find();
     const int ask_step = lanes * c.dim;
+    const bool aligned = ((reinterpret_cast<uintptr_t>(p.k) | reinterpret_cast<uintptr_t>(p.v) | reinterpret_cast<uintptr_t>(p.q) | (uintptr_t)p.k_stride |
+                           (uintptr_t)p.v_stride | (uintptr_t)p.q_stride) & 31u) == 0;
+    Unit<T, S> ahead;
     auto ask = [&]() {
         if (ask_r < n) {
-            Unit<T, S>::ask(ring + ask_at * kSlot + tid, ask_a, ask_b, ask_second);
+            if constexpr (X::kRing) Unit<T, S>::ask(ring + ask_at * kSlot + tid, ask_a, ask_b, ask_second);
+            else ahead.load(ask_a, ask_b, aligned);
             ask_a += ask_step;
             ask_b += ask_step;
             ask_left -= lanes;
@@ -256,8 +270,10 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
                 find();
             }
         }
-        cp_async_commit();
-        ask_at = ask_at + 1 == kDepth ? 0 : ask_at + 1;
+        if constexpr (X::kRing) {
+            cp_async_commit();
+            ask_at = ask_at + 1 == kDepth ? 0 : ask_at + 1;
+        }
     };
 #pragma unroll 1
     for (int d = 0; d < kDepth - 1; ++d) ask();
@@ -296,10 +312,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
         next_pos = position_of(r + r_step);
         const size_t row = (size_t)(o0 + r), first_row = (size_t)((page * (unsigned)c.kv_heads) << c.shift) + place;   // of key head 0 in the pools
         auto next_unit = [&](Unit<T, S> &v) {
-            ask();
-            cp_async_wait<kDepth - 1>();
-            v.load(ring + have_at * kSlot + tid);
-            have_at = have_at + 1 == kDepth ? 0 : have_at + 1;
+            if constexpr (X::kRing) {
+                ask();
+                cp_async_wait<kDepth - 1>();
+                v.load(ring + have_at * kSlot + tid);
+                have_at = have_at + 1 == kDepth ? 0 : have_at + 1;
+            } else {
+                v = ahead;
+                ask();
+            }
         };
         auto turn_in_place = [&](Unit<T, S> &v) {
             if constexpr (P != kNone)

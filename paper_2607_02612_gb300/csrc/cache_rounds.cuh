@@ -33,19 +33,19 @@ __device__ __forceinline__ void cp_async16_zfill(uint32_t dst, const void *src, 
 }
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Where in the batch a round lies.
+// Where in the batch a round lies.  TAIL: rounds without tokens at the end of each (sequence, key head).
 struct Place {
     int b, h, ch, u;       // sequence, key head, chunk of its query heads, round
     int n, vis, rounds;    // length, visible tokens, rounds of one key head
 };
-template <bool kEarly = false>
+template <bool kEarly = false, int TAIL = 0>
 __device__ __forceinline__ void place_sequence(const CacheAttnParams &p, Place &s, int tokens, int b) {
     s.b = b;
     s.n = max(cache_length<kEarly>(p.c, b), 0);
     s.vis = visible(p, s.n);
-    s.rounds = (s.vis + tokens - 1) / tokens;
+    s.rounds = (s.vis + tokens - 1) / tokens + (TAIL && s.vis > 0 ? TAIL : 0);
 }
-template <bool kEarly = false>
+template <bool kEarly = false, int TAIL = 0>
 __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, int tokens, int heads, int chunks) {
     if (++s.u < s.rounds) return;
     s.u = 0;
@@ -58,7 +58,7 @@ __device__ __forceinline__ void place_next(const CacheAttnParams &p, Place &s, i
             s.rounds = s.vis = 0;
             return;
         }
-        place_sequence<kEarly>(p, s, tokens, s.b);
+        place_sequence<kEarly, TAIL>(p, s, tokens, s.b);
     } while (s.rounds == 0);
 }
 
@@ -104,7 +104,7 @@ struct Finder {
 // warps' sums go through shared memory, and the thread whose sequences hold a boundary looks it up (one barrier before and
 // one after: 2.2 us with 64-bit scans by one thread, 1.2 now, 0.7 of them the reading of the lengths).  min_rounds: of a run.
 // SNAP: the boundaries move to ends of (sequence, key head)s.  kEarly: called before the kernel's wait.
-template <int THREADS, bool SNAP, bool kEarly, int MOST = kSnap>
+template <int THREADS, bool SNAP, bool kEarly, int MOST = kSnap, int TAIL = 0>
 __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREADS> &s, int tokens, int heads, int chunks, unsigned min_rounds,
                                          Run &run, Place &at) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -112,7 +112,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
     const int per = ceil_div(p.c.max_batch, THREADS), b0 = min(tid * per, p.c.max_batch), b1 = min(b0 + per, p.c.max_batch);
     unsigned mine = 0;
     for (int b = b0; b < b1; ++b) {
-        place_sequence<kEarly>(p, at, tokens, b);
+        place_sequence<kEarly, TAIL>(p, at, tokens, b);
         mine += (unsigned)at.rounds * vheads;
     }
     const unsigned sum = __reduce_add_sync(0xFFFFFFFFu, mine);
@@ -143,7 +143,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
         unsigned rem = x - base - (incl - mine);   // rounds of this thread's sequences before x (if it is one of theirs)
         if (x - base >= incl - mine && rem < mine) {
             for (int b = b0; b < b1; ++b) {
-                if (per > 1) place_sequence<kEarly>(p, at, tokens, b);
+                if (per > 1) place_sequence<kEarly, TAIL>(p, at, tokens, b);
                 if (rem < (unsigned)at.rounds * vheads) break;
                 rem -= (unsigned)at.rounds * vheads;
             }
@@ -164,7 +164,7 @@ __device__ __forceinline__ bool find_run(const CacheAttnParams &p, Finder<THREAD
         if (moved < 0) at.u = 0;
         if (moved > 0) {
             at.u = at.rounds - 1;
-            place_next<kEarly>(p, at, tokens, heads, chunks);
+            place_next<kEarly, TAIL>(p, at, tokens, heads, chunks);
         }
     }
     return true;
@@ -407,9 +407,9 @@ inline bool warps_alone(const CacheAttnParams &p, int chunks) {
 // Whether the rounds of any batch that the host lets pass, of TT tokens for each of W warps, are fewer than 2^32.  A (sequence, part
 // of a key head's query heads) has at most its places / round + 1 of them, and there are at most max_batch * heads; warps alone (TT
 // down to 8) take calls of at most kAloneMost visible tokens only.
-constexpr bool counts_fit(long long tt, long long w) {
+constexpr bool counts_fit(long long tt, long long w, long long tail = 0) {
     constexpr long long kHeads = (long long)FUSION_CACHE_MAX_BATCH * FUSION_CACHE_MAX_HEADS;
-    return (w == 1 ? kHeads * ((kAloneMost + tt - 1) / tt) : kCacheMaxHeadTokens / (tt * w) + kHeads) < 1ll << 32;
+    return (w == 1 ? kHeads * ((kAloneMost + tt - 1) / tt) : kCacheMaxHeadTokens / (tt * w) + kHeads * (1 + tail)) < 1ll << 32;
 }
 
 // Host: as many CTAs as the GPU holds at once, or as there can be rounds.  What depends on the kernel and the device alone is

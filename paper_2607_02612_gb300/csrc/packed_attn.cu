@@ -25,7 +25,10 @@ namespace {
 using namespace rounds;
 
 constexpr float kUp = 7.0f;
-constexpr int kSnap = 2;      // rounds: of 128 tokens, twice bf16's
+constexpr int kSnap = 1;      // rounds, of 128 tokens: twice bf16's
+// Rounds that the end of a (sequence, key head) counts for, one in which the warps join (64 x 4096 with weights 61 us without it, 56 so)
+// and nothing else is done.  A warp alone joins nothing (200 x 60: 9.7 and 8.2).
+template <int W> constexpr int kTail = W == 1 ? 0 : 1;
 constexpr int kTokens = 32;   // of a warp and round
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {   // an 8 x 8 matrix of b16, a row per four lanes
@@ -126,7 +129,7 @@ struct PackedStream {
                 r.place = cache_page(p.c, ahead.b, pos, r.page) ? pos & ((1 << p.c.shift) - 1) : -2;
             }
             ++ahead_r;
-            place_next(p, ahead, kRound, p.c.kv_heads, chunks);
+            place_next<false, kTail<W>>(p, ahead, kRound, p.c.kv_heads, chunks);
         }
         return r;
     }
@@ -239,7 +242,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
     wait_for_previous();
     Run run;
     Place at;
-    if (!find_run<kThreads, true, false, kSnap>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
+    if (!find_run<kThreads, true, false, kSnap, kTail<W>>(p, finder, kRound, c.kv_heads, chunks, kMinRounds, run, at)) {
         empty_sequences<T, kThreads>(p);
         return;
     }
@@ -265,7 +268,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
         if (r + at.rounds - at.u >= r1) return;
         Place next = at;
         next.u = at.rounds - 1;
-        place_next(p, next, kRound, c.kv_heads, chunks);
+        place_next<false, kTail<W>>(p, next, kRound, c.kv_heads, chunks);
         ask_q(next, q_at ^ 1);
     };
     ask_q(at, q_at);
@@ -608,14 +611,14 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
             if (r + 1 == r1) break;
             const int had = at.u;
             const bool first = seg0 < r0 && r - r0 < (unsigned)S;   // (the run began inside)
-            place_next(p, at, kRound, c.kv_heads, chunks);
+            place_next<false, kTail<W>>(p, at, kRound, c.kv_heads, chunks);
             if (had + 1 < S || first) cp_async_wait<0>();   // the next queries were asked for fewer rounds ago than wait() waits for
             q_at ^= 1;
             __syncthreads();
             begin_head();
             seg0 = r + 1;
         } else {
-            place_next(p, at, kRound, c.kv_heads, chunks);
+            place_next<false, kTail<W>>(p, at, kRound, c.kv_heads, chunks);
         }
         if (++st == S) st = 0;
     }
@@ -624,7 +627,7 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
 
 template <typename T, int DP, int NT, int S, int W>
 cudaError_t launch_warps(const PackedAttnParams &p, int chunks, cudaStream_t s) {
-    static_assert(counts_fit(kTokens, W), "rounds are counted in 32 bits");
+    static_assert(counts_fit(kTokens, W, kTail<W>), "rounds are counted in 32 bits");
     return launch_rounds<k_packed_attn<T, DP, NT, S, W>, W>(Layout<T, DP, NT, S, W>::kTotal, p, chunks, W * kTokens, s);
 }
 template <typename T, int DP, int NT>

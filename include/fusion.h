@@ -600,7 +600,7 @@ int fusion_packed_append_rotated(int dtype, fusion_packed_cache cache, fusion_ra
 /*
  * fusion_packed_attention: fusion_cache_attention over a cache in 4 bits, q and out of type dtype.  Keys and values enter the
  * products as the values that the cache holds, exactly; a query as a float16 (for FUSION_F32 the sum of two) times a power of
- * two of its head's own; a probability as a float16 (two), within 2^-11 (2^-21) of itself or of 2^-21 (2^-31) of the largest.
+ * two of its head's own; a probability as a float16 (two), within 2^-11 (2^-22) of itself or within 2^-32 of the largest.
  */
 int fusion_packed_attention(int dtype, fusion_packed_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
                             int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,

@@ -5,14 +5,14 @@
 // 4 bits: fp4.cuh.  Bound by memory: every row is read once and written once, a row of the table is read once per row and
 // comes mostly from the caches.
 //
-// A thread has one unit of a row, two segments of S dims (16 bytes) that a rotation by halves turns with one another: that unit of
-// several heads of keys, queries and values in turn, then of its next row.  The cosines and sines stay in registers for a row.
-// Units lie next to each other in the lanes, then heads, then rows; a unit's segments lie half of the dims apart in any case, so that
-// the lanes' segments make whole lines (one behind the other in a thread, 64 x 577 float32 took 158 us, now 100; a whole group of
-// 16 dims in a thread, a prompt of 32768 to 4 bits 88, now 55: the copies' pieces of 16 bytes were written to shared memory one by
-// one).  A group of 16 dims is the segments of two lanes (four in float32), which find its largest magnitude together.
-// What a thread will need it asks for itself, up to kDepth units ahead into a ring of its own in shared memory (cp.async, no
-// barriers), so that about 190 KB per SM are on their way.
+// A thread has one unit of a row, two segments of S dims that a rotation by halves turns with one another: that unit of several heads
+// of keys, queries and values in turn, then of its next row.  The cosines and sines stay in registers for a row.  Units lie next to
+// each other in the lanes, then heads, then rows; a unit's segments lie half of the dims apart in any case, so that the lanes'
+// segments make whole lines (one behind the other in a thread, 64 x 577 float32 took 158 us, now 100).
+// A segment is 16 bytes, asked for up to kDepth units ahead into the thread's own places of a ring in shared memory (cp.async, no
+// barriers), so that about 190 KB per SM are on their way; a group of 16 dims to be rounded to 4 bits is the segments of four float32
+// lanes, which find its largest magnitude together.  bf16 to be rounded is a group per segment and comes 32 bytes a load, one unit
+// ahead in registers (Shape says why).
 #include <atomic>
 
 #include "cache_rows.cuh"

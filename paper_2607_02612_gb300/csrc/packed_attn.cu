@@ -347,11 +347,10 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
             float x[kMt][NT][4];
 #pragma unroll
             for (int i = 0; i < kMt; ++i) {
-                float y[NT][4];   // every other step's sums
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[i][n][e] = y[n][e] = 0.0f;
+                    for (int e = 0; e < 4; ++e) x[i][n][e] = 0.0f;
                 uint32_t sc[2][kVw];
                 const unsigned char *from[2];
 #pragma unroll
@@ -402,10 +401,6 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
                                                  [&](int term, int e) { return qf[term][2 * j + kk][n][e]; });
                     }
                 }
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[i][n][e] += y[n][e];
             }
             // ---- logits in base 2; a masked token's are -inf
             if (plain) {

@@ -387,6 +387,53 @@ def test_read(dtype, four, kv_heads, dim, page):
     assert (per[0][:5] == 1).all() and (per[1][:5] == 0).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", [None, "halves", "adjacent"])
+@pytest.mark.parametrize("moved", ["k", "v", "q", "stride"])
+def test_rows_aligned_to_16_bytes_only(dtype, pairs, moved):
+    """One of the row tensors, or their strides, 16 bytes off a multiple of 32."""
+    kv, dim, heads, rows = 3, 96, 6, 41
+    g = torch.Generator().manual_seed(30)
+    c = pk.make([5, 0], kv, dim, 8, room=rows, seed=31)
+    dc, f = packed(dtype, c, kv), runner.Fusion(2)
+    off = 16 // torch.empty(0, dtype=ref.TYPES[dtype]).element_size()
+    given, host = {}, {}
+    for name, n in (("k", kv), ("v", kv), ("q", heads)):
+        x = hard_rows(g, rows, n, dim, dtype) if name == "v" else torch.randn((rows, n, dim), generator=g).to(ref.TYPES[dtype])
+        wide = torch.full((rows * (n * dim + 2 * off) + off,), math.nan, dtype=x.dtype, device=DEV)
+        wide = wide[off * (moved == name):].as_strided((rows, n, dim), ((n * dim + off * (2 - (moved == "stride"))), dim, 1))
+        assert wide.data_ptr() % 32 == 16 * (moved == name) and wide.data_ptr() % 16 == 0
+        wide.copy_(x)
+        given[name], host[name] = wide, x
+    offsets, ids = [0, 30, rows], [1, 0]
+    if pairs is None:
+        f.cache_append(dc, given["k"], given["v"], ragged(offsets, ids))
+        kt = host["k"].float()
+    else:
+        table = torch.randn((64, dim), generator=g)
+        at = torch.cat([torch.arange(30), torch.arange(11) + 5])
+        q = f.cache_append_rotated(dc, given["k"], given["v"], runner.Rotation(table.to(DEV), pairs), ragged(offsets, ids), q=given["q"])
+        kt = pk.turn(host["k"].float(), table, at, pairs)
+        assert equal_bits(q, pk.turn(host["q"].float(), table, at, pairs).to(ref.TYPES[dtype]))
+    assert status(f) == 0
+    new = pk.append(c, kt, host["v"].float(), offsets, ids)
+    same(dc, c, new)
+    # and back
+    n = 46
+    flat = [torch.full((n * kv * dim + 2 * off,), 7.0, dtype=ref.TYPES[dtype], device=DEV) for _ in range(2)]
+    outs = [x[off * (moved == name):][:n * kv * dim].view(n, kv, dim) for x, name in zip(flat, "kv")]
+    f.cache_read(dc, ragged([0, 30, n], ids), k_out=outs[0], v_out=outs[1])
+    assert status(f) == 0
+    for i, t in enumerate(ids):
+        places = ref.places(c, t, torch.arange(int(new[t])))
+        for name, out in zip("kv", outs):
+            want = pk.unpack(c[name][places[0], :, places[1]], c[name + "_scales"][places[0], :, places[1]])
+            got = out[[0, 30][i]:[30, n][i]].cpu().double()
+            assert torch.equal(got[want.isfinite()], want[want.isfinite()]) and torch.isnan(got[~want.isfinite()]).all()
+    for x, name in zip(flat, "kv"):
+        assert (x[:off * (moved == name)] == 7).all() and (x[off * (moved == name) + n * kv * dim:] == 7).all()
+
+
 @pytest.mark.parametrize("four", [False, True])
 def test_read_leaves_bad_samples_out(four):
     cache_bit, offs, ids_bit = fz.FUSION_DEV_BAD_CACHE, fz.FUSION_DEV_BAD_OFFSETS, fz.FUSION_DEV_BAD_IDS

@@ -26,8 +26,6 @@ constexpr int kBadShift = 16;   // a sample's counter: its CTAs that are done, a
 constexpr int kMostX = 2432;    // CTAs of a sample, at most
 static_assert(kMostX < 1 << kBadShift, "a sample's CTAs are counted below the bad ones");
 
-constexpr int kTurns = 2;
-
 enum Pairs { kNone, kHalves, kAdjacent };
 
 // Dims of a segment: 16 bytes, or a group that is bf16 to be rounded to 4 bits, which saves more instructions than its half sectors
@@ -280,9 +278,25 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
 
     int bad = !rows_ok ? FUSION_DEV_BAD_OFFSETS : at < 0 || at > c.capacity || n > c.capacity - at ? FUSION_DEV_BAD_CACHE : 0;
     const unsigned *pages = reinterpret_cast<const unsigned *>(c.table) + (size_t)slot * c.max_pages;
+    // page and position of a row, read a row ahead (0 and 0 behind the last), and its angles, asked for behind the last use of those
+    // of the row before
+    auto page_of = [&](int r) { return r < n ? pages[(at + r) >> c.shift] : 0u; };
+    auto position_of = [&](int r) { return P == kNone ? 0u : r >= n ? 0u : (unsigned)(p.positions ? p.positions[o0 + r] : at + r); };
+    auto known_of = [&](unsigned pos) { return P == kNone || pos < (unsigned)p.table_rows; };   // a row without a position in the table is left out
+    Angles<S, P> w;
+    const bool turned = turn_a || turn_b;
+    auto load_angles = [&](int r, unsigned pos) {
+        if constexpr (P != kNone)
+            if (turned && r < n && known_of(pos)) w.load(p.table + (size_t)pos * p.turned, p.turned / 2, a, b, turn_a, turn_b);
+    };
     bool wrong = false;
-    if (!bad)
+    unsigned page = 0u, pos = 0u;
+    if (!bad) {
+        page = page_of(r_first);
+        pos = position_of(r_first);
         for (int e = (at >> c.shift) + tid; n > 0 && e <= (at + n - 1) >> c.shift; e += kThreads) wrong |= pages[e] >= c.num_pages;
+        load_angles(r_first, pos);
+    }
     if (named_twice<kThreads>(p.in, B, i, slot)) bad |= FUSION_DEV_BAD_IDS;
     if (__syncthreads_or(wrong)) bad |= FUSION_DEV_BAD_CACHE;
     if (bad) {   // nothing of this sample is written, and its slot's length stays (also where it is named twice)
@@ -294,22 +308,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
         return;
     }
     const unsigned low = (1u << c.shift) - 1u;
-    // page and position of a row, read a row ahead (0 and 0 behind the last)
-    auto page_of = [&](int r) { return r < n ? pages[(at + r) >> c.shift] : 0u; };
-    auto position_of = [&](int r) { return P == kNone ? 0u : r >= n ? 0u : (unsigned)(p.positions ? p.positions[o0 + r] : at + r); };
-    unsigned next_page = page_of(r_first), next_pos = position_of(r_first);
     bool bad_position = false;
     int have_at = 0;
     for (int r = r_first; r < n; r += r_step) {
-        const unsigned page = next_page, pos = next_pos, place = (unsigned)(at + r) & low;
-        const bool known = P == kNone || pos < (unsigned)p.table_rows;   // a row without a position in the table is left out
+        const unsigned place = (unsigned)(at + r) & low;
+        const bool known = known_of(pos);
         bad_position |= !known;
-        Angles<S, P> w;
-        const bool turned = turn_a || turn_b;
-        if constexpr (P != kNone)
-            if (known && turned) w.load(p.table + (size_t)pos * p.turned, p.turned / 2, a, b, turn_a, turn_b);
-        next_page = page_of(r + r_step);
-        next_pos = position_of(r + r_step);
+        const unsigned next_page = page_of(r + r_step), next_pos = position_of(r + r_step);
         const size_t row = (size_t)(o0 + r), first_row = (size_t)((page * (unsigned)c.kv_heads) << c.shift) + place;   // of key head 0 in the pools
         auto next_unit = [&](Unit<T, S> &v) {
             if constexpr (X::kRing) {
@@ -384,12 +389,15 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
             T *dst = reinterpret_cast<T *>(p.q_out) + (row * heads + h) * c.dim;
             v.store(dst + a, dst + b, second);
         }
+        load_angles(r + r_step, next_pos);
         to_pool(c.v, p.s.v, plain_a, plain_b, plain_second, false);
         if (u == 0 && lane == 0 && known) {
             const size_t s = ((size_t)page << c.shift) + place;
             if (c.sizes) c.sizes[s] = p.sizes ? p.sizes[row] : 1.0f;
             if (c.weights) c.weights[s] = p.scores ? p.scores[row] : 0.0f;
         }
+        page = next_page;
+        pos = next_pos;
     }
     cp_async_wait<0>();
     // every CTA of the sample has read its length before the last one raises it
@@ -411,9 +419,12 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
 
 // Units of a row that a thread has, if `lanes` threads share a unit's heads.
 int units_of(int lanes, int kv_heads, int heads) { return 2 * ceil_div(kv_heads, lanes) + ceil_div(heads, lanes); }
+// Units of a row that a thread has at most, where it can choose, and has at least in all of its CTA's rows, where there is work
+// enough: a CTA starts with four loads that wait for one another.  (At most 8 of a row and 16 in all: 1 x 32768 packed 115 us, now 103;
+// 32 in all 119, since the last CTAs then leave SMs idle.  64 x 577 float32 100, now 96; 256 samples of 100 to 197 41, now 39.)
+constexpr int kUnits = 24;
 // How many threads share a unit's heads: of the numbers that let no more rows lie side by side than there are, one that leaves the
-// fewest threads idle; of those a small one, since a thread reads the angles of its unit once per row, but not below kUnits units.
-constexpr int kUnits = 8;
+// fewest threads idle; of those the smallest, since a thread reads the angles of its unit once per row.
 int lanes_of(int units, int kv_heads, int heads, long long rows) {
     const int more = heads > kv_heads ? heads : kv_heads, most = more < kThreads / units ? more : kThreads / units;
     int best = most;
@@ -433,7 +444,7 @@ int lanes_of(int units, int kv_heads, int heads, long long rows) {
 template <typename T, bool kFour, int P>
 cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
     using X = Shape<T, kFour, P>;
-    constexpr int S = X::S, kDepth = X::kDepth;
+    constexpr int S = X::S;
     constexpr int kDevices = 64;
     static std::atomic<bool> allowed[kDevices];   // the kernel's shared memory, asked for once per device
     int device = 0;
@@ -449,9 +460,9 @@ cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
     if (most > p.in.max_rows) most = p.in.max_rows;
     if (most < 1) most = 1;
     const int lanes = lanes_of(units, p.c.kv_heads, heads, most), side = kThreads / (units * lanes);
-    // as many rows a CTA as make its start worth while (kTurns rings), unless that leaves SMs without two rounds of CTAs
+    // as many rows a CTA as make its start worth while, unless that leaves SMs without two rounds of CTAs
     const long long steps = (most + side - 1) / side, per_step = units_of(lanes, p.c.kv_heads, heads);
-    long long turns = (kTurns * kDepth + per_step - 1) / per_step;
+    long long turns = (kUnits + per_step - 1) / per_step;
     const long long least = (2ll * 152 * X::kCtas + p.in.max_batch) / (p.in.max_batch + 1);   // CTAs of a sample
     if (turns > steps / least) turns = steps / least;
     if (turns < 1) turns = 1;

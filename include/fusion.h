@@ -199,7 +199,7 @@ typedef struct fusion_rotation {
     int32_t table_rows;       /* positions 0 .. table_rows - 1 */
     int32_t dims;             /* a multiple of 16 (of 32 for a cache in 4 bits) up to head_dim */
     int32_t pairs;            /* FUSION_PAIRS_HALVES or FUSION_PAIRS_ADJACENT */
-    const int32_t *positions; /* [max_rows], of every row; NULL: the row's place in its sequence */
+    const int32_t *positions; /* [max_rows], of every row; NULL: the row's place in its sequence (which evictions lower) */
 } fusion_rotation;
 
 /* Human-readable name of a return code or of a single FUSION_DEV_* bit. */

@@ -2,7 +2,7 @@
 // scale, exact in bf16 and in float32: fp4.cuh).  Bound by memory: every row is read once and written once.
 //
 // A CTA takes as many rows of one sample as give each thread kPer pieces of K and of V, all asked for at once; a piece of a packed row
-// is what gives 32 bytes, which go out in one store (in pieces of 16: 48000 rows of 8 x 128 bf16 51 us).
+// is what gives 32 bytes, which go out in one store (48000 rows of 8 x 128 bf16: 42 us, 88 % of the copy's rate; in pieces of 16 bytes 51).
 #include "cache_rows.cuh"
 #include "fp4.cuh"
 

@@ -13,7 +13,10 @@
 // 2^14 .. 2^15 (float32 queries as the sum of two float16).  Probabilities are 2^(x - shift), at most 2^(kLag + kUp) = 2^15: kUp
 // keeps the small ones out of float16's subnormal numbers.  One float16 term (two for float32): its 11 bits lie 3 below the output's.
 //
-// What bounds it: memory (a token and key head: 9/8 dim bytes), closely followed by the issue of instructions: 6 for eight codes.
+// What bounds it: memory (9/8 dim bytes of a token and key head) and the issue of instructions (8 for eight codes of K, 11 of V, and a
+// round's own) together: 64 sequences of up to 4096, 32 / 8 heads of 128, 47 us for 152 MB, which memory alone would give in 22; as
+// many tokens again cost 32.  14 us do not depend on the tokens: the run is found after 2, its first round here after 5, the joins take 4.
+// A round is 32 tokens of a warp, asked for one round ahead (two rounds ahead 48 us), three CTAs per SM (four, of 128 registers, 48.5).
 #include <float.h>
 
 #include "cache_rounds.cuh"
@@ -96,8 +99,9 @@ template <int DP> __device__ __forceinline__ int swizzle(int r) {
     return DP == 64 ? 0 : DP == 128 ? r & 2 : (r & 3) << 1 | (r >> 2 & 1);
 }
 
-// Shared memory of a CTA: per warp S stages of kTokens rows of K's and of V's codes and of their scales; the tokens' log2 sizes; the queries of this (sequence, key head) and the next; the warps' outputs on their way to each other, at the
-// end of a (sequence, key head), kJoinDims dims at a time.
+// Shared memory of a CTA: per warp S stages of kTokens rows of K's and of V's codes and of their scales; the tokens' log2 sizes; the
+// queries of this (sequence, key head) and the next; the warps' outputs on their way to each other, at the end of a (sequence, key head),
+// kJoinDims dims at a time.
 template <typename T, int DP, int NT, int S, int W>
 struct Layout {
     static constexpr int kNq = 8 * NT, kRow = DP / 2, kScales = DP / 16, kStage = 2 * kTokens * (kRow + kScales);

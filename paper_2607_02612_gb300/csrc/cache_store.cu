@@ -10,9 +10,8 @@
 // each other in the lanes, then heads, then rows; a unit's segments lie half of the dims apart in any case, so that the lanes'
 // segments make whole lines (one behind the other in a thread, 64 x 577 float32 took 158 us, now 100).
 // A segment is 16 bytes, asked for up to kDepth units ahead into the thread's own places of a ring in shared memory (cp.async, no
-// barriers), so that about 190 KB per SM are on their way; a group of 16 dims to be rounded to 4 bits is the segments of four float32
-// lanes, which find its largest magnitude together.  bf16 to be rounded is a group per segment and comes 32 bytes a load, one unit
-// ahead in registers (Shape says why).
+// barriers), so that about 190 KB per SM are on their way.  On the way to 4 bits it is 32 bytes, a group of 16 dims in bf16 and half a
+// group in float32, one unit ahead in registers (Shape).
 #include <atomic>
 
 #include "cache_rows.cuh"
@@ -28,18 +27,23 @@ static_assert(kMostX < 1 << kBadShift, "a sample's CTAs are counted below the ba
 
 enum Pairs { kNone, kHalves, kAdjacent };
 
-// Dims of a segment: 16 bytes, or a group that is bf16 to be rounded to 4 bits, which saves more instructions than its half sectors
-// cost (256 samples of 100 to 197 tokens of 6 x 64: 42 us with groups of two lanes, 33 so; float32, four lanes or one: 107, 131).
-// Those of 32 bytes are not asked for through the ring, but one unit ahead in registers, 32 bytes a load.
-// CTAs of an SM, and units of a thread's ring.
+// Dims of a segment: 16 bytes, or 32 on the way to 4 bits, which saves more instructions than the half sectors of codes and scales cost
+// (256 samples of 100 to 197 tokens of 6 x 64 bf16: 42 us with groups of two lanes, 33 of one; 300 of 100 to 300 of 4 x 64 float32: 62 with
+// groups of four lanes, 47 of two, 54 of one, whose units fill the registers).  Those of 32 bytes are not asked for through the ring, whose
+// copies would be written 16 bytes at a time, but one unit ahead in registers.  CTAs of an SM, and units of a thread's ring.
 template <typename T, bool kFour, int P>
 struct Shape {
-    static constexpr int S = kFour && sizeof(T) == 2 ? 16 : 16 / (int)sizeof(T), kChunks = S * (int)sizeof(T) / 16;   // 16 bytes of a segment
-    static constexpr bool kRing = kChunks == 1;
-    static constexpr int kCtas = S == 16 && P != kNone ? 2 : 3;
+    static constexpr int S = (kFour ? 32 : 16) / (int)sizeof(T), kChunks = S * (int)sizeof(T) / 16;   // 16 bytes of a segment
+    static constexpr bool kRing = !kFour;
+    static constexpr int kCtas = kFour && P != kNone ? 2 : 3;
     static constexpr int kDepth = kRing ? 8 : 2, kSmem = kRing ? kDepth * 2 * kThreads * 16 : 0;
 };
 
+// The next unit but one comes as far as the L2 meanwhile (1 x 32768 packed 103 us without it, 99 so; two units further 102).
+__device__ __forceinline__ void to_l2(const void *a, const void *b) {
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(a));
+    asm volatile("prefetch.global.L2 [%0];" ::"l"(b));
+}
 template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // S dims, the even ones in e, the odd ones in o, two to a register pair.
@@ -74,7 +78,6 @@ template <int S> __device__ __forceinline__ void pack(const Segment<S> &x, int i
 template <int S> struct CodesOf;   // the codes of a segment
 template <> struct CodesOf<16> { using Type = unsigned long long; };
 template <> struct CodesOf<8> { using Type = uint32_t; };
-template <> struct CodesOf<4> { using Type = uint16_t; };
 
 // Two segments of S dims, as they lie in memory.
 template <typename T, int S>
@@ -92,20 +95,20 @@ struct Unit {
     }
     // From memory: segments of 32 bytes, aligned to that or in two halves.
     __device__ __forceinline__ void load(const T *a, const T *b, bool aligned) {
-        if constexpr (kChunks == 2) {
-            load32(a, w[0], aligned);
-            load32(b, w[1], aligned);
+#pragma unroll
+        for (int i = 0; i + 1 < kChunks; i += 2) {
+            load32(a + i * kChunk, w[0][i], w[0][i + 1], aligned);
+            load32(b + i * kChunk, w[1][i], w[1][i + 1], aligned);
         }
     }
-    static __device__ __forceinline__ void load32(const T *src, uint4 (&w)[kChunks], bool aligned) {
+    static __device__ __forceinline__ void load32(const T *src, uint4 &x, uint4 &y, bool aligned) {
         if (aligned) {
             asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                         : "=r"(w[0].x), "=r"(w[0].y), "=r"(w[0].z), "=r"(w[0].w), "=r"(w[kChunks - 1].x), "=r"(w[kChunks - 1].y),
-                           "=r"(w[kChunks - 1].z), "=r"(w[kChunks - 1].w)
+                         : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w), "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w)
                          : "l"(src));
         } else {
-            w[0] = reinterpret_cast<const uint4 *>(src)[0];
-            w[kChunks - 1] = reinterpret_cast<const uint4 *>(src)[1];
+            x = reinterpret_cast<const uint4 *>(src)[0];
+            y = reinterpret_cast<const uint4 *>(src)[1];
         }
     }
     __device__ __forceinline__ void store(T *a, T *b, bool second) const {
@@ -263,6 +266,8 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
             ask_a += ask_step;
             ask_b += ask_step;
             ask_left -= lanes;
+            if constexpr (!X::kRing)
+                if (ask_left > 0) to_l2(ask_a, ask_b);
             if (ask_left <= 0) {
                 ++ask_kind;
                 find();

@@ -85,7 +85,7 @@ template <int S> __device__ __forceinline__ unsigned long long quantise(const fl
         codes[i / 2] |= (uint32_t)w << (i % 2 * 16);
     }
     const uint32_t flip = some ? 0xFFFFFFFFu : 0u;
-    const uint32_t low = (codes[0] ^ (S == 4 ? 0x8888u : 0x88888888u)) & flip;
+    const uint32_t low = (codes[0] ^ 0x88888888u) & flip;
     if constexpr (S > 8) return low | (unsigned long long)((codes[1] ^ 0x88888888u) & flip) << 32;
     else return low;
 }

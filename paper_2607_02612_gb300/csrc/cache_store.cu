@@ -426,11 +426,13 @@ __global__ void __launch_bounds__(kThreads, Shape<T, kFour, P>::kCtas) k_cache_s
 int units_of(int lanes, int kv_heads, int heads) { return 2 * ceil_div(kv_heads, lanes) + ceil_div(heads, lanes); }
 // Units of a row that a thread has at most, where it can choose, and has at least in all of its CTA's rows, where there is work
 // enough: a CTA starts with four loads that wait for one another.  (At most 8 of a row and 16 in all: 1 x 32768 packed 115 us, now 103;
-// 32 in all 119, since the last CTAs then leave SMs idle.  64 x 577 float32 100, now 96; 256 samples of 100 to 197 41, now 39.)
+// 32 in all 119, since the last CTAs then leave SMs idle.  64 x 577 float32 100, now 96; 256 samples of 100 to 197 41, now 39.)  Half as
+// many of a row where the CTAs would not fill the GPU one and a half times (10 samples of 47 of 16 + 16 + 64 heads of 128 float32 20.6
+// us, now 13; 195 of 249 of 8 + 8 + 16 heads of 32 63, now 56).
 constexpr int kUnits = 24;
 // How many threads share a unit's heads: of the numbers that let no more rows lie side by side than there are, one that leaves the
 // fewest threads idle; of those the smallest, since a thread reads the angles of its unit once per row.
-int lanes_of(int units, int kv_heads, int heads, long long rows) {
+int lanes_of(int units, int kv_heads, int heads, long long rows, long long batch, int places) {
     const int more = heads > kv_heads ? heads : kv_heads, most = more < kThreads / units ? more : kThreads / units;
     int best = most;
     double best_used = 0.0;
@@ -438,7 +440,8 @@ int lanes_of(int units, int kv_heads, int heads, long long rows) {
         const int side = kThreads / (units * lanes), mine = units_of(lanes, kv_heads, heads);
         if (side > rows && lanes < most) break;
         const double used = (double)side * units * (2 * kv_heads + heads) / mine;
-        if (used > best_used * 1.02 || (used >= best_used * 0.999 && mine <= kUnits)) {
+        const int at_most = (rows + side - 1) / side * batch * 2 >= 3 * places ? kUnits : kUnits / 2;
+        if (used > best_used * 1.02 || (used >= best_used * 0.999 && mine <= at_most)) {
             best = lanes;
             best_used = used;
         }
@@ -459,16 +462,20 @@ cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
         if (e == cudaSuccess && device < kDevices) allowed[device].store(true, std::memory_order_release);
     }
     if (e != cudaSuccess) return e;
-    const int units = ceil_div(p.c.dim, 2 * S), heads = p.q ? p.heads : 0;
+    const int places = 152 * X::kCtas, heads = p.q ? p.heads : 0;
+    // in segments of 16 bytes an even number, if there is room for it, so that the lanes' segments end where sectors do (11 samples of 556
+    // of 16 + 16 + 64 heads of 80 bf16 51.8 us, now 39.4)
+    int units = ceil_div(p.c.dim, 2 * S);
+    if (!kFour && units % 2 && S * (units + 1) <= p.c.dim - (P == kHalves ? p.turned / 2 : 0)) ++units;
     // (samples of more rows than the cache has room for, or than there are, write nothing)
     long long most = p.in.max_tokens < p.c.capacity ? p.in.max_tokens : p.c.capacity;
     if (most > p.in.max_rows) most = p.in.max_rows;
     if (most < 1) most = 1;
-    const int lanes = lanes_of(units, p.c.kv_heads, heads, most), side = kThreads / (units * lanes);
+    const int lanes = lanes_of(units, p.c.kv_heads, heads, most, p.in.max_batch, places), side = kThreads / (units * lanes);
     // as many rows a CTA as make its start worth while, unless that leaves SMs without two rounds of CTAs
     const long long steps = (most + side - 1) / side, per_step = units_of(lanes, p.c.kv_heads, heads);
     long long turns = (kUnits + per_step - 1) / per_step;
-    const long long least = (2ll * 152 * X::kCtas + p.in.max_batch) / (p.in.max_batch + 1);   // CTAs of a sample
+    const long long least = (2ll * places + p.in.max_batch) / (p.in.max_batch + 1);   // CTAs of a sample
     if (turns > steps / least) turns = steps / least;
     if (turns < 1) turns = 1;
     long long x = (steps + turns - 1) / turns;

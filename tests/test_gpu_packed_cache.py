@@ -216,6 +216,14 @@ def test_rotated_append(dtype, pairs, kv, dim, turned, heads):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("pairs", ["halves", "adjacent"])
+@pytest.mark.parametrize("kv,dim,turned,heads", [(1, 80, 32, 3), (16, 80, 32, 64), (3, 40, 16, 7), (2, 40, 32, 1), (2, 24, 16, 5), (5, 48, 16, 2),
+                                                 (2, 112, 48, 4), (1, 56, 32, 9), (2, 144, 16, 3), (2, 208, 192, 2), (1, 16, 16, 1), (1, 240, 240, 2)])
+def test_rotated_append_odd_numbers_of_segments(dtype, pairs, kv, dim, turned, heads):
+    rotated(dtype, False, kv, dim, turned, heads, pairs, "given", 40)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pairs", ["halves", "adjacent"])
 @pytest.mark.parametrize("kv,dim,turned,heads", [t for t in TURNS if t[1] % 32 == 0 and t[2] % 32 == 0] + [(3, 160, 96, 6), (2, 32, 32, 2)])
 def test_rotated_append_in_4_bits(dtype, pairs, kv, dim, turned, heads):
     rotated(dtype, True, kv, dim, turned, heads, pairs, "given", 7)

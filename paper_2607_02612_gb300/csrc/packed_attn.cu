@@ -16,7 +16,8 @@
 // What bounds it: memory (9/8 dim bytes of a token and key head) and the issue of instructions (8 for eight codes of K, 11 of V, and a
 // round's own) together: 64 sequences of up to 4096, 32 / 8 heads of 128, 47 us for 152 MB, which memory alone would give in 22; as
 // many tokens again cost 32.  14 us do not depend on the tokens: the run is found after 2, its first round here after 5, the joins take 4.
-// A round is 32 tokens of a warp, asked for one round ahead (two rounds ahead 48 us), three CTAs per SM (four, of 128 registers, 48.5).
+// A round is 32 tokens of a warp (or 64: launch), asked for one round ahead (two rounds ahead 48 us), three CTAs per SM (four, of 128 registers,
+// 48.5).
 #include <float.h>
 
 #include "cache_rounds.cuh"
@@ -28,11 +29,10 @@ namespace {
 using namespace rounds;
 
 constexpr float kUp = 7.0f;
-constexpr int kSnap = 1;      // rounds, of 128 tokens: twice bf16's
+constexpr int kSnap = 1;      // rounds, of at least 128 tokens: twice bf16's
 // Rounds that the end of a (sequence, key head) counts for, one in which the warps join (64 x 4096 with weights 61 us without it, 56 so)
 // and nothing else is done.  A warp alone joins nothing (200 x 60: 9.7 and 8.2).
 template <int W> constexpr int kTail = W == 1 ? 0 : 1;
-constexpr int kTokens = 32;   // of a warp and round
 
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {   // an 8 x 8 matrix of b16, a row per four lanes
     uint32_t r;
@@ -99,90 +99,110 @@ template <int DP> __device__ __forceinline__ int swizzle(int r) {
     return DP == 64 ? 0 : DP == 128 ? r & 2 : (r & 3) << 1 | (r >> 2 & 1);
 }
 
-// Shared memory of a CTA: per warp S stages of kTokens rows of K's and of V's codes and of their scales; the tokens' log2 sizes; the
+// Shared memory of a CTA: per warp S stages of TT rows of K's and of V's codes and of their scales; the tokens' log2 sizes; the
 // queries of this (sequence, key head) and the next; the warps' outputs on their way to each other, at the end of a (sequence, key head),
 // kJoinDims dims at a time.
-template <typename T, int DP, int NT, int S, int W>
+template <typename T, int DP, int NT, int S, int W, int TT>
 struct Layout {
-    static constexpr int kNq = 8 * NT, kRow = DP / 2, kScales = DP / 16, kStage = 2 * kTokens * (kRow + kScales);
+    static constexpr int kNq = 8 * NT, kRow = DP / 2, kScales = DP / 16, kStage = 2 * TT * (kRow + kScales);
     static constexpr int kQPitch = DP * (int)sizeof(T) + 16, kQ = kNq * kQPitch;
     static constexpr int kJoinDims = DP < 128 ? DP : 128, kPitch = kJoinDims + 8;
     static constexpr int kLsz = W * S * kStage;
-    static constexpr int kQueries = kLsz + W * S * kTokens * 4;
+    static constexpr int kQueries = kLsz + W * S * TT * 4;
     static constexpr int kJoin = kQueries + 2 * kQ;
     static constexpr int kJoinBytes = W * kNq * kPitch * 4, kScratch = kJoinScratch<kNq>;
     static constexpr int kTotal = kJoin + (kJoinBytes > kScratch ? kJoinBytes : kScratch);
 };
 
-// The tokens of the rounds to come, one to a lane (rounds::Stream with rows in 4 bits).
-template <int DP, int W>
+// The tokens of the rounds to come, kPer to a lane (rounds::Stream with rows in 4 bits).
+template <int DP, int W, int TT>
 struct PackedStream {
-    static constexpr int kRow = DP / 2, kScales = DP / 16, kCpr = kRow / 16, kStage = 2 * kTokens * (kRow + kScales), kRound = W * kTokens;
+    static constexpr int kRow = DP / 2, kScales = DP / 16, kCpr = kRow / 16, kStage = 2 * TT * (kRow + kScales), kRound = W * TT, kPer = TT / 32;
     Place ahead;             // of the next round to look up
     unsigned ahead_r, r1;
-    Token t0, t1;            // t0's rows are asked for next (its size is here), then t1's
-    float size0;
+    Token t0[kPer], t1[kPer];   // t0's rows are asked for next (their sizes are here), then t1's
+    float size0[kPer];
     unsigned plain;          // a bit per stage: all of its tokens are there, of size 1
 
-    __device__ __forceinline__ Token look_up(const PackedAttnParams &p, int chunks, int warp, int lane) {
-        Token r{0u, -1, ahead.h};
+    __device__ __forceinline__ void look_up(const PackedAttnParams &p, int chunks, int warp, int lane, Token (&t)[kPer]) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) t[i] = Token{0u, -1, ahead.h};
         if (ahead_r < r1) {
-            const int j = ahead.u * kRound + warp * kTokens + lane;
-            if (j < ahead.vis) {
-                const int pos = p.window && j >= p.sinks ? j + ahead.n - ahead.vis : j;
-                r.place = cache_page(p.c, ahead.b, pos, r.page) ? pos & ((1 << p.c.shift) - 1) : -2;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const int j = ahead.u * kRound + warp * TT + i * 32 + lane;
+                if (j < ahead.vis) {
+                    const int pos = p.window && j >= p.sinks ? j + ahead.n - ahead.vis : j;
+                    t[i].place = cache_page(p.c, ahead.b, pos, t[i].page) ? pos & ((1 << p.c.shift) - 1) : -2;
+                }
             }
             ++ahead_r;
             place_next<false, kTail<W>>(p, ahead, kRound, p.c.kv_heads, chunks);
         }
-        return r;
     }
-    __device__ __forceinline__ float size_of(const PackedAttnParams &p, const Token &t) const {
-        return t.place < 0 ? 0.0f : p.c.sizes ? p.c.sizes[((size_t)t.page << p.c.shift) + t.place] : 1.0f;
+    __device__ __forceinline__ void sizes_of(const PackedAttnParams &p, const Token (&t)[kPer], float (&size)[kPer]) const {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            size[i] = t[i].place < 0 ? 0.0f : p.c.sizes ? p.c.sizes[((size_t)t[i].page << p.c.shift) + t[i].place] : 1.0f;
     }
     // Asks for the rows of a round's tokens, and notes their log2 sizes unless all are 0.
-    __device__ __forceinline__ void ask(const PackedAttnParams &p, const Token &t, float size, int lane, int st, unsigned char *stages, float *lsz) {
+    __device__ __forceinline__ void ask(const PackedAttnParams &p, const Token (&t)[kPer], const float (&size)[kPer], int lane, int st,
+                                        unsigned char *stages, float *lsz) {
         const unsigned row_bytes = (unsigned)p.c.dim / 2;
-        const bool live = t.place >= 0 && size != 0.0f;
-        const unsigned row = live ? ((t.page * (unsigned)p.c.kv_heads + (unsigned)t.h) << p.c.shift) + (unsigned)t.place : 0u;
-        const unsigned lives = __ballot_sync(0xFFFFFFFFu, live);
-        const bool all_plain = __all_sync(0xFFFFFFFFu, live && size == 1.0f);
+        unsigned row[kPer], lives[kPer];
+        bool live[kPer], one = true;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            live[i] = t[i].place >= 0 && size[i] != 0.0f;
+            one = one && live[i] && size[i] == 1.0f;
+            row[i] = live[i] ? ((t[i].page * (unsigned)p.c.kv_heads + (unsigned)t[i].h) << p.c.shift) + (unsigned)t[i].place : 0u;
+            lives[i] = __ballot_sync(0xFFFFFFFFu, live[i]);
+        }
+        const bool all_plain = __all_sync(0xFFFFFFFFu, one);
         plain = (plain & ~(1u << st)) | (unsigned)all_plain << st;
-        if (!all_plain) lsz[st * kTokens + lane] = t.place == -2 ? kNoPage : live ? log2f(size) : -INFINITY;
+        if (!all_plain) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                lsz[st * TT + i * 32 + lane] = t[i].place == -2 ? kNoPage : live[i] ? log2f(size[i]) : -INFINITY;
+        }
         constexpr int kWide = 32 / kCpr;   // rows of a step
         const int r_lane = lane / kCpr, cc = lane % kCpr;
         const bool exists = (unsigned)cc * 16u < row_bytes;
         const unsigned char *k = p.c.k + (exists ? cc : 0) * 16, *v = p.c.v + (exists ? cc : 0) * 16;
         const uint32_t stage = smem_addr(stages) + st * kStage, dst = stage + r_lane * kRow, at = (uint32_t)(cc ^ swizzle<DP>(r_lane)) * 16u;
-        const unsigned mine = exists ? lives >> r_lane : 0u;
 #pragma unroll
-        for (int e = 0; e < kTokens / kWide; ++e) {
-            const unsigned theirs = __shfl_sync(0xFFFFFFFFu, row, e * kWide + r_lane);
-            const bool read = mine >> (e * kWide) & 1u;
+        for (int e = 0; e < TT / kWide; ++e) {
+            const int i = e * kWide / 32, r = e * kWide % 32;
+            const unsigned theirs = __shfl_sync(0xFFFFFFFFu, row[i], r + r_lane);
+            const bool read = exists && (lives[i] >> r_lane >> r & 1u);
             const uint32_t to = dst + e * kWide * kRow + (at ^ (uint32_t)(swizzle<DP>(e * kWide) * 16));
             copy_or_zero<16>(to, at_row(k, theirs, row_bytes), read);
-            copy_or_zero<16>(to + kTokens * kRow, at_row(v, theirs, row_bytes), read);
+            copy_or_zero<16>(to + TT * kRow, at_row(v, theirs, row_bytes), read);
         }
-        const uint32_t ks = stage + 2 * kTokens * kRow + lane * kScales, vs = ks + kTokens * kScales;
-        const unsigned long long kz = at_row(p.s.k, row, (unsigned)p.s.bytes), vz = at_row(p.s.v, row, (unsigned)p.s.bytes);
-        if constexpr (kScales <= 8) {
-            copy_or_zero<kScales>(ks, kz, live);
-            copy_or_zero<kScales>(vs, vz, live);
-        } else {   // rows of 12 or 16 bytes
 #pragma unroll
-            for (int e = 0; e < kScales; e += 4) {
-                const bool read = live && e < p.s.bytes;
-                copy_or_zero<4>(ks + e, kz + (read ? e : 0), read);
-                copy_or_zero<4>(vs + e, vz + (read ? e : 0), read);
+        for (int i = 0; i < kPer; ++i) {
+            const uint32_t ks = stage + 2 * TT * kRow + (i * 32 + lane) * kScales, vs = ks + TT * kScales;
+            const unsigned long long kz = at_row(p.s.k, row[i], (unsigned)p.s.bytes), vz = at_row(p.s.v, row[i], (unsigned)p.s.bytes);
+            if constexpr (kScales <= 8) {
+                copy_or_zero<kScales>(ks, kz, live[i]);
+                copy_or_zero<kScales>(vs, vz, live[i]);
+            } else {   // rows of 12 or 16 bytes
+#pragma unroll
+                for (int e = 0; e < kScales; e += 4) {
+                    const bool read = live[i] && e < p.s.bytes;
+                    copy_or_zero<4>(ks + e, kz + (read ? e : 0), read);
+                    copy_or_zero<4>(vs + e, vz + (read ? e : 0), read);
+                }
             }
         }
         cp_async_commit();
     }
     __device__ __forceinline__ void next(const PackedAttnParams &p, int chunks, int warp, int lane, int st, unsigned char *stages, float *lsz) {
         ask(p, t0, size0, lane, st, stages, lsz);
-        t0 = t1;
-        size0 = size_of(p, t0);
-        t1 = look_up(p, chunks, warp, lane);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) t0[i] = t1[i];
+        sizes_of(p, t0, size0);
+        look_up(p, chunks, warp, lane, t1);
     }
     // The first S - 1 rounds' rows (all pages asked for at once, then all sizes).
     template <int S>
@@ -192,17 +212,20 @@ struct PackedStream {
         ahead_r = run.r0;
         r1 = run.r1;
         plain = 0u;
-        Token t[S + 1];
-        float size[S];
+        Token t[S + 1][kPer];
+        float size[S][kPer];
 #pragma unroll
-        for (int s = 0; s <= S; ++s) t[s] = look_up(p, chunks, warp, lane);
+        for (int s = 0; s <= S; ++s) look_up(p, chunks, warp, lane, t[s]);
 #pragma unroll
-        for (int s = 0; s < S; ++s) size[s] = size_of(p, t[s]);
+        for (int s = 0; s < S; ++s) sizes_of(p, t[s], size[s]);
 #pragma unroll
         for (int s = 0; s < S - 1; ++s) ask(p, t[s], size[s], lane, s, stages, lsz);
-        t0 = t[S - 1];
-        size0 = size[S - 1];
-        t1 = t[S];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            t0[i] = t[S - 1][i];
+            size0[i] = size[S - 1][i];
+            t1[i] = t[S][i];
+        }
     }
 };
 
@@ -225,12 +248,12 @@ __device__ __forceinline__ float2 load2(const __nv_bfloat16 *src, int i) {
 }
 __device__ __forceinline__ float2 load2(const float *src, int i) { return reinterpret_cast<const float2 *>(src)[i]; }
 
-// T: type of queries and output.  W: warps of a CTA.
-template <typename T, int DP, int NT, int S, int W>
+// T: type of queries and output.  W: warps of a CTA.  TT: tokens of a warp and round.
+template <typename T, int DP, int NT, int S, int W, int TT>
 __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3 : 2) k_packed_attn(PackedAttnParams p, int chunks) {
-    using L = Layout<T, DP, NT, S, W>;
+    using L = Layout<T, DP, NT, S, W, TT>;
     constexpr int kThreads = 32 * W, kTerms = sizeof(T) == 4 ? 2 : 1;
-    constexpr int kNq = L::kNq, kRound = W * kTokens, kRow = L::kRow, kScales = L::kScales, kKs = DP / 16, kMt = kTokens / 16;
+    constexpr int kNq = L::kNq, kRound = W * TT, kRow = L::kRow, kScales = L::kScales, kKs = DP / 16, kMt = TT / 16;
     constexpr int kKw = DP / 32, kVw = DP / 64;   // words of a K row and of a V row that a lane has
     extern __shared__ __align__(128) unsigned char sm[];
     __shared__ Finder<kThreads> finder;
@@ -240,9 +263,9 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
     const Cache &c = p.c;
 
     unsigned char *stages = sm + warp * S * L::kStage;
-    float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * kTokens;
+    float *lsz = reinterpret_cast<float *>(sm + L::kLsz) + warp * S * TT;
     float *join = reinterpret_cast<float *>(sm + L::kJoin);
-    PackedStream<DP, W> in;
+    PackedStream<DP, W, TT> in;
     wait_for_previous();
     Run run;
     Place at;
@@ -343,9 +366,9 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
 
         const bool plain = in.plain >> st & 1u;
         const int nq = min(kNq, p.group - at.ch * kNq), head0 = at.h * p.group + at.ch * kNq;
-        const unsigned char *ks = stages + st * L::kStage, *vs = ks + kTokens * kRow, *kz = vs + kTokens * kRow, *vz = kz + kTokens * kScales;
-        const float *lz = lsz + st * kTokens;
-        const int j0 = at.u * kRound + warp * kTokens;
+        const unsigned char *ks = stages + st * L::kStage, *vs = ks + TT * kRow, *kz = vs + TT * kRow, *vz = kz + TT * kScales;
+        const float *lz = lsz + st * TT;
+        const int j0 = at.u * kRound + warp * TT;
         if (j0 < at.vis) {
             // ---- S^T = K Q^T
             float x[kMt][NT][4];
@@ -624,18 +647,21 @@ __global__ void __launch_bounds__(32 * W, W == 1 ? 12 : DP <= 128 && NT == 1 ? 3
     cp_async_wait<0>();   // (of rounds past the run: nothing but zeros)
 }
 
-template <typename T, int DP, int NT, int S, int W>
+template <typename T, int DP, int NT, int S, int W, int TT>
 cudaError_t launch_warps(const PackedAttnParams &p, int chunks, cudaStream_t s) {
-    static_assert(counts_fit(kTokens, W, kTail<W>), "rounds are counted in 32 bits");
-    return launch_rounds<k_packed_attn<T, DP, NT, S, W>, W>(Layout<T, DP, NT, S, W>::kTotal, p, chunks, W * kTokens, s);
+    static_assert(counts_fit(TT, W, kTail<W>), "rounds are counted in 32 bits");
+    return launch_rounds<k_packed_attn<T, DP, NT, S, W, TT>, W>(Layout<T, DP, NT, S, W, TT>::kTotal, p, chunks, W * TT, s);
 }
 template <typename T, int DP, int NT>
 cudaError_t launch(const PackedAttnParams &p, cudaStream_t s) {
-    constexpr int kStages = 2;
+    // Rounds of 64 tokens a warp where as many bytes as 32 of 128 dims are in flight then, that is up to 64 dims (bf16, 38 sequences of up to
+    // 25130, 48 / 3 heads: 59.7 us with 32, now 47.9; 53 of up to 25537, 32 / 8 heads of 32: 197 and 157; 145 of up to 2435, 24 / 6 heads,
+    // weights: 48.1 and 43.8), but not for float32, which the products bound (16 x 577 13.2 and 13.8, 13 x 10469 27.5 and 26.9), nor alone.
+    constexpr int kStages = 2, kTokens = DP == 64 && sizeof(T) == 2 ? 64 : 32;
     const int chunks = ceil_div(p.group, 8 * NT);
     if constexpr (DP <= 128)
-        if (warps_alone(p, chunks)) return launch_warps<T, DP, NT, kStages, 1>(p, chunks, s);
-    return launch_warps<T, DP, NT, kStages, 4>(p, chunks, s);
+        if (warps_alone(p, chunks)) return launch_warps<T, DP, NT, kStages, 1, 32>(p, chunks, s);
+    return launch_warps<T, DP, NT, kStages, 4, kTokens>(p, chunks, s);
 }
 template <typename T, int NT>
 cudaError_t launch_dim(const PackedAttnParams &p, cudaStream_t s) {

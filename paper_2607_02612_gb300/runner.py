@@ -322,7 +322,9 @@ def packed_cache_of(dtype: str, k: torch.Tensor, v: torch.Tensor, k_scales: torc
 
 def device_packed_cache(dtype: str, max_batch: int, max_tokens: int, heads: int, kv_heads: int, head_dim: int, *,
                   page_tokens: int = 16, sizes: bool = False, weights: bool = False, device="cuda") -> DevicePackedCache:
-    """An empty cache in 4 bits (device_cache)."""
+    """An empty cache in 4 bits (device_cache); head_dim is a multiple of 32."""
+    if head_dim < 32 or head_dim % 32:   # (pools of head_dim // 2 bytes would not tell an odd number)
+        raise fb.FusionError(f"head_dim: a multiple of 32 expected, not {head_dim}")
     per = -(-max_tokens // page_tokens)
     pages = max(1, max_batch * per)
     pool = lambda row: torch.zeros((pages, kv_heads, page_tokens, row), dtype=torch.uint8, device=device)   # noqa: E731

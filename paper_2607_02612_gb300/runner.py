@@ -290,6 +290,8 @@ class Rotation:
 
 def rotation_table(positions: int, dims: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """The usual table of a Rotation: angles position * base ** (-2 i / dims), in 64 bits, their cosines and sines rounded once."""
+    if dims < 2 or dims % 2:
+        raise fb.FusionError(f"dims: an even number expected, not {dims}")
     i = torch.arange(dims // 2, dtype=torch.float64, device=device)
     a = torch.arange(positions, dtype=torch.float64, device=device)[:, None] * float(base) ** (-2.0 * i / dims)
     return torch.cat([a.cos(), a.sin()], dim=1).float()

@@ -150,6 +150,13 @@ def _rows_here(c, rows) -> None:
         raise fb.FusionError(f"the rows' offsets, count and ids on the cache's device ({c.index}) expected")
 
 
+def _has_sequences(c, rows) -> bool:
+    """Whether there is anything to do; samples for a cache without sequences name none of it."""
+    if c.max_batch == 0 and rows.max_batch > 0:
+        raise fb.FusionError("samples for a cache that has no sequences")
+    return c.max_batch > 0
+
+
 def _heads_out(c, t: Optional[torch.Tensor], rows: int, heads: int, what: str):
     """An output [rows, heads, head_dim] of the cache's type and device: t, checked, or a new one; and its address."""
     if t is None:
@@ -502,6 +509,7 @@ class Fusion:
         o = lengths_out if lengths_out is not None else c.lengths
         if rows is None:
             rows = c.one_row_each()
+        some = _has_sequences(c, rows)
         heads, qp, qs, qo = 0, None, 0, None
         if q is not None:
             shape = q.shape
@@ -514,7 +522,7 @@ class Fusion:
                 qp = qo = None
         elif q_out is not None:
             raise fb.FusionError("q_out without q")
-        if c.max_batch == 0:
+        if not some:
             return q_out
         rows, kp, ks, vp, vs, zp, wp, op = _append_args(c, k, v, rows, sizes, scores, o)
         pp = _need(positions, torch.int32, c.index, "positions", rows.max_rows)
@@ -531,13 +539,14 @@ class Fusion:
         starts[i] + r (starts [max_batch] int32; None: 0) of its sequence.  Returns keys and values [rows, kv_heads,
         head_dim] (k_out and v_out, where they are given; rows of no sample stay); sizes_out and weights_out [rows] get the
         tokens' sizes and weights."""
+        some = _has_sequences(c, rows)
         _rows_here(c, rows)
         k_out, kp = _heads_out(c, k_out, rows.max_rows, c.kv_heads, "k_out")
         v_out, vp = _heads_out(c, v_out, rows.max_rows, c.kv_heads, "v_out")
         sp = _need(starts, torch.int32, c.index, "starts", rows.max_batch)
         zp = _need(sizes_out, torch.float32, c.index, "sizes_out", rows.max_rows)
         wp = _need(weights_out, torch.float32, c.index, "weights_out", rows.max_rows)
-        if rows.max_batch and rows.max_rows and c.max_batch:
+        if some and rows.max_batch and rows.max_rows:
             _enqueue(c.lib.fusion_cache_read, c.index, self.status, c.code, c.c_struct(), rows.ragged(), sp, kp, vp, zp, wp)
         return k_out, v_out
 

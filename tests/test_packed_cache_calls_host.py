@@ -1,6 +1,9 @@
 """Calls on caches in 4 bits, rotations and caches without sequences that the runner refuses before anything is allocated or
 enqueued (no GPU needed)."""
+import types
+
 import pytest
+import torch
 
 import paper_2607_02612_gb300 as fz
 from paper_2607_02612_gb300 import runner
@@ -22,3 +25,28 @@ def test_rotation_tables_of_odd_dims_are_refused():
             runner.rotation_table(10, dims, device="cpu")
     assert runner.rotation_table(10, 2, device="cpu").shape == (10, 2)
     assert runner.rotation_table(0, 32, device="cpu").shape == (0, 32)
+
+
+def test_samples_for_a_cache_without_sequences_are_refused(monkeypatch):
+    """They name no sequence of it: nothing would be written to what the calls return."""
+    monkeypatch.setattr(runner, "_enqueue", lambda *args: pytest.fail("enqueued"))
+    none = torch.zeros(0, dtype=torch.int32)
+    c = types.SimpleNamespace(max_batch=0, kv_heads=2, head_dim=64, heads=4, index=-1, torch_dtype=torch.float32, device="cpu", lengths=none,
+                              code=0, _ws=0, ws_bytes=0, c_struct=lambda: None, one_row_each=lambda: rows(0, 0),
+                              lib=types.SimpleNamespace(fusion_cache_append_rotated=None, fusion_cache_read=None))
+    f, rot = types.SimpleNamespace(status=None), types.SimpleNamespace(table=torch.zeros(9, 64), c_struct=lambda p: None)
+
+    def rows(batch, n):
+        return types.SimpleNamespace(max_batch=batch, max_tokens=1, max_rows=n, offsets=torch.zeros(batch + 1, dtype=torch.int32), batch=None,
+                                     ids=None, ragged=lambda: None)
+
+    k, q = torch.zeros(3, 2, 64), torch.zeros(3, 7, 64)
+    with pytest.raises(fz.FusionError, match="no sequences"):
+        runner.Fusion.cache_read(f, c, rows(3, 3))
+    for kw in (dict(q=q), dict(q=q, q_out=torch.zeros(3, 7, 64)), {}):
+        with pytest.raises(fz.FusionError, match="no sequences"):
+            runner.Fusion.cache_append_rotated(f, c, k, k, rot, rows(3, 3), **kw)
+    # no samples, as before: nothing to do
+    assert runner.Fusion.cache_append_rotated(f, c, k[:0], k[:0], rot, q=q[:0]).shape == (0, 7, 64)
+    assert runner.Fusion.cache_append_rotated(f, c, k, k, rot, rows(0, 3), q=q).shape == (3, 7, 64)
+    assert [t.shape for t in runner.Fusion.cache_read(f, c, rows(0, 5))] == [(5, 2, 64)] * 2

@@ -4,6 +4,8 @@
 
 #include <cuda_runtime.h>
 
+#include <atomic>
+
 #include "common.cuh"
 
 namespace fz {
@@ -60,6 +62,27 @@ inline cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, si
     cfg.attrs = a;
     cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
+// Host: as many CTAs of a kernel as the GPU holds at once, and its `smem` bytes of dynamic shared memory allowed.  What depends on the
+// kernel and the device alone is asked once (asking costs the host 4 us a call).
+template <auto Kernel, int THREADS>
+cudaError_t resident_ctas(int smem, int &ctas) {
+    constexpr int kDevices = 64;
+    static std::atomic<int> known[kDevices];
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    ctas = dev < kDevices ? known[dev].load(std::memory_order_acquire) : 0;
+    if (ctas > 0) return cudaSuccess;
+    int sms = 0, occ = 0;
+    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, Kernel, THREADS, smem);
+    if (e != cudaSuccess) return e;
+    ctas = sms * (occ < 1 ? 1 : occ);
+    if (dev < kDevices) known[dev].store(ctas, std::memory_order_release);
+    return cudaSuccess;
 }
 
 // Query heads times places of a cache, at most (the host refuses more).

@@ -2,8 +2,6 @@
 // round on their way into shared memory, and the join of runs that share a (sequence, key head).
 #pragma once
 
-#include <atomic>
-
 #include "cache.cuh"
 
 namespace fz {
@@ -412,26 +410,7 @@ constexpr bool counts_fit(long long tt, long long w, long long tail = 0) {
     return (w == 1 ? kHeads * ((kAloneMost + tt - 1) / tt) : kCacheMaxHeadTokens / (tt * w) + kHeads * (1 + tail)) < 1ll << 32;
 }
 
-// Host: as many CTAs as the GPU holds at once, or as there can be rounds.  What depends on the kernel and the device alone is
-// asked once (asking costs the host 4 us a call).
-template <auto Kernel, int THREADS>
-cudaError_t resident_ctas(int smem, int &ctas) {
-    constexpr int kDevices = 64;
-    static std::atomic<int> known[kDevices];
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
-    if (e != cudaSuccess) return e;
-    ctas = dev < kDevices ? known[dev].load(std::memory_order_acquire) : 0;
-    if (ctas > 0) return cudaSuccess;
-    int sms = 0, occ = 0;
-    e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&occ, Kernel, THREADS, smem);
-    if (e != cudaSuccess) return e;
-    ctas = sms * (occ < 1 ? 1 : occ);
-    if (dev < kDevices) known[dev].store(ctas, std::memory_order_release);
-    return cudaSuccess;
-}
+// Host: as many CTAs as the GPU holds at once, or as there can be rounds.
 template <auto Kernel, int W, typename P>
 cudaError_t launch_rounds(int smem, const P &p, int chunks, int tokens, cudaStream_t s) {
     int ctas = 0;

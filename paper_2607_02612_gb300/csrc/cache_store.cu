@@ -12,8 +12,6 @@
 // A segment is 16 bytes, asked for up to kDepth units ahead into the thread's own places of a ring in shared memory (cp.async, no
 // barriers), so that about 190 KB per SM are on their way.  On the way to 4 bits it is 32 bytes, a group of 16 dims in bf16 and half a
 // group in float32, one unit ahead in registers (Shape).
-#include <atomic>
-
 #include "cache_rows.cuh"
 #include "fp4.cuh"
 
@@ -453,16 +451,10 @@ template <typename T, bool kFour, int P>
 cudaError_t launch(const CacheStoreParams &p, cudaStream_t s) {
     using X = Shape<T, kFour, P>;
     constexpr int S = X::S;
-    constexpr int kDevices = 64;
-    static std::atomic<bool> allowed[kDevices];   // the kernel's shared memory, asked for once per device
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e == cudaSuccess && !(device < kDevices && allowed[device].load(std::memory_order_acquire))) {
-        e = cudaFuncSetAttribute(k_cache_store<T, kFour, P>, cudaFuncAttributeMaxDynamicSharedMemorySize, X::kSmem);
-        if (e == cudaSuccess && device < kDevices) allowed[device].store(true, std::memory_order_release);
-    }
+    int places = 0;
+    const cudaError_t e = resident_ctas<k_cache_store<T, kFour, P>, kThreads>(X::kSmem, places);
     if (e != cudaSuccess) return e;
-    const int places = 152 * X::kCtas, heads = p.q ? p.heads : 0;
+    const int heads = p.q ? p.heads : 0;
     // in segments of 16 bytes an even number, if there is room for it, so that the lanes' segments end where sectors do (11 samples of 556
     // of 16 + 16 + 64 heads of 80 bf16 51.8 us, now 39.4)
     int units = ceil_div(p.c.dim, 2 * S);

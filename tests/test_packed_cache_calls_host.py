@@ -1,5 +1,7 @@
 """Calls on caches in 4 bits, rotations and caches without sequences that the runner refuses before anything is allocated or
 enqueued (no GPU needed)."""
+import os
+import re
 import types
 
 import pytest
@@ -50,3 +52,10 @@ def test_samples_for_a_cache_without_sequences_are_refused(monkeypatch):
     assert runner.Fusion.cache_append_rotated(f, c, k[:0], k[:0], rot, q=q[:0]).shape == (0, 7, 64)
     assert runner.Fusion.cache_append_rotated(f, c, k, k, rot, rows(0, 3), q=q).shape == (3, 7, 64)
     assert [t.shape for t in runner.Fusion.cache_read(f, c, rows(0, 5))] == [(5, 2, 64)] * 2
+
+
+@pytest.mark.parametrize("name", ["cache_store.cu", "cache_read.cu", "packed_attn.cu", "cache_rows.cuh", "cache_rounds.cuh", "fp4.cuh"])
+def test_no_number_of_multiprocessors_in_the_sources(name):
+    """How many CTAs a device holds at once is asked of it, not written down (comments may speak of the one that was measured)."""
+    text = open(os.path.join(os.path.dirname(fz.__file__), "csrc", name)).read()
+    assert not re.findall(r"\b(?:152|148|144|132)\b", re.sub(r"//[^\n]*|/\*.*?\*/", "", text, flags=re.S))

@@ -1,5 +1,5 @@
-"""Rotated appends whose CTAs take several rows, with queries rotated in place, on the GPU against the definitions on the host
-(packed_reference.py), bit by bit."""
+"""Rotated and packed appends whose CTAs take several rows: queries rotated in place, and more rows than the CTAs of a sample take at
+once, on the GPU against the definitions on the host (packed_reference.py) and against shorter calls, bit by bit."""
 import os
 import sys
 
@@ -10,6 +10,7 @@ sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 
 import cache_reference as ref  # noqa: E402
 import packed_reference as pk  # noqa: E402
+import paper_2607_02612_gb300 as fz  # noqa: E402
 from paper_2607_02612_gb300 import runner  # noqa: E402
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +62,50 @@ def test_queries_in_place(dtype, four, pairs, dim, turned, longest):
             assert torch.equal(held, codes) and torch.equal(getattr(dc, name + "_scales").cpu()[page, :, off], scales)
         else:
             assert torch.equal(ref.bits(held), ref.bits(rows.to(t)))
+
+
+# 12 key heads of 256 dims: rows that a CTA has side by side, whose 24 units a row are all that it takes
+@pytest.mark.parametrize("dtype,four,turned,side", [("f32", False, 256, 8), ("bf16", False, 128, 16), ("f32", True, 256, 16), ("bf16", True, 256, 32),
+                                                    ("f32", True, 0, 16), ("bf16", True, 0, 32)])
+def test_more_rows_than_the_ctas_of_a_sample_take_at_once(dtype, four, turned, side):
+    """One sample of 2500 times as many rows as a CTA has at once, of which 2432 CTAs take some in a second turn, against the same rows in
+    calls that need no such turn.  Then positions that the table does not have, in one CTA and in most of them."""
+    kv, dim, n = 12, 256, 2500 * side
+    g = torch.Generator(device=DEV).manual_seed(side)
+    new = runner.device_packed_cache if four else runner.device_cache
+    (dc, parts), f = (new(dtype, 1, n, kv, kv, dim, page_tokens=1024) for _ in range(2)), runner.Fusion(1)
+    k, v = (torch.randn((n, kv, dim), generator=g, device=DEV, dtype=ref.TYPES[dtype]) for _ in range(2))
+    rot = runner.Rotation(torch.randn((700, turned), generator=g, device=DEV)) if turned else None
+    pos = torch.randint(0, 700, (n,), generator=g, device=DEV, dtype=torch.int32)
+
+    def append(c, a, b, at=pos):
+        if rot is None:
+            f.cache_append(c, k[a:b], v[a:b], ragged([0, b - a], b - a))
+        else:
+            f.cache_append_rotated(c, k[a:b], v[a:b], rot, ragged([0, b - a], b - a), positions=at[a:b])
+
+    append(dc, 0, n)
+    step = 900 * side + 7
+    for a in range(0, n, step):
+        append(parts, a, min(n, a + step))
+    assert status(f) == 0 and dc.lengths.tolist() == parts.lengths.tolist() == [n]
+    pools = ("k", "v", "k_scales", "v_scales") if four else ("k", "v")
+
+    def same():
+        return all(torch.equal(getattr(dc, name).view(torch.uint8), getattr(parts, name).view(torch.uint8)) for name in pools)
+
+    assert same() and int(dc.workspace[:1 << 18].max()) == 0
+    if rot is None:
+        return
+    for bad in ([n - 1], range(3, n, 11), [0]):
+        wrong = pos.clone()
+        wrong[torch.tensor(bad, device=DEV)] = 700
+        f = runner.Fusion(1)
+        dc.lengths.zero_()
+        for name in pools:
+            getattr(dc, name).zero_()
+        append(dc, 0, n, wrong)
+        assert status(f) == fz.FUSION_DEV_BAD_POSITION and dc.lengths.tolist() == [0] and int(dc.workspace[:1 << 18].max()) == 0
+    f = runner.Fusion(1)
+    append(dc, 0, n)
+    assert status(f) == 0 and dc.lengths.tolist() == [n] and same()

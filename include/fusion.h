@@ -177,13 +177,18 @@ typedef struct fusion_cache {
     const int32_t *lengths;    /* [max_batch] tokens held, in [0, max_pages * page_tokens] */
 } fusion_cache;
 
-/* The same cache with keys and values in 4 bits (4.5 with their scales).  A row of a head is held in groups of 16 dims: a scale,
+/* The same cache with keys and values in 4 bits (with their scales 4.5 where head_dim is a multiple of 64, up to 5 otherwise, whose rows
+ * of scales end in padding).  A row of a head is held in groups of 16 dims: a scale,
  * of type e4m3 (a sign, 4 bits of exponent, 3 of mantissa), and 16 codes of type e2m1 (a sign and one of 0, 0.5, 1, 1.5, 2, 3,
  * 4, 6 by the code's lower three bits).  A dim's value is its code's times the scale: at most 6 significant bits, exact in bf16.
  * cache.k, cache.v: [num_pages, kv_heads, page_tokens, head_dim / 2] bytes, dim 2 i in the lower four bits of byte i, 2 i + 1
  * in the upper ones.  k_scales, v_scales: [num_pages, kv_heads, page_tokens, FUSION_PACKED_SCALE_BYTES(head_dim)] bytes, the
- * scale of dims 16 i .. 16 i + 15 in byte i; bytes behind the last scale are not read (fusion_packed_append writes zeros there).
- * All 16-byte aligned.  head_dim is a multiple of 32; everything else as in fusion_cache. */
+ * scale of dims 16 i .. 16 i + 15 in byte i; bytes behind the last scale count for nothing (fusion_packed_append writes zeros there).
+ * All 16-byte aligned.  head_dim is a multiple of 32; everything else as in fusion_cache.
+ * There is one level of scales, so what a group can hold depends on its largest magnitude m: up to about 6 * 2^-10 (0.0059) it becomes
+ * zeros, below 6 * 2^-6 (0.094) its scale has fewer than 4 significant bits, and dims beyond 6 * 448 = 2688 are cut off there.  The calls
+ * take no factor: a caller with keys or values of such magnitudes multiplies them before the append, and divides the attention's
+ * scale or output. */
 #define FUSION_PACKED_SCALE_BYTES(head_dim) (((head_dim) / 16 + 3) / 4 * 4)
 typedef struct fusion_packed_cache {
     fusion_cache cache;
@@ -568,6 +573,8 @@ int fusion_cache_evict(int dtype, fusion_cache cache, const int32_t *budget, int
  * dtype; values are copied.  q: [in.max_rows, heads, head_dim] with rows q_stride elements apart (>= 0, rows 16-byte
  * aligned), NULL: none; q_out: [in.max_rows, heads, head_dim], may be q where its rows lie that way and overlaps nothing else.
  * heads: in [1, FUSION_CACHE_MAX_HEADS], read only with q; any number beside the cache's.  Rows of no sample are left in q_out.
+ * As for all appends and reads, the launch has room for in.max_tokens rows of every sample: long prompts beside many single tokens are
+ * faster in a call of their own.
  * Errors: those of fusion_cache_append; FUSION_ERR_INVALID_ARG for a NULL or misaligned table, bad pairs, q without q_out;
  * FUSION_ERR_SHAPE for table_rows < 1 or dims or heads out of range.  Device bits: those of fusion_cache_append (which leave that
  * sample's rows of q_out unwritten too) and BAD_POSITION, which leaves the sequence's length as it is; places past its end, and
@@ -600,7 +607,8 @@ int fusion_packed_append_rotated(int dtype, fusion_packed_cache cache, fusion_ra
 /*
  * fusion_packed_attention: fusion_cache_attention over a cache in 4 bits, q and out of type dtype.  Keys and values enter the
  * products as the values that the cache holds, exactly; a query as a float16 (for FUSION_F32 the sum of two) times a power of
- * two of its head's own; a probability as a float16 (two), within 2^-11 (2^-22) of itself or within 2^-32 of the largest.
+ * two of its head's own; a probability as a float16 (two), within 2^-11 (2^-22) of itself or within 2^-32 of the largest.  So
+ * an output is off by up to 2^-11 (2^-22) of sum p_j |v_j| and 2^-32 of sum |v_j|, beside its sums in float32 and its own rounding.
  */
 int fusion_packed_attention(int dtype, fusion_packed_cache cache, const void *q, int64_t q_stride, int32_t heads, float scale,
                             int32_t window, int32_t sinks, void *out, void *workspace, size_t workspace_bytes,
